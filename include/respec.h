@@ -78,6 +78,14 @@ typedef enum {
                                index with it, skip the request and leave every
                                array outside their own outputs untouched     */
 
+#define RS_ST_BAD_PAGE  64   /* an entry of the request's page table that its tokens need
+                               lies outside the pool: nothing outside it is touched,
+                               the request's outputs are empty                       */
+
+/* type of a 16-bit tensor (uint16_t bit patterns) */
+#define RS_BF16 0
+#define RS_F16  1
+
 /* -------------------------------------------------------------- parameters */
 /* Hyper-parameters of Algorithm 1 (its inputs), Eq. 6-7 and Section 3.4.
  * Passed by value.  Defaults used by this project where the paper gives no
@@ -412,6 +420,99 @@ rs_status rs_tree_sample(const float *logits, int R, int V, const int32_t *node_
                          float temperature, const float *uniforms, int acc_cap, int32_t *draw,
                          int32_t *acc_len, int32_t *acc_nodes, int32_t *bonus, int32_t *status,
                          void *workspace, size_t workspace_bytes, void *stream);
+
+/* ====================================================== rs_prompt_attn ===
+ * Causal attention over whole prompts, packed one behind the other: the pass
+ * that fills the cache before the first verify step.  Row i of sequence b
+ * (rows seq_off[b] .. seq_off[b+1]) computes
+ *     out_i = sum_{j <= i} exp(scale q_i.k_j - lse_i) v_j,
+ *     lse_i = log sum_{j <= i} exp(scale q_i.k_j)      (natural log)
+ * over the rows j of its own sequence.
+ *
+ *   q [T, Hq, D], k and v [T, Hkv, D] of type dtype (RS_BF16 or RS_F16), each
+ *            with its own distance between rows in elements (q_stride,
+ *            k_stride, v_stride: at least heads x D, multiples of 8), so that
+ *            they may be parts of one projection's rows; 16-byte aligned.
+ *   seq_off  [B+1] int32; sequences may have no rows; B <= 4096.
+ *   D in {64, 128}; Hq a multiple of Hkv, at most 128 times (query head h
+ *   reads KV head h / (Hq / Hkv)); scale > 0.
+ *   out      [T, Hq, D] of type dtype;  lse [T, Hq] fp32;  rows behind the
+ *            last sequence are left as they are.
+ *   status   [B]: RS_ST_BAD_OFFSET for a range outside [0, T) or one that
+ *            starts before an earlier sequence does (its own rows, where they
+ *            lie inside, are zeroed); RS_ST_TIMEOUT.
+ * Products run on the tensor cores with fp32 accumulation; softmax statistics
+ * are fp32; P is rounded to dtype for the second product.  A row whose scores
+ * are all -inf gives zeros and lse -inf.  NaN or infinity in a row of K or V
+ * reaches rows of its own sequence only (also earlier ones of the same 128).
+ * The result does not depend on what else runs: the same bits every time.
+ */
+size_t rs_prompt_attn_workspace_size(int B, int T, int Hq, int Hkv, int D);
+rs_status rs_prompt_attn(const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride,
+                         const uint16_t *v, int64_t v_stride, int dtype, const int32_t *seq_off, int B,
+                         int T, int Hq, int Hkv, int D, float scale, uint16_t *out, float *lse,
+                         int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ================================================== the paged KV cache ===
+ * k_pages and v_pages [n_pages, page_size, Hkv, D] hold 16-bit keys and values
+ * (16-byte aligned); page_size is a power of two from 8 to 65536.  Token slot
+ * s of request b is row s % page_size of page
+ * page_table[b * max_pages + s / page_size].  A request with ctx_len[b] cached
+ * tokens and n_b new ones (rows new_off[b] .. new_off[b+1] of the call's
+ * arrays) uses slots 0 .. ctx_len[b] + n_b - 1, the new ones last; entries of
+ * the table behind those are never read.  Requests may share pages that are
+ * only read; a page that a call writes belongs to one request.
+ *
+ * Beside the pages a cache may keep, per KV head and slot of the pool,
+ *   weights   [Hkv, n_pages * page_size] fp32: accumulated attention weight;
+ *   positions [Hkv, n_pages * page_size] int32: the token's position.
+ * rs_paged_append writes them, rs_paged_weights adds to the weights, and
+ * rs_paged_evict chooses by them (each head keeps its own tokens, so slot s
+ * may hold different positions in different heads afterwards).
+ */
+
+/* ==================================================== rs_paged_append ====
+ * New tokens enter the cache: row i of request b goes to slot ctx_len[b] + i
+ * of its pages, with weight 0 and position pos[row] (the slot number where
+ * pos is NULL).
+ *   k, v     [T, Hkv, D], k_stride / v_stride elements from row to row (at
+ *            least Hkv x D, multiples of 8; 16-byte aligned).
+ *   new_off  [B+1] int32 (one that decreases anywhere rejects every request);
+ *            ctx_len [B] int32: tokens cached before.
+ *   weights, positions: NULL where the cache keeps none.
+ *   status   [B]: RS_ST_BAD_OFFSET (rows outside T, slots past max_pages
+ *            pages): nothing of the request is written; RS_ST_BAD_PAGE: tokens
+ *            of bad pages are not written.
+ */
+rs_status rs_paged_append(const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride,
+                          const int32_t *pos, const int32_t *new_off, int B, int T, int Hkv, int D,
+                          uint16_t *k_pages, uint16_t *v_pages, int n_pages, int page_size,
+                          const int32_t *page_table, int max_pages, const int32_t *ctx_len,
+                          float *weights, int32_t *positions, int32_t *status, void *stream);
+
+/* ====================================================== rs_paged_attn ====
+ * Attention of a chunk of new tokens per request over its paged cache, the
+ * chunk's own keys included (append them first): a piece of a prompt, a single
+ * token, or a draft tree.
+ *   q        [T, Hq, D] of type dtype, q_stride elements from row to row.
+ *   parents  NULL: row i sees slots j <= ctx_len[b] + i (causal).  Otherwise
+ *            [T] int32 as for rs_tree_verify_attn (at most RS_MAX_NODES rows a
+ *            request): row i sees the ctx_len[b] cached slots, and of the new
+ *            ones its ancestors and itself.
+ *   out      [T, Hq, D] of type dtype;  lse [T, Hq] fp32;  rows behind the
+ *            last request are left as they are.
+ *   status   [B]: RS_ST_BAD_OFFSET, RS_ST_BAD_PAGE, RS_ST_BAD_TREE,
+ *            RS_ST_TOO_LARGE (the request's rows are zeroed), RS_ST_TIMEOUT.
+ * Types, arithmetic, B, head counts, alignment: as for rs_prompt_attn.  What
+ * slots behind a request's last token hold (NaN too) does not matter.
+ */
+size_t rs_paged_attn_workspace_size(int B, int T, int Hq, int Hkv, int D);
+rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtype, const int32_t *new_off,
+                        const int32_t *parents, int B, int T, int Hq, int Hkv, int D,
+                        const uint16_t *k_pages, const uint16_t *v_pages, int n_pages, int page_size,
+                        const int32_t *page_table, int max_pages, const int32_t *ctx_len, float scale,
+                        uint16_t *out, float *lse, int32_t *status, void *workspace,
+                        size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -24,7 +24,8 @@
 
 #define RS_ENTRIES(X)                                                                                            \
     X(entropy_gate) X(entropy_gate_noalloc) X(entropy_gate_rows) X(match_scan) X(tree_verify_attn) X(accept)     \
-    X(match_index_build) X(match_index_append) X(match_scan_indexed) X(tree_sample)
+    X(match_index_build) X(match_index_append) X(match_scan_indexed) X(tree_sample) X(prompt_attn) X(paged_append)  \
+    X(paged_attn)
 
 namespace {
 
@@ -143,6 +144,35 @@ struct Args {
         if (o == Py_None) return nullptr;
         if (PyLong_Check(o)) return reinterpret_cast<T *>(masked(o));
         return static_cast<T *>(address(o, nullptr));
+    }
+    // Rows of heads, followed by the distance between them in elements: a tensor
+    // may be part of wider rows; its heads' values are contiguous and its rows
+    // as far apart as the argument says.
+    const uint16_t *rows(int64_t *stride) {
+        PyObject *o = next();
+        const bool tensor = THPVariable_CheckExact(o);
+        void *p = nullptr;
+        if (tensor) {
+            const at::Tensor &t = THPVariable_Unpack(o);
+            check(t.is_cuda(), true, o);
+            const int64_t d = t.dim();
+            bool inner = d >= 2 && t.element_size() == 2 && (t.stride(d - 1) == 1 || t.size(d - 1) == 1);
+            for (int64_t i = d - 2; inner && i > 0; --i) inner = t.size(i) == 1 || t.stride(i) == t.stride(i + 1) * t.size(i + 1);
+            if (!inner && t.numel() > 0) refuse("rows of contiguous 16-bit values expected", o);
+            p = t.data_ptr();
+        } else {
+            --i;
+            p = ptr<void>();
+        }
+        *stride = i64();
+        if (tensor) {
+            const at::Tensor &t = THPVariable_Unpack(o);
+            if (t.numel() > 0 && t.size(0) > 1 && t.stride(0) != *stride) {
+                PyErr_Format(PyExc_ValueError, "rows are %lld elements apart, not %lld", (long long)t.stride(0), (long long)*stride);
+                throw PyFail{};
+            }
+        }
+        return static_cast<const uint16_t *>(p);
     }
     unsigned long long masked(PyObject *o) {
         const unsigned long long x = PyLong_AsUnsignedLongLongMask(o);
@@ -432,6 +462,71 @@ RS_BIND(tree_sample) {
         return [=] {
             return lib.tree_sample(logits, R, V, node_off, B, tokens, parents, source, T, uniforms, cap, draw, acc_len, acc_nodes,
                                   bonus, status, ws, wb, st);
+        };
+    });
+}
+
+RS_BIND(prompt_attn) {
+    return guarded(v, n, [](Args &a) {
+        int64_t qs, ks, vs;
+        auto *q = a.rows(&qs), *k = a.rows(&ks), *vv = a.rows(&vs);
+        const int dtype = a.i32();
+        auto *off = a.ptr<const int32_t>();
+        const int B = a.i32(), T = a.i32(), Hq = a.i32(), Hkv = a.i32(), D = a.i32();
+        const float scale = a.f32();
+        auto *out = a.ptr<uint16_t>();
+        auto *lse = a.ptr<float>();
+        auto *status = a.ptr<int32_t>();
+        size_t wb;
+        void *ws = a.sized(&wb, true), *st = a.stream();
+        return [=] {
+            return lib.prompt_attn(q, qs, k, ks, vv, vs, dtype, off, B, T, Hq, Hkv, D, scale, out, lse, status, ws, wb, st);
+        };
+    });
+}
+
+RS_BIND(paged_append) {
+    return guarded(v, n, [](Args &a) {
+        int64_t ks, vs;
+        auto *k = a.rows(&ks), *vv = a.rows(&vs);
+        auto *pos = a.ptr<const int32_t>(), *off = a.ptr<const int32_t>();
+        const int B = a.i32(), T = a.i32(), Hkv = a.i32(), D = a.i32();
+        auto *kp = a.ptr<uint16_t>(), *vp = a.ptr<uint16_t>();
+        const int pages = a.i32(), size = a.i32();
+        auto *table = a.ptr<const int32_t>();
+        const int most = a.i32();
+        auto *ctx = a.ptr<const int32_t>();
+        auto *weights = a.ptr<float>();
+        auto *positions = a.ptr<int32_t>(), *status = a.ptr<int32_t>();
+        void *st = a.stream();
+        return [=] {
+            return lib.paged_append(k, ks, vv, vs, pos, off, B, T, Hkv, D, kp, vp, pages, size, table, most, ctx, weights, positions,
+                                    status, st);
+        };
+    });
+}
+
+RS_BIND(paged_attn) {
+    return guarded(v, n, [](Args &a) {
+        int64_t qs;
+        auto *q = a.rows(&qs);
+        const int dtype = a.i32();
+        auto *off = a.ptr<const int32_t>(), *parents = a.ptr<const int32_t>();
+        const int B = a.i32(), T = a.i32(), Hq = a.i32(), Hkv = a.i32(), D = a.i32();
+        auto *kp = a.ptr<const uint16_t>(), *vp = a.ptr<const uint16_t>();
+        const int pages = a.i32(), size = a.i32();
+        auto *table = a.ptr<const int32_t>();
+        const int most = a.i32();
+        auto *ctx = a.ptr<const int32_t>();
+        const float scale = a.f32();
+        auto *out = a.ptr<uint16_t>();
+        auto *lse = a.ptr<float>();
+        auto *status = a.ptr<int32_t>();
+        size_t wb;
+        void *ws = a.sized(&wb, true), *st = a.stream();
+        return [=] {
+            return lib.paged_attn(q, qs, dtype, off, parents, B, T, Hq, Hkv, D, kp, vp, pages, size, table, most, ctx, scale, out, lse,
+                                  status, ws, wb, st);
         };
     });
 }

@@ -178,6 +178,11 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N, bool b_mn_ma
            | ((uint32_t)(M >> 4) << 24);      // M / 16
 }
 
+// The same for either 16-bit type (A and B of one type).
+__host__ __device__ constexpr uint32_t idesc_16_f32(bool bf16, int M, int N, bool b_mn_major) {
+    return bf16 ? idesc_bf16_f32(M, N, b_mn_major) : idesc_bf16_f32(M, N, b_mn_major) & ~((1u << 7) | (1u << 10));
+}
+
 // D[tmem] (+)= A[smem desc] * B[smem desc]^T
 __device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                         uint32_t accumulate) {

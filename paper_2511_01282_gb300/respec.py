@@ -21,7 +21,8 @@ BIND_PATH = os.path.join(_HERE, "_respec_bind.so")
 
 RS_OK, RS_ERR_INVALID_ARG, RS_ERR_UNSUPPORTED, RS_ERR_CAPACITY, RS_ERR_CUDA = range(5)
 RS_ST_BAD_TREE, RS_ST_TRUNCATED, RS_ST_BAD_POS, RS_ST_TOO_LARGE, RS_ST_TIMEOUT = 1, 2, 4, 8, 16
-RS_ST_BAD_OFFSET = 32
+RS_ST_BAD_OFFSET, RS_ST_BAD_PAGE = 32, 64
+RS_BF16, RS_F16 = 0, 1
 RS_MAX_L, RS_MAX_TOPC, RS_MAX_SPAN, RS_MAX_BETA, RS_MAX_NODES = 8, 8, 256, 16, 256
 
 
@@ -78,6 +79,14 @@ _SIGS = {
     "rs_tree_sample_workspace_size": (C.c_size_t, [C.c_int, C.c_int]),
     "rs_tree_sample": (C.c_int, [_P, C.c_int, C.c_int, _P, C.c_int, _P, _P, _P, C.c_float, _P, C.c_int,
                                  _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "rs_prompt_attn_workspace_size": (C.c_size_t, [C.c_int] * 5),
+    "rs_prompt_attn": (C.c_int, [_P, C.c_int64] * 3 + [C.c_int, _P] + [C.c_int] * 5 + [C.c_float] + [_P] * 4
+                       + [C.c_size_t, _P]),
+    "rs_paged_append": (C.c_int, [_P, C.c_int64] * 2 + [_P] * 2 + [C.c_int] * 4 + [_P] * 2 + [C.c_int] * 2
+                        + [_P, C.c_int] + [_P] * 5),
+    "rs_paged_attn_workspace_size": (C.c_size_t, [C.c_int] * 5),
+    "rs_paged_attn": (C.c_int, [_P, C.c_int64, C.c_int] + [_P] * 2 + [C.c_int] * 5 + [_P] * 2 + [C.c_int] * 2
+                      + [_P, C.c_int, _P, C.c_float] + [_P] * 4 + [C.c_size_t, _P]),
     "rs_entropy_gate_rows": (C.c_int, [_P, _P, _P, C.c_int, rs_params, _P, _P, _P, _P, _P, _P]),
 }
 
@@ -229,3 +238,33 @@ def rs_entropy_gate_rows(entropy, row_off, row_commit, B, p, hist, hist_n, k_sta
                          entropy_ok, stream=None):
     _check((_bind or _native()).rs_entropy_gate_rows(entropy, row_off, row_commit, B, p, hist, hist_n, k_star,
                                                      h_best, entropy_ok, stream))
+
+
+def rs_prompt_attn_workspace_size(B, T, Hq, Hkv, D):
+    return int(lib().rs_prompt_attn_workspace_size(B, T, Hq, Hkv, D))
+
+
+def rs_prompt_attn(q, q_stride, k, k_stride, v, v_stride, dtype, seq_off, B, T, Hq, Hkv, D, scale, out, lse,
+                   status, workspace, stream=None):
+    """q, k and v may be parts of wider rows (``qkv[:, :Hq]``): their heads' values are contiguous and the
+    strides given are theirs."""
+    _check((_bind or _native()).rs_prompt_attn(q, q_stride, k, k_stride, v, v_stride, dtype, seq_off, B, T, Hq,
+                                               Hkv, D, scale, out, lse, status, workspace, stream))
+
+
+def rs_paged_append(k, k_stride, v, v_stride, pos, new_off, B, T, Hkv, D, k_pages, v_pages, n_pages, page_size,
+                    page_table, max_pages, ctx_len, weights, positions, status, stream=None):
+    _check((_bind or _native()).rs_paged_append(k, k_stride, v, v_stride, pos, new_off, B, T, Hkv, D, k_pages,
+                                                v_pages, n_pages, page_size, page_table, max_pages, ctx_len,
+                                                weights, positions, status, stream))
+
+
+def rs_paged_attn_workspace_size(B, T, Hq, Hkv, D):
+    return int(lib().rs_paged_attn_workspace_size(B, T, Hq, Hkv, D))
+
+
+def rs_paged_attn(q, q_stride, dtype, new_off, parents, B, T, Hq, Hkv, D, k_pages, v_pages, n_pages, page_size,
+                  page_table, max_pages, ctx_len, scale, out, lse, status, workspace, stream=None):
+    _check((_bind or _native()).rs_paged_attn(q, q_stride, dtype, new_off, parents, B, T, Hq, Hkv, D, k_pages,
+                                              v_pages, n_pages, page_size, page_table, max_pages, ctx_len, scale,
+                                              out, lse, status, workspace, stream))
