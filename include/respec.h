@@ -514,6 +514,53 @@ rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtype, const in
                         uint16_t *out, float *lse, int32_t *status, void *workspace,
                         size_t workspace_bytes, void *stream);
 
+/* =================================================== rs_paged_weights ====
+ * The attention weight that a chunk's rows give to every key they see, added
+ * to the cache's weights: for each KV head, slot s of request b gains
+ *     sum over rows i with s <= ctx_len[b] + i, and over the query heads of
+ *     the group, of exp(scale q_i.k_s - lse_i).
+ * Call it after rs_paged_attn (causal), or after rs_prompt_attn and
+ * rs_paged_append, with the same q and their lse; rows whose lse is not finite
+ * count for nothing.
+ *   q, q_stride, dtype, new_off, page arguments: as for rs_paged_attn.
+ *   lse      [T, Hq] fp32;  weights [Hkv, n_pages * page_size] fp32 in/out.
+ *   status   [B]: RS_ST_BAD_OFFSET (nothing of the request is added),
+ *            RS_ST_BAD_PAGE (nothing is added in bad pages), RS_ST_TIMEOUT.
+ * Sums are fp32, in a fixed order.
+ */
+size_t rs_paged_weights_workspace_size(int B, int T, int Hq, int Hkv, int D);
+rs_status rs_paged_weights(const uint16_t *q, int64_t q_stride, int dtype, const float *lse,
+                           const int32_t *new_off, int B, int T, int Hq, int Hkv, int D,
+                           const uint16_t *k_pages, int n_pages, int page_size,
+                           const int32_t *page_table, int max_pages, const int32_t *ctx_len,
+                           float scale, float *weights, int32_t *status, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/* ===================================================== rs_paged_evict ====
+ * Cuts every request's cache down to `budget` tokens per KV head.  Of the
+ * slots s < cache_len[b] of a head those stay that come first in the order:
+ * recent ones (position >= next_pos[b] - recent), then higher weight (NaN
+ * last), then lower slot.  Kept tokens behind slot `budget` move into the
+ * slots below it that are given up, both in ascending order: K, V, weight and
+ * position; everything else below the budget stays where it is, and what lies
+ * behind it is left as it is.  A request of at most `budget` tokens is not
+ * touched.
+ *   cache_len, next_pos [B] int32: tokens in the cache; position of the next
+ *            token (tokens seen so far).
+ *   budget >= 1;  0 <= recent <= budget;  B * Hkv <= 65535.
+ *   weights, positions: see above, both needed; in/out.
+ *   new_len  [B] int32 out: min(cache_len, budget).
+ *   status   [B]: RS_ST_BAD_OFFSET, RS_ST_BAD_PAGE: the request is left as it
+ *            is (new_len = cache_len).
+ * No page may belong to two requests of the call.
+ */
+size_t rs_paged_evict_workspace_size(int B, int Hkv, int budget);
+rs_status rs_paged_evict(uint16_t *k_pages, uint16_t *v_pages, int Hkv, int D, int n_pages,
+                         int page_size, const int32_t *page_table, int max_pages,
+                         const int32_t *cache_len, const int32_t *next_pos, int B, int budget,
+                         int recent, float *weights, int32_t *positions, int32_t *new_len,
+                         int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,7 +25,7 @@
 #define RS_ENTRIES(X)                                                                                            \
     X(entropy_gate) X(entropy_gate_noalloc) X(entropy_gate_rows) X(match_scan) X(tree_verify_attn) X(accept)     \
     X(match_index_build) X(match_index_append) X(match_scan_indexed) X(tree_sample) X(prompt_attn) X(paged_append)  \
-    X(paged_attn)
+    X(paged_attn) X(paged_weights) X(paged_evict)
 
 namespace {
 
@@ -527,6 +527,50 @@ RS_BIND(paged_attn) {
         return [=] {
             return lib.paged_attn(q, qs, dtype, off, parents, B, T, Hq, Hkv, D, kp, vp, pages, size, table, most, ctx, scale, out, lse,
                                   status, ws, wb, st);
+        };
+    });
+}
+
+RS_BIND(paged_weights) {
+    return guarded(v, n, [](Args &a) {
+        int64_t qs;
+        auto *q = a.rows(&qs);
+        const int dtype = a.i32();
+        auto *lse = a.ptr<const float>();
+        auto *off = a.ptr<const int32_t>();
+        const int B = a.i32(), T = a.i32(), Hq = a.i32(), Hkv = a.i32(), D = a.i32();
+        auto *kp = a.ptr<const uint16_t>();
+        const int pages = a.i32(), size = a.i32();
+        auto *table = a.ptr<const int32_t>();
+        const int most = a.i32();
+        auto *ctx = a.ptr<const int32_t>();
+        const float scale = a.f32();
+        auto *weights = a.ptr<float>();
+        auto *status = a.ptr<int32_t>();
+        size_t wb;
+        void *ws = a.sized(&wb, true), *st = a.stream();
+        return [=] {
+            return lib.paged_weights(q, qs, dtype, lse, off, B, T, Hq, Hkv, D, kp, pages, size, table, most, ctx, scale, weights,
+                                     status, ws, wb, st);
+        };
+    });
+}
+
+RS_BIND(paged_evict) {
+    return guarded(v, n, [](Args &a) {
+        auto *kp = a.ptr<uint16_t>(), *vp = a.ptr<uint16_t>();
+        const int Hkv = a.i32(), D = a.i32(), pages = a.i32(), size = a.i32();
+        auto *table = a.ptr<const int32_t>();
+        const int most = a.i32();
+        auto *len = a.ptr<const int32_t>(), *next = a.ptr<const int32_t>();
+        const int B = a.i32(), budget = a.i32(), recent = a.i32();
+        auto *weights = a.ptr<float>();
+        auto *positions = a.ptr<int32_t>(), *new_len = a.ptr<int32_t>(), *status = a.ptr<int32_t>();
+        size_t wb;
+        void *ws = a.sized(&wb, true), *st = a.stream();
+        return [=] {
+            return lib.paged_evict(kp, vp, Hkv, D, pages, size, table, most, len, next, B, budget, recent, weights, positions, new_len,
+                                   status, ws, wb, st);
         };
     });
 }

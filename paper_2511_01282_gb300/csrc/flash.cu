@@ -103,7 +103,7 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
         plan_tree(a, parents, anc, blockIdx.x - 1);
         return;
     }
-    __shared__ int s_pref[kFlMaxB + 1];  // pairs before each request
+    __shared__ int s_pref[kBatchMax + 1];  // pairs before each request
     __shared__ int s_wi[32];
     __shared__ long long s_wl[32];
     const int tid = threadIdx.x;
@@ -202,34 +202,11 @@ Work carve(void *base, int B, int T, int Hq, int Hkv, int D) {
 }
 
 bool sizes_ok(int B, int T, int Hq, int Hkv, int D) {
-    return B >= 0 && T >= 0 && Hkv >= 1 && Hq >= 1 && Hq % Hkv == 0 && Hq / Hkv <= kBM && (D == 64 || D == 128) && B <= kFlMaxB;
+    return B >= 0 && T >= 0 && Hkv >= 1 && Hq >= 1 && Hq % Hkv == 0 && Hq / Hkv <= kBM && (D == 64 || D == 128) && B <= kBatchMax;
 }
 
 size_t workspace_size(int B, int T, int Hq, int Hkv, int D) {
     return sizes_ok(B, T, Hq, Hkv, D) ? carve(nullptr, B, T, Hq, Hkv, D).bytes : 0;
-}
-
-rs_status check_sizes(const char *what, int dtype, int B, int T, int Hq, int Hkv, int D, float scale) {
-    RS_CHECK_ARG(B >= 0 && T >= 0, "%s: negative size", what);
-    RS_CHECK_ARG(dtype == RS_BF16 || dtype == RS_F16, "%s: dtype %d is neither RS_BF16 nor RS_F16", what, dtype);
-    if (D != 64 && D != 128) {
-        set_error("%s: head dim %d unsupported (64 or 128)", what, D);
-        return RS_ERR_UNSUPPORTED;
-    }
-    if (Hkv < 1 || Hq < 1 || Hq % Hkv != 0 || Hq / Hkv > kBM) {
-        set_error("%s: Hq=%d must be a multiple of Hkv=%d, 1 to %d times", what, Hq, Hkv, kBM);
-        return RS_ERR_UNSUPPORTED;
-    }
-    RS_CHECK_ARG(B <= kFlMaxB, "%s: B=%d above %d", what, B, kFlMaxB);
-    RS_CHECK_ARG(isfinite(scale) && scale > 0.f, "%s: scale must be finite and > 0", what);
-    return RS_OK;
-}
-
-rs_status check_stride(const char *what, const char *name, const void *p, int64_t stride, int heads, int D) {
-    RS_CHECK_ARG((reinterpret_cast<uintptr_t>(p) & 15) == 0, "%s: %s must be 16-byte aligned", what, name);
-    RS_CHECK_ARG(stride >= (int64_t)heads * D && stride % 8 == 0 && stride < (1ll << 38),
-                 "%s: %s rows of %lld elements: at least heads x D, a multiple of 8", what, name, (long long)stride);
-    return RS_OK;
 }
 
 // The launches of both calls.  a: everything but what comes out of the sizes.

@@ -38,7 +38,6 @@ namespace rs {
 constexpr int kFlThreads = 384;
 constexpr uint32_t kFlRegsSoft = 216, kFlRegsProd = 72;
 static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "register split");
-constexpr int kFlMaxB = 4096;     // requests per call (their prefix lives in the plan's shared memory)
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
 constexpr int kFlRows = 2 * kBM;  // rows of a segment and of a partial slot
 constexpr int kFlWF = 5, kFlWH = 3;  // cost of a key tile for a pair and for a single row tile

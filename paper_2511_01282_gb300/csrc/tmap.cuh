@@ -4,6 +4,7 @@
 
 #include <cuda.h>
 #include <cudaTypedefs.h>
+#include <math.h>
 #include <stdlib.h>
 
 #include <algorithm>
@@ -47,6 +48,31 @@ inline int page_log2(int page_size) {
     int l = 0;
     while ((1 << l) < page_size) ++l;
     return l;
+}
+
+// Sizes and types that the attention calls share.
+constexpr int kBatchMax = 4096;  // requests per call (a prefix over them lives in shared memory)
+inline rs_status check_sizes(const char *what, int dtype, int B, int T, int Hq, int Hkv, int D, float scale) {
+    RS_CHECK_ARG(B >= 0 && T >= 0, "%s: negative size", what);
+    RS_CHECK_ARG(dtype == RS_BF16 || dtype == RS_F16, "%s: dtype %d is neither RS_BF16 nor RS_F16", what, dtype);
+    if (D != 64 && D != 128) {
+        set_error("%s: head dim %d unsupported (64 or 128)", what, D);
+        return RS_ERR_UNSUPPORTED;
+    }
+    if (Hkv < 1 || Hq < 1 || Hq % Hkv != 0 || Hq / Hkv > kBM) {
+        set_error("%s: Hq=%d must be a multiple of Hkv=%d, 1 to %d times", what, Hq, Hkv, kBM);
+        return RS_ERR_UNSUPPORTED;
+    }
+    RS_CHECK_ARG(B <= kBatchMax, "%s: B=%d above %d", what, B, kBatchMax);
+    RS_CHECK_ARG(isfinite(scale) && scale > 0.f, "%s: scale must be finite and > 0", what);
+    return RS_OK;
+}
+
+inline rs_status check_stride(const char *what, const char *name, const void *p, int64_t stride, int heads, int D) {
+    RS_CHECK_ARG((reinterpret_cast<uintptr_t>(p) & 15) == 0, "%s: %s must be 16-byte aligned", what, name);
+    RS_CHECK_ARG(stride >= (int64_t)heads * D && stride % 8 == 0 && stride < (1ll << 38),
+                 "%s: %s rows of %lld elements: at least heads x D, a multiple of 8", what, name, (long long)stride);
+    return RS_OK;
 }
 
 // A page holds a power of two of tokens, 8 at least (one swizzle atom of a TMA

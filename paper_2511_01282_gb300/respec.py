@@ -87,6 +87,12 @@ _SIGS = {
     "rs_paged_attn_workspace_size": (C.c_size_t, [C.c_int] * 5),
     "rs_paged_attn": (C.c_int, [_P, C.c_int64, C.c_int] + [_P] * 2 + [C.c_int] * 5 + [_P] * 2 + [C.c_int] * 2
                       + [_P, C.c_int, _P, C.c_float] + [_P] * 4 + [C.c_size_t, _P]),
+    "rs_paged_weights_workspace_size": (C.c_size_t, [C.c_int] * 5),
+    "rs_paged_weights": (C.c_int, [_P, C.c_int64, C.c_int] + [_P] * 2 + [C.c_int] * 5 + [_P] + [C.c_int] * 2
+                         + [_P, C.c_int, _P, C.c_float] + [_P] * 3 + [C.c_size_t, _P]),
+    "rs_paged_evict_workspace_size": (C.c_size_t, [C.c_int] * 3),
+    "rs_paged_evict": (C.c_int, [_P] * 2 + [C.c_int] * 4 + [_P, C.c_int] + [_P] * 2 + [C.c_int] * 3 + [_P] * 5
+                       + [C.c_size_t, _P]),
     "rs_entropy_gate_rows": (C.c_int, [_P, _P, _P, C.c_int, rs_params, _P, _P, _P, _P, _P, _P]),
 }
 
@@ -268,3 +274,25 @@ def rs_paged_attn(q, q_stride, dtype, new_off, parents, B, T, Hq, Hkv, D, k_page
     _check((_bind or _native()).rs_paged_attn(q, q_stride, dtype, new_off, parents, B, T, Hq, Hkv, D, k_pages,
                                               v_pages, n_pages, page_size, page_table, max_pages, ctx_len, scale,
                                               out, lse, status, workspace, stream))
+
+
+def rs_paged_weights_workspace_size(B, T, Hq, Hkv, D):
+    return int(lib().rs_paged_weights_workspace_size(B, T, Hq, Hkv, D))
+
+
+def rs_paged_weights(q, q_stride, dtype, lse, new_off, B, T, Hq, Hkv, D, k_pages, n_pages, page_size, page_table,
+                     max_pages, ctx_len, scale, weights, status, workspace, stream=None):
+    _check((_bind or _native()).rs_paged_weights(q, q_stride, dtype, lse, new_off, B, T, Hq, Hkv, D, k_pages,
+                                                 n_pages, page_size, page_table, max_pages, ctx_len, scale,
+                                                 weights, status, workspace, stream))
+
+
+def rs_paged_evict_workspace_size(B, Hkv, budget):
+    return int(lib().rs_paged_evict_workspace_size(B, Hkv, budget))
+
+
+def rs_paged_evict(k_pages, v_pages, Hkv, D, n_pages, page_size, page_table, max_pages, cache_len, next_pos, B,
+                   budget, recent, weights, positions, new_len, status, workspace, stream=None):
+    _check((_bind or _native()).rs_paged_evict(k_pages, v_pages, Hkv, D, n_pages, page_size, page_table,
+                                               max_pages, cache_len, next_pos, B, budget, recent, weights,
+                                               positions, new_len, status, workspace, stream))

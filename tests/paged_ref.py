@@ -63,3 +63,36 @@ def check(got, want, tol, what):
     err = (got.to(F64) - want).abs()
     bad = ~(err <= tol)
     assert not bad.any(), "%s: %d of %d off; worst %g against %g" % (what, int(bad.sum()), bad.numel(), float(err.max()), float(tol.max()))
+
+
+def weights(q, k, lse, see, scale):
+    """[Hkv, m]: the weight that the rows give to each key, and the bound of its error in fp32."""
+    n, Hq, D = q.shape
+    Hkv = k.shape[1]
+    G = Hq // Hkv
+    total = torch.zeros(Hkv, k.shape[0], dtype=F64, device=q.device)
+    tol = torch.zeros_like(total)
+    see = see.to(q.device)
+    for h in range(Hq):
+        Q, K, z = q[:, h].to(F64), k[:, h // G].to(F64), lse[:, h].to(F64)
+        on = see & torch.isfinite(z)[:, None]
+        p = torch.where(on, torch.exp(Q @ K.T * scale - torch.where(torch.isfinite(z), z, 0.0)[:, None]), 0.0)
+        reach = Q.abs() @ K.abs().T * scale + z.abs()[:, None]
+        e = 2.0 * (D * 2.0 ** -23 * torch.where(on, reach, 0.0) + 2.0 ** -20)
+        total[h // G] += p.sum(0)
+        tol[h // G] += (p * (e + 2.0 ** -24 * n * G)).sum(0)  # n G fp32 additions at most
+    return total, tol
+
+
+def evict_order(weights, positions, next_pos, recent, budget):
+    """Which slots of one (request, head) stay, by the definition: host lists."""
+    def place(s):
+        if positions[s] >= next_pos - recent:
+            return (0, 0, 0.0, s)
+        return (1, 1, 0.0, s) if math.isnan(weights[s]) else (1, 0, -weights[s], s)
+
+    rank = sorted(range(len(weights)), key=place)
+    kept = set(rank[:budget])
+    holes = [s for s in range(budget) if s not in kept]
+    movers = [s for s in range(budget, len(weights)) if s in kept]
+    return list(zip(movers, holes))
