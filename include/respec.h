@@ -436,8 +436,8 @@ rs_status rs_tree_sample(const float *logits, int R, int V, const int32_t *node_
  *   seq_off  [B+1] int32; sequences may have no rows; B <= 4096.
  *   D in {64, 128}; Hq a multiple of Hkv, at most 128 times (query head h
  *   reads KV head h / (Hq / Hkv)); scale > 0.
- *   out      [T, Hq, D] of type dtype;  lse [T, Hq] fp32;  rows behind the
- *            last sequence are left as they are.
+ *   out      [T, Hq, D] of type dtype, 32-byte aligned;  lse [T, Hq] fp32;
+ *            rows behind the last sequence are left as they are.
  *   status   [B]: RS_ST_BAD_OFFSET for a range outside [0, T) or one that
  *            starts before an earlier sequence does (its own rows, where they
  *            lie inside, are zeroed); RS_ST_TIMEOUT.
@@ -499,8 +499,8 @@ rs_status rs_paged_append(const uint16_t *k, int64_t k_stride, const uint16_t *v
  *            [T] int32 as for rs_tree_verify_attn (at most RS_MAX_NODES rows a
  *            request): row i sees the ctx_len[b] cached slots, and of the new
  *            ones its ancestors and itself.
- *   out      [T, Hq, D] of type dtype;  lse [T, Hq] fp32;  rows behind the
- *            last request are left as they are.
+ *   out      [T, Hq, D] of type dtype, 32-byte aligned;  lse [T, Hq] fp32;
+ *            rows behind the last request are left as they are.
  *   status   [B]: RS_ST_BAD_OFFSET, RS_ST_BAD_PAGE, RS_ST_BAD_TREE,
  *            RS_ST_TOO_LARGE (the request's rows are zeroed), RS_ST_TIMEOUT.
  * Types, arithmetic, B, head counts, alignment: as for rs_prompt_attn.  What

@@ -133,7 +133,7 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
             if (!a.anc) a.status[b] = st;
         }
         long long t = 0;
-        if (rq.y > 0) t = (long long)mine * (pair_keys(a, rq, 0) + pair_keys(a, rq, mine - 1)) / (2 * kBN) + 1;
+        if (rq.y > 0) t = (long long)mine * (pair_keys(a, rq.y, rq.z, 0) + (long long)pair_keys(a, rq.y, rq.z, mine - 1)) / (2 * kBN) + 1;
         block_scan(t, tiles, s_wl);
     }
     if (tid == 0) s_pref[0] = 0;
@@ -152,8 +152,11 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
                 if (s_pref[mid] <= i) lo = mid;
                 else hi = mid - 1;
             }
-            a.ent[i] = make_int2(lo, i - s_pref[lo]);
-            cost = seg_cost(a, a.req[lo], i - s_pref[lo], beta);
+            const int4 rq = a.req[lo];
+            const int p = i - s_pref[lo];
+            a.ent[i] = make_int4(lo, p, rq.x, rq.y);
+            a.ent_ctx[i] = rq.z;
+            cost = tile_cost(a, rq.y, p) * pair_tiles(a, rq.y, rq.z, p) + beta;
         }
         const long long end = block_scan(cost, carry, s_wl);
         if (i < M) a.cum[i + 1] = end;
@@ -190,7 +193,8 @@ Work carve(void *base, int B, int T, int Hq, int Hkv, int D) {
     Carve cv(base);
     a.req = cv.take<int4>((size_t)B);
     a.cum = cv.take<long long>(pairs + 1);
-    a.ent = cv.take<int2>(pairs);
+    a.ent = cv.take<int4>(pairs);
+    a.ent_ctx = cv.take<int>(pairs);
     a.n_pairs = cv.take<int>(2);
     a.bound = cv.take<int4>(F * (grid + 1));
     w.anc = cv.take<uint32_t>((size_t)T * kAncWords);
@@ -258,7 +262,7 @@ extern "C" rs_status rs_prompt_attn(const uint16_t *q, int64_t q_stride, const u
     if ((st = check_stride(what, "q", q, q_stride, Hq, D)) != RS_OK) return st;
     if ((st = check_stride(what, "k", k, k_stride, Hkv, D)) != RS_OK) return st;
     if ((st = check_stride(what, "v", v, v_stride, Hkv, D)) != RS_OK) return st;
-    RS_CHECK_ARG((((uintptr_t)out | (uintptr_t)workspace) & 15) == 0, "%s: out and workspace must be 16-byte aligned", what);
+    RS_CHECK_ARG((((uintptr_t)out | (uintptr_t)workspace) & 31) == 0, "%s: out and workspace must be 32-byte aligned", what);
     if (B == 0) return RS_OK;
     Work w = carve(workspace, B, T, Hq, Hkv, D);
     if (workspace_bytes < w.bytes || !workspace) {
@@ -300,7 +304,7 @@ extern "C" rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtyp
     RS_CHECK_ARG(n_pages == 0 || (k_pages && v_pages), "%s: null page pointer", what);
     if ((st = check_stride(what, "q", q, q_stride, Hq, D)) != RS_OK) return st;
     RS_CHECK_ARG((((uintptr_t)k_pages | (uintptr_t)v_pages) & 15) == 0, "%s: pages must be 16-byte aligned", what);
-    RS_CHECK_ARG((((uintptr_t)out | (uintptr_t)workspace) & 15) == 0, "%s: out and workspace must be 16-byte aligned", what);
+    RS_CHECK_ARG((((uintptr_t)out | (uintptr_t)workspace) & 31) == 0, "%s: out and workspace must be 32-byte aligned", what);
     if (B == 0) return RS_OK;
     Work w = carve(workspace, B, T, Hq, Hkv, D);
     if (workspace_bytes < w.bytes || !workspace) {

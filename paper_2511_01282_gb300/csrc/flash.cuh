@@ -22,27 +22,41 @@
 // not stay in L2).  A segment cut by a share's end leaves partial (O, m, l),
 // which flash_combine joins in key order: no atomics, the same bits each run.
 //
-// Warps: 0-3 softmax of row tile A (thread = row), 4-7 of tile B, 8 TMA, 9 MMA
-// issue, 10-11 idle (they only give registers up).  A pair whose second tile
-// is empty runs in half mode: A's S is double buffered.  Tensor memory: O_A
-// [0, 128), O_B [128, 256), S/P buffers [256, 384) and [384, 512).
+// Warps: 0 and 1 MMA issue for row tiles A and B, 2 TMA, 3 idle (it only gives
+// registers up), 4-7 softmax of tile A (thread = row), 8-11 of tile B.  Tensor memory (512 columns):
+//   D = 64: O_A O_B (64 each), S_A S_B (128 each), P_A P_B (64 each).  S of the
+//     next key tile is issued as soon as its softmax has read the last one, so
+//     that a softmax finds its next S ready and the exponentials bound the loop.
+//   D = 128: O_A O_B (128 each), S_A S_B (128 each), P written over S: S of the
+//     next tile follows P V of this one.  The two row tiles take turns, and P goes
+//     to the product in two halves.
 #pragma once
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "attn_core.cuh"
 
 namespace rs {
 
 constexpr int kFlThreads = 384;
-constexpr uint32_t kFlRegsSoft = 216, kFlRegsProd = 72;
+constexpr int kFlMmaWarp = 0, kFlTmaWarp = 2, kFlSoftWarp = 4;  // two warps issue products
+constexpr uint32_t kFlRegsSoft = 224, kFlRegsProd = 56;
 static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "register split");
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
 constexpr int kFlRows = 2 * kBM;  // rows of a segment and of a partial slot
 constexpr int kFlWF = 5, kFlWH = 3;  // cost of a key tile for a pair and for a single row tile
 constexpr int kFlSegCost = 8;        // cost of a segment's start, in single-tile key tiles, at most
-constexpr uint32_t kFlTmS = 256;
+// Tensor memory columns
+template <int D>
+struct FlTm {
+    static constexpr bool kApart = D == 64;  // P has columns of its own
+    __host__ __device__ static constexpr uint32_t o(int x) { return (uint32_t)(x * D); }
+    __host__ __device__ static constexpr uint32_t s(int x) { return (uint32_t)(2 * D + x * 128); }
+    __host__ __device__ static constexpr uint32_t p(int x) { return kApart ? (uint32_t)(384 + x * 64) : s(x); }
+};
 
 struct FlashArgs {
     const int32_t *off, *ctx;    // ctx: null for prompts
@@ -51,7 +65,8 @@ struct FlashArgs {
     int max_pages, n_pages, page_log2;
     int4 *req;                   // per request: first row, rows (0: rejected), ctx
     long long *cum;              // [pairs + 1] cost prefix of the pairs of one KV head
-    int2 *ent;                   // [pairs] (request, pair)
+    int4 *ent;                   // [pairs] request, pair, first row and rows of the request
+    int *ent_ctx;                // [pairs] its ctx
     int *n_pairs;
     int4 *bound;                 // [phase][CTA] where the CTA's share starts: (head in phase, pair, tile)
     float *part_o, *part_m, *part_l;
@@ -65,9 +80,16 @@ struct FlashArgs {
     long long wait_limit;
 };
 
-// keys of pair p of a request: what its last token sees
-__device__ __forceinline__ int pair_keys(const FlashArgs &a, int4 rq, int p) {
-    return rq.z + (a.anc ? rq.y : min(rq.y, (p + 1) * 2 * a.tq));
+// keys of pair p of a request of n rows behind ctx: what its last token sees
+__device__ __forceinline__ int pair_keys(const FlashArgs &a, int n, int ctx, int p) {
+    return ctx + (a.anc ? n : min(n, (p + 1) * 2 * a.tq));
+}
+__device__ __forceinline__ int pair_tiles(const FlashArgs &a, int n, int ctx, int p) {
+    return (pair_keys(a, n, ctx, p) + kBN - 1) / kBN;
+}
+// cost of one of its key tiles
+__device__ __forceinline__ int tile_cost(const FlashArgs &a, int n, int p) {
+    return n - p * 2 * a.tq > a.tq ? kFlWF : kFlWH;
 }
 
 struct FlPiece {
@@ -77,50 +99,55 @@ struct FlPiece {
     bool full;                    // the second row tile has rows
 };
 
-// A CTA's pieces in order; every role walks them by itself.
+// A CTA's pieces in order; every role walks them by itself.  The next piece's
+// record is loaded a piece ahead.
 struct FlCursor {
     const FlashArgs &a;
     const int4 *bounds;  // shared: [phase][2]
-    int M, f = -1, s = 0, t = 0, s_end = -1, t_end = 0;
+    int M, f = -1, hh = 0, i = 0, t = 0;  // phase, head in it, pair, key tile
+    int hh_end = -1, i_end = 0, t_end = 0;
+    int at = -1, ctx = 0;                 // the pair whose record is at hand
+    int4 e;
     __device__ __forceinline__ FlCursor(const FlashArgs &a_, const int4 *b, int M_) : a(a_), bounds(b), M(M_) {}
+    __device__ __forceinline__ void load(int k) {
+        at = k;
+        e = a.ent[k];
+        ctx = a.ent_ctx[k];
+    }
     __device__ __forceinline__ bool next(FlPiece &pc) {
-        for (;;) {
-            if (s > s_end || (s == s_end && t >= t_end)) {
-                if (++f >= a.phases) return false;
-                const int4 lo = bounds[2 * f], hi = bounds[2 * f + 1];
-                s = lo.x * M + lo.y;
-                t = lo.z;
-                s_end = hi.x * M + hi.y;
-                t_end = hi.z;
-                continue;
-            }
-            const int hh = s / M;
-            const int2 e = a.ent[s - hh * M];
-            const int4 rq = a.req[e.x];
-            pc.b = e.x;
-            pc.p = e.y;
-            pc.n0 = rq.x;
-            pc.n = rq.y;
-            pc.ctx = rq.z;
-            pc.kvh = f * a.Hkv / a.phases + hh;
-            pc.keys = pair_keys(a, rq, e.y);
-            const int nt = (pc.keys + kBN - 1) / kBN;
-            pc.j0 = t;
-            pc.j1 = s == s_end ? t_end : nt;
-            pc.full = rq.y - e.y * 2 * a.tq > a.tq;
-            const int share = 2 * (f * a.grid + (int)blockIdx.x);
-            pc.slot = t > 0 ? share : (pc.j1 < nt ? share + 1 : -1);
-            ++s;
-            t = 0;
-            return true;
+        while (hh > hh_end || (hh == hh_end && (i > i_end || (i == i_end && t >= t_end)))) {
+            if (++f >= a.phases) return false;
+            const int4 lo = bounds[2 * f], hi = bounds[2 * f + 1];
+            hh = lo.x;
+            i = lo.y;
+            t = lo.z;
+            hh_end = hi.x;
+            i_end = hi.y;
+            t_end = hi.z;
         }
+        if (at != i) load(i);
+        pc.b = e.x;
+        pc.p = e.y;
+        pc.n0 = e.z;
+        pc.n = e.w;
+        pc.ctx = ctx;
+        pc.kvh = f * a.Hkv / a.phases + hh;
+        pc.keys = pair_keys(a, e.w, ctx, e.y);
+        const int nt = (pc.keys + kBN - 1) / kBN;
+        pc.j0 = t;
+        pc.j1 = hh == hh_end && i == i_end ? t_end : nt;
+        pc.full = e.w - e.y * 2 * a.tq > a.tq;
+        const int share = 2 * (f * a.grid + (int)blockIdx.x);
+        pc.slot = t > 0 ? share : (pc.j1 < nt ? share + 1 : -1);
+        t = 0;
+        if (++i == M) {
+            i = 0;
+            ++hh;
+        }
+        load(i);
+        return true;
     }
 };
-
-__device__ __forceinline__ int seg_cost(const FlashArgs &a, int4 rq, int p, int beta) {
-    const int w = rq.y - p * 2 * a.tq > a.tq ? kFlWF : kFlWH;
-    return w * ((pair_keys(a, rq, p) + kBN - 1) / kBN) + beta;
-}
 
 // Where cost position x of a phase of hn heads falls: (head, pair, tile).
 // Whole warp; the pair is searched 32 ways at a time.
@@ -137,11 +164,9 @@ __device__ __forceinline__ int4 fl_locate(const FlashArgs &a, long long x, int h
         lo += (31 - __clz(m)) * step;
         hi = min(lo + step, hi);
     }
-    const int2 e = a.ent[lo];
-    const int4 rq = a.req[e.x];
-    const int w = rq.y - e.y * 2 * a.tq > a.tq ? kFlWF : kFlWH;
+    const int4 e = a.ent[lo];
     const long long in = rem - a.cum[lo] - beta;
-    return make_int4(hh, lo, in > 0 ? (int)(in / w) : 0, 0);
+    return make_int4(hh, lo, in > 0 ? (int)(in / tile_cost(a, e.w, e.y)) : 0, 0);
 }
 
 template <bool BF16>
@@ -155,14 +180,79 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
 template <bool BF16>
 constexpr float kFlBias = BF16 ? 0.f : 7.f;
 
+// 64 weights of a row: xp = 2^(c s + nb) in 16 bits, their fp32 sums added to
+// sum4.  The exponentials (4 cycles a warp) bound it; volatile statements keep
+// the other instructions between them, where the compiler's own order puts
+// them into bursts (a probe of two warps per scheduler: 1360 cycles for both
+// warps' 128 weights against 1600).
+template <bool BF16>
+__device__ __forceinline__ void exp_pairs(const uint32_t (&s0)[32], const uint32_t (&s1)[32], float c, float nb,
+                                          float (&sum4)[4], uint32_t (&xp)[32]) {
+    constexpr int kAhead = 4, kBehind = 4;  // pairs
+    float d[64], p[64];
+    auto fma1 = [&](int i) {
+        const float v = __uint_as_float(i < 32 ? s0[i] : s1[i - 32]);
+        asm volatile("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d[i]) : "f"(v), "f"(c), "f"(nb));
+    };
+#pragma unroll
+    for (int i = 0; i < 2 * kAhead; ++i) fma1(i);
+#pragma unroll
+    for (int e = 0; e < 32 + kBehind; ++e) {
+        if (e < 32) {
+            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[2 * e]) : "f"(d[2 * e]));
+            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[2 * e + 1]) : "f"(d[2 * e + 1]));
+        }
+        if (e + kAhead < 32) {
+            fma1(2 * (e + kAhead));
+            fma1(2 * (e + kAhead) + 1);
+        }
+        if (e >= kBehind) {
+            const int q = e - kBehind;
+            asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(sum4[(2 * q) & 3]) : "f"(p[2 * q]));
+            asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(sum4[(2 * q + 1) & 3]) : "f"(p[2 * q + 1]));
+            if (BF16) asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(xp[q]) : "f"(p[2 * q + 1]), "f"(p[2 * q]));
+            else asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(xp[q]) : "f"(p[2 * q + 1]), "f"(p[2 * q]));
+        }
+    }
+}
+
+// Keys whose bit is not set: -inf (whole warp; most chunks are open to all rows).
+__device__ __forceinline__ void hide(uint32_t (&v)[32], uint32_t seen) {
+    if (__all_sync(0xffffffffu, seen == 0xffffffffu)) return;
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        if (!((seen >> e) & 1u)) v[e] = 0xff800000u;
+}
+
+// warp_wait with its usual case, a phase that is complete, on a short path.
+__device__ __forceinline__ bool quick_wait(uint64_t *bar, uint32_t parity, volatile int *abort, long long limit) {
+    if (__builtin_expect(__all_sync(0xffffffffu, sm100::mbar_try_wait(bar, parity)), 1)) return true;
+    return warp_wait(bar, parity, abort, limit);
+}
+
+// Both barriers at once (they may be the same).
+__device__ __forceinline__ bool quick_wait2(uint64_t *b1, uint32_t p1, uint64_t *b2, uint32_t p2, volatile int *abort,
+                                            long long limit) {
+    const bool r1 = sm100::mbar_try_wait(b1, p1), r2 = sm100::mbar_try_wait(b2, p2);
+    if (__builtin_expect(__all_sync(0xffffffffu, r1 && r2), 1)) return true;
+    return warp_wait(b1, p1, abort, limit) && warp_wait(b2, p2, abort, limit);
+}
+
+// 32 bytes in one store (p 32-byte aligned): a whole sector, so that a thread
+// may write its own row.
+__device__ __forceinline__ void store32(void *p, const uint32_t *v) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
 template <int D>
 struct FlSmem {
     static constexpr int kTile = kBN * D * 2;
-    static constexpr int kNS = D == 128 ? 2 : 4;
-    static constexpr int kK = 0, kV = kNS * kTile, kQ = 2 * kNS * kTile;
-    static constexpr int kStage = kQ + 2 * kTile;        // 4 KB per softmax warp
-    static constexpr int kBar = kStage + 8 * 4096;
-    static constexpr int kNumBars = 4 * kNS + 12;
+    static constexpr int kNK = D == 128 ? 3 : 4, kNV = D == 128 ? 2 : 4;  // stages of K and V
+    static constexpr int kK = 0, kV = kNK * kTile, kQ = kV + kNV * kTile;
+    static constexpr int kBar = kQ + 2 * kTile;
+    static constexpr int kNumBars = 2 * kNK + 2 * kNV + 22;
     static constexpr int kMisc = kBar + kNumBars * 8;    // tensor memory base, abort flag
     static constexpr int kBounds = (kMisc + 8 + 15) / 16 * 16;
     static constexpr int kBytes = kBounds + 2 * kFlMaxPhases * 16;
@@ -176,39 +266,49 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
              const __grid_constant__ CUtensorMap tmv) {
     using namespace sm100;
     using S = FlSmem<D>;
-    constexpr int NS = S::kNS;
+    constexpr uint32_t NK = S::kNK, NV = S::kNV;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                             ~uintptr_t(1023));
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kBar);
-    uint64_t *kfull = bars, *vfull = kfull + NS, *kempty = vfull + NS, *vempty = kempty + NS;
-    uint64_t *sfull = vempty + NS, *pfull = sfull + 2, *qfull = pfull + 2, *qfree = qfull + 2;
-    uint64_t *ofree = qfree + 2, *drain = ofree + 1;
+    uint64_t *kfull = bars, *kempty = kfull + NK, *vfull = kempty + NK, *vempty = vfull + NV;
+    // per row tile: S there, S read (kApart), P there (its two halves), P V complete
+    // (its first half), Q there, Q read, O read, turn at the tensor core
+    uint64_t *sfull = vempty + NV, *sfree = sfull + 2, *pfull = sfree + 2, *pfull2 = pfull + 2, *pvdone = pfull2 + 2;
+    uint64_t *phalf = pvdone + 2, *qfull = phalf + 2, *qfree = qfull + 2, *ofree = qfree + 2, *turn = ofree + 2;
+    uint64_t *drain = turn + 2;
     uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + S::kMisc);
     volatile int *s_abort = reinterpret_cast<volatile int *>(smem + S::kMisc + 4);
     int4 *s_bound = reinterpret_cast<int4 *>(smem + S::kBounds);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int s = 0; s < NS; ++s) {
+        for (int s = 0; s < (int)NK; ++s) {
             mbar_init(&kfull[s], 1);
+            mbar_init(&kempty[s], 2);  // a commit for each row tile
+        }
+        for (int s = 0; s < (int)NV; ++s) {
             mbar_init(&vfull[s], 1);
-            mbar_init(&kempty[s], kBM);  // the softmax warps that see the last S reading K arrive
-            mbar_init(&vempty[s], 1);
+            mbar_init(&vempty[s], 2);
         }
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(&sfull[s], 1);
-            mbar_init(&pfull[s], kBM);
-            mbar_init(&qfull[s], 1);
-            mbar_init(&qfree[s], kBM);
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&sfull[x], 1);
+            mbar_init(&sfree[x], kBM);
+            mbar_init(&pfull[x], kBM);
+            mbar_init(&pfull2[x], kBM);
+            mbar_init(&pvdone[x], 1);
+            mbar_init(&qfull[x], 1);
+            mbar_init(&qfree[x], kBM);
+            mbar_init(&ofree[x], kBM);
+            mbar_init(&phalf[x], 1);
+            mbar_init(&turn[x], 1);
+            mbar_init(&drain[x], 1);
         }
-        mbar_init(ofree, kSoftThreads);
-        mbar_init(drain, 1);
         *s_abort = 0;
         fence_mbar_init();
     }
-    if (warp == kMmaWarp) tmem_alloc(s_tmem, kTmemCols);
-    if (warp == kTmaWarp && lane == 0) {
+    if (warp == kFlMmaWarp) tmem_alloc(s_tmem, kTmemCols);
+    if (warp == kFlTmaWarp && lane == 0) {
         prefetch_tmap(&tmq);
         prefetch_tmap(&tmk);
         prefetch_tmap(&tmv);
@@ -231,13 +331,16 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
     const int G = a.G, tq = a.tq;
+    using Tm = FlTm<D>;
+    constexpr bool kApart = Tm::kApart;
+    constexpr int kParts = kApart ? 1 : 2;  // P goes to the product in so many parts
     constexpr int kKB = D / 64;  // 64-column swizzle blocks per row
     FlCursor cur(a, s_bound, M);
     FlPiece pc;
 
-    if (warp >= kTmaWarp) {
+    if (warp < kFlSoftWarp) {
       reg_dealloc<kFlRegsProd>();
-      if (warp == kTmaWarp) {
+      if (warp == kFlTmaWarp) {
         // ---------------------------------------------------------- TMA producer
         // Whole warp: in a paged cache lane x copies page x of the tile.
         const uint32_t q_tx = (uint32_t)(tq * G) * D * 2;
@@ -263,20 +366,19 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             };
             int row = row_of(pc.j0);
             for (int jt = pc.j0; jt < pc.j1; ++jt, ++g) {
-                const int st = (int)(g % NS);
-                const uint32_t free_par = ((g / NS) & 1) ^ 1;
+                const uint32_t ks = g % NK, vs = g % NV;
                 const int next_row = jt + 1 < pc.j1 ? row_of(jt + 1) : -1;
                 const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, row >= 0)) * (uint32_t)(box * D * 2);
-                unsigned char *sk = smem + S::kK + st * S::kTile + lane * box * 128;
-                unsigned char *sv = smem + S::kV + st * S::kTile + lane * box * 128;
-                if (!(ok = warp_wait(&kempty[st], free_par, s_abort, a.wait_limit))) break;
-                if (lane == 0) mbar_expect_tx(&kfull[st], tx);
+                unsigned char *sk = smem + S::kK + ks * S::kTile + lane * box * 128;
+                unsigned char *sv = smem + S::kV + vs * S::kTile + lane * box * 128;
+                if (!(ok = warp_wait(&kempty[ks], ((g / NK) & 1) ^ 1, s_abort, a.wait_limit))) break;
+                if (lane == 0) mbar_expect_tx(&kfull[ks], tx);
                 __syncwarp();
                 if (row >= 0) {
 #pragma unroll
                     for (int kb = 0; kb < kKB; ++kb) {
-                        if (evict) tma_load_3d_hint(sk + kb * 16384, &tmk, &kfull[st], kb * 64, pc.kvh, row, once);
-                        else tma_load_3d(sk + kb * 16384, &tmk, &kfull[st], kb * 64, pc.kvh, row);
+                        if (evict) tma_load_3d_hint(sk + kb * 16384, &tmk, &kfull[ks], kb * 64, pc.kvh, row, once);
+                        else tma_load_3d(sk + kb * 16384, &tmk, &kfull[ks], kb * 64, pc.kvh, row);
                     }
                 }
                 if (jt == pc.j0) {  // the piece's Q tiles, once its previous S products are done with the buffers
@@ -293,38 +395,37 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                         __syncwarp();
                     }
                 }
-                if (!ok || !(ok = warp_wait(&vempty[st], free_par, s_abort, a.wait_limit))) {
+                if (!ok || !(ok = warp_wait(&vempty[vs], ((g / NV) & 1) ^ 1, s_abort, a.wait_limit))) {
                     volatile int no_abort = 0;  // this tile's K copy is in flight: let it land
-                    mbar_wait(&kfull[st], (g / NS) & 1, &no_abort, kWaitLimit);
+                    mbar_wait(&kfull[ks], (g / NK) & 1, &no_abort, kWaitLimit);
                     break;
                 }
-                if (lane == 0) mbar_expect_tx(&vfull[st], tx);
+                if (lane == 0) mbar_expect_tx(&vfull[vs], tx);
                 __syncwarp();
                 if (row >= 0) {
 #pragma unroll
                     for (int kb = 0; kb < kKB; ++kb) {
-                        if (evict) tma_load_3d_hint(sv + kb * 16384, &tmv, &vfull[st], kb * 64, pc.kvh, row, once);
-                        else tma_load_3d(sv + kb * 16384, &tmv, &vfull[st], kb * 64, pc.kvh, row);
+                        if (evict) tma_load_3d_hint(sv + kb * 16384, &tmv, &vfull[vs], kb * 64, pc.kvh, row, once);
+                        else tma_load_3d(sv + kb * 16384, &tmv, &vfull[vs], kb * 64, pc.kvh, row);
                     }
                 }
                 row = next_row;
             }
         }
         if (!ok) {  // let the copies already issued land before the CTA exits
-            for (uint32_t t = g >= NS ? g - NS : 0; t < g; ++t) {
-                volatile int no_abort = 0;
-                mbar_wait(&kfull[t % NS], (t / NS) & 1, &no_abort, kWaitLimit);
-                mbar_wait(&vfull[t % NS], (t / NS) & 1, &no_abort, kWaitLimit);
-            }
+            volatile int no_abort = 0;
+            for (uint32_t t = g >= NK ? g - NK : 0; t < g; ++t) mbar_wait(&kfull[t % NK], (t / NK) & 1, &no_abort, kWaitLimit);
+            for (uint32_t t = g >= NV ? g - NV : 0; t < g; ++t) mbar_wait(&vfull[t % NV], (t / NV) & 1, &no_abort, kWaitLimit);
             for (int x = 0; x < 2; ++x)
-                if (quse[x] > 0) {
-                    volatile int no_abort = 0;
-                    mbar_wait(&qfull[x], (quse[x] - 1) & 1, &no_abort, kWaitLimit);
-                }
+                if (quse[x] > 0) mbar_wait(&qfull[x], (quse[x] - 1) & 1, &no_abort, kWaitLimit);
         }
-      } else if (warp == kMmaWarp) {
-       if (lane == 0) {
-        // ---------------------------------------------------------- MMA issuer
+      } else if (warp <= kFlMmaWarp + 1) {
+        // ---------------------------------------------------------- MMA issuers, one per row tile
+        // The whole warp walks the loop, so that descriptors and addresses are the
+        // same in all lanes and stay in uniform registers; one elected lane issues.
+        // A wait costs some 110 cycles even for a phase that is complete, which two
+        // warps and waits for two barriers at a time keep off the tensor core.
+        const int x = warp - kFlMmaWarp;
         constexpr uint32_t idS = idesc_16_f32(BF16, kBM, kBN, false);
         constexpr uint32_t idO = idesc_16_f32(BF16, kBM, D, true);
         const uint64_t dK0 = sdesc_sw128(smem_u32(smem + S::kK), 16, 1024);
@@ -333,302 +434,303 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
         const uint32_t q_lo0 = (uint32_t)sdesc_sw128(smem_u32(smem + S::kQ), 16, 1024);
         const uint32_t v_lo0 = (uint32_t)sdesc_sw128(smem_u32(smem + S::kV), 16384, 1024);
         constexpr uint32_t kTileDesc = S::kTile >> 4;
-        uint32_t g = 0, use0 = 0, use1 = 0, quse0 = 0, quse1 = 0;
-        int piece = 0;
+        const uint32_t tm = uniform(tmem), xu = uniform((uint32_t)x);
+        const uint32_t q_lo = q_lo0 + xu * kTileDesc, s_tm = tm + Tm::s(0) + xu * 128;
+        const uint32_t o_tm = tm + Tm::o(0) + xu * D, p_tm = tm + Tm::p(0) + xu * (kApart ? 64 : 128);
+        uint32_t g = 0, done = 0, pieces = 0, turns = 0;  // key tiles of the CTA; key tiles, pieces of this row tile
         bool ok = true;
-        // S of key tile t for row tile x into buffer buf
-        auto issue_s = [=](uint32_t t, int x, int buf) {
-            uint32_t k_lo = k_lo0 + (t % NS) * kTileDesc, q_lo = q_lo0 + (uint32_t)x * kTileDesc;
-            asm volatile("" : "+r"(k_lo), "+r"(q_lo));  // offsets rebuilt per burst, not kept for every stage
-            const uint32_t d_s = tmem + kFlTmS + (uint32_t)buf * 128;
+        auto wait = [&](uint64_t *b1, uint32_t p1, uint64_t *b2, uint32_t p2) -> bool {
+            return ok = quick_wait2(b1, p1 & 1, b2, p2 & 1, s_abort, a.wait_limit);
+        };
+        // S of key tile t (K and, at D = 64, S's columns are there)
+        auto issue_s = [&](uint32_t t) {
+            tc_fence_after();
+            const uint32_t k_lo = uniform(k_lo0 + (t % NK) * kTileDesc);
+            if (elect_one()) {
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t off = (uint32_t)(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4);
-                umma_ss(d_s, desc_of(q_lo + off, d_hi), desc_of(k_lo + off, d_hi), idS, kk > 0);
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint32_t off = (uint32_t)(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4);
+                    umma_ss(s_tm, desc_of(q_lo + off, d_hi), desc_of(k_lo + off, d_hi), idS, kk > 0);
+                }
+                umma_commit(&sfull[x]);
+                umma_commit(&kempty[t % NK]);
+                if (!pc.full) umma_commit(&kempty[t % NK]);  // for the row tile that is not there
             }
-            umma_commit(&sfull[buf]);
+            __syncwarp();
         };
-        // O of row tile x += P (buffer buf) V of key tile t
-        auto issue_pv = [=](uint32_t t, int x, int buf, bool acc) {
-            uint32_t v_lo = v_lo0 + (t % NS) * kTileDesc;
-            asm volatile("" : "+r"(v_lo));
-            const uint32_t p_tm = tmem + kFlTmS + (uint32_t)buf * 128;
-#pragma unroll
-            for (int ks = 0; ks < kBN / 16; ++ks)
-                umma_ts(tmem + (uint32_t)x * 128, p_tm + ks * 8, desc_of(v_lo + (uint32_t)((ks * 2048) >> 4), d_hi), idO,
-                        (acc || ks > 0) ? 1u : 0u);
-        };
-        auto wait = [&](uint64_t *bar, uint32_t par) -> bool { return ok = mbar_wait(bar, par & 1, s_abort, a.wait_limit); };
         while (ok && cur.next(pc)) {
             const int n = pc.j1 - pc.j0;
-            if (!wait(&qfull[0], quse0++)) break;
-            if (pc.full && !wait(&qfull[1], quse1++)) break;
-            if (!wait(&kfull[g % NS], g / NS)) break;
-            tc_fence_after();
-            issue_s(g, 0, 0);
-            if (pc.full) issue_s(g, 1, 1);
-            for (int tl = 0; tl < n; ++tl) {
-                const uint32_t t = g + tl;
-                const bool more = tl + 1 < n;
-                const int b = pc.full ? 0 : tl & 1;
-                if (!pc.full && more) {
-                    if (!wait(&kfull[(t + 1) % NS], (t + 1) / NS)) break;
-                    tc_fence_after();
-                    issue_s(t + 1, 0, b ^ 1);
-                }
-                if (!wait(&pfull[b], pc.full ? use0 + tl : (b ? use1 : use0) + (tl >> 1))) break;
-                if (!wait(&vfull[t % NS], t / NS)) break;
-                if (tl == 0 && piece > 0 && !wait(ofree, (uint32_t)(piece - 1))) break;
-                tc_fence_after();
-                issue_pv(t, 0, b, tl > 0);
-                if (pc.full) {
-                    if (more) {
-                        if (!wait(&kfull[(t + 1) % NS], (t + 1) / NS)) break;
-                        tc_fence_after();
-                        issue_s(t + 1, 0, 0);
-                    }
-                    if (!wait(&pfull[1], use1 + tl)) break;
-                    tc_fence_after();
-                    issue_pv(t, 1, 1, tl > 0);
-                }
-                umma_commit(&vempty[t % NS]);
-                if (pc.full && more) issue_s(t + 1, 1, 1);
+            if (x == 1 && !pc.full) {
+                g += n;
+                continue;
             }
-            use0 += pc.full ? n : (n + 1) >> 1;
-            use1 += pc.full ? n : n >> 1;
+            if (!wait(&kfull[g % NK], g / NK, &qfull[x], pieces)) break;
+            if (kApart && done > 0 && !wait(&sfree[x], done - 1, &sfree[x], done - 1)) break;
+            issue_s(g);
+#pragma unroll 1
+            for (int tl = 0; tl < n; ++tl, ++done) {
+                const uint32_t t = g + tl, st = t % NV;
+                const bool more = tl + 1 < n;
+                if (kApart) {  // S of the next tile goes ahead of this one's P V
+                    if (more) {
+                        if (!wait(&kfull[(t + 1) % NK], (t + 1) / NK, &sfree[x], done)) break;
+                        issue_s(t + 1);
+                    }
+                    if (!wait(&vfull[st], t / NV, &pfull[x], done)) break;
+                } else {
+                    // what does not depend on the softmax first; then P and, where both row
+                    // tiles are at work, the turn: they alternate, so that one's softmax
+                    // runs beside the other's products
+                    const uint32_t tn = t + 1;
+                    if (!wait(&vfull[st], t / NV, more ? &kfull[tn % NK] : &vfull[st], more ? tn / NK : t / NV)) break;
+                    const bool must = pc.full && (x == 1 || turns > 0);
+                    if (!wait(&pfull[x], done, must ? &turn[x] : &pfull[x], must ? turns - (x == 0 ? 1 : 0) : done)) break;
+                }
+                if (tl == 0 && pieces > 0 && !wait(&ofree[x], pieces - 1, &ofree[x], pieces - 1)) break;
+                tc_fence_after();
+                const uint32_t v_lo = uniform(v_lo0 + st * kTileDesc);
+#pragma unroll
+                for (int part = 0; part < kParts; ++part) {
+                    if (part > 0) {
+                        if (!wait(&pfull2[x], done, &pfull2[x], done)) break;
+                        tc_fence_after();
+                    }
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = part * 8 / kParts; ks < (part + 1) * 8 / kParts; ++ks)
+                            umma_ts(o_tm, p_tm + ks * 8, desc_of(v_lo + (uint32_t)((ks * 2048) >> 4), d_hi), idO,
+                                    (tl > 0 || ks > 0) ? 1u : 0u);
+                        if (part == kParts - 1) {
+                            umma_commit(&pvdone[x]);
+                            umma_commit(&vempty[st]);
+                            if (!pc.full) umma_commit(&vempty[st]);
+                        } else {
+                            umma_commit(&phalf[x]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+                if (!kApart) {
+                    if (more) issue_s(t + 1);
+                    if (pc.full) {
+                        if (lane == 0) mbar_arrive_cnt(&turn[x ^ 1], 1);
+                        __syncwarp();
+                        ++turns;
+                    }
+                }
+            }
+            ++pieces;
             g += n;
-            ++piece;
         }
         if (!ok) {  // drain the MMAs in flight before tensor memory is released
-            umma_commit(drain);
+            if (elect_one()) umma_commit(&drain[x]);
+            __syncwarp();
             volatile int no_abort = 0;
-            mbar_wait(drain, 0, &no_abort, kWaitLimit);
+            mbar_wait(&drain[x], 0, &no_abort, kWaitLimit);
         }
-       }
-       __syncwarp();
       }
     } else {
         reg_alloc<kFlRegsSoft>();
         // ---------------------------------------------------------- softmax / epilogue (rows)
-        const int x = warp >> 2;        // row tile of this warpgroup
+        const int x = (warp - kFlSoftWarp) >> 2;  // row tile of this warpgroup
         const int r = tid & (kBM - 1);  // row of the tile == tensor memory lane
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const float cexp = a.scale * 1.4426950408889634f;  // scores -> log2 domain (scale > 0)
         const int rt = r / G, rg = r - rt * G;
-        unsigned char *stage = smem + S::kStage + warp * 4096;
-        uint32_t g = 0, use0 = 0, use1 = 0;
-        int piece = 0;
+        const uint32_t s_tm0 = tmem + lane_off + Tm::s(0) + (uint32_t)x * 128;
+        const uint32_t p_tm0 = tmem + lane_off + Tm::p(0) + (uint32_t)x * (kApart ? 64 : 128);
+        uint32_t g = 0, done = 0;  // key tiles of the CTA; of this row tile
         bool ok = true;
         while (ok && cur.next(pc)) {
             const int n = pc.j1 - pc.j0;
-            const bool active = x == 0 || pc.full;
-            if (active) {
-                const int tok = (pc.p * 2 + x) * tq + rt;
-                const bool valid = rt < tq && tok < pc.n;
-                const unsigned vmask = __ballot_sync(0xffffffffu, valid);
-                // keys that every row of the tile sees
-                const int open = pc.ctx + (a.anc ? 0 : (pc.p * 2 + x) * tq + 1);
-                const int seen = pc.ctx + tok + 1;  // causal: keys this row sees
-                float m_used = -INFINITY, l = 0.f;
-                for (int tl = 0; tl < n; ++tl) {
-                    const uint32_t t = g + tl;
-                    const int key0 = (pc.j0 + tl) * kBN;
-                    const int b = pc.full ? x : (tl & 1);
-                    const uint32_t par = (pc.full ? (b ? use1 : use0) + tl : (b ? use1 : use0) + (tl >> 1)) & 1;
-                    const bool masked = key0 + kBN > open;
-                    uint32_t anc[kAncWords];
+            if (x == 1 && !pc.full) {
+                g += n;
+                continue;
+            }
+            const int tok0 = (pc.p * 2 + x) * tq, tok = tok0 + rt;
+            const bool valid = rt < tq && tok < pc.n;
+            const unsigned vmask = __ballot_sync(0xffffffffu, valid);
+            const int open = pc.ctx + (a.anc ? 0 : tok0 + 1);  // keys that every row of the tile sees
+            const int seen = pc.ctx + tok + 1;                 // causal: keys this row sees
+            float m_used = -INFINITY, l = 0.f;
+            // One key tile; masked: some row does not see all of the keys.
+            auto tile = [&](auto masked_t, int tl) -> bool {
+                constexpr bool masked = decltype(masked_t)::value;
+                const uint32_t t = g + tl;
+                const int key0 = (pc.j0 + tl) * kBN;
+                uint32_t mk[4] = {};                    // the keys this row sees
+                if (masked) {
+                    if (a.anc) {
+                        uint32_t anc[kAncWords];
 #pragma unroll
-                    for (int w = 0; w < kAncWords; ++w)
-                        anc[w] = (a.anc && valid && masked) ? a.anc[(long long)(pc.n0 + tok) * kAncWords + w] : 0u;
-                    if (!(ok = warp_wait(&sfull[b], par, s_abort, a.wait_limit))) break;
-                    tc_fence_after();
-                    // every S reading K of this tile is complete (S_A was issued before S_B)
-                    if (x == 1 || !pc.full) warp_arrive(&kempty[t % NS]);
-                    // the tile's S was the last to read Q: its buffer is free
-                    if (tl == n - 1) warp_arrive(&qfree[x]);
-                    if (x == 0 && key0 + kBN > pc.keys) {
-                        // slots behind the last key hold anything, NaN too: their V rows are zeroed
-                        if (!(ok = warp_wait(&vfull[t % NS], (t / NS) & 1, s_abort, a.wait_limit))) break;
-                        unsigned char *sv = smem + S::kV + (t % NS) * S::kTile;
-                        const int first = pc.keys - key0, count = (kBN - first) * 8;
-                        for (int e = r; e < count * kKB; e += kBM) {
-                            const int kb = e / count, c = e - kb * count;
-                            *reinterpret_cast<uint4 *>(sv + kb * 16384 + first * 128 + c * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_async_smem();
-                    }
-                    if (vmask == 0) {  // no rows in this warp: its P feeds rows that are never read
-                        warp_arrive(&pfull[b]);
-                        continue;
-                    }
-                    const uint32_t s_tm = tmem + lane_off + kFlTmS + (uint32_t)b * 128;
-                    float s[kBN];
-                    {
-                        uint32_t xa[32], xb[32], xc[32], xd[32];
-                        tmem_ld32(s_tm, xa);
-                        tmem_ld32(s_tm + 32, xb);
-                        tmem_ld32(s_tm + 64, xc);
-                        tmem_ld32(s_tm + 96, xd);
-                        tmem_wait_ld();
-                        tmem_regs_ready(xa);
-                        tmem_regs_ready(xb);
-                        tmem_regs_ready(xc);
-                        tmem_regs_ready(xd);
+                        for (int w = 0; w < kAncWords; ++w) anc[w] = valid ? a.anc[(long long)(pc.n0 + tok) * kAncWords + w] : 0u;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            s[e] = __uint_as_float(xa[e]);
-                            s[32 + e] = __uint_as_float(xb[e]);
-                            s[64 + e] = __uint_as_float(xc[e]);
-                            s[96 + e] = __uint_as_float(xd[e]);
-                        }
-                    }
-                    if (masked) {
-#pragma unroll
-                        for (int ch = 0; ch < kBN / 32; ++ch) {
-                            const int base = key0 + ch * 32;
-                            uint32_t msk;
-                            if (a.anc) {
-                                msk = tree_window(anc, base - pc.ctx);
-                            } else {
-                                const int c = seen - base;
-                                msk = c >= 32 ? 0xffffffffu : c <= 0 ? 0u : (1u << c) - 1u;
-                            }
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (!((msk >> e) & 1u)) s[ch * 32 + e] = -INFINITY;
-                        }
-                    }
-                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int j = 0; j < kBN; j += 2) mx4[(j >> 1) & 3] = fmaxf(mx4[(j >> 1) & 3], fmaxf(s[j], s[j + 1]));
-                    const float mt = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * cexp;
-                    // lazy rescale: move the reference maximum only when it grows
-                    // by more than 2^8 (warp-wide O pass, factor 1 for other rows)
-                    const bool grow = mt > m_used + 8.f;
-                    const float corr = grow ? ex2(m_used - mt) : 1.f;  // 0 when m_used is -inf
-                    if (grow) {
-                        l *= corr;
-                        m_used = mt;
-                    }
-                    const float nb = (m_used == -INFINITY) ? 0.f : kFlBias<BF16> - m_used;
-                    const float2 c2 = make_float2(cexp, cexp), nb2 = make_float2(nb, nb);
-                    float2 sum2[4] = {};
-#pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        uint32_t xp[32];
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float2 d = fma2(make_float2(s[hh * 64 + 2 * e], s[hh * 64 + 2 * e + 1]), c2, nb2);
-                            const float2 p = make_float2(ex2(d.x), ex2(d.y));
-                            sum2[e & 3] = add2(sum2[e & 3], p);
-                            xp[e] = pack16<BF16>(p.x, p.y);
-                        }
-                        tmem_st32(s_tm + hh * 32, xp);
-                    }
-                    const float2 sum = add2(add2(sum2[0], sum2[1]), add2(sum2[2], sum2[3]));
-                    l += sum.x + sum.y;
-                    if (tl > 0 && __any_sync(0xffffffffu, grow)) {
-                        // O must hold P V of the previous tile: in full mode that
-                        // P V was issued before this S; in half mode after it
-                        if (!pc.full) {
-                            const uint32_t pv = t - 1;
-                            if (!(ok = warp_wait(&vempty[pv % NS], (pv / NS) & 1, s_abort, a.wait_limit))) break;
-                            tc_fence_after();
-                        }
-#pragma unroll
-                        for (int ch = 0; ch < D / 32; ++ch) {
-                            uint32_t xo[32];
-                            const uint32_t o_tm = tmem + lane_off + (uint32_t)x * 128 + ch * 32;
-                            tmem_ld32(o_tm, xo);
-                            tmem_wait_ld();
-                            tmem_regs_ready(xo);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) xo[e] = __float_as_uint(__uint_as_float(xo[e]) * corr);
-                            tmem_st32(o_tm, xo);
-                        }
-                    }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    warp_arrive(&pfull[b]);
-                }
-                if (ok) {  // P V of the last tile (its V stage's release is committed after it)
-                    const uint32_t pv = g + n - 1;
-                    ok = warp_wait(&vempty[pv % NS], (pv / NS) & 1, s_abort, a.wait_limit);
-                }
-                if (!ok) break;
-                tc_fence_after();
-                if (vmask) {
-                    const long long orow = (long long)(pc.n0 + tok) * a.Hq + pc.kvh * G + rg;
-                    if (pc.slot < 0) {
-                        // rows leave through shared memory, 64 columns at a time, so that a
-                        // store writes whole 128-byte lines (16-byte chunk c of row r at
-                        // c ^ (r & 7): no bank conflicts either way)
-                        const float f = l > 0.f ? 1.f / l : l;  // no key with weight: 0; NaN stays
-                        uint16_t *dst = a.out + orow * D;
-#pragma unroll 1
-                        for (int ch = 0; ch < D / 64; ++ch) {
-#pragma unroll
-                            for (int hh = 0; hh < 2; ++hh) {
-                                uint32_t xo[32];
-                                tmem_ld32(tmem + lane_off + (uint32_t)x * 128 + ch * 64 + hh * 32, xo);
-                                tmem_wait_ld();
-                                tmem_regs_ready(xo);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    uint4 v;
-                                    v.x = pack16<BF16>(__uint_as_float(xo[8 * e]) * f, __uint_as_float(xo[8 * e + 1]) * f);
-                                    v.y = pack16<BF16>(__uint_as_float(xo[8 * e + 2]) * f, __uint_as_float(xo[8 * e + 3]) * f);
-                                    v.z = pack16<BF16>(__uint_as_float(xo[8 * e + 4]) * f, __uint_as_float(xo[8 * e + 5]) * f);
-                                    v.w = pack16<BF16>(__uint_as_float(xo[8 * e + 6]) * f, __uint_as_float(xo[8 * e + 7]) * f);
-                                    *reinterpret_cast<uint4 *>(stage + lane * 128 + (((hh * 4 + e) ^ (lane & 7)) << 4)) = v;
-                                }
-                            }
-                            __syncwarp();
-#pragma unroll
-                            for (int it = 0; it < 8; ++it) {
-                                const int rw = it * 4 + (lane >> 3);  // row of the warp this lane writes
-                                uint16_t *d = reinterpret_cast<uint16_t *>(
-                                    __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), rw));
-                                const uint4 v = *reinterpret_cast<const uint4 *>(stage + rw * 128 + (((lane & 7) ^ (rw & 7)) << 4));
-                                if ((vmask >> rw) & 1u) *reinterpret_cast<uint4 *>(d + ch * 64 + (lane & 7) * 8) = v;
-                            }
-                            __syncwarp();
-                        }
-                        if (valid) a.lse[orow] = l > 0.f ? (m_used - kFlBias<BF16> + log2f(l)) * 0.6931471805599453f
-                                                         : (l == 0.f ? -INFINITY : l);
+                        for (int ch = 0; ch < 4; ++ch) mk[ch] = tree_window(anc, key0 + ch * 32 - pc.ctx);
                     } else {
-                        const long long prow = (long long)pc.slot * kFlRows + x * kBM + r;
-#pragma unroll 1
-                        for (int ch = 0; ch < D / 32; ++ch) {
-                            uint32_t xo[32];
-                            tmem_ld32(tmem + lane_off + (uint32_t)x * 128 + ch * 32, xo);
-                            tmem_wait_ld();
-                            tmem_regs_ready(xo);
-                            if (valid) {
-                                uint4 *d = reinterpret_cast<uint4 *>(a.part_o + prow * D + ch * 32);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) d[e] = make_uint4(xo[4 * e], xo[4 * e + 1], xo[4 * e + 2], xo[4 * e + 3]);
-                            }
-                        }
-                        if (valid) {
-                            a.part_m[prow] = m_used - kFlBias<BF16>;
-                            a.part_l[prow] = l;
+                        for (int ch = 0; ch < 4; ++ch) {
+                            const int c = seen - key0 - ch * 32;
+                            mk[ch] = c >= 32 ? 0xffffffffu : c <= 0 ? 0u : (1u << c) - 1u;
                         }
                     }
-                    tc_fence_before();
+                }
+                if (!(ok = quick_wait(&sfull[x], done & 1, s_abort, a.wait_limit))) return false;
+                tc_fence_after();
+                // the piece's last S has read Q: its buffer is free
+                if (tl == n - 1) warp_arrive(&qfree[x]);
+                if (key0 + kBN > pc.keys) {
+                    // slots behind the last key hold anything, NaN too: their V rows are zeroed (by
+                    // each row tile for its own product)
+                    if (!(ok = quick_wait(&vfull[t % NV], (t / NV) & 1, s_abort, a.wait_limit))) return false;
+                    unsigned char *sv = smem + S::kV + (t % NV) * S::kTile;
+                    const int first = pc.keys - key0, count = (kBN - first) * 8;
+#pragma unroll 1
+                    for (int e = r; e < count * kKB; e += kBM) {
+                        const int kb = e / count, c = e - kb * count;
+                        *reinterpret_cast<uint4 *>(sv + kb * 16384 + first * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                }
+                // P V of the last tile must be complete before P's columns (where they are
+                // apart) are written; at D = 128 S was issued behind it
+                auto wait_idle = [&]() -> bool {
+                    if (!kApart || done == 0) return true;
+                    if (!(ok = quick_wait(&pvdone[x], (done - 1) & 1, s_abort, a.wait_limit))) return false;
+                    tc_fence_after();
+                    return true;
+                };
+                if (vmask == 0) {  // no rows in this warp: its P feeds rows that are never read
+                    if (kApart) warp_arrive(&sfree[x]);
+                    // (the next S may be there already: no arrival for it before this P is used)
+                    if (!wait_idle()) return false;
+                    warp_arrive(&pfull[x]);
+                    if (!kApart) warp_arrive(&pfull2[x]);
+                    ++done;
+                    return true;
+                }
+                const uint32_t s_tm = s_tm0, p_tm = p_tm0;
+                // the row's maximum; 64 keys at a time, here and below, in loops that
+                // are not unrolled: tensor memory is read again at little cost, and the
+                // loop stays small enough for the instruction cache
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    uint32_t va[32], vb[32];
+                    tmem_ld32(s_tm + hh * 64, va);
+                    tmem_ld32(s_tm + hh * 64 + 32, vb);
+                    tmem_wait_ld();
+                    tmem_regs_ready(va);
+                    tmem_regs_ready(vb);
+                    if (masked) {
+                        hide(va, hh ? mk[2] : mk[0]);
+                        hide(vb, hh ? mk[3] : mk[1]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        mx[e & 3] = fmaxf(mx[e & 3], fmaxf(__uint_as_float(va[e]), __uint_as_float(vb[e])));
+                }
+                const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * cexp;
+                // lazy rescale: move the reference maximum only when it grows
+                // by more than 2^8 (warp-wide O pass, factor 1 for other rows)
+                const bool grow = mt > m_used + 8.f;
+                const float corr = grow ? ex2(m_used - mt) : 1.f;  // 0 when m_used is -inf
+                if (grow) {
+                    l *= corr;
+                    m_used = mt;
+                }
+                if (tl > 0 && __any_sync(0xffffffffu, grow)) {
+                    if (!wait_idle()) return false;
+#pragma unroll 1
+                    for (int ch = 0; ch < D / 32; ++ch) {
+                        uint32_t xo[32];
+                        const uint32_t o_tm = tmem + lane_off + Tm::o(x) + ch * 32;
+                        tmem_ld32(o_tm, xo);
+                        tmem_wait_ld();
+                        tmem_regs_ready(xo);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) xo[e] = __float_as_uint(__uint_as_float(xo[e]) * corr);
+                        tmem_st32(o_tm, xo);
+                    }
+                }
+                const float nb = (m_used == -INFINITY) ? 0.f : kFlBias<BF16> - m_used;
+                float sum4[4] = {l, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int hh = 0; hh < 2; ++hh) {
+                    uint32_t va[32], vb[32], xp[32];
+                    tmem_ld32(s_tm + hh * 64, va);
+                    tmem_ld32(s_tm + hh * 64 + 32, vb);
+                    tmem_wait_ld();
+                    tmem_regs_ready(va);
+                    tmem_regs_ready(vb);
+                    if (masked) {
+                        hide(va, hh ? mk[2] : mk[0]);
+                        hide(vb, hh ? mk[3] : mk[1]);
+                    }
+                    if (kApart && hh) {  // S has been read: the next one may be written
+                        tc_fence_before();
+                        warp_arrive(&sfree[x]);
+                    }
+                    exp_pairs<BF16>(va, vb, cexp, nb, sum4, xp);
+                    if (kApart && !hh && !wait_idle()) return false;
+                    tmem_st32(p_tm + hh * 32, xp);
+                    if (!kApart || hh) {
+                        tmem_wait_st();
+                        tc_fence_before();
+                        warp_arrive(kApart || !hh ? &pfull[x] : &pfull2[x]);
+                    }
+                }
+                l = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+                ++done;
+                return true;
+            };
+            int tl = 0;
+            const int n_open = min(n, open / kBN - pc.j0);
+#pragma unroll 1
+            for (; ok && tl < n_open; ++tl) tile(std::false_type(), tl);
+#pragma unroll 1
+            for (; ok && tl < n; ++tl) tile(std::true_type(), tl);
+            // P V of the last tile; that of the tile before it is known to be complete (by
+            // the wait above or by the order of the products), as a phase's parity demands
+            if (!ok || !(ok = quick_wait(&pvdone[x], (done - 1) & 1, s_abort, a.wait_limit))) break;
+            tc_fence_after();
+            if (vmask) {
+                const long long orow = (long long)(pc.n0 + tok) * a.Hq + pc.kvh * G + rg;
+                const long long prow = (long long)pc.slot * kFlRows + x * kBM + r;
+                const bool final = pc.slot < 0;
+                const float f = l > 0.f ? 1.f / l : l;  // no key with weight: 0; NaN stays
+#pragma unroll 1
+                for (int ch = 0; ch < D / 32; ++ch) {
+                    uint32_t xo[32];
+                    tmem_ld32(tmem + lane_off + Tm::o(0) + (uint32_t)x * D + ch * 32, xo);
+                    tmem_wait_ld();
+                    tmem_regs_ready(xo);
+                    if (!valid) continue;
+                    if (final) {
+                        uint32_t v[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = pack16<BF16>(__uint_as_float(xo[2 * e]) * f, __uint_as_float(xo[2 * e + 1]) * f);
+                        store32(a.out + orow * D + ch * 32, v);
+                        store32(a.out + orow * D + ch * 32 + 16, v + 8);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) store32(a.part_o + prow * D + ch * 32 + 8 * e, xo + 8 * e);
+                    }
+                }
+                if (valid && final) {
+                    a.lse[orow] = l > 0.f ? (m_used - kFlBias<BF16> + log2f(l)) * 0.6931471805599453f : (l == 0.f ? -INFINITY : l);
+                } else if (valid) {
+                    a.part_m[prow] = m_used - kFlBias<BF16>;
+                    a.part_l[prow] = l;
                 }
             }
-            use0 += pc.full ? n : (n + 1) >> 1;
-            use1 += pc.full ? n : n >> 1;
-            warp_arrive(ofree);
-            // the tile-B warps may not run ahead through pieces in which they have nothing to do
-            if (x == 1 && !(ok = warp_wait(ofree, (uint32_t)(piece & 1), s_abort, a.wait_limit))) break;
-            ++piece;
+            tc_fence_before();
+            warp_arrive(&ofree[x]);
             g += n;
         }
     }
     __syncthreads();
-    if (warp == kMmaWarp) {
+    if (warp == kFlMmaWarp) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
     }

@@ -209,6 +209,15 @@ __device__ __forceinline__ void umma_commit(uint64_t *bar) {
                  : "memory");
 }
 
+// One lane of a fully active warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// A value that all lanes share, so that the compiler may keep it in a uniform register.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // Per-warpgroup register budget (all four warps of the warpgroup execute
 // it): lower it in the warpgroups that need few registers so that others can
 // raise theirs; the raises must fit in what the block was launched with.
