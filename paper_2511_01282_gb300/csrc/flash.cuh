@@ -22,8 +22,7 @@
 // not stay in L2).  A segment cut by a share's end leaves partial (O, m, l),
 // which flash_combine joins in key order: no atomics, the same bits each run.
 //
-// Warps: 0 and 1 MMA issue for row tiles A and B, 2 TMA, 3 idle (it only gives
-// registers up), 4-7 softmax of tile A (thread = row), 8-11 of tile B.  Tensor memory (512 columns):
+// Warps: 0 and 1 MMA issue for row tiles A and B, 2 and 3 TMA (K and Q, V), 4-7 softmax of tile A (thread = row), 8-11 of tile B.  Tensor memory (512 columns):
 //   D = 64: O_A O_B (64 each), S_A S_B (128 each), P_A P_B (64 each).  S of the
 //     next key tile is issued as soon as its softmax has read the last one, so
 //     that a softmax finds its next S ready and the exponentials bound the loop.
@@ -42,7 +41,7 @@
 namespace rs {
 
 constexpr int kFlThreads = 384;
-constexpr int kFlMmaWarp = 0, kFlTmaWarp = 2, kFlSoftWarp = 4;  // two warps issue products
+constexpr int kFlMmaWarp = 0, kFlTmaWarp = 2, kFlSoftWarp = 4;  // two warps issue products, two copy
 constexpr uint32_t kFlRegsSoft = 224, kFlRegsProd = 56;
 static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "register split");
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
@@ -340,14 +339,23 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
 
     if (warp < kFlSoftWarp) {
       reg_dealloc<kFlRegsProd>();
-      if (warp == kFlTmaWarp) {
-        // ---------------------------------------------------------- TMA producer
-        // Whole warp: in a paged cache lane x copies page x of the tile.
+      if (warp >= kFlTmaWarp) {
+        // ---------------------------------------------------------- TMA producers
+        // One warp for K (and Q), one for V.  Whole warps: in a paged cache lane x
+        // copies page x of the tile (a copy takes a warp some 75 cycles to issue, and
+        // a tile in pages of 16 tokens is 16 copies: with one warp for both they bound
+        // long chunks, 665 us for 500).
+        const bool is_v = warp == kFlTmaWarp + 1;
+        const CUtensorMap *map = is_v ? &tmv : &tmk;
+        uint64_t *full = is_v ? vfull : kfull, *empty = is_v ? vempty : kempty;
+        unsigned char *ring = smem + (is_v ? S::kV : S::kK);
+        const uint32_t stages = is_v ? NV : NK;
         const uint32_t q_tx = (uint32_t)(tq * G) * D * 2;
         const int page = a.page_table ? 1 << a.page_log2 : kBN;
         const int box = page < kBN ? page : kBN;      // keys per copy
         const uint64_t once = l2_evict_first_policy();
-        uint32_t g = 0, quse[2] = {0, 0};
+        uint32_t st = 0, phase = 0, quse[2] = {0, 0};  // stage, its phase; Q tiles copied
+        uint32_t used = 0;                             // stages in use so far (at most all)
         bool ok = true;
         while (ok && cur.next(pc)) {
             const int32_t *table = a.page_table ? a.page_table + (long long)pc.b * a.max_pages : nullptr;
@@ -365,57 +373,54 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                 return (id << a.page_log2) + (key & (page - 1));
             };
             int row = row_of(pc.j0);
-            for (int jt = pc.j0; jt < pc.j1; ++jt, ++g) {
-                const uint32_t ks = g % NK, vs = g % NV;
+            for (int jt = pc.j0; jt < pc.j1; ++jt) {
                 const int next_row = jt + 1 < pc.j1 ? row_of(jt + 1) : -1;
                 const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, row >= 0)) * (uint32_t)(box * D * 2);
-                unsigned char *sk = smem + S::kK + ks * S::kTile + lane * box * 128;
-                unsigned char *sv = smem + S::kV + vs * S::kTile + lane * box * 128;
-                if (!(ok = warp_wait(&kempty[ks], ((g / NK) & 1) ^ 1, s_abort, a.wait_limit))) break;
-                if (lane == 0) mbar_expect_tx(&kfull[ks], tx);
+                if (!(ok = warp_wait(&empty[st], phase ^ 1, s_abort, a.wait_limit))) break;
+                if (lane == 0) mbar_expect_tx(&full[st], tx);
                 __syncwarp();
                 if (row >= 0) {
+                    unsigned char *dst = ring + st * S::kTile + lane * box * 128;
 #pragma unroll
                     for (int kb = 0; kb < kKB; ++kb) {
-                        if (evict) tma_load_3d_hint(sk + kb * 16384, &tmk, &kfull[ks], kb * 64, pc.kvh, row, once);
-                        else tma_load_3d(sk + kb * 16384, &tmk, &kfull[ks], kb * 64, pc.kvh, row);
+                        if (evict) tma_load_3d_hint(dst + kb * 16384, map, &full[st], kb * 64, pc.kvh, row, once);
+                        else tma_load_3d(dst + kb * 16384, map, &full[st], kb * 64, pc.kvh, row);
                     }
                 }
-                if (jt == pc.j0) {  // the piece's Q tiles, once its previous S products are done with the buffers
-                    for (int x = 0; x < (pc.full ? 2 : 1); ++x) {
-                        if (quse[x] > 0 && !(ok = warp_wait(&qfree[x], (quse[x] - 1) & 1, s_abort, a.wait_limit))) break;
-                        ++quse[x];
-                        if (lane == 0) {
-                            mbar_expect_tx(&qfull[x], q_tx);
-#pragma unroll
-                            for (int kb = 0; kb < kKB; ++kb)
-                                tma_load_3d(smem + S::kQ + x * S::kTile + kb * 16384, &tmq, &qfull[x], kb * 64, pc.kvh * G,
-                                            pc.n0 + (pc.p * 2 + x) * tq);
-                        }
-                        __syncwarp();
-                    }
-                }
-                if (!ok || !(ok = warp_wait(&vempty[vs], ((g / NV) & 1) ^ 1, s_abort, a.wait_limit))) {
-                    volatile int no_abort = 0;  // this tile's K copy is in flight: let it land
-                    mbar_wait(&kfull[ks], (g / NK) & 1, &no_abort, kWaitLimit);
-                    break;
-                }
-                if (lane == 0) mbar_expect_tx(&vfull[vs], tx);
                 __syncwarp();
-                if (row >= 0) {
-#pragma unroll
-                    for (int kb = 0; kb < kKB; ++kb) {
-                        if (evict) tma_load_3d_hint(sv + kb * 16384, &tmv, &vfull[vs], kb * 64, pc.kvh, row, once);
-                        else tma_load_3d(sv + kb * 16384, &tmv, &vfull[vs], kb * 64, pc.kvh, row);
-                    }
+                used = min(used + 1, stages);
+                if (++st == stages) {
+                    st = 0;
+                    phase ^= 1;
                 }
                 row = next_row;
+                if (is_v || jt != pc.j0) continue;
+                // the piece's Q tiles, once its previous S products are done with the buffers
+                for (int x = 0; x < (pc.full ? 2 : 1); ++x) {
+                    if (quse[x] > 0 && !(ok = warp_wait(&qfree[x], (quse[x] - 1) & 1, s_abort, a.wait_limit))) break;
+                    ++quse[x];
+                    if (lane == 0) {
+                        mbar_expect_tx(&qfull[x], q_tx);
+#pragma unroll
+                        for (int kb = 0; kb < kKB; ++kb)
+                            tma_load_3d(smem + S::kQ + x * S::kTile + kb * 16384, &tmq, &qfull[x], kb * 64, pc.kvh * G,
+                                        pc.n0 + (pc.p * 2 + x) * tq);
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
             }
         }
         if (!ok) {  // let the copies already issued land before the CTA exits
             volatile int no_abort = 0;
-            for (uint32_t t = g >= NK ? g - NK : 0; t < g; ++t) mbar_wait(&kfull[t % NK], (t / NK) & 1, &no_abort, kWaitLimit);
-            for (uint32_t t = g >= NV ? g - NV : 0; t < g; ++t) mbar_wait(&vfull[t % NV], (t / NV) & 1, &no_abort, kWaitLimit);
+            for (uint32_t u = 0; u < used; ++u) {
+                if (st == 0) {
+                    st = stages;
+                    phase ^= 1;
+                }
+                --st;
+                mbar_wait(&full[st], phase, &no_abort, kWaitLimit);
+            }
             for (int x = 0; x < 2; ++x)
                 if (quse[x] > 0) mbar_wait(&qfull[x], (quse[x] - 1) & 1, &no_abort, kWaitLimit);
         }
