@@ -37,6 +37,7 @@
 #include <type_traits>
 
 #include "attn_core.cuh"
+#include "roles.cuh"
 
 namespace rs {
 
@@ -213,28 +214,6 @@ __device__ __forceinline__ void exp_pairs(const uint32_t (&s0)[32], const uint32
             else asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(xp[q]) : "f"(p[2 * q + 1]), "f"(p[2 * q]));
         }
     }
-}
-
-// Keys whose bit is not set: -inf (whole warp; most chunks are open to all rows).
-__device__ __forceinline__ void hide(uint32_t (&v)[32], uint32_t seen) {
-    if (__all_sync(0xffffffffu, seen == 0xffffffffu)) return;
-#pragma unroll
-    for (int e = 0; e < 32; ++e)
-        if (!((seen >> e) & 1u)) v[e] = 0xff800000u;
-}
-
-// warp_wait with its usual case, a phase that is complete, on a short path.
-__device__ __forceinline__ bool quick_wait(uint64_t *bar, uint32_t parity, volatile int *abort, long long limit) {
-    if (__builtin_expect(__all_sync(0xffffffffu, sm100::mbar_try_wait(bar, parity)), 1)) return true;
-    return warp_wait(bar, parity, abort, limit);
-}
-
-// Both barriers at once (they may be the same).
-__device__ __forceinline__ bool quick_wait2(uint64_t *b1, uint32_t p1, uint64_t *b2, uint32_t p2, volatile int *abort,
-                                            long long limit) {
-    const bool r1 = sm100::mbar_try_wait(b1, p1), r2 = sm100::mbar_try_wait(b2, p2);
-    if (__builtin_expect(__all_sync(0xffffffffu, r1 && r2), 1)) return true;
-    return warp_wait(b1, p1, abort, limit) && warp_wait(b2, p2, abort, limit);
 }
 
 // 32 bytes in one store (p 32-byte aligned): a whole sector, so that a thread

@@ -3,24 +3,27 @@
 //     w_j += sum_{rows i that see j} sum_{heads h of the group} exp(scale q_ih.k_j - lse_ih).
 //
 // The product runs with the keys as its rows, S^T = K Q^T, so that a thread
-// holds one key's scores of 128 (token, head) columns and its sum stays in a
-// register: no exchange between threads, and K, which is read once, stays in
-// shared memory while the Q tiles pass by.  Work: a segment is (KV head,
-// request, 128 keys), its units the Q tiles of tq = 128 / G tokens that see
-// the keys.  The segments lie end to end, a CTA takes an equal share of their
-// cost, and the sums of a segment that a share's end cuts are joined by
-// weigh_combine in order (no atomics: the same bits every time).
-// Bound: K and the weights, read once, for single tokens; the exponentials and
-// the product (2 D flop each) for long chunks.
+// holds one key's scores of up to 128 (token, head) columns and its sum stays in
+// a register: no exchange between threads, and K, which is read once, stays in
+// shared memory while the Q tiles pass by.  A segment is (KV head, request, 256
+// keys): two key tiles, one per warpgroup, so that a Q tile serves 256 keys (with
+// one they would ask L2 for 12 TB/s).  Its units are the Q tiles of tq tokens
+// that see the keys; tq follows the average chunk, up to 128 / G, so that single
+// tokens neither copy nor multiply rows they do not have.  The segments lie end
+// to end, a CTA takes an equal share of their cost, and the sums of a segment that
+// a share's end cuts are joined by weigh_combine in order (the same bits every time).
+// Bound: K and the weights, read once, for single tokens; the exponentials (16
+// cycles a warp for 32 keys x 4 columns) and the product (2 D flop) for long chunks.
 //
-// Warps: 0-3 and 4-7 two warpgroups that take turns at the Q tiles, 8 TMA, 9
-// MMA issue.  Tensor memory: four S buffers of 128 columns.
+// Warps: 0 MMA issue, 1 copies Q, 2 copies K, 3 reads the columns' lse, 4-7 and
+// 8-11 the two key tiles.  Tensor memory: two S buffers of 128 columns for each.
 #include <math.h>
 
 #include <algorithm>
 #include <atomic>
 
 #include "common.cuh"
+#include "roles.cuh"
 #include "tmap.cuh"
 
 namespace rs {
@@ -28,8 +31,11 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kWgThreads = 320;
-constexpr int kWgBeta = 2;  // cost of a segment's start (its K tile), in Q tiles
+constexpr int kWgThreads = 384;
+constexpr uint32_t kWgRegsSum = 208, kWgRegsCopy = 88;
+static_assert(2 * 128 * kWgRegsSum + 128 * kWgRegsCopy == kWgThreads * 168, "register split");
+constexpr int kWgKeys = 2 * kBN;  // keys of a segment
+constexpr int kWgBeta = 2;  // cost of a segment's start (its K tiles), in Q tiles
 
 struct WeighArgs {
     const int32_t *off, *ctx, *table;
@@ -38,22 +44,22 @@ struct WeighArgs {
     int32_t *status;
     int4 *req;        // first row, rows (0: nothing to do), ctx
     long long *cum;   // [B + 1] cost prefix of one KV head
-    int4 *bound;      // [CTA] start of its share: (KV head, request, key tile, Q tile)
-    float *part;      // [2 grid][128]
+    int4 *bound;      // [CTA] start of its share: (KV head, request, key pair, Q tile)
+    float *part;      // [2 grid][256]
     int B, T, Hq, Hkv, G, tq, grid, max_pages, n_pages, page_log2;
     float scale;
     long long wait_limit;
 };
 
-__device__ __forceinline__ int key_tiles(int4 rq) { return rq.y > 0 ? (rq.z + rq.y + kBN - 1) / kBN : 0; }
-// first Q tile that sees key tile jt, and the cost of the request's tiles before
-// jt: (Q tiles + beta) tq each, 128 less for every tile that lies behind the
+__device__ __forceinline__ int key_tiles(int4 rq) { return rq.y > 0 ? (rq.z + rq.y + kWgKeys - 1) / kWgKeys : 0; }
+// first Q tile that sees key pair jt, and the cost of the request's pairs before
+// jt: (Q tiles + beta) tq each, 256 less for every one that lies behind the
 // cached tokens (what it sees, up to rounding: the split needs no more)
-__device__ __forceinline__ int first_q(const WeighArgs &a, int4 rq, int jt) { return max(0, jt * kBN - rq.z) / a.tq; }
+__device__ __forceinline__ int first_q(const WeighArgs &a, int4 rq, int jt) { return max(0, jt * kWgKeys - rq.z) / a.tq; }
 __device__ __forceinline__ long long tiles_cost(const WeighArgs &a, int4 rq, int jt) {
     const long long full = (long long)((rq.y + a.tq - 1) / a.tq + kWgBeta) * a.tq;
-    const long long m = max(0, jt - (rq.z + kBN - 1) / kBN);
-    return full * jt - (long long)kBN * (m * (m - 1) / 2);
+    const long long m = max(0, jt - (rq.z + kWgKeys - 1) / kWgKeys);
+    return full * jt - (long long)kWgKeys * (m * (m - 1) / 2);
 }
 
 // Where cost position x falls (whole warp): 32-way searches for the request
@@ -189,29 +195,51 @@ __device__ __forceinline__ long long key_slot(const WeighArgs &a, int b, int j) 
 template <int D>
 struct WgSmem {
     static constexpr int kTile = kBN * D * 2;
-    static constexpr int kNK = 2, kNQ = 4, kNS = 4;
-    static constexpr int kK = 0, kQ = kNK * kTile;
-    static constexpr int kLse = kQ + kNQ * kTile;      // [8 warps][2][128] floats
-    static constexpr int kSum = kLse + 8 * 2 * 512;    // [128] floats, from one warpgroup to the other
-    static constexpr int kBar = kSum + 512;
-    static constexpr int kNumBars = 2 * (kNK + kNQ + kNS) + 3;
+    static constexpr int kNK = 2, kNQ = D == 128 ? 2 : 5, kNL = 4;  // key pairs, Q tiles, columns' lse
+    static constexpr int kK = 0, kQ = kNK * 2 * kTile;
+    static constexpr int kLse = kQ + kNQ * kTile;     // [kNL][128] floats: -lse in the log2 domain
+    static constexpr int kMask = kLse + kNL * 512;    // [kNL][4] words: the columns that count
+    static constexpr int kBar = kMask + kNL * 16;
+    static constexpr int kNumBars = 2 * (kNK + kNQ + kNL + 4) + 1;
     static constexpr int kMisc = kBar + kNumBars * 8;
     static constexpr int kBounds = (kMisc + 8 + 15) / 16 * 16;
     static constexpr int kTotal = kBounds + 32 + 1024;
     static_assert(kTotal <= 232448, "shared memory of one CTA");
 };
 
+// sum4 += 2^(c s_i + nl_i) over 64 columns; the order of the statements as in exp_pairs.
+__device__ __forceinline__ void exp_sums(const uint32_t (&s0)[32], const uint32_t (&s1)[32], float c, const float4 *nl,
+                                         float (&sum4)[4]) {
+    constexpr int kAhead = 8, kBehind = 8;  // columns
+    float d[64], p[64];
+    float4 l;
+    auto fma1 = [&](int i) {
+        if (i % 4 == 0) l = nl[i / 4];
+        const float n = i % 4 == 0 ? l.x : i % 4 == 1 ? l.y : i % 4 == 2 ? l.z : l.w;
+        const float v = __uint_as_float(i < 32 ? s0[i] : s1[i - 32]);
+        asm volatile("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d[i]) : "f"(v), "f"(c), "f"(n));
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fma1(i);
+#pragma unroll
+    for (int i = 0; i < 64 + kBehind; ++i) {
+        if (i < 64) asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[i]) : "f"(d[i]));
+        if (i + kAhead < 64) fma1(i + kAhead);
+        if (i >= kBehind) asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(sum4[i & 3]) : "f"(p[i - kBehind]));
+    }
+}
+
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kWgThreads, 1)
 weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_constant__ CUtensorMap tmk) {
     using S = WgSmem<D>;
-    constexpr int NK = S::kNK, NQ = S::kNQ, NS = S::kNS;
+    constexpr uint32_t NK = S::kNK, NQ = S::kNQ, NL = S::kNL;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                             ~uintptr_t(1023));
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kBar);
     uint64_t *kfull = bars, *kempty = kfull + NK, *qfull = kempty + NK, *qempty = qfull + NQ;
-    uint64_t *sfull = qempty + NQ, *sempty = sfull + NS, *given = sempty + NS, *taken = given + 1, *drain = taken + 1;
+    uint64_t *lfull = qempty + NQ, *lempty = lfull + NL, *sfull = lempty + NL, *sempty = sfull + 4, *drain = sempty + 4;
     uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + S::kMisc);
     volatile int *s_abort = reinterpret_cast<volatile int *>(smem + S::kMisc + 4);
     int4 *s_bound = reinterpret_cast<int4 *>(smem + S::kBounds);
@@ -219,37 +247,31 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
     constexpr int kKB = D / 64;
 
     if (tid == 0) {
-        for (int s = 0; s < NK; ++s) {
+        for (uint32_t s = 0; s < NK; ++s) {
             mbar_init(&kfull[s], 1);
             mbar_init(&kempty[s], 1);
         }
-        for (int s = 0; s < NQ; ++s) {
+        for (uint32_t s = 0; s < NQ; ++s) {
             mbar_init(&qfull[s], 1);
-            mbar_init(&qempty[s], kBM);
+            mbar_init(&qempty[s], 1);
         }
-        for (int s = 0; s < NS; ++s) {
+        for (uint32_t s = 0; s < NL; ++s) {
+            mbar_init(&lfull[s], 32);
+            mbar_init(&lempty[s], 2 * kBM);
+        }
+        for (int s = 0; s < 4; ++s) {  // buffer u of key tile x: 2 x + u
             mbar_init(&sfull[s], 1);
             mbar_init(&sempty[s], kBM);
         }
-        mbar_init(given, kBM);
-        mbar_init(taken, kBM);
         mbar_init(drain, 1);
         *s_abort = 0;
         fence_mbar_init();
     }
-    if (warp == kMmaWarp) tmem_alloc(s_tmem, kTmemCols);
-    if (warp == kTmaWarp && lane == 0) {
+    if (warp == 0) tmem_alloc(s_tmem, kTmemCols);
+    if (warp == 1 && lane == 0) {
         prefetch_tmap(&tmq);
         prefetch_tmap(&tmk);
     }
-    // rows of the Q tiles that no token fills (G does not divide 128) are never
-    // copied to: zeroed once, their scores are 0
-    const int idle = kBN - a.tq * a.G;
-    for (int e = tid; e < NQ * kKB * idle * 8; e += kWgThreads) {
-        const int t = e / (idle * 8), c = e - t * idle * 8;
-        *reinterpret_cast<uint4 *>(smem + S::kQ + t * 16384 + a.tq * a.G * 128 + c * 16) = make_uint4(0, 0, 0, 0);
-    }
-    fence_async_smem();
     pdl_wait_prev();
     pdl_launch_next();
     if (warp < 2) {
@@ -267,192 +289,207 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
     const uint32_t tmem = *s_tmem;
     WgCursor cur(a, s_bound[0], s_bound[1]);
     WgPiece pc;
+    const int cols = a.tq * a.G;
+    bool ok = true;
 
-    if (warp == kTmaWarp) {
-        // ---------------------------------------------------------- TMA producer
-        const int page = 1 << a.page_log2, box = page < kBN ? page : kBN;
-        const uint32_t q_tx = (uint32_t)(a.tq * a.G) * D * 2;
-        uint32_t g = 0, piece = 0;
-        bool ok = true;
-        while (ok && cur.next(pc)) {
-            const int ks = (int)(piece % NK);
-            const int key = pc.jt * kBN + lane * box, keys = pc.rq.z + pc.rq.y;
-            int row = -1;
-            if (lane * box < kBN && key < keys) {
-                const long long s = key_slot(a, pc.b, key);
-                row = s < 0 ? a.n_pages << a.page_log2 : (int)s;  // outside the pool: the copy fills zeros
-            }
-            const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, row >= 0)) * (uint32_t)(box * D * 2);
-            if (!(ok = warp_wait(&kempty[ks], ((piece / NK) & 1) ^ 1, s_abort, a.wait_limit))) break;
-            if (lane == 0) mbar_expect_tx(&kfull[ks], tx);
-            __syncwarp();
-            if (row >= 0) {
-#pragma unroll
-                for (int kb = 0; kb < kKB; ++kb)
-                    tma_load_3d(smem + S::kK + ks * S::kTile + kb * 16384 + lane * box * 128, &tmk, &kfull[ks], kb * 64, pc.kvh, row);
-            }
-            ++piece;
-            const int q_first = first_q(a, pc.rq, pc.jt);
-            for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
-                const int qs = (int)(g % NQ);
-                if (!(ok = warp_wait(&qempty[qs], ((g / NQ) & 1) ^ 1, s_abort, a.wait_limit))) break;
-                if (lane == 0) {
-                    mbar_expect_tx(&qfull[qs], q_tx);
-#pragma unroll
-                    for (int kb = 0; kb < kKB; ++kb)
-                        tma_load_3d(smem + S::kQ + qs * S::kTile + kb * 16384, &tmq, &qfull[qs], kb * 64, pc.kvh * a.G,
-                                    pc.rq.x + (q_first + qt) * a.tq);
-                }
-                __syncwarp();
-            }
-        }
-        if (!ok) {  // let the copies already issued land before the CTA exits
-            volatile int no_abort = 0;
-            for (uint32_t t = piece >= NK ? piece - NK : 0; t < piece; ++t) mbar_wait(&kfull[t % NK], (t / NK) & 1, &no_abort, kWaitLimit);
-            for (uint32_t t = g >= NQ ? g - NQ : 0; t < g; ++t) mbar_wait(&qfull[t % NQ], (t / NQ) & 1, &no_abort, kWaitLimit);
-        }
-    } else if (warp == kMmaWarp) {
-        if (lane == 0) {
-            // ------------------------------------------------------ MMA issuer
-            constexpr uint32_t id = idesc_16_f32(BF16, kBN, kBM, false);
+    if (warp < 4) {
+        reg_dealloc<kWgRegsCopy>();
+        if (warp == 0) {
+            // ------------------------------------------------------ MMA issuer (whole warp, one lane issues)
+            // columns in units of 16, the product's granularity
+            const uint32_t id = (idesc_16_f32(BF16, kBN, 16, false) & ~(0x3fu << 17)) | ((uint32_t)((cols + 15) / 16 * 2) << 17);
             const uint64_t d0 = sdesc_sw128(smem_u32(smem + S::kK), 16, 1024);
             const uint32_t d_hi = (uint32_t)(d0 >> 32), k_lo0 = (uint32_t)d0;
             const uint32_t q_lo0 = (uint32_t)sdesc_sw128(smem_u32(smem + S::kQ), 16, 1024);
-            uint32_t g = 0, piece = 0;
-            bool ok = true;
-            auto wait = [&](uint64_t *bar, uint32_t par) -> bool { return ok = mbar_wait(bar, par & 1, s_abort, a.wait_limit); };
+            const uint32_t tm = uniform(tmem), idu = uniform(id);
+            constexpr uint32_t kTileDesc = S::kTile >> 4;
+            uint32_t g = 0, g1 = 0, piece = 0;  // Q tiles, those with two key tiles, segments
+            auto wait = [&](uint64_t *b1, uint32_t p1, uint64_t *b2, uint32_t p2) -> bool {
+                return ok = quick_wait2(b1, p1 & 1, b2, p2 & 1, s_abort, a.wait_limit);
+            };
             while (ok && cur.next(pc)) {
                 const uint32_t ks = piece % NK;
-                if (!wait(&kfull[ks], piece / NK)) break;
+                const bool two = pc.rq.z + pc.rq.y > pc.jt * kWgKeys + kBN;
+                if (!wait(&kfull[ks], piece / NK, &kfull[ks], piece / NK)) break;
                 for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
-                    const uint32_t qs = g % NQ, buf = g % NS;
-                    if (!wait(&qfull[qs], g / NQ)) break;
-                    if (!wait(&sempty[buf], (g / NS) ^ 1)) break;
+                    const uint32_t qs = g % NQ;
+                    if (!wait(&qfull[qs], g / NQ, &sempty[g & 1], (g >> 1) ^ 1)) break;
+                    if (two && !wait(&sempty[2 + (g1 & 1)], (g1 >> 1) ^ 1, &sempty[2 + (g1 & 1)], (g1 >> 1) ^ 1)) break;
                     tc_fence_after();
-                    uint32_t k_lo = k_lo0 + ks * (S::kTile >> 4), q_lo = q_lo0 + qs * (S::kTile >> 4);
-                    asm volatile("" : "+r"(k_lo), "+r"(q_lo));
+                    const uint32_t q_lo = uniform(q_lo0 + qs * kTileDesc);
+#pragma unroll 1
+                    for (uint32_t x = 0; x < (two ? 2u : 1u); ++x) {
+                        const uint32_t u = x ? g1 & 1 : g & 1;
+                        const uint32_t k_lo = uniform(k_lo0 + (2 * ks + x) * kTileDesc), d = uniform(tm + (2 * x + u) * 128);
+                        if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        const uint32_t o = (uint32_t)(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4);
-                        umma_ss(tmem + buf * 128, desc_of(k_lo + o, d_hi), desc_of(q_lo + o, d_hi), id, kk > 0);
+                            for (int kk = 0; kk < D / 16; ++kk) {
+                                const uint32_t o = (uint32_t)(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4);
+                                umma_ss(d, desc_of(k_lo + o, d_hi), desc_of(q_lo + o, d_hi), idu, kk > 0);
+                            }
+                            umma_commit(&sfull[2 * x + u]);
+                        }
+                        __syncwarp();
                     }
-                    umma_commit(&sfull[buf]);
+                    if (elect_one()) {
+                        umma_commit(&qempty[qs]);
+                        if (qt == pc.q1 - 1) umma_commit(&kempty[ks]);
+                    }
+                    __syncwarp();
+                    g1 += two;
                 }
-                if (!ok) break;
-                umma_commit(&kempty[ks]);
                 ++piece;
             }
             if (!ok) {
-                umma_commit(drain);
+                if (elect_one()) umma_commit(drain);
+                __syncwarp();
                 volatile int no_abort = 0;
                 mbar_wait(drain, 0, &no_abort, kWaitLimit);
             }
-        }
-        __syncwarp();
-    } else {
-        // ---------------------------------------------------------- sums (a thread per key)
-        const int x = warp >> 2, r = tid & (kBN - 1);
-        const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-        const float c = a.scale * 1.4426950408889634f;
-        float *s_lse = reinterpret_cast<float *>(smem + S::kLse) + warp * 256;
-        float *s_sum = reinterpret_cast<float *>(smem + S::kSum);
-        uint32_t g = 0, gifts = 0;
-        bool ok = true;
-        while (ok && cur.next(pc)) {
-            const int n = pc.q1 - pc.q0, key = pc.jt * kBN + r, keys = pc.rq.z + pc.rq.y;
-            const int q_first = first_q(a, pc.rq, pc.jt);
-            float2 sum = make_float2(0.f, 0.f);
-            for (int t = 0; t < n; ++t) {
-                const uint32_t gt = g + t;
-                if ((int)(gt & 1) != x) continue;
-                const int buf = (int)(gt % NS), tok0 = (q_first + pc.q0 + t) * a.tq;
-                // the columns' lse in the log2 domain; +inf for those that count for nothing
-                float *lse = s_lse + ((gt >> 1) & 1) * 128;
-                bool odd = false;
-                for (int e = lane; e < 128; e += 32) {
-                    const int tk = e / a.G, tok = tok0 + tk;
-                    float l = INFINITY;
-                    if (tk < a.tq && tok < pc.rq.y) {
-                        l = a.lse[(long long)(pc.rq.x + tok) * a.Hq + pc.kvh * a.G + (e - tk * a.G)] * 1.4426950408889634f;
-                        if (!isfinite(l)) {
-                            l = INFINITY;
-                            odd = true;
-                        }
+        } else if (warp == 1) {
+            // ------------------------------------------------------ Q tiles
+            const uint32_t q_tx = (uint32_t)cols * D * 2;
+            uint32_t g = 0;
+            while (ok && cur.next(pc)) {
+                const int q_first = first_q(a, pc.rq, pc.jt);
+                for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
+                    const uint32_t qs = g % NQ;
+                    if (!(ok = warp_wait(&qempty[qs], ((g / NQ) & 1) ^ 1, s_abort, a.wait_limit))) break;
+                    if (lane == 0) {
+                        mbar_expect_tx(&qfull[qs], q_tx);
+#pragma unroll
+                        for (int kb = 0; kb < kKB; ++kb)
+                            tma_load_3d(smem + S::kQ + qs * S::kTile + kb * 16384, &tmq, &qfull[qs], kb * 64, pc.kvh * a.G,
+                                        pc.rq.x + (q_first + qt) * a.tq);
                     }
-                    lse[e] = l;
+                    __syncwarp();
+                }
+            }
+            if (!ok) {  // let the copies already issued land before the CTA exits
+                volatile int no_abort = 0;
+                for (uint32_t t = g >= NQ ? g - NQ : 0; t < g; ++t) mbar_wait(&qfull[t % NQ], (t / NQ) & 1, &no_abort, kWaitLimit);
+            }
+        } else if (warp == 2) {
+            // ------------------------------------------------------ key pairs; lane x copies page x
+            const int page = 1 << a.page_log2, box = page < kBN ? page : kBN;
+            uint32_t piece = 0;
+            while (ok && cur.next(pc)) {
+                const uint32_t ks = piece % NK;
+                const int key = pc.jt * kWgKeys + lane * box, keys = pc.rq.z + pc.rq.y;
+                int row = -1;
+                if (lane * box < kWgKeys && key < keys) {
+                    const long long s = key_slot(a, pc.b, key);
+                    row = s < 0 ? a.n_pages << a.page_log2 : (int)s;  // outside the pool: the copy fills zeros
+                }
+                const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, row >= 0)) * (uint32_t)(box * D * 2);
+                if (!(ok = warp_wait(&kempty[ks], ((piece / NK) & 1) ^ 1, s_abort, a.wait_limit))) break;
+                if (lane == 0) mbar_expect_tx(&kfull[ks], tx);
+                __syncwarp();
+                if (row >= 0) {
+                    const int at = lane * box;  // key tile at / 128, its row at % 128
+                    unsigned char *dst = smem + S::kK + (2 * ks + at / kBN) * S::kTile + at % kBN * 128;
+#pragma unroll
+                    for (int kb = 0; kb < kKB; ++kb) tma_load_3d(dst + kb * 16384, &tmk, &kfull[ks], kb * 64, pc.kvh, row);
                 }
                 __syncwarp();
-                // columns [lo, hi) see the key: its token is cached or not later than theirs
-                const int lo = max(0, key - pc.rq.z - tok0) * a.G, hi = min(a.tq, pc.rq.y - tok0) * a.G;
-                const bool checked = __any_sync(0xffffffffu, odd || lo > 0 || hi < a.tq * a.G);
-                if (!(ok = warp_wait(&sfull[buf], (gt / NS) & 1, s_abort, a.wait_limit))) break;
-                tc_fence_after();
-                warp_arrive(&qempty[gt % NQ]);
-                uint32_t xa[32], xb[32], xc[32], xd[32];
-                const uint32_t s_tm = tmem + lane_off + buf * 128;
-                tmem_ld32(s_tm, xa);
-                tmem_ld32(s_tm + 32, xb);
-                tmem_ld32(s_tm + 64, xc);
-                tmem_ld32(s_tm + 96, xd);
-                tmem_wait_ld();
-                tmem_regs_ready(xa);
-                tmem_regs_ready(xb);
-                tmem_regs_ready(xc);
-                tmem_regs_ready(xd);
-                tc_fence_before();
-                warp_arrive(&sempty[buf]);
-                const float2 c2 = make_float2(c, c);
-                auto add = [&](const uint32_t(&s)[32], int base) {
+                ++piece;
+            }
+            if (!ok) {
+                volatile int no_abort = 0;
+                for (uint32_t t = piece >= NK ? piece - NK : 0; t < piece; ++t) mbar_wait(&kfull[t % NK], (t / NK) & 1, &no_abort, kWaitLimit);
+            }
+        } else {
+            // ------------------------------------------------------ the columns' lse
+            uint32_t g = 0;
+            while (ok && cur.next(pc)) {
+                const int q_first = first_q(a, pc.rq, pc.jt);
+                for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
+                    const uint32_t ls = g % NL;
+                    const int tok0 = (q_first + qt) * a.tq;
+                    float v[4];
+                    uint32_t m[4];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float4 l = *reinterpret_cast<const float4 *>(lse + base + e);
-                        float2 u = fma2(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, make_float2(-l.x, -l.y));
-                        float2 v = fma2(make_float2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c2, make_float2(-l.z, -l.w));
-                        if (checked) {  // by selection: what is hidden may be NaN
-                            const int i = base + e;
-                            u.x = i >= lo && i < hi && l.x != INFINITY ? u.x : -INFINITY;
-                            u.y = i + 1 >= lo && i + 1 < hi && l.y != INFINITY ? u.y : -INFINITY;
-                            v.x = i + 2 >= lo && i + 2 < hi && l.z != INFINITY ? v.x : -INFINITY;
-                            v.y = i + 3 >= lo && i + 3 < hi && l.w != INFINITY ? v.y : -INFINITY;
-                        }
-                        sum = add2(sum, add2(make_float2(ex2(u.x), ex2(u.y)), make_float2(ex2(v.x), ex2(v.y))));
+                    for (int i = 0; i < 4; ++i) {  // column c = 32 i + lane: token tok0 + c / G, head c % G of the group
+                        const int c = 32 * i + lane, tk = c / a.G, tok = tok0 + tk;
+                        v[i] = INFINITY;
+                        if (tk < a.tq && tok < pc.rq.y)
+                            v[i] = a.lse[(long long)(pc.rq.x + tok) * a.Hq + pc.kvh * a.G + (c - tk * a.G)];
                     }
-                };
-                add(xa, 0);
-                add(xb, 32);
-                add(xc, 64);
-                add(xd, 96);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m[i] = __ballot_sync(0xffffffffu, isfinite(v[i]));
+                    if (!(ok = warp_wait(&lempty[ls], ((g / NL) & 1) ^ 1, s_abort, a.wait_limit))) break;
+                    float *nl = reinterpret_cast<float *>(smem + S::kLse) + ls * 128;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) nl[32 * i + lane] = isfinite(v[i]) ? v[i] * -1.4426950408889634f : 0.f;
+                    if (lane < 4)
+                        reinterpret_cast<uint32_t *>(smem + S::kMask)[ls * 4 + lane] = lane == 0 ? m[0] : lane == 1 ? m[1] : lane == 2 ? m[2] : m[3];
+                    warp_arrive(&lfull[ls]);
+                }
+            }
+        }
+    } else {
+        reg_alloc<kWgRegsSum>();
+        // ---------------------------------------------------------- sums (a thread per key)
+        const int x = (warp - 4) >> 2, r = tid & (kBN - 1);
+        const uint32_t s_tm0 = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)x * 256;
+        const float c = a.scale * 1.4426950408889634f;
+        const int halves = (cols + 63) / 64;
+        uint32_t g = 0, u = 0;  // Q tiles; those of this key tile
+        while (ok && cur.next(pc)) {
+            const int key = pc.jt * kWgKeys + x * kBN + r, keys = pc.rq.z + pc.rq.y;
+            const bool here = keys > pc.jt * kWgKeys + x * kBN;  // this key tile has keys
+            const int q_first = first_q(a, pc.rq, pc.jt);
+            const long long slot = key < keys ? key_slot(a, pc.b, key) : -1;
+            float sum4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
+                const uint32_t ls = g % NL;
+                if (!here) {
+                    if (!(ok = quick_wait(&lfull[ls], (g / NL) & 1, s_abort, a.wait_limit))) break;
+                    warp_arrive(&lempty[ls]);
+                    continue;
+                }
+                const uint32_t buf = 2 * x + (u & 1);
+                if (!(ok = quick_wait2(&lfull[ls], (g / NL) & 1, &sfull[buf], (u >> 1) & 1, s_abort, a.wait_limit))) break;
+                tc_fence_after();
+                // columns from lo on see the key: its token is cached or not later than theirs
+                const int lo = max(0, key - pc.rq.z - (q_first + qt) * a.tq) * a.G;
+                const float4 *nl = reinterpret_cast<const float4 *>(smem + S::kLse) + ls * 32;
+                const uint32_t *mask = reinterpret_cast<const uint32_t *>(smem + S::kMask) + ls * 4;
+#pragma unroll 1
+                for (int hh = 0; hh < halves; ++hh) {
+                    uint32_t va[32], vb[32];
+                    const uint32_t s_tm = s_tm0 + (u & 1) * 128 + hh * 64;
+                    tmem_ld32(s_tm, va);
+                    tmem_ld32(s_tm + 32, vb);
+                    const int l0 = lo - hh * 64, l1 = l0 - 32;
+                    const uint32_t ma = mask[2 * hh] & (l0 <= 0 ? 0xffffffffu : l0 >= 32 ? 0u : ~((1u << l0) - 1u));
+                    const uint32_t mb = mask[2 * hh + 1] & (l1 <= 0 ? 0xffffffffu : l1 >= 32 ? 0u : ~((1u << l1) - 1u));
+                    tmem_wait_ld();
+                    tmem_regs_ready(va);
+                    tmem_regs_ready(vb);
+                    if (hh == halves - 1) {
+                        tc_fence_before();
+                        warp_arrive(&sempty[buf]);
+                    }
+                    hide(va, ma);  // by selection: what is hidden may be NaN
+                    hide(vb, mb);
+                    exp_sums(va, vb, c, nl + hh * 16, sum4);
+                }
+                warp_arrive(&lempty[ls]);
+                ++u;
             }
             if (!ok) break;
-            float total = sum.x + sum.y;
-            // the warpgroup of the last tile adds what the other one has and writes
-            const bool writer = (int)((g + n - 1) & 1) == x;
-            if (n > 1) {
-                if (!writer) {
-                    if (gifts > 0 && !(ok = warp_wait(taken, (gifts - 1) & 1, s_abort, a.wait_limit))) break;
-                    s_sum[r] = total;
-                    warp_arrive(given);
-                } else {
-                    if (!(ok = warp_wait(given, gifts & 1, s_abort, a.wait_limit))) break;
-                    total += s_sum[r];
-                    warp_arrive(taken);
-                }
-                ++gifts;
+            const float total = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+            if (key < keys) {
+                if (pc.slot >= 0) a.part[pc.slot * kWgKeys + x * kBN + r] = total;
+                else if (slot < 0) atomicOr(&a.status[pc.b], RS_ST_BAD_PAGE);
+                else atomicAdd(&a.weights[((long long)pc.kvh * a.n_pages << a.page_log2) + slot], total);  // the key's only one
             }
-            if (writer && key < keys) {
-                if (pc.slot >= 0) {
-                    a.part[pc.slot * kBN + r] = total;
-                } else {
-                    const long long s = key_slot(a, pc.b, key);
-                    if (s < 0) atomicOr(&a.status[pc.b], RS_ST_BAD_PAGE);
-                    else a.weights[((long long)pc.kvh * a.n_pages << a.page_log2) + s] += total;
-                }
-            }
-            g += n;
         }
     }
     __syncthreads();
-    if (warp == kMmaWarp) {
+    if (warp == 0) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
     }
@@ -465,26 +502,26 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
 // Joins the sums of the segments that the shares' ends cut: block c looks at
 // where CTA c + 1's share starts and, if that is the first cut of a segment,
 // adds up its pieces in order.
-__global__ void __launch_bounds__(kBN)
+__global__ void __launch_bounds__(kWgKeys)
 weigh_combine(WeighArgs a) {
     pdl_enter();
     const int c = blockIdx.x + 1, r = threadIdx.x;
     const int4 at = a.bound[c], before = a.bound[c - 1];
     auto same = [&](int4 p) { return p.x == at.x && p.y == at.y && p.z == at.z && p.w > 0; };
     if (at.w == 0 || same(before)) return;
-    float total = a.part[(2 * (c - 1) + 1) * kBN + r];
+    float total = a.part[(2 * (c - 1) + 1) * kWgKeys + r];
     for (int c1 = c; c1 < a.grid; ++c1) {
         const int4 p = a.bound[c1], q = a.bound[c1 + 1];
         if (!same(p)) break;
         if (same(q) && q.w == p.w) continue;  // an empty share
-        total += a.part[2 * c1 * kBN + r];
+        total += a.part[2 * c1 * kWgKeys + r];
     }
     const int4 rq = a.req[at.y];
-    const int key = at.z * kBN + r;
+    const int key = at.z * kWgKeys + r;
     if (key >= rq.z + rq.y) return;
     const long long s = key_slot(a, at.y, key);
     if (s < 0) atomicOr(&a.status[at.y], RS_ST_BAD_PAGE);
-    else a.weights[((long long)at.x * a.n_pages << a.page_log2) + s] += total;
+    else atomicAdd(&a.weights[((long long)at.x * a.n_pages << a.page_log2) + s], total);
 }
 
 size_t carve(WeighArgs &a, void *base, int B, int grid) {
@@ -492,7 +529,7 @@ size_t carve(WeighArgs &a, void *base, int B, int grid) {
     a.req = cv.take<int4>((size_t)B);
     a.cum = cv.take<long long>((size_t)B + 1);
     a.bound = cv.take<int4>((size_t)grid + 1);
-    a.part = cv.take<float>(2 * (size_t)grid * kBN);
+    a.part = cv.take<float>(2 * (size_t)grid * kWgKeys);
     return cv.used();
 }
 
@@ -500,26 +537,33 @@ int weigh_grid() { return std::min(num_sms(), kAttnMaxGrid); }
 
 template <int D, bool BF16>
 rs_status weigh_launch(const WeighArgs &a, const CUtensorMap &tmq, const CUtensorMap &tmk, const char *what, cudaStream_t st) {
+    // per device: 0 not asked, 1 ready, -1 too few registers for the warpgroups' split
     static std::atomic<int> ready[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
         set_error("%s: no current device", what);
         return RS_ERR_CUDA;
     }
-    if (!ready[dev].load()) {
-        const cudaError_t e = cudaFuncSetAttribute(weigh_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, WgSmem<D>::kTotal);
-        if (e != cudaSuccess) {
-            set_error("%s: cudaFuncSetAttribute: %s", what, cudaGetErrorString(e));
+    if (ready[dev].load() == 0) {
+        cudaFuncAttributes fa;
+        const cudaError_t e1 = cudaFuncGetAttributes(&fa, weigh_kernel<D, BF16>);
+        const cudaError_t e2 = cudaFuncSetAttribute(weigh_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, WgSmem<D>::kTotal);
+        if (e1 != cudaSuccess || e2 != cudaSuccess) {
+            set_error("%s: kernel attributes: %s", what, cudaGetErrorString(e1 != cudaSuccess ? e1 : e2));
             return RS_ERR_CUDA;
         }
-        ready[dev].store(1);
+        ready[dev].store(fa.numRegs * kWgThreads >= (int)(2 * 128 * kWgRegsSum + 128 * kWgRegsCopy) ? 1 : -1);
+    }
+    if (ready[dev].load() != 1) {
+        set_error("%s: kernel built with too few registers per thread", what);
+        return RS_ERR_CUDA;
     }
     launch_pdl(weigh_plan, dim3(1), dim3(1024), 0, st, a);
     RS_CHECK_LAUNCH(what);
     launch_pdl(weigh_kernel<D, BF16>, dim3(a.grid), dim3(kWgThreads), WgSmem<D>::kTotal, st, a, tmq, tmk);
     RS_CHECK_LAUNCH(what);
     if (a.grid > 1) {
-        launch_pdl(weigh_combine, dim3(a.grid - 1), dim3(kBN), 0, st, a);
+        launch_pdl(weigh_combine, dim3(a.grid - 1), dim3(kWgKeys), 0, st, a);
         RS_CHECK_LAUNCH(what);
     }
     return RS_OK;
@@ -569,7 +613,8 @@ extern "C" rs_status rs_paged_weights(const uint16_t *q, int64_t q_stride, int d
     a.Hq = Hq;
     a.Hkv = Hkv;
     a.G = Hq / Hkv;
-    a.tq = kBM / a.G;
+    // tokens of a Q tile: the average chunk, as far as 128 columns hold them
+    a.tq = std::max(1, std::min(kBM / a.G, (T + B - 1) / B));
     a.max_pages = n_pages ? max_pages : 0;
     a.n_pages = n_pages;
     a.page_log2 = page_log2(page_size);
