@@ -198,7 +198,9 @@ struct WgSmem {
     static constexpr int kNK = 2, kNQ = D == 128 ? 2 : 5, kNL = 4;  // key pairs, Q tiles, columns' lse
     static constexpr int kK = 0, kQ = kNK * 2 * kTile;
     static constexpr int kLse = kQ + kNQ * kTile;     // [kNL][128] floats: -lse in the log2 domain
-    static constexpr int kMask = kLse + kNL * 512;    // [kNL][4] words: the columns that count
+    static constexpr int kMask = kLse + kNL * 512;  // 16-byte aligned
+    static_assert(kMask % 16 == 0, "");
+       // [kNL][4] words: the columns that count
     static constexpr int kBar = kMask + kNL * 16;
     static constexpr int kNumBars = 2 * (kNK + kNQ + kNL + 4) + 1;
     static constexpr int kMisc = kBar + kNumBars * 8;
@@ -207,25 +209,31 @@ struct WgSmem {
     static_assert(kTotal <= 232448, "shared memory of one CTA");
 };
 
-// sum4 += 2^(c s_i + nl_i) over 64 columns; the order of the statements as in exp_pairs.
-__device__ __forceinline__ void exp_sums(const uint32_t (&s0)[32], const uint32_t (&s1)[32], float c, const float4 *nl,
-                                         float (&sum4)[4]) {
-    constexpr int kAhead = 8, kBehind = 8;  // columns
-    float d[64], p[64];
-    float4 l;
-    auto fma1 = [&](int i) {
-        if (i % 4 == 0) l = nl[i / 4];
-        const float n = i % 4 == 0 ? l.x : i % 4 == 1 ? l.y : i % 4 == 2 ? l.z : l.w;
-        const float v = __uint_as_float(i < 32 ? s0[i] : s1[i - 32]);
-        asm volatile("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d[i]) : "f"(v), "f"(c), "f"(n));
+// sum += 2^(c s_i + nl_i) over 64 columns, two at a time; the statements in an
+// order that keeps the other work between the exponentials (see exp_pairs).
+__device__ __forceinline__ void exp_sums(const uint32_t (&s0)[32], const uint32_t (&s1)[32], float2 c, const ulonglong2 *nl,
+                                         uint64_t (&sum)[4]) {
+    constexpr int kAhead = 4, kBehind = 4;  // pairs of columns
+    float2 d[32], p[32];
+    ulonglong2 l;
+    auto fma1 = [&](int e) {
+        if (e % 2 == 0) l = nl[e / 2];
+        const float2 v = e < 16 ? make_float2(__uint_as_float(s0[2 * e]), __uint_as_float(s0[2 * e + 1]))
+                                : make_float2(__uint_as_float(s1[2 * e - 32]), __uint_as_float(s1[2 * e - 31]));
+        uint64_t r;
+        asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_b64(v)), "l"(as_b64(c)), "l"(e % 2 ? l.y : l.x));
+        d[e] = as_float2(r);
     };
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) fma1(i);
+    for (int e = 0; e < kAhead; ++e) fma1(e);
 #pragma unroll
-    for (int i = 0; i < 64 + kBehind; ++i) {
-        if (i < 64) asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[i]) : "f"(d[i]));
-        if (i + kAhead < 64) fma1(i + kAhead);
-        if (i >= kBehind) asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(sum4[i & 3]) : "f"(p[i - kBehind]));
+    for (int e = 0; e < 32 + kBehind; ++e) {
+        if (e < 32) {
+            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[e].x) : "f"(d[e].x));
+            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[e].y) : "f"(d[e].y));
+        }
+        if (e + kAhead < 32) fma1(e + kAhead);
+        if (e >= kBehind) asm volatile("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[e & 3]) : "l"(as_b64(p[e - kBehind])));
     }
 }
 
@@ -401,20 +409,31 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
         } else {
             // ------------------------------------------------------ the columns' lse
             uint32_t g = 0;
+            int tk[4], hg[4];  // column c = 32 i + lane: token c / G of the tile, head c % G of the group
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                tk[i] = (32 * i + lane) / a.G;
+                hg[i] = 32 * i + lane - tk[i] * a.G;
+            }
             while (ok && cur.next(pc)) {
                 const int q_first = first_q(a, pc.rq, pc.jt);
+                auto read = [&](int qt, float(&v)[4]) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int tok = (q_first + qt) * a.tq + tk[i];
+                        v[i] = INFINITY;
+                        if (tk[i] < a.tq && tok < pc.rq.y) v[i] = a.lse[(long long)(pc.rq.x + tok) * a.Hq + pc.kvh * a.G + hg[i]];
+                    }
+                };
+                float next[4];
+                read(pc.q0, next);
                 for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
                     const uint32_t ls = g % NL;
-                    const int tok0 = (q_first + qt) * a.tq;
                     float v[4];
                     uint32_t m[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {  // column c = 32 i + lane: token tok0 + c / G, head c % G of the group
-                        const int c = 32 * i + lane, tk = c / a.G, tok = tok0 + tk;
-                        v[i] = INFINITY;
-                        if (tk < a.tq && tok < pc.rq.y)
-                            v[i] = a.lse[(long long)(pc.rq.x + tok) * a.Hq + pc.kvh * a.G + (c - tk * a.G)];
-                    }
+                    for (int i = 0; i < 4; ++i) v[i] = next[i];
+                    if (qt + 1 < pc.q1) read(qt + 1, next);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) m[i] = __ballot_sync(0xffffffffu, isfinite(v[i]));
                     if (!(ok = warp_wait(&lempty[ls], ((g / NL) & 1) ^ 1, s_abort, a.wait_limit))) break;
@@ -432,7 +451,7 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
         // ---------------------------------------------------------- sums (a thread per key)
         const int x = (warp - 4) >> 2, r = tid & (kBN - 1);
         const uint32_t s_tm0 = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)x * 256;
-        const float c = a.scale * 1.4426950408889634f;
+        const float2 c2 = make_float2(a.scale * 1.4426950408889634f, a.scale * 1.4426950408889634f);
         const int halves = (cols + 63) / 64;
         uint32_t g = 0, u = 0;  // Q tiles; those of this key tile
         while (ok && cur.next(pc)) {
@@ -440,7 +459,7 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             const bool here = keys > pc.jt * kWgKeys + x * kBN;  // this key tile has keys
             const int q_first = first_q(a, pc.rq, pc.jt);
             const long long slot = key < keys ? key_slot(a, pc.b, key) : -1;
-            float sum4[4] = {0.f, 0.f, 0.f, 0.f};
+            uint64_t sum[4] = {0, 0, 0, 0};  // pairs of floats
 #pragma unroll 1
             for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
                 const uint32_t ls = g % NL;
@@ -454,17 +473,15 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                 tc_fence_after();
                 // columns from lo on see the key: its token is cached or not later than theirs
                 const int lo = max(0, key - pc.rq.z - (q_first + qt) * a.tq) * a.G;
-                const float4 *nl = reinterpret_cast<const float4 *>(smem + S::kLse) + ls * 32;
-                const uint32_t *mask = reinterpret_cast<const uint32_t *>(smem + S::kMask) + ls * 4;
+                const ulonglong2 *nl = reinterpret_cast<const ulonglong2 *>(smem + S::kLse) + ls * 32;
+                const uint4 mask = reinterpret_cast<const uint4 *>(smem + S::kMask)[ls];
+                const bool open = __all_sync(0xffffffffu, lo == 0 && (mask.x & mask.y & mask.z & mask.w) == 0xffffffffu);
 #pragma unroll 1
                 for (int hh = 0; hh < halves; ++hh) {
                     uint32_t va[32], vb[32];
                     const uint32_t s_tm = s_tm0 + (u & 1) * 128 + hh * 64;
                     tmem_ld32(s_tm, va);
                     tmem_ld32(s_tm + 32, vb);
-                    const int l0 = lo - hh * 64, l1 = l0 - 32;
-                    const uint32_t ma = mask[2 * hh] & (l0 <= 0 ? 0xffffffffu : l0 >= 32 ? 0u : ~((1u << l0) - 1u));
-                    const uint32_t mb = mask[2 * hh + 1] & (l1 <= 0 ? 0xffffffffu : l1 >= 32 ? 0u : ~((1u << l1) - 1u));
                     tmem_wait_ld();
                     tmem_regs_ready(va);
                     tmem_regs_ready(vb);
@@ -472,15 +489,19 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                         tc_fence_before();
                         warp_arrive(&sempty[buf]);
                     }
-                    hide(va, ma);  // by selection: what is hidden may be NaN
-                    hide(vb, mb);
-                    exp_sums(va, vb, c, nl + hh * 16, sum4);
+                    if (!open) {  // by selection: what is hidden may be NaN
+                        const int l0 = lo - hh * 64, l1 = l0 - 32;
+                        hide(va, (hh ? mask.z : mask.x) & (l0 <= 0 ? 0xffffffffu : l0 >= 32 ? 0u : ~((1u << l0) - 1u)));
+                        hide(vb, (hh ? mask.w : mask.y) & (l1 <= 0 ? 0xffffffffu : l1 >= 32 ? 0u : ~((1u << l1) - 1u)));
+                    }
+                    exp_sums(va, vb, c2, nl + hh * 16, sum);
                 }
                 warp_arrive(&lempty[ls]);
                 ++u;
             }
             if (!ok) break;
-            const float total = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+            const float2 t = add2(add2(as_float2(sum[0]), as_float2(sum[1])), add2(as_float2(sum[2]), as_float2(sum[3])));
+            const float total = t.x + t.y;
             if (key < keys) {
                 if (pc.slot >= 0) a.part[pc.slot * kWgKeys + x * kBN + r] = total;
                 else if (slot < 0) atomicOr(&a.status[pc.b], RS_ST_BAD_PAGE);
