@@ -55,7 +55,10 @@ __device__ __forceinline__ int key_tiles(int4 rq) { return rq.y > 0 ? (rq.z + rq
 // first Q tile that sees key pair jt, and the cost of the request's pairs before
 // jt: (Q tiles + beta) tq each, 256 less for every one that lies behind the
 // cached tokens (what it sees, up to rounding: the split needs no more)
-__device__ __forceinline__ int first_q(const WeighArgs &a, int4 rq, int jt) { return max(0, jt * kWgKeys - rq.z) / a.tq; }
+__device__ __forceinline__ int first_q(const WeighArgs &a, int4 rq, int jt) {
+    const int behind = jt * kWgKeys - rq.z;  // most often none: no division
+    return behind > 0 ? behind / a.tq : 0;
+}
 __device__ __forceinline__ long long tiles_cost(const WeighArgs &a, int4 rq, int jt) {
     const long long full = (long long)((rq.y + a.tq - 1) / a.tq + kWgBeta) * a.tq;
     const long long m = max(0, jt - (rq.z + kWgKeys - 1) / kWgKeys);
@@ -147,13 +150,14 @@ weigh_plan(WeighArgs a) {
 }
 
 struct WgPiece {
-    int kvh, b, jt, q0, q1;  // Q tiles [q0, q1), counted from the first that sees the keys
+    int kvh, b, jt, q_first, q0, q1;  // Q tiles [q0, q1), counted from q_first, the first that sees the keys
     int4 rq;
     int slot;                // -1: the segment is complete here
 };
 struct WgCursor {
     const WeighArgs &a;
-    int4 at, end;
+    int4 at, end, rq;
+    int rq_of = -1, nq_all = 0;  // the request that rq describes, its Q tiles
     __device__ __forceinline__ WgCursor(const WeighArgs &a_, int4 lo, int4 hi) : a(a_), at(lo), end(hi) {}
     __device__ __forceinline__ bool next(WgPiece &pc) {
         for (;;) {
@@ -161,7 +165,11 @@ struct WgCursor {
             if (at.x > end.x || (at.x == end.x && at.y > end.y) ||
                 (same_b && (at.z > end.z || (at.z == end.z && at.w >= end.w))))
                 return false;
-            const int4 rq = a.req[at.y];
+            if (rq_of != at.y) {
+                rq = a.req[at.y];
+                rq_of = at.y;
+                nq_all = (rq.y + a.tq - 1) / a.tq;
+            }
             if (at.z >= key_tiles(rq)) {  // next request, next head
                 at.z = at.w = 0;
                 if (++at.y == a.B) {
@@ -170,7 +178,8 @@ struct WgCursor {
                 }
                 continue;
             }
-            const int nq = (rq.y + a.tq - 1) / a.tq - first_q(a, rq, at.z);
+            pc.q_first = first_q(a, rq, at.z);
+            const int nq = nq_all - pc.q_first;
             pc.kvh = at.x;
             pc.b = at.y;
             pc.jt = at.z;
@@ -195,7 +204,7 @@ __device__ __forceinline__ long long key_slot(const WeighArgs &a, int b, int j) 
 template <int D>
 struct WgSmem {
     static constexpr int kTile = kBN * D * 2;
-    static constexpr int kNK = 2, kNQ = D == 128 ? 2 : 5, kNL = 4;  // key pairs, Q tiles, columns' lse
+    static constexpr int kNK = D == 128 ? 2 : 4, kNQ = D == 128 ? 2 : 4, kNL = 4;  // key pairs, Q tiles, columns' lse
     static constexpr int kK = 0, kQ = kNK * 2 * kTile;
     static constexpr int kLse = kQ + kNQ * kTile;     // [kNL][128] floats: -lse in the log2 domain
     static constexpr int kMask = kLse + kNL * 512;  // 16-byte aligned
@@ -209,12 +218,13 @@ struct WgSmem {
     static_assert(kTotal <= 232448, "shared memory of one CTA");
 };
 
-// sum += 2^(c s_i + nl_i) over 64 columns, two at a time; the statements in an
+// sum += 2^(c s_i + nl_i) over N columns, two at a time; the statements in an
 // order that keeps the other work between the exponentials (see exp_pairs).
+template <int N>
 __device__ __forceinline__ void exp_sums(const uint32_t (&s0)[32], const uint32_t (&s1)[32], float2 c, const ulonglong2 *nl,
                                          uint64_t (&sum)[4]) {
     constexpr int kAhead = 4, kBehind = 4;  // pairs of columns
-    float2 d[32], p[32];
+    float2 d[N / 2], p[N / 2];
     ulonglong2 l;
     auto fma1 = [&](int e) {
         if (e % 2 == 0) l = nl[e / 2];
@@ -227,12 +237,12 @@ __device__ __forceinline__ void exp_sums(const uint32_t (&s0)[32], const uint32_
 #pragma unroll
     for (int e = 0; e < kAhead; ++e) fma1(e);
 #pragma unroll
-    for (int e = 0; e < 32 + kBehind; ++e) {
-        if (e < 32) {
+    for (int e = 0; e < N / 2 + kBehind; ++e) {
+        if (e < N / 2) {
             asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[e].x) : "f"(d[e].x));
             asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[e].y) : "f"(d[e].y));
         }
-        if (e + kAhead < 32) fma1(e + kAhead);
+        if (e + kAhead < N / 2) fma1(e + kAhead);
         if (e >= kBehind) asm volatile("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[e & 3]) : "l"(as_b64(p[e - kBehind])));
     }
 }
@@ -359,7 +369,7 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             const uint32_t q_tx = (uint32_t)cols * D * 2;
             uint32_t g = 0;
             while (ok && cur.next(pc)) {
-                const int q_first = first_q(a, pc.rq, pc.jt);
+                const int q_first = pc.q_first;
                 for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
                     const uint32_t qs = g % NQ;
                     if (!(ok = warp_wait(&qempty[qs], ((g / NQ) & 1) ^ 1, s_abort, a.wait_limit))) break;
@@ -381,23 +391,29 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             // ------------------------------------------------------ key pairs; lane x copies page x
             const int page = 1 << a.page_log2, box = page < kBN ? page : kBN;
             uint32_t piece = 0;
-            while (ok && cur.next(pc)) {
+            // pool row of lane x's copy; the table is read a segment ahead
+            auto row_of = [&](const WgPiece &p) -> int {
+                const int key = p.jt * kWgKeys + lane * box;
+                if (lane * box >= kWgKeys || key >= p.rq.z + p.rq.y) return -1;
+                const long long s = key_slot(a, p.b, key);
+                return s < 0 ? a.n_pages << a.page_log2 : (int)s;  // outside the pool: the copy fills zeros
+            };
+            bool more = cur.next(pc);
+            int row = more ? row_of(pc) : -1;
+            while (more) {
                 const uint32_t ks = piece % NK;
-                const int key = pc.jt * kWgKeys + lane * box, keys = pc.rq.z + pc.rq.y;
-                int row = -1;
-                if (lane * box < kWgKeys && key < keys) {
-                    const long long s = key_slot(a, pc.b, key);
-                    row = s < 0 ? a.n_pages << a.page_log2 : (int)s;  // outside the pool: the copy fills zeros
-                }
-                const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, row >= 0)) * (uint32_t)(box * D * 2);
+                const int kvh = pc.kvh, from = row;
+                more = cur.next(pc);
+                row = more ? row_of(pc) : -1;
+                const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, from >= 0)) * (uint32_t)(box * D * 2);
                 if (!(ok = warp_wait(&kempty[ks], ((piece / NK) & 1) ^ 1, s_abort, a.wait_limit))) break;
                 if (lane == 0) mbar_expect_tx(&kfull[ks], tx);
                 __syncwarp();
-                if (row >= 0) {
+                if (from >= 0) {
                     const int at = lane * box;  // key tile at / 128, its row at % 128
                     unsigned char *dst = smem + S::kK + (2 * ks + at / kBN) * S::kTile + at % kBN * 128;
 #pragma unroll
-                    for (int kb = 0; kb < kKB; ++kb) tma_load_3d(dst + kb * 16384, &tmk, &kfull[ks], kb * 64, pc.kvh, row);
+                    for (int kb = 0; kb < kKB; ++kb) tma_load_3d(dst + kb * 16384, &tmk, &kfull[ks], kb * 64, kvh, from);
                 }
                 __syncwarp();
                 ++piece;
@@ -416,7 +432,7 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                 hg[i] = 32 * i + lane - tk[i] * a.G;
             }
             while (ok && cur.next(pc)) {
-                const int q_first = first_q(a, pc.rq, pc.jt);
+                const int q_first = pc.q_first;
                 auto read = [&](int qt, float(&v)[4]) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -457,7 +473,7 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
         while (ok && cur.next(pc)) {
             const int key = pc.jt * kWgKeys + x * kBN + r, keys = pc.rq.z + pc.rq.y;
             const bool here = keys > pc.jt * kWgKeys + x * kBN;  // this key tile has keys
-            const int q_first = first_q(a, pc.rq, pc.jt);
+            const int q_first = pc.q_first;
             const long long slot = key < keys ? key_slot(a, pc.b, key) : -1;
             uint64_t sum[4] = {0, 0, 0, 0};  // pairs of floats
 #pragma unroll 1
@@ -476,25 +492,36 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                 const ulonglong2 *nl = reinterpret_cast<const ulonglong2 *>(smem + S::kLse) + ls * 32;
                 const uint4 mask = reinterpret_cast<const uint4 *>(smem + S::kMask)[ls];
                 const bool open = __all_sync(0xffffffffu, lo == 0 && (mask.x & mask.y & mask.z & mask.w) == 0xffffffffu);
-#pragma unroll 1
-                for (int hh = 0; hh < halves; ++hh) {
-                    uint32_t va[32], vb[32];
-                    const uint32_t s_tm = s_tm0 + (u & 1) * 128 + hh * 64;
-                    tmem_ld32(s_tm, va);
-                    tmem_ld32(s_tm + 32, vb);
+                if (cols <= 32) {  // single tokens, short chunks
+                    uint32_t va[32];
+                    tmem_ld32(s_tm0 + (u & 1) * 128, va);
                     tmem_wait_ld();
                     tmem_regs_ready(va);
-                    tmem_regs_ready(vb);
-                    if (hh == halves - 1) {
-                        tc_fence_before();
-                        warp_arrive(&sempty[buf]);
+                    tc_fence_before();
+                    warp_arrive(&sempty[buf]);
+                    hide(va, mask.x & (lo <= 0 ? 0xffffffffu : lo >= 32 ? 0u : ~((1u << lo) - 1u)));
+                    exp_sums<32>(va, va, c2, nl, sum);
+                } else {
+#pragma unroll 1
+                    for (int hh = 0; hh < halves; ++hh) {
+                        uint32_t va[32], vb[32];
+                        const uint32_t s_tm = s_tm0 + (u & 1) * 128 + hh * 64;
+                        tmem_ld32(s_tm, va);
+                        tmem_ld32(s_tm + 32, vb);
+                        tmem_wait_ld();
+                        tmem_regs_ready(va);
+                        tmem_regs_ready(vb);
+                        if (hh == halves - 1) {
+                            tc_fence_before();
+                            warp_arrive(&sempty[buf]);
+                        }
+                        if (!open) {  // by selection: what is hidden may be NaN
+                            const int l0 = lo - hh * 64, l1 = l0 - 32;
+                            hide(va, (hh ? mask.z : mask.x) & (l0 <= 0 ? 0xffffffffu : l0 >= 32 ? 0u : ~((1u << l0) - 1u)));
+                            hide(vb, (hh ? mask.w : mask.y) & (l1 <= 0 ? 0xffffffffu : l1 >= 32 ? 0u : ~((1u << l1) - 1u)));
+                        }
+                        exp_sums<64>(va, vb, c2, nl + hh * 16, sum);
                     }
-                    if (!open) {  // by selection: what is hidden may be NaN
-                        const int l0 = lo - hh * 64, l1 = l0 - 32;
-                        hide(va, (hh ? mask.z : mask.x) & (l0 <= 0 ? 0xffffffffu : l0 >= 32 ? 0u : ~((1u << l0) - 1u)));
-                        hide(vb, (hh ? mask.w : mask.y) & (l1 <= 0 ? 0xffffffffu : l1 >= 32 ? 0u : ~((1u << l1) - 1u)));
-                    }
-                    exp_sums(va, vb, c2, nl + hh * 16, sum);
                 }
                 warp_arrive(&lempty[ls]);
                 ++u;
