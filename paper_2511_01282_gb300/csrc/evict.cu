@@ -10,6 +10,7 @@
 // evict_move.
 // Bound: weights and positions read once, the movers' rows read and written.
 #include <algorithm>
+#include <atomic>
 
 #include "common.cuh"
 #include "tmap.cuh"
@@ -22,7 +23,7 @@ struct EvictArgs {
     const int32_t *table, *len, *next_pos;
     float *weights;
     int32_t *positions, *new_len, *status;
-    int2 *moves;      // [B][Hkv][budget] (from, to) rows of the pool
+    int2 *moves;      // [B][Hkv][budget] (from, to) slots of the request
     int *n_moves;     // [B][Hkv]
     int B, Hkv, D, n_pages, page_log2, max_pages, budget, recent;
 };
@@ -34,41 +35,188 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return (u >> 31) ? ~u : (u | 0x80000000u);
 }
 
+// evict_select: a warp owns a run of consecutive slots, 32 at a time.  The keys
+// are read once into shared memory, as many as it holds (49152 tokens a CTA);
+// longer caches are read again in each pass.  (In registers, with every loop
+// unrolled, 32 keys a thread took twice as long: the code runs once and is all
+// instruction misses.)  The budget-th largest key is
+// found by three digits of 11, 11 and 10 bits (the sign, the exponent and two bits
+// of the fraction are the first, so that weights of one distribution spread over
+// many counters); a warp whose lanes all hold one digit counts once.  Then the
+// ties, the holes and the movers are ranked in slot order by ballots and two
+// prefixes over the 32 warps.
+// Bound: latency (table, then weights and positions; the passes' counters).
 constexpr int kSelThreads = 1024;
+constexpr int kSelKeys = 49152;
+constexpr int kSelBins = 2048;
 
-// Inclusive prefix of two small counts at once (16 bits each would overflow:
-// two ints) over the block, on top of a carry that every thread keeps.
-__device__ __forceinline__ int block_prefix(int v, int &carry, int *s_w) {
+struct SelShared {
+    int hist[kSelBins];
+    int warp[3][32];
+    uint32_t prefix;
+    int left;
+};
+
+// Exclusive prefix of the warps' counts in row, and their sum (whole block).
+__device__ __forceinline__ int warps_before(int (&row)[32], int count, int &sum) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int x = v;
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-    }
-    if (lane == 31) s_w[warp] = x;
+    if (lane == 0) row[warp] = count;
     __syncthreads();
-    int w = s_w[lane];
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, w, o);
-        if (lane >= o) w += y;
+    const int v = row[lane];
+    sum = __reduce_add_sync(0xffffffffu, v);
+    return __reduce_add_sync(0xffffffffu, lane < warp ? v : 0);
+}
+
+struct SelKeys {
+    const int32_t *table, *positions;
+    const float *weights;
+    long long newest;
+    int page_log2;
+    // pool rows of N slots, 32 apart, then their keys: the loads of a step go out together
+    template <int N>
+    __device__ __forceinline__ void read(int s, int len, uint32_t (&k)[N]) const {
+        int id[N];
+        float w[N];
+        int32_t p[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) id[i] = s + 32 * i < len ? table[(s + 32 * i) >> page_log2] : 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = s + 32 * i;
+            const long long r = ((long long)id[i] << page_log2) + (at & ((1 << page_log2) - 1));
+            w[i] = at < len ? weights[r] : 0.f;
+            p[i] = at < len ? positions[r] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) k[i] = p[i] >= newest ? 0xffffffffu : weight_key(w[i]);
     }
-    const int before = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
-    x += carry + (warp ? before : 0);
-    carry += __shfl_sync(0xffffffffu, w, 31);
+};
+
+template <bool HELD>
+__device__ __forceinline__ void select_moves(const EvictArgs &a, SelShared &sh, uint32_t *keys, int len, int bh,
+                                             const SelKeys &src) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int steps = (len + kSelThreads - 1) / kSelThreads;  // of 32 slots a warp
+    const int first = warp * steps * 32 + lane;
+    constexpr int kAtOnce = 8;
+    if (HELD) {
+#pragma unroll 1
+        for (int i = 0; i < steps; i += kAtOnce) {
+            uint32_t k[kAtOnce];
+            src.read(first + i * 32, len, k);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+                if (i + j < steps) keys[(i + j) * kSelThreads + tid] = k[j];
+        }
+    }
+    // use(slot, key, in): every step of the warp, in order
+    auto each = [&](auto use) {
+        if (HELD) {
+#pragma unroll 2
+            for (int i = 0; i < steps; ++i) use(first + i * 32, keys[i * kSelThreads + tid], first + i * 32 < len);
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < steps; i += kAtOnce) {
+                uint32_t k[kAtOnce];
+                src.read(first + i * 32, len, k);
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (i + j < steps) use(first + (i + j) * 32, k[j], first + (i + j) * 32 < len);
+            }
+        }
+    };
+    uint32_t prefix = 0;
+    int left = a.budget;  // of the keys that share the prefix, how many stay
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int bits = pass == 2 ? 10 : 11, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = 1 << bits;
+        for (int i = tid; i < bins; i += kSelThreads) sh.hist[i] = 0;
+        __syncthreads();
+        each([&](int, uint32_t k, bool in) {
+            const bool on = in && (pass == 0 || (k >> (shift + bits)) == (prefix >> (shift + bits)));
+            const unsigned m = __ballot_sync(0xffffffffu, on);
+            if (m == 0) return;
+            const int d = (int)((k >> shift) & (uint32_t)(bins - 1));
+            const int d0 = __shfl_sync(0xffffffffu, d, __ffs(m) - 1);
+            if (__all_sync(0xffffffffu, !on || d == d0)) {
+                if (lane == 0) atomicAdd(&sh.hist[d0], __popc(m));
+            } else if (on) {
+                atomicAdd(&sh.hist[d], 1);
+            }
+        });
+        __syncthreads();
+        // thread t owns bins / 1024 digits, the highest first
+        const int per = bins / kSelThreads;
+        int mine = 0;
+        for (int i = 0; i < per; ++i) mine += sh.hist[bins - 1 - (tid * per + i)];
+        int incl = mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        int all;
+        const int before = warps_before(sh.warp[pass], __shfl_sync(0xffffffffu, incl, 31), all);
+        int above = before + incl - mine;
+        if (above < left && above + mine >= left) {
+            for (int i = 0; i < per; ++i) {
+                const int d = bins - 1 - (tid * per + i), n = sh.hist[d];
+                if (above + n >= left) {
+                    sh.prefix = prefix | ((uint32_t)d << shift);
+                    sh.left = left - above;
+                    break;
+                }
+                above += n;
+            }
+        }
+        __syncthreads();
+        prefix = sh.prefix;
+        left = sh.left;
+    }
+    // keys above the threshold stay, and the first `left` equal to it
+    const unsigned below = (1u << lane) - 1u;
+    int ties = 0, sum;
+    each([&](int, uint32_t k, bool in) { ties += __popc(__ballot_sync(0xffffffffu, in && k == prefix)); });
     __syncthreads();
-    return x;
+    const int ties0 = warps_before(sh.warp[0], ties, sum);
+    auto marks = [&](int s, uint32_t k, bool in, int &rank, bool &hole, bool &mover) {
+        const bool tie = in && k == prefix;
+        const unsigned m = __ballot_sync(0xffffffffu, tie);
+        const bool kept = in && (k > prefix || (tie && rank + __popc(m & below) < left));
+        rank += __popc(m);
+        hole = s < a.budget && in && !kept;
+        mover = s >= a.budget && kept;
+    };
+    int rank = ties0, holes = 0, movers = 0;
+    each([&](int s, uint32_t k, bool in) {
+        bool hole, mover;
+        marks(s, k, in, rank, hole, mover);
+        holes += __popc(__ballot_sync(0xffffffffu, hole));
+        movers += __popc(__ballot_sync(0xffffffffu, mover));
+    });
+    int n;
+    int hole_at = warps_before(sh.warp[1], holes, n), mover_at = warps_before(sh.warp[2], movers, n);
+    int2 *moves = a.moves + (long long)bh * a.budget;
+    rank = ties0;
+    each([&](int s, uint32_t k, bool in) {
+        bool hole, mover;
+        marks(s, k, in, rank, hole, mover);
+        const unsigned mh = __ballot_sync(0xffffffffu, hole), mm = __ballot_sync(0xffffffffu, mover);
+        if (hole) moves[hole_at + __popc(mh & below)].y = s;
+        if (mover) moves[mover_at + __popc(mm & below)].x = s;
+        hole_at += __popc(mh);
+        mover_at += __popc(mm);
+    });
+    if (tid == 0) a.n_moves[bh] = n;
 }
 
 __global__ void __launch_bounds__(kSelThreads)
 evict_select(EvictArgs a) {
     pdl_enter();
-    __shared__ int s_hist[256], s_w[32];
-    __shared__ uint32_t s_prefix;
-    __shared__ int s_left;
+    __shared__ SelShared sh;
+    extern __shared__ uint32_t s_keys[];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int len = a.len[b];
     const int32_t *table = a.table + (long long)b * a.max_pages;
-    const int pmask = (1 << a.page_log2) - 1;
     const long long slots = (long long)a.n_pages << a.page_log2;
     int st = 0, bad = 0;
     if (len < 0 || len > ((long long)a.max_pages << a.page_log2)) {
@@ -78,78 +226,18 @@ evict_select(EvictArgs a) {
     }
     if (__syncthreads_or(bad)) st = RS_ST_BAD_PAGE;
     const bool work = st == 0 && len > a.budget;
+    const int bh = b * a.Hkv + h;
     if (tid == 0) {
-        if (!work) a.n_moves[b * a.Hkv + h] = 0;
+        if (!work) a.n_moves[bh] = 0;
         if (h == 0) {
             a.status[b] = st;
             a.new_len[b] = work ? a.budget : len;
         }
     }
     if (!work) return;
-    const float *weights = a.weights + h * slots;
-    const int32_t *positions = a.positions ? a.positions + h * slots : nullptr;
-    const long long newest = (long long)a.next_pos[b] - a.recent;
-    auto row_of = [&](int s) -> long long { return ((long long)table[s >> a.page_log2] << a.page_log2) + (s & pmask); };
-    auto key_of = [&](int s) -> uint32_t {
-        const long long r = row_of(s);
-        return positions[r] >= newest ? 0xffffffffu : weight_key(weights[r]);
-    };
-    // the budget-th largest key, eight bits at a time
-    uint32_t prefix = 0;
-    int left = a.budget;  // of the keys that share the prefix, how many stay
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) s_hist[tid] = 0;
-        __syncthreads();
-        for (int s = tid; s < len; s += kSelThreads) {
-            const uint32_t k = key_of(s);
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[(k >> shift) & 255u], 1);
-        }
-        __syncthreads();
-        if (tid < 32) {  // lane: eight digits, highest first
-            int sum = 0;
-            for (int i = 0; i < 8; ++i) sum += s_hist[255 - (tid * 8 + i)];
-            int incl = sum;
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, incl, o);
-                if (tid >= o) incl += y;
-            }
-            int above = incl - sum;
-            if (above < left && incl >= left) {
-                for (int i = 0; i < 8; ++i) {
-                    const int d = 255 - (tid * 8 + i), n = s_hist[d];
-                    if (above + n >= left) {
-                        s_prefix = prefix | ((uint32_t)d << shift);
-                        s_left = left - above;
-                        break;
-                    }
-                    above += n;
-                }
-            }
-        }
-        __syncthreads();
-        prefix = s_prefix;
-        left = s_left;
-    }
-    // in slot order: keys above the threshold stay, and the first `left` equal to it
-    int2 *moves = a.moves + ((long long)b * a.Hkv + h) * a.budget;
-    int ties = 0, holes = 0, movers = 0;
-    for (int base = 0; base < len; base += kSelThreads) {
-        const int s = base + tid;
-        const uint32_t k = s < len ? key_of(s) : 0u;
-        const int tie = s < len && k == prefix;
-        const int rank = block_prefix(tie, ties, s_w);
-        const bool kept = s < len && (k > prefix || (tie && rank <= left));
-        const int hole = s < a.budget && !kept, mover = s >= a.budget && kept;
-        if (base < a.budget) {
-            const int i = block_prefix(hole, holes, s_w);
-            if (hole) moves[i - 1].y = (int)row_of(s);
-        }
-        if (base + kSelThreads > a.budget) {
-            const int i = block_prefix(mover, movers, s_w);
-            if (mover) moves[i - 1].x = (int)row_of(s);
-        }
-    }
-    if (tid == 0) a.n_moves[b * a.Hkv + h] = movers;
+    const SelKeys src{table, a.positions + h * slots, a.weights + h * slots, (long long)a.next_pos[b] - a.recent, a.page_log2};
+    if (len <= kSelKeys) select_moves<true>(a, sh, s_keys, len, bh, src);
+    else select_moves<false>(a, sh, s_keys, len, bh, src);
 }
 
 constexpr int kMoveThreads = 256;
@@ -164,9 +252,13 @@ evict_move(EvictArgs a) {
     const int n = a.n_moves[bh];
     const int2 *moves = a.moves + (long long)bh * a.budget;
     const long long slots = (long long)a.n_pages << a.page_log2;
+    const int32_t *table = a.table + (long long)(bh / a.Hkv) * a.max_pages;
+    const int pmask = (1 << a.page_log2) - 1;
     const int per = kMoveThreads / lanes;
     for (int i = blockIdx.x * per + threadIdx.x / lanes; i < n; i += gridDim.x * per) {
-        const int2 m = moves[i];
+        const int2 slot = moves[i];
+        const int2 m = make_int2((table[slot.x >> a.page_log2] << a.page_log2) + (slot.x & pmask),
+                                 (table[slot.y >> a.page_log2] << a.page_log2) + (slot.y & pmask));
         const long long from = ((long long)m.x * a.Hkv + h) * lanes + sub, to = ((long long)m.y * a.Hkv + h) * lanes + sub;
         const uint4 x = reinterpret_cast<const uint4 *>(a.k)[from], y = reinterpret_cast<const uint4 *>(a.v)[from];
         reinterpret_cast<uint4 *>(a.k)[to] = x;
@@ -242,7 +334,24 @@ extern "C" rs_status rs_paged_evict(uint16_t *k_pages, uint16_t *v_pages, int Hk
     a.max_pages = n_pages ? max_pages : 0;
     a.budget = budget;
     a.recent = recent;
-    launch_pdl(evict_select, dim3(Hkv, B), dim3(kSelThreads), 0, (cudaStream_t)stream, a);
+    // keys of the longest cache that the page tables allow
+    const long long most = std::min((long long)a.max_pages << a.page_log2, (long long)kSelKeys);
+    const size_t smem = (size_t)((most + kSelThreads - 1) / kSelThreads * kSelThreads) * sizeof(uint32_t);
+    static std::atomic<int> ready[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        set_error("%s: no current device", what);
+        return RS_ERR_CUDA;
+    }
+    if (!ready[dev].load()) {
+        const cudaError_t e = cudaFuncSetAttribute(evict_select, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeys * (int)sizeof(uint32_t));
+        if (e != cudaSuccess) {
+            set_error("%s: cudaFuncSetAttribute: %s", what, cudaGetErrorString(e));
+            return RS_ERR_CUDA;
+        }
+        ready[dev].store(1);
+    }
+    launch_pdl(evict_select, dim3(Hkv, B), dim3(kSelThreads), smem, (cudaStream_t)stream, a);
     RS_CHECK_LAUNCH(what);
     const int per = kMoveThreads / (D / 8);
     const int chunks = std::max(1, std::min((budget + per - 1) / per, 16 * num_sms() / (B * Hkv) + 1));
