@@ -2,6 +2,7 @@
 
 ``respec``   -- binding of the C ABI in ``include/respec.h``
 ``pipeline`` -- ``VerifyStep``: device buffers + the four calls of one step
+``paged``    -- ``PagedCache``: a paged KV cache and its calls; prompt attention
 ``build``    -- in-tree nvcc build of ``librespec.so``
 """
 from . import respec  # noqa: F401

@@ -22,6 +22,13 @@ plain torch matmuls.  Every step:
   5. commit: the accepted tokens and the bonus token are appended; the
      accepted slots' K/V are moved into the prefix.
 
+With ``cache="paged"`` both models keep their keys and values in pages
+(``paged.PagedCache``): the prompt goes through in one pass
+(``rs_prompt_attn``, ``rs_paged_append``), trees are verified by
+``rs_paged_attn``, and with a ``budget`` every commit adds the committed rows'
+attention weights to the keys they see (``rs_paged_weights``) and a cache
+that has outgrown the budget is cut back to it (``rs_paged_evict``).
+
 With tau = 0 the relaxed check accepts only argmax tokens, so the loop must
 reproduce the target's plain greedy decoding token for token
 (``greedy_reference`` computes that with dense attention in torch).
@@ -39,6 +46,7 @@ import numpy as np
 import torch
 
 from . import respec as rs
+from .paged import PagedCache, prompt_attention
 
 
 def _rms(x, eps=1e-6):
@@ -75,11 +83,78 @@ class TinyLM:
         z = lambda: torch.zeros((cap, self.Hkv, self.D), dtype=torch.bfloat16, device=self.device)  # noqa: E731
         return dict(K=[z() for _ in range(self.L)], V=[z() for _ in range(self.L)], cap=cap, S=0)
 
+    def new_paged_cache(self, cap, page_size=32, budget=None, recent=0):
+        """The same in pages; with a budget it is cut back to that many tokens whenever it has more after a commit."""
+        layers = [PagedCache(1, cap, page_size, self.Hkv, self.D, track_weights=budget is not None, device=self.device)
+                  for _ in range(self.L)]
+        return dict(layers=layers, cap=cap, S=0, seen=0, budget=budget, recent=recent, rows=[None] * self.L, ws=None)
+
+    def _qkv(self, x, i):
+        h, N = _rms(x), x.shape[0]
+        heads = lambda w, n: (h @ self.p["%s.%d" % (w, i)]).view(N, n, self.D).to(torch.bfloat16)  # noqa: E731
+        return heads("wq", self.Hq), heads("wk", self.Hkv), heads("wv", self.Hkv)
+
+    def _layer_end(self, x, out, i):
+        x = x + out.reshape(x.shape[0], self.Hq * self.D) @ self.p["wo.%d" % i]
+        h = _rms(x)
+        return x + (torch.nn.functional.silu(h @ self.p["w1.%d" % i]) * (h @ self.p["w3.%d" % i])) @ self.p["w2.%d" % i]
+
+    def forward_prompt(self, cache, tokens):
+        """A whole prompt into an empty paged cache, in one pass."""
+        N = tokens.numel()
+        assert cache["S"] == 0 and N <= cache["cap"]
+        off = torch.tensor([0, N], dtype=torch.int32, device=self.device)
+        x = self.p["emb"][tokens]
+        for i, layer in enumerate(cache["layers"]):
+            q, k, v = self._qkv(x, i)
+            out, lse, _, cache["ws"] = prompt_attention(q, k, v, off, self.D ** -0.5, cache["ws"])
+            layer.append(k, v, off)
+            cache["rows"][i] = (q, lse)
+            x = self._layer_end(x, out.float(), i)
+        self.commit(cache, list(range(N)))
+
+    def _forward_paged(self, cache, tokens, parents):
+        N, S = tokens.numel(), cache["S"]
+        assert S + N <= cache["cap"] and N <= 256
+        dev = self.device
+        off = torch.tensor([0, N], dtype=torch.int32, device=dev)
+        pos = torch.arange(cache["seen"], cache["seen"] + N, dtype=torch.int32, device=dev)
+        x = self.p["emb"][tokens]
+        for i, layer in enumerate(cache["layers"]):
+            q, k, v = self._qkv(x, i)
+            layer.append(k, v, off, pos)
+            out, lse = layer.attend(q, off, self.D ** -0.5, parents)
+            cache["rows"][i] = (q, lse)
+            x = self._layer_end(x, out.float(), i)
+        return (_rms(x) @ self.p["head"]) * self.logit_scale
+
+    def _commit_paged(self, cache, slots):
+        n, dev = len(slots), self.device
+        off = torch.tensor([0, n], dtype=torch.int32, device=dev)
+        at = torch.as_tensor(slots, dtype=torch.int64, device=dev)
+        pos = torch.arange(cache["seen"], cache["seen"] + n, dtype=torch.int32, device=dev)
+        cache["S"] += n
+        cache["seen"] += n
+        for i, layer in enumerate(cache["layers"]):
+            layer.keep(0, slots)
+            if cache["budget"] is not None:
+                # an accepted row sees the prefix and the accepted rows before it: causal
+                layer.positions[:, layer.rows(0, torch.arange(n, device=dev) + layer.lengths[0])] = pos
+                q, lse = cache["rows"][i]
+                layer.weigh(q[at], lse[at], off, self.D ** -0.5)
+            layer.advance([n])
+            if cache["budget"] is not None and cache["S"] > cache["budget"]:
+                layer.evict([cache["seen"]], cache["budget"], cache["recent"])
+        if cache["budget"] is not None:
+            cache["S"] = min(cache["S"], cache["budget"])
+
     def forward_tree(self, cache, tokens, parents, ws):
         """Logits [N, V] of a draft tree hanging after the cached prefix.
 
         tokens [N] int64, parents [N] int32 (local, -1 at the root), both on
         the device.  The tree's K/V are written to slots S .. S + N - 1."""
+        if "layers" in cache:
+            return self._forward_paged(cache, tokens, parents)
         N, S = tokens.numel(), cache["S"]
         assert S + N <= cache["cap"] and N <= 256
         dev = self.device
@@ -105,6 +180,10 @@ class TinyLM:
 
     def commit(self, cache, slots):
         """Move tree slots S + slots[j] to S + j (j in order) and grow the prefix."""
+        if "layers" in cache:
+            if len(slots):
+                self._commit_paged(cache, slots)
+            return
         S, n = cache["S"], len(slots)
         if n:
             src = torch.tensor([S + s for s in slots], dtype=torch.int64, device=self.device)
@@ -148,13 +227,16 @@ class SpecLoop:
     """One request decoded by the full step of Algorithm 1 (B = 1)."""
 
     def __init__(self, target, draft, prompt, p, widths=(4, 3, 2), cap=4096, acc_cap=64, trace=False,
-                 retrieval="scan"):
+                 retrieval="scan", cache="flat", page_size=32, budget=None, recent=64):
         self.t, self.dr, self.p = target, draft, p
         # retrieval: "scan" (rs_match_scan over the buffer) or "index" (an
         # index built over the prompt, the committed tokens appended to it
         # every step, queried with rs_match_scan_indexed)
         assert retrieval in ("scan", "index")
         self.retrieval = retrieval
+        # cache: "flat" (one row per token) or "paged", there with a budget of
+        # tokens per KV head (None: nothing is evicted), the `recent` newest kept
+        assert cache in ("flat", "paged") and (budget is None or cache == "paged")
         # with trace, every step appends host copies of each call's inputs and
         # outputs to self.trace (for checking a run call by call)
         self.trace = [] if trace else None
@@ -172,14 +254,20 @@ class SpecLoop:
         self.k_star = torch.zeros(1, dtype=torch.int32, device=dev)
         self.h_best = torch.zeros(1, dtype=torch.float32, device=dev)
         self.ok = torch.zeros(1, dtype=torch.uint8, device=dev)
-        self.tc = target.new_cache(cap)
-        self.dc = draft.new_cache(cap)
+        if cache == "paged":
+            self.tc, self.dc = (m.new_paged_cache(cap, page_size, budget, recent) for m in (target, draft))
+        else:
+            self.tc, self.dc = target.new_cache(cap), draft.new_cache(cap)
         self.ws_attn = torch.empty(max(rs.rs_tree_verify_attn_workspace_size(1, 256, target.Hq, target.Hkv,
                                                                               target.D), 256),
                                    dtype=torch.uint8, device=dev)
-        # prefill both caches with every prompt token but the root (chains of <= 256)
+        # prefill both caches with every prompt token but the root (chains of <= 256, or one pass)
         for m in (target, draft):
             cache = self.tc if m is target else self.dc
+            if "layers" in cache:  # one pass for all of it
+                if len(prompt) > 1:
+                    m.forward_prompt(cache, self.buf[:len(prompt) - 1].long())
+                continue
             for a in range(0, len(prompt) - 1, 256):
                 toks = self.buf[a:min(a + 256, len(prompt) - 1)].long()
                 m.forward_tree(cache, toks, self._chain_parents(toks.numel()), self.ws_attn)
@@ -335,11 +423,11 @@ def model_prompt(model, n, seed=0):
     return np.concatenate([start, greedy_reference(model, start, n - 16)]).astype(np.int32)
 
 
-def run(tau, m, n_new=256, prompt_len=512, seed=0, noise=0.1):
+def run(tau, m, n_new=256, prompt_len=512, seed=0, noise=0.1, **cache):
     target = TinyLM(seed=seed)
     draft = TinyLM(seed=seed + 1, base=target, noise=noise)
     p = rs.params(tau=tau, m=m, span_len=8)
-    loop = SpecLoop(target, draft, model_prompt(target, prompt_len, seed), p)
+    loop = SpecLoop(target, draft, model_prompt(target, prompt_len, seed), p, **cache)
     loop.generate(n_new)
     s = loop.stats
     return dict(tau=tau, m=m, steps=s["steps"], mean_tokens_per_step=s["emitted"] / max(1, s["steps"]),
@@ -352,11 +440,16 @@ def main():
     ap.add_argument("--sweep", action="store_true", help="tau in {0,1,2,3} x m in {1,2,3}")
     ap.add_argument("--tokens", type=int, default=256)
     ap.add_argument("--seeds", type=int, default=1)
+    ap.add_argument("--paged", action="store_true", help="keep the caches in pages")
+    ap.add_argument("--budget", type=int, default=None, help="tokens a paged cache keeps per KV head")
     args = ap.parse_args()
+    if args.budget is not None and not args.paged:
+        ap.error("--budget needs --paged")
+    cache = dict(cache="paged", budget=args.budget) if args.paged else {}
     taus, ms = ([0.0, 1.0, 2.0, 3.0], [1, 2, 3]) if args.sweep else ([3.0], [2])
     for tau in taus:
         for m in ms:
-            runs = [run(tau, m, n_new=args.tokens, seed=s) for s in range(args.seeds)]
+            runs = [run(tau, m, n_new=args.tokens, seed=s, **cache) for s in range(args.seeds)]
             steps = sum(r["steps"] for r in runs)
             row = dict(tau=tau, m=m, seeds=args.seeds, tokens=args.tokens * args.seeds, steps=steps,
                        mean_tokens_per_step=round(sum(r["mean_tokens_per_step"] * r["steps"] for r in runs) / steps, 3),
