@@ -439,8 +439,8 @@ rs_status rs_tree_sample(const float *logits, int R, int V, const int32_t *node_
  *   out      [T, Hq, D] of type dtype, 32-byte aligned;  lse [T, Hq] fp32;
  *            rows behind the last sequence are left as they are.
  *   status   [B]: RS_ST_BAD_OFFSET for a range outside [0, T) or one that
- *            starts before an earlier sequence does (its own rows, where they
- *            lie inside, are zeroed); RS_ST_TIMEOUT.
+ *            starts before an earlier sequence does (nothing of it is written);
+ *            RS_ST_TIMEOUT.
  * Products run on the tensor cores with fp32 accumulation; softmax statistics
  * are fp32; P is rounded to dtype for the second product.  A row whose scores
  * are all -inf gives zeros and lse -inf.  NaN or infinity in a row of K or V
@@ -502,7 +502,8 @@ rs_status rs_paged_append(const uint16_t *k, int64_t k_stride, const uint16_t *v
  *   out      [T, Hq, D] of type dtype, 32-byte aligned;  lse [T, Hq] fp32;
  *            rows behind the last request are left as they are.
  *   status   [B]: RS_ST_BAD_OFFSET, RS_ST_BAD_PAGE, RS_ST_BAD_TREE,
- *            RS_ST_TOO_LARGE (the request's rows are zeroed), RS_ST_TIMEOUT.
+ *            RS_ST_TOO_LARGE (the request's rows are zeroed; those of a range
+ *            that rs_prompt_attn rejects are left), RS_ST_TIMEOUT.
  * Types, arithmetic, B, head counts, alignment: as for rs_prompt_attn.  What
  * slots behind a request's last token hold (NaN too) does not matter.
  */

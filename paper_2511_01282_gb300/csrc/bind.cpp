@@ -13,6 +13,7 @@
 // anything else is refused.  A tensor subclass answers for itself.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <string.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -57,6 +58,14 @@ struct Ref {
 struct Args {
     PyObject *const *v;
     Py_ssize_t n, i = 0;
+    int device = -1;  // of the tensors so far (-2: not one)
+    void seen(const at::Tensor &t) { device = device == -1 || device == t.get_device() ? t.get_device() : -2; }
+    // The library launches on the current device: tensors elsewhere would be bad addresses there.
+    void on_current_device() {
+        if (device == -1 || device == c10::cuda::current_device()) return;
+        PyErr_SetString(PyExc_ValueError, "expected all tensors on the current CUDA device");
+        throw PyFail{};
+    }
     PyObject *next() {
         if (i >= n) {
             PyErr_SetString(PyExc_TypeError, "too few arguments");
@@ -108,6 +117,7 @@ struct Args {
         if (THPVariable_CheckExact(o)) {
             const at::Tensor &t = THPVariable_Unpack(o);
             check(t.is_cuda(), t.is_contiguous(), o);
+            seen(t);
             if (bytes) *bytes = (size_t)t.numel() * (size_t)t.element_size();
             return t.data_ptr();
         }
@@ -155,6 +165,7 @@ struct Args {
         if (tensor) {
             const at::Tensor &t = THPVariable_Unpack(o);
             check(t.is_cuda(), true, o);
+            seen(t);
             const int64_t d = t.dim();
             bool inner = d >= 2 && t.element_size() == 2 && (t.stride(d - 1) == 1 || t.size(d - 1) == 1);
             for (int64_t i = d - 2; inner && i > 0; --i) inner = t.size(i) == 1 || t.stride(i) == t.stride(i + 1) * t.size(i + 1);
@@ -479,6 +490,7 @@ RS_BIND(prompt_attn) {
         auto *status = a.ptr<int32_t>();
         size_t wb;
         void *ws = a.sized(&wb, true), *st = a.stream();
+        a.on_current_device();
         return [=] {
             return lib.prompt_attn(q, qs, k, ks, vv, vs, dtype, off, B, T, Hq, Hkv, D, scale, out, lse, status, ws, wb, st);
         };
@@ -499,6 +511,7 @@ RS_BIND(paged_append) {
         auto *weights = a.ptr<float>();
         auto *positions = a.ptr<int32_t>(), *status = a.ptr<int32_t>();
         void *st = a.stream();
+        a.on_current_device();
         return [=] {
             return lib.paged_append(k, ks, vv, vs, pos, off, B, T, Hkv, D, kp, vp, pages, size, table, most, ctx, weights, positions,
                                     status, st);
@@ -524,6 +537,7 @@ RS_BIND(paged_attn) {
         auto *status = a.ptr<int32_t>();
         size_t wb;
         void *ws = a.sized(&wb, true), *st = a.stream();
+        a.on_current_device();
         return [=] {
             return lib.paged_attn(q, qs, dtype, off, parents, B, T, Hq, Hkv, D, kp, vp, pages, size, table, most, ctx, scale, out, lse,
                                   status, ws, wb, st);
@@ -549,6 +563,7 @@ RS_BIND(paged_weights) {
         auto *status = a.ptr<int32_t>();
         size_t wb;
         void *ws = a.sized(&wb, true), *st = a.stream();
+        a.on_current_device();
         return [=] {
             return lib.paged_weights(q, qs, dtype, lse, off, B, T, Hq, Hkv, D, kp, pages, size, table, most, ctx, scale, weights,
                                      status, ws, wb, st);
@@ -568,6 +583,7 @@ RS_BIND(paged_evict) {
         auto *positions = a.ptr<int32_t>(), *new_len = a.ptr<int32_t>(), *status = a.ptr<int32_t>();
         size_t wb;
         void *ws = a.sized(&wb, true), *st = a.stream();
+        a.on_current_device();
         return [=] {
             return lib.paged_evict(kp, vp, Hkv, D, pages, size, table, most, len, next, B, budget, recent, weights, positions, new_len,
                                    status, ws, wb, st);

@@ -51,13 +51,15 @@ __device__ __forceinline__ T block_scan(T v, T &carry, T *s_w, Op op = Op()) {
 }
 
 // A request's rows and keys against the arrays: 0, or the status that rejects it.
+// rq: first row, rows to work on, ctx, rows of its own (to be emptied if it is rejected).
 __device__ __forceinline__ int check_rows(const FlashArgs &a, int b, int4 &rq) {
     const int n0 = a.off[b], n1 = a.off[b + 1], ctx = a.ctx ? a.ctx[b] : 0;
     rq = make_int4(0, 0, 0, 0);
-    if (n0 < 0 || n1 < n0 || n1 > a.T || ctx < 0) return RS_ST_BAD_OFFSET;
-    if (a.page_table && (long long)ctx + (n1 - n0) > ((long long)a.max_pages << a.page_log2)) return RS_ST_BAD_OFFSET;
+    if (n0 < 0 || n1 < n0 || n1 > a.T) return RS_ST_BAD_OFFSET;
+    rq = make_int4(n0, 0, 0, n1 - n0);
+    if (ctx < 0 || (a.page_table && (long long)ctx + (n1 - n0) > ((long long)a.max_pages << a.page_log2))) return RS_ST_BAD_OFFSET;
     if (a.anc && n1 - n0 > RS_MAX_NODES) return RS_ST_TOO_LARGE;
-    rq = make_int4(n0, n1 - n0, ctx, 0);
+    rq = make_int4(n0, n1 - n0, ctx, n1 - n0);
     return 0;
 }
 

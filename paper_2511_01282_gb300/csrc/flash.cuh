@@ -63,7 +63,7 @@ struct FlashArgs {
     const uint32_t *anc;         // ancestor sets of tree nodes, or null: causal
     const int32_t *page_table;   // null: keys of request b are rows off[b] ..
     int max_pages, n_pages, page_log2;
-    int4 *req;                   // per request: first row, rows (0: rejected), ctx
+    int4 *req;                   // per request: first row, rows (0: rejected), ctx, rows of its own
     long long *cum;              // [pairs + 1] cost prefix of the pairs of one KV head
     int4 *ent;                   // [pairs] request, pair, first row and rows of the request
     int *ent_ctx;                // [pairs] its ctx

