@@ -34,14 +34,14 @@ __device__ __forceinline__ T warp_scan(T x, Op op) {
     }
     return x;
 }
-// Inclusive prefix over the block's 32 warps, on top of `carry` (kept by every thread).
+// Inclusive prefix over the block, on top of `carry` (kept by every thread).
 template <class T, class Op = Add>
 __device__ __forceinline__ T block_scan(T v, T &carry, T *s_w, Op op = Op()) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     T x = warp_scan(v, op);
     if (lane == 31) s_w[warp] = x;
     __syncthreads();
-    const T w = warp_scan(s_w[lane], op);
+    const T w = warp_scan(lane < (int)(blockDim.x >> 5) ? s_w[lane] : T(0), op);
     const T before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
     if (warp > 0) x = op(x, before);
     x = op(x, carry);
@@ -69,19 +69,19 @@ __device__ void plan_tree(const FlashArgs &a, const int32_t *parents, uint32_t *
     int4 rq;
     int st = check_rows(a, b, rq);
     int late = 0;  // an earlier request starts behind this one
-    for (int i = threadIdx.x; i < b; i += kPlanThreads) late |= a.off[i] > a.off[b];
+    for (int i = threadIdx.x; i < b; i += blockDim.x) late |= a.off[i] > a.off[b];
     if (__syncthreads_or(late)) {
         st = RS_ST_BAD_OFFSET;
         rq = make_int4(0, 0, 0, 0);
     }
     int bad = 0;
-    for (int i = threadIdx.x; i < rq.y; i += kPlanThreads) {
+    for (int i = threadIdx.x; i < rq.y; i += blockDim.x) {
         const int pa = parents[rq.x + i];
         s_par[i] = pa;
         bad |= i == 0 ? pa != -1 : (pa < 0 || pa >= i);
     }
     if (__syncthreads_or(bad)) st = RS_ST_BAD_TREE;
-    for (int i = threadIdx.x; i < rq.y; i += kPlanThreads) {
+    for (int i = threadIdx.x; i < rq.y; i += blockDim.x) {
         uint32_t bits[kAncWords] = {};
         if (st == 0) {
             for (int x = i; x >= 0; x = s_par[x]) {
@@ -111,7 +111,7 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
     const int tid = threadIdx.x;
     int pairs = 0, latest = 0;
     long long tiles = 0;  // about how many key tiles one KV head has
-    for (int base = 0; base < a.B; base += kPlanThreads) {
+    for (int base = 0; base < a.B; base += blockDim.x) {
         const int b = base + tid;
         int4 rq = make_int4(0, 0, 0, 0);
         int st = 0, mine = 0;
@@ -144,7 +144,7 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
     const long long per = tiles * a.Hkv / (2 * a.grid);
     const int beta = kFlWH * (int)(per < kFlSegCost ? per : kFlSegCost);
     long long carry = 0;
-    for (int base = 0; base < M; base += kPlanThreads) {
+    for (int base = 0; base < M; base += blockDim.x) {
         const int i = base + tid;
         long long cost = 0;
         if (i < M) {
@@ -229,6 +229,8 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     const double bytes = 4.0 * (double)kv_rows * a.Hkv * D;
     a.kv_stream = bytes > 0.5 * (double)l2_bytes();
     a.phases = 1;
+    // a segment has no more rows than the call's tokens fill
+    a.comb_blocks = (a.T > a.tq ? kFlRows : std::max(a.T, 1) * a.G + kFlCombRows - 1) / kFlCombRows;
     const int box = a.page_table ? std::min(1 << a.page_log2, kBN) : kBN;
     CUtensorMap tmq, tmk, tmv;
     if (!rows_map(&tmq, q, type, D, a.Hq, a.T, q_stride, a.G, a.tq) ||
@@ -237,7 +239,10 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
         set_error("%s: cuTensorMapEncodeTiled failed", what);
         return RS_ERR_CUDA;
     }
-    launch_pdl(flash_plan, dim3(1 + (parents ? a.B : 0)), dim3(kPlanThreads), 0, st, a, parents, w.anc);
+    // a thread per request and per pair, as far as a block goes (fewer warps, shorter barriers)
+    const int wide = std::max(a.B, a.T / (2 * a.tq) + a.B);
+    const int threads = std::min(std::max((wide + 31) / 32 * 32, parents ? RS_MAX_NODES : 32), kPlanThreads);
+    launch_pdl(flash_plan, dim3(1 + (parents ? a.B : 0)), dim3(threads), 0, st, a, parents, w.anc);
     RS_CHECK_LAUNCH(what);
     return type ? flash_launch<true>(a, D, tmq, tmk, tmv, what, st) : flash_launch<false>(a, D, tmq, tmk, tmv, what, st);
 }

@@ -47,6 +47,7 @@ constexpr uint32_t kFlRegsSoft = 224, kFlRegsProd = 56;
 static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "register split");
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
 constexpr int kFlRows = 2 * kBM;  // rows of a segment and of a partial slot
+constexpr int kFlCombRows = 32;   // of them for a block of flash_combine
 constexpr int kFlWF = 5, kFlWH = 3;  // cost of a key tile for a pair and for a single row tile
 constexpr int kFlSegCost = 8;        // cost of a segment's start, in single-tile key tiles, at most
 // Tensor memory columns
@@ -71,6 +72,7 @@ struct FlashArgs {
     int4 *bound;                 // [phase][CTA] where the CTA's share starts: (head in phase, pair, tile)
     float *part_o, *part_m, *part_l;
     int phases, grid;
+    int comb_blocks;             // blocks of flash_combine per cut segment
     int B, T, Hq, Hkv, G, tq;
     int kv_stream;               // K/V is large next to L2: tiles read once are evicted first
     float scale;

@@ -11,28 +11,25 @@
 namespace rs {
 
 // flash_combine: joins the pieces of the segments that the shares' ends cut.
-// Block (c, y) looks at where CTA c + 1's share of phase y / 8 starts; if that
-// is inside a segment, and the first cut of it, the block joins 32 of its rows,
-// four to a warp, all loads of a step under way together:
+// Block (c, y) looks at where CTA c + 1's share of a phase starts; if that is
+// inside a segment, and the first cut of it, the block joins 32 of its rows,
+// a row to a warp at a time, its lanes the pieces' (m, l) first and then the columns:
 //     M = max m_p, L = sum 2^(m_p - M) l_p, O = sum 2^(m_p - M) O_p / L
 // It also empties the rows of rejected requests (after the pieces' writers).
-// Bound: latency (a handful of dependent loads), and the pieces, read once
-// from L2, where every share's end cuts a pair of full row tiles.
+// Bound: latency, of a handful of dependent loads and of the instructions, which
+// are fetched anew for every launch: the loop over the rows is not unrolled (four
+// rows at once in 600 instructions took 8 us for single tokens, this 6).
 constexpr int kFlCombThreads = 256;
-constexpr int kFlCombRows = 32;  // of a block
-constexpr int kFlCombPar = kFlCombRows / (kFlCombThreads / 32);  // rows of a warp
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kFlCombThreads)
 flash_combine(FlashArgs a) {
     pdl_enter();
-    __shared__ int s_slot[kAttnMaxGrid + 2];
-    __shared__ int s_np;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int f = blockIdx.y / (kFlRows / kFlCombRows), y = blockIdx.y % (kFlRows / kFlCombRows);
+    const int f = blockIdx.y / a.comb_blocks, y = blockIdx.y % a.comb_blocks;
     const int4 *bound = a.bound + f * (a.grid + 1);
     const int c = min((int)blockIdx.x + 1, a.grid);
-    const int4 at = bound[c], before = bound[c - 1];
+    const int4 start = bound[c], before = bound[c - 1];
     const int blocks = gridDim.x * gridDim.y;
     for (int b = blockIdx.y * gridDim.x + blockIdx.x; b < a.B; b += blocks) {
         if (!(a.status[b] & ~RS_ST_TIMEOUT)) continue;
@@ -42,94 +39,60 @@ flash_combine(FlashArgs a) {
         for (long long i = threadIdx.x; i < rows * (D / 8); i += kFlCombThreads) o[i] = make_uint4(0, 0, 0, 0);
         for (long long i = threadIdx.x; i < rows; i += kFlCombThreads) a.lse[(long long)rq.x * a.Hq + i] = 0.f;
     }
-    auto same = [&](int4 p) { return p.x == at.x && p.y == at.y && p.z > 0; };
-    if (c >= a.grid || at.z == 0 || same(before)) return;  // between segments, or not the first cut
-    const int4 e = a.ent[at.y];  // request, pair, first row, rows
+    auto same = [&](int4 r) { return r.x == start.x && r.y == start.y && r.z > 0; };
+    if (c >= a.grid || start.z == 0 || same(before)) return;  // between segments, or not the first cut
+    const int4 e = a.ent[start.y];  // request, pair, first row, rows
     const int x = y * kFlCombRows / kBM;  // row tile of the block's rows
     const int first = (e.y * 2 + x) * a.tq, r0 = y * kFlCombRows - x * kBM;
     if (r0 / a.G >= a.tq || first + r0 / a.G >= e.w) return;
-    const bool rejected = a.status[e.x] & ~RS_ST_TIMEOUT;
-    if (warp == 0) {  // the pieces' slots, in order
-        if (lane == 0) s_slot[0] = 2 * (f * a.grid + c - 1) + 1;
-        int np = 1;
-        for (int c0 = c; c0 < a.grid; c0 += 32) {
+    if (a.status[e.x] & ~RS_ST_TIMEOUT) return;
+    const int kvh = f * a.Hkv / a.phases + start.x;
+    constexpr int kC = D / 32;  // columns of a lane
+#pragma unroll 1
+    for (int k = warp; k < kFlCombRows; k += kFlCombThreads / 32) {
+        const int r = r0 + k, t = r / a.G, tok = first + t;
+        if (t >= a.tq || tok >= e.w) break;
+        const long long row = x * kBM + r;
+        float M = -INFINITY, L = 0.f, acc[kC] = {};
+#pragma unroll 1
+        for (int c0 = c - 1;; c0 += 32) {  // 32 shares at a time; the first piece is the end of share c - 1
             const int c1 = c0 + lane;
             const int4 p = bound[min(c1, a.grid)], q = bound[min(c1 + 1, a.grid)];
-            const bool in = c1 < a.grid && same(p), has = in && !(same(q) && q.z == p.z);  // not an empty share
-            const unsigned m = __ballot_sync(0xffffffffu, has);
-            if (has) s_slot[np + __popc(m & ((1u << lane) - 1u))] = 2 * (f * a.grid + c1);
-            np += __popc(m);
-            if (__ballot_sync(0xffffffffu, in) != 0xffffffffu) break;
-        }
-        if (lane == 0) s_np = np;
-    }
-    __syncthreads();
-    if (rejected) return;
-    const int np = s_np, kvh = f * a.Hkv / a.phases + at.x;
-    constexpr int kC = D / 32;  // columns of a lane
-    long long row[kFlCombPar];
-    int tok[kFlCombPar], hg[kFlCombPar];
-    bool on[kFlCombPar];
-    float M[kFlCombPar], L[kFlCombPar], acc[kFlCombPar][kC];
+            const bool head = c1 == c - 1;
+            const bool in = head || (c1 < a.grid && same(p)), have = head || (in && !(same(q) && q.z == p.z));  // not an empty share
+            const long long at = (long long)(2 * (f * a.grid + c1) + (head ? 1 : 0)) * kFlRows + row;
+            const float m = have ? a.part_m[at] : -INFINITY, l = have ? a.part_l[at] : 0.f;
+            const float Mn = fmaxf(M, warp_max(m));
+            const float old = Mn == -INFINITY ? 1.f : sm100::ex2(M - Mn);
+            const float w = Mn == -INFINITY ? (have ? 1.f : 0.f) : sm100::ex2(m - Mn);
+            L = L * old + warp_sum(have ? w * l : 0.f);
 #pragma unroll
-    for (int i = 0; i < kFlCombPar; ++i) {
-        const int r = r0 + warp + i * (kFlCombThreads / 32), t = r / a.G;
-        tok[i] = first + t;
-        hg[i] = r - t * a.G;
-        on[i] = t < a.tq && tok[i] < e.w;
-        row[i] = x * kBM + r;
-        M[i] = -INFINITY;
-        L[i] = 0.f;
-#pragma unroll
-        for (int j = 0; j < kC; ++j) acc[i][j] = 0.f;
-    }
-    for (int p0 = 0; p0 < np; p0 += 32) {
-        const bool have = p0 + lane < np;
-        const long long slot = have ? (long long)s_slot[p0 + lane] * kFlRows : 0;
-        float m[kFlCombPar], l[kFlCombPar], w[kFlCombPar];
-#pragma unroll
-        for (int i = 0; i < kFlCombPar; ++i) {
-            m[i] = have && on[i] ? a.part_m[slot + row[i]] : -INFINITY;
-            l[i] = have && on[i] ? a.part_l[slot + row[i]] : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < kFlCombPar; ++i) {
-            const float Mn = fmaxf(M[i], warp_max(m[i]));
-            const float old = Mn == -INFINITY ? 1.f : sm100::ex2(M[i] - Mn);
-            w[i] = Mn == -INFINITY ? (have ? 1.f : 0.f) : sm100::ex2(m[i] - Mn);
-            L[i] = L[i] * old + warp_sum(have ? w[i] * l[i] : 0.f);
-#pragma unroll
-            for (int j = 0; j < kC; ++j) acc[i][j] *= old;
-            M[i] = Mn;
-        }
-        const int cnt = min(32, np - p0);
+            for (int j = 0; j < kC; ++j) acc[j] *= old;
+            M = Mn;
+            const unsigned pieces = __ballot_sync(0xffffffffu, have);
+            const int cnt = 32 - __clz(pieces);  // 0 where the run ended with the last 32
+            const float *o = a.part_o + ((long long)(2 * (f * a.grid + c0)) * kFlRows + row) * D + lane * kC;
 #pragma unroll 4
-        for (int p = 0; p < cnt; ++p) {
-            const long long at_slot = (long long)s_slot[p0 + p] * kFlRows;
-#pragma unroll
-            for (int i = 0; i < kFlCombPar; ++i) {
-                const float wp = __shfl_sync(0xffffffffu, w[i], p);
-                if (!on[i]) continue;
-                const float *o = a.part_o + (at_slot + row[i]) * D + lane * kC;
+            for (int k1 = 0; k1 < cnt; ++k1) {
+                const float wp = __shfl_sync(0xffffffffu, w, k1);
+                if (!((pieces >> k1) & 1u)) continue;
+                const float *src = o + (long long)(2 * k1 + (c0 + k1 == c - 1 ? 1 : 0)) * kFlRows * D;
                 float v[kC];
-                if constexpr (kC == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(o);
-                else *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(o);
+                if constexpr (kC == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(src);
+                else *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
 #pragma unroll
-                for (int j = 0; j < kC; ++j) acc[i][j] = fmaf(wp, v[j], acc[i][j]);
+                for (int j = 0; j < kC; ++j) acc[j] = fmaf(wp, v[j], acc[j]);
             }
+            if (!__all_sync(0xffffffffu, in)) break;
         }
-    }
-#pragma unroll
-    for (int i = 0; i < kFlCombPar; ++i) {
-        if (!on[i]) continue;
-        const float fr = L[i] > 0.f ? 1.f / L[i] : L[i];  // no key with weight: 0; NaN stays
-        const long long orow = (long long)(e.z + tok[i]) * a.Hq + kvh * a.G + hg[i];
+        const float fr = L > 0.f ? 1.f / L : L;  // no key with weight: 0; NaN stays
+        const long long orow = (long long)(e.z + tok) * a.Hq + kvh * a.G + (r - t * a.G);
         uint32_t *d = reinterpret_cast<uint32_t *>(a.out + orow * D + lane * kC);
         if constexpr (kC == 4)
-            *reinterpret_cast<uint2 *>(d) = make_uint2(pack16<BF16>(acc[i][0] * fr, acc[i][1] * fr), pack16<BF16>(acc[i][2] * fr, acc[i][3] * fr));
+            *reinterpret_cast<uint2 *>(d) = make_uint2(pack16<BF16>(acc[0] * fr, acc[1] * fr), pack16<BF16>(acc[2] * fr, acc[3] * fr));
         else
-            *d = pack16<BF16>(acc[i][0] * fr, acc[i][1] * fr);
-        if (lane == 0) a.lse[orow] = L[i] > 0.f ? (M[i] + log2f(L[i])) * 0.6931471805599453f : (L[i] == 0.f ? -INFINITY : L[i]);
+            *d = pack16<BF16>(acc[0] * fr, acc[1] * fr);
+        if (lane == 0) a.lse[orow] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : (L == 0.f ? -INFINITY : L);
     }
 }
 
@@ -162,7 +125,7 @@ rs_status flash_launch_d(const FlashArgs &a, const CUtensorMap &tmq, const CUten
     }
     launch_pdl(flash_kernel<D, BF16>, dim3(a.grid), dim3(kFlThreads), FlSmem<D>::kTotal, st, a, tmq, tmk, tmv);
     RS_CHECK_LAUNCH(what);
-    launch_full(flash_combine<D, BF16>, dim3(std::max(a.grid - 1, 1), a.phases * (kFlRows / kFlCombRows)), dim3(kFlCombThreads), 0, st, a);
+    launch_full(flash_combine<D, BF16>, dim3(std::max(a.grid - 1, 1), a.phases * a.comb_blocks), dim3(kFlCombThreads), 0, st, a);
     RS_CHECK_LAUNCH(what);
     return RS_OK;
 }
