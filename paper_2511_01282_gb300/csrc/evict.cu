@@ -13,6 +13,7 @@
 #include <atomic>
 
 #include "common.cuh"
+#include "sm100.cuh"
 #include "tmap.cuh"
 
 namespace rs {
@@ -26,6 +27,7 @@ struct EvictArgs {
     int2 *moves;      // [B][Hkv][budget] (from, to) slots of the request
     int *n_moves;     // [B][Hkv]
     int B, Hkv, D, n_pages, page_log2, max_pages, budget, recent;
+    int cluster, held;  // CTAs of evict_select per (request, head); the longest cache whose keys they hold
 };
 
 // Weights as unsigned keys of the same order; NaN comes last, -0 equals 0.
@@ -35,7 +37,10 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return (u >> 31) ? ~u : (u | 0x80000000u);
 }
 
-// evict_select: a warp owns a run of consecutive slots, 32 at a time.  The keys
+// evict_select: a cluster of CTAs per (request, head), each over a part of the
+// slots (more than one where there are fewer pairs than SMs and the caches are
+// long: 32768 tokens of 32 pairs took one CTA each 37 us).  A warp owns a run of
+// consecutive slots, 32 at a time.  The keys
 // are read once into shared memory, as many as it holds (49152 tokens a CTA);
 // longer caches are read again in each pass.  (In registers, with every loop
 // unrolled, 32 keys a thread took twice as long: the code runs once and is all
@@ -50,12 +55,39 @@ constexpr int kSelThreads = 1024;
 constexpr int kSelKeys = 49152;
 constexpr int kSelBins = 2048;
 
+constexpr int kSelLeast = 4096;  // slots of a CTA, at least, where a cluster shares them
+
 struct SelShared {
     int hist[kSelBins];
     int warp[3][32];
+    int total[3];  // of the CTA: ties, holes, movers
     uint32_t prefix;
     int left;
 };
+
+// (MANY: a cluster of more than one; alone, the CTA's own barrier and memory do,
+// 10 us for 14 on 2112 tokens.)
+template <bool MANY>
+__device__ __forceinline__ int cluster_read(const int *p, int rank) {
+    if (!MANY) return *p;
+    uint32_t at = sm100::smem_u32(p);
+    int v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.u32 %0, [a];\n\t}"
+                 : "=r"(v)
+                 : "r"(at), "r"(rank)
+                 : "memory");
+    return v;
+}
+// Every CTA's earlier shared-memory writes are there for the others.
+template <bool MANY>
+__device__ __forceinline__ void cluster_sync() {
+    if (MANY) {
+        cluster_arrive_release();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
+}
 
 // Exclusive prefix of the warps' counts in row, and their sum (whole block).
 __device__ __forceinline__ int warps_before(int (&row)[32], int count, int &sum) {
@@ -92,12 +124,23 @@ struct SelKeys {
     }
 };
 
-template <bool HELD>
-__device__ __forceinline__ void select_moves(const EvictArgs &a, SelShared &sh, uint32_t *keys, int len, int bh,
+template <bool MANY, bool HELD>
+__device__ __forceinline__ void select_moves(const EvictArgs &a, SelShared &sh, uint32_t *keys, int len, int bh, int rank,
                                              const SelKeys &src) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int steps = (len + kSelThreads - 1) / kSelThreads;  // of 32 slots a warp
-    const int first = warp * steps * 32 + lane;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cs = MANY ? a.cluster : 1;
+    const int steps = (len + kSelThreads * cs - 1) / (kSelThreads * cs);  // of 32 slots a warp
+    const int first = (rank * (kSelThreads / 32) + warp) * steps * 32 + lane;
+    // the CTAs' counts before this one's, and their sum
+    auto ctas_before = [&](int i, int &sum) {
+        int before = 0;
+        sum = 0;
+        for (int r = 0; r < cs; ++r) {
+            const int v = cluster_read<MANY>(&sh.total[i], r);
+            sum += v;
+            before += r < rank ? v : 0;
+        }
+        return before;
+    };
     constexpr int kAtOnce = 8;
     if (HELD) {
 #pragma unroll 1
@@ -144,11 +187,14 @@ __device__ __forceinline__ void select_moves(const EvictArgs &a, SelShared &sh, 
                 atomicAdd(&sh.hist[d], 1);
             }
         });
-        __syncthreads();
-        // thread t owns bins / 1024 digits, the highest first
+        cluster_sync<MANY>();
+        // thread t owns bins / 1024 digits, the highest first, of all CTAs
         const int per = bins / kSelThreads;
-        int mine = 0;
-        for (int i = 0; i < per; ++i) mine += sh.hist[bins - 1 - (tid * per + i)];
+        int mine = 0, own[2] = {0, 0};
+        for (int i = 0; i < per; ++i) {
+            for (int r = 0; r < cs; ++r) own[i] += cluster_read<MANY>(&sh.hist[bins - 1 - (tid * per + i)], r);
+            mine += own[i];
+        }
         int incl = mine;
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, incl, o);
@@ -159,7 +205,7 @@ __device__ __forceinline__ void select_moves(const EvictArgs &a, SelShared &sh, 
         int above = before + incl - mine;
         if (above < left && above + mine >= left) {
             for (int i = 0; i < per; ++i) {
-                const int d = bins - 1 - (tid * per + i), n = sh.hist[d];
+                const int d = bins - 1 - (tid * per + i), n = own[i];
                 if (above + n >= left) {
                     sh.prefix = prefix | ((uint32_t)d << shift);
                     sh.left = left - above;
@@ -168,7 +214,7 @@ __device__ __forceinline__ void select_moves(const EvictArgs &a, SelShared &sh, 
                 above += n;
             }
         }
-        __syncthreads();
+        cluster_sync<MANY>();  // the counters have been read everywhere
         prefix = sh.prefix;
         left = sh.left;
     }
@@ -176,45 +222,55 @@ __device__ __forceinline__ void select_moves(const EvictArgs &a, SelShared &sh, 
     const unsigned below = (1u << lane) - 1u;
     int ties = 0, sum;
     each([&](int, uint32_t k, bool in) { ties += __popc(__ballot_sync(0xffffffffu, in && k == prefix)); });
-    __syncthreads();
-    const int ties0 = warps_before(sh.warp[0], ties, sum);
-    auto marks = [&](int s, uint32_t k, bool in, int &rank, bool &hole, bool &mover) {
+    int ties0 = warps_before(sh.warp[0], ties, sum);
+    if (tid == 0) sh.total[0] = sum;
+    cluster_sync<MANY>();
+    ties0 += ctas_before(0, sum);
+    auto marks = [&](int s, uint32_t k, bool in, int &tie_rank, bool &hole, bool &mover) {
         const bool tie = in && k == prefix;
         const unsigned m = __ballot_sync(0xffffffffu, tie);
-        const bool kept = in && (k > prefix || (tie && rank + __popc(m & below) < left));
-        rank += __popc(m);
+        const bool kept = in && (k > prefix || (tie && tie_rank + __popc(m & below) < left));
+        tie_rank += __popc(m);
         hole = s < a.budget && in && !kept;
         mover = s >= a.budget && kept;
     };
-    int rank = ties0, holes = 0, movers = 0;
+    int tie_rank = ties0, holes = 0, movers = 0;
     each([&](int s, uint32_t k, bool in) {
         bool hole, mover;
-        marks(s, k, in, rank, hole, mover);
+        marks(s, k, in, tie_rank, hole, mover);
         holes += __popc(__ballot_sync(0xffffffffu, hole));
         movers += __popc(__ballot_sync(0xffffffffu, mover));
     });
     int n;
-    int hole_at = warps_before(sh.warp[1], holes, n), mover_at = warps_before(sh.warp[2], movers, n);
+    int hole_at = warps_before(sh.warp[1], holes, n);
+    if (tid == 0) sh.total[1] = n;
+    int mover_at = warps_before(sh.warp[2], movers, n);
+    if (tid == 0) sh.total[2] = n;
+    cluster_sync<MANY>();
+    hole_at += ctas_before(1, n);
+    mover_at += ctas_before(2, n);
     int2 *moves = a.moves + (long long)bh * a.budget;
-    rank = ties0;
+    tie_rank = ties0;
     each([&](int s, uint32_t k, bool in) {
         bool hole, mover;
-        marks(s, k, in, rank, hole, mover);
+        marks(s, k, in, tie_rank, hole, mover);
         const unsigned mh = __ballot_sync(0xffffffffu, hole), mm = __ballot_sync(0xffffffffu, mover);
         if (hole) moves[hole_at + __popc(mh & below)].y = s;
         if (mover) moves[mover_at + __popc(mm & below)].x = s;
         hole_at += __popc(mh);
         mover_at += __popc(mm);
     });
-    if (tid == 0) a.n_moves[bh] = n;
+    if (tid == 0 && rank == 0) a.n_moves[bh] = n;
+    cluster_sync<MANY>();  // no CTA leaves while another reads its counts
 }
 
+template <bool MANY>
 __global__ void __launch_bounds__(kSelThreads)
 evict_select(EvictArgs a) {
     pdl_enter();
     __shared__ SelShared sh;
     extern __shared__ uint32_t s_keys[];
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    const int cs = MANY ? a.cluster : 1, h = blockIdx.x / cs, rank = blockIdx.x % cs, b = blockIdx.y, tid = threadIdx.x;
     const int len = a.len[b];
     const int32_t *table = a.table + (long long)b * a.max_pages;
     const long long slots = (long long)a.n_pages << a.page_log2;
@@ -227,7 +283,7 @@ evict_select(EvictArgs a) {
     if (__syncthreads_or(bad)) st = RS_ST_BAD_PAGE;
     const bool work = st == 0 && len > a.budget;
     const int bh = b * a.Hkv + h;
-    if (tid == 0) {
+    if (tid == 0 && rank == 0) {
         if (!work) a.n_moves[bh] = 0;
         if (h == 0) {
             a.status[b] = st;
@@ -236,8 +292,8 @@ evict_select(EvictArgs a) {
     }
     if (!work) return;
     const SelKeys src{table, a.positions + h * slots, a.weights + h * slots, (long long)a.next_pos[b] - a.recent, a.page_log2};
-    if (len <= kSelKeys) select_moves<true>(a, sh, s_keys, len, bh, src);
-    else select_moves<false>(a, sh, s_keys, len, bh, src);
+    if (len <= a.held) select_moves<MANY, true>(a, sh, s_keys, len, bh, rank, src);
+    else select_moves<MANY, false>(a, sh, s_keys, len, bh, rank, src);
 }
 
 constexpr int kMoveThreads = 256;
@@ -334,9 +390,13 @@ extern "C" rs_status rs_paged_evict(uint16_t *k_pages, uint16_t *v_pages, int Hk
     a.max_pages = n_pages ? max_pages : 0;
     a.budget = budget;
     a.recent = recent;
-    // keys of the longest cache that the page tables allow
-    const long long most = std::min((long long)a.max_pages << a.page_log2, (long long)kSelKeys);
-    const size_t smem = (size_t)((most + kSelThreads - 1) / kSelThreads * kSelThreads) * sizeof(uint32_t);
+    // as many CTAs as share the longest cache that the page tables allow, and its keys
+    const long long most = (long long)a.max_pages << a.page_log2;
+    a.cluster = 1;
+    while (a.cluster < 8 && B * Hkv * a.cluster * 2 <= num_sms() && most / (a.cluster * 2) >= kSelLeast) a.cluster *= 2;
+    const long long steps = std::min((most + kSelThreads * a.cluster - 1) / (kSelThreads * a.cluster), (long long)(kSelKeys / kSelThreads));
+    a.held = (int)steps * kSelThreads * a.cluster;
+    const size_t smem = (size_t)steps * kSelThreads * sizeof(uint32_t);
     static std::atomic<int> ready[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
@@ -344,14 +404,18 @@ extern "C" rs_status rs_paged_evict(uint16_t *k_pages, uint16_t *v_pages, int Hk
         return RS_ERR_CUDA;
     }
     if (!ready[dev].load()) {
-        const cudaError_t e = cudaFuncSetAttribute(evict_select, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeys * (int)sizeof(uint32_t));
-        if (e != cudaSuccess) {
-            set_error("%s: cudaFuncSetAttribute: %s", what, cudaGetErrorString(e));
+        const int most_smem = kSelKeys * (int)sizeof(uint32_t);
+        const cudaError_t e1 = cudaFuncSetAttribute(evict_select<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem);
+        const cudaError_t e2 = cudaFuncSetAttribute(evict_select<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem);
+        if (e1 != cudaSuccess || e2 != cudaSuccess) {
+            set_error("%s: cudaFuncSetAttribute: %s", what, cudaGetErrorString(e1 != cudaSuccess ? e1 : e2));
             return RS_ERR_CUDA;
         }
         ready[dev].store(1);
     }
-    launch_pdl(evict_select, dim3(Hkv, B), dim3(kSelThreads), smem, (cudaStream_t)stream, a);
+    cudaStream_t s = (cudaStream_t)stream;
+    if (a.cluster > 1) launch_pdl_cluster(evict_select<true>, dim3(Hkv * a.cluster, B), dim3(kSelThreads), smem, s, a.cluster, a);
+    else launch_pdl(evict_select<false>, dim3(Hkv, B), dim3(kSelThreads), smem, s, a);
     RS_CHECK_LAUNCH(what);
     const int per = kMoveThreads / (D / 8);
     const int chunks = std::max(1, std::min((budget + per - 1) / per, 16 * num_sms() / (B * Hkv) + 1));
