@@ -98,7 +98,7 @@ __device__ void plan_tree(const FlashArgs &a, const int32_t *parents, uint32_t *
 // Block 0: the pairs of row tiles of all requests end to end and the prefix of
 // their costs.  Blocks 1 ..: the draft trees.
 __global__ void __launch_bounds__(kPlanThreads)
-flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
+flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc, double kv_bytes, double l2) {
     pdl_wait_prev();
     pdl_launch_next();
     if (blockIdx.x > 0) {
@@ -110,7 +110,7 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
     __shared__ long long s_wl[32];
     const int tid = threadIdx.x;
     int pairs = 0, latest = 0;
-    long long tiles = 0;  // about how many key tiles one KV head has
+    long long tiles = 0, keys = 0;  // about how many key tiles one KV head has; keys of all requests
     for (int base = 0; base < a.B; base += blockDim.x) {
         const int b = base + tid;
         int4 rq = make_int4(0, 0, 0, 0);
@@ -137,6 +137,7 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
         long long t = 0;
         if (rq.y > 0) t = (long long)mine * (pair_keys(a, rq.y, rq.z, 0) + (long long)pair_keys(a, rq.y, rq.z, mine - 1)) / (2 * kBN) + 1;
         block_scan(t, tiles, s_wl);
+        block_scan((long long)(rq.y > 0 ? rq.y + rq.z : 0), keys, s_wl);
     }
     if (tid == 0) s_pref[0] = 0;
     __syncthreads();
@@ -167,6 +168,12 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc) {
         a.cum[0] = 0;
         a.n_pairs[0] = M;
         a.n_pairs[1] = beta;
+        // groups of KV heads whose keys and values fill half of L2 each, where all are
+        // more than it holds and a share stays long (200 key tiles) for its two more pieces
+        int phases = 1;
+        const double used = (double)keys * kv_bytes;
+        while (phases < a.max_phases && used > 1.5 * l2 && used > 0.5 * l2 * phases && tiles * a.Hkv / (a.grid * 2 * phases) >= 200) phases *= 2;
+        a.n_pairs[2] = phases;
     }
 }
 
@@ -175,10 +182,13 @@ int flash_grid() { return std::min(num_sms(), kAttnMaxGrid); }
 // tokens of a row tile
 int flash_tq(int G) { return kBM / G; }
 
-// groups of KV heads that a call may be worked off in (the workspace holds
-// their partial slots)
+// groups of KV heads that a call may be worked off in (the workspace holds their
+// partial slots): several only where requests have several pairs of row tiles, so
+// that keys are read again
 int max_phases(int B, int T, int Hkv, int tq) {
-    return (long long)T > 2ll * tq * B ? std::min(kFlMaxPhases, Hkv) : 1;
+    int p = 1;
+    while ((long long)T > 2ll * tq * B && p < kFlMaxPhases && 2 * p <= Hkv) p *= 2;
+    return p;
 }
 
 struct Work {
@@ -197,7 +207,7 @@ Work carve(void *base, int B, int T, int Hq, int Hkv, int D) {
     a.cum = cv.take<long long>(pairs + 1);
     a.ent = cv.take<int4>(pairs);
     a.ent_ctx = cv.take<int>(pairs);
-    a.n_pairs = cv.take<int>(2);
+    a.n_pairs = cv.take<int>(3);
     a.bound = cv.take<int4>(F * (grid + 1));
     w.anc = cv.take<uint32_t>((size_t)T * kAncWords);
     a.part_m = cv.take<float>(2 * grid * F * kFlRows);
@@ -228,7 +238,7 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     a.wait_limit = wait_limit();
     const double bytes = 4.0 * (double)kv_rows * a.Hkv * D;
     a.kv_stream = bytes > 0.5 * (double)l2_bytes();
-    a.phases = 1;
+    a.max_phases = bytes > 1.5 * (double)l2_bytes() ? max_phases(a.B, a.T, a.Hkv, a.tq) : 1;
     // a segment has no more rows than the call's tokens fill
     a.comb_blocks = (a.T > a.tq ? kFlRows : std::max(a.T, 1) * a.G + kFlCombRows - 1) / kFlCombRows;
     const int box = a.page_table ? std::min(1 << a.page_log2, kBN) : kBN;
@@ -242,7 +252,8 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     // a thread per request and per pair, as far as a block goes (fewer warps, shorter barriers)
     const int wide = std::max(a.B, a.T / (2 * a.tq) + a.B);
     const int threads = std::min(std::max((wide + 31) / 32 * 32, parents ? RS_MAX_NODES : 32), kPlanThreads);
-    launch_pdl(flash_plan, dim3(1 + (parents ? a.B : 0)), dim3(threads), 0, st, a, parents, w.anc);
+    launch_pdl(flash_plan, dim3(1 + (parents ? a.B : 0)), dim3(threads), 0, st, a, parents, w.anc, 4.0 * a.Hkv * D,
+               (double)l2_bytes());
     RS_CHECK_LAUNCH(what);
     return type ? flash_launch<true>(a, D, tmq, tmk, tmv, what, st) : flash_launch<false>(a, D, tmq, tmk, tmv, what, st);
 }

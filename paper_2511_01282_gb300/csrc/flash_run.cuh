@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(kFlCombThreads)
 flash_combine(FlashArgs a) {
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int f = blockIdx.y / a.comb_blocks, y = blockIdx.y % a.comb_blocks;
+    const int phases = a.n_pairs[2], f = blockIdx.y / a.comb_blocks, y = blockIdx.y % a.comb_blocks;
     const int4 *bound = a.bound + f * (a.grid + 1);
     const int c = min((int)blockIdx.x + 1, a.grid);
     const int4 start = bound[c], before = bound[c - 1];
@@ -40,13 +40,13 @@ flash_combine(FlashArgs a) {
         for (long long i = threadIdx.x; i < rows; i += kFlCombThreads) a.lse[(long long)rq.x * a.Hq + i] = 0.f;
     }
     auto same = [&](int4 r) { return r.x == start.x && r.y == start.y && r.z > 0; };
-    if (c >= a.grid || start.z == 0 || same(before)) return;  // between segments, or not the first cut
+    if (f >= phases || c >= a.grid || start.z == 0 || same(before)) return;  // between segments, or not the first cut
     const int4 e = a.ent[start.y];  // request, pair, first row, rows
     const int x = y * kFlCombRows / kBM;  // row tile of the block's rows
     const int first = (e.y * 2 + x) * a.tq, r0 = y * kFlCombRows - x * kBM;
     if (r0 / a.G >= a.tq || first + r0 / a.G >= e.w) return;
     if (a.status[e.x] & ~RS_ST_TIMEOUT) return;
-    const int kvh = f * a.Hkv / a.phases + start.x;
+    const int kvh = f * a.Hkv / phases + start.x;
     constexpr int kC = D / 32;  // columns of a lane
 #pragma unroll 1
     for (int k = warp; k < kFlCombRows; k += kFlCombThreads / 32) {
@@ -125,7 +125,7 @@ rs_status flash_launch_d(const FlashArgs &a, const CUtensorMap &tmq, const CUten
     }
     launch_pdl(flash_kernel<D, BF16>, dim3(a.grid), dim3(kFlThreads), FlSmem<D>::kTotal, st, a, tmq, tmk, tmv);
     RS_CHECK_LAUNCH(what);
-    launch_full(flash_combine<D, BF16>, dim3(std::max(a.grid - 1, 1), a.phases * a.comb_blocks), dim3(kFlCombThreads), 0, st, a);
+    launch_full(flash_combine<D, BF16>, dim3(std::max(a.grid - 1, 1), a.max_phases * a.comb_blocks), dim3(kFlCombThreads), 0, st, a);
     RS_CHECK_LAUNCH(what);
     return RS_OK;
 }

@@ -63,6 +63,7 @@ inline rs_status check_sizes(const char *what, int dtype, int B, int T, int Hq, 
         set_error("%s: Hq=%d must be a multiple of Hkv=%d, 1 to %d times", what, Hq, Hkv, kBM);
         return RS_ERR_UNSUPPORTED;
     }
+    RS_CHECK_ARG(T <= 1 << 30, "%s: T=%d above 2^30", what, T);
     RS_CHECK_ARG(B <= kBatchMax, "%s: B=%d above %d", what, B, kBatchMax);
     RS_CHECK_ARG(isfinite(scale) && scale > 0.f, "%s: scale must be finite and > 0", what);
     return RS_OK;

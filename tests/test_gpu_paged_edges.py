@@ -308,3 +308,92 @@ def test_a_long_cache():
     kept = set(torch.sort(key, descending=True, stable=True).indices[:1000].tolist())
     assert set(pos[0, at[:1000]].tolist()) == kept
     assert torch.equal(kp.view(-1, Hkv, D)[at[:1000], 0], K[pos[0, at[:1000]].long(), 0])
+
+
+FIRST = """
+import sys, torch
+sys.path[:0] = [%r, %r]
+from paper_2511_01282_gb300 import respec as rs
+dev, bf = "cuda", torch.bfloat16
+i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
+q, k, v = (torch.randn(40, h, 128, device=dev).to(bf) for h in (4, 2, 2))
+kp, vp = torch.zeros(8, 16, 2, 128, dtype=bf, device=dev), torch.zeros(8, 16, 2, 128, dtype=bf, device=dev)
+table, off, ctx, length = i32([[3, 1, 7, 5]]), i32([0, 40]), i32([0]), i32([40])
+out, lse, st = torch.zeros(40, 4, 128, dtype=bf, device=dev), torch.zeros(40, 4, device=dev), i32([-1])
+out2, lse2 = torch.zeros_like(out), torch.zeros_like(lse)
+w, pos, new = torch.zeros(2, 128, device=dev), torch.zeros(2, 128, dtype=torch.int32, device=dev), i32([0])
+ws = torch.empty(1 << 28, dtype=torch.uint8, device=dev)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    rs.rs_prompt_attn(q, 512, k, 256, v, 256, 0, off, 1, 40, 4, 2, 128, 0.09, out, lse, st, ws)
+    rs.rs_paged_append(k, 256, v, 256, None, off, 1, 40, 2, 128, kp, vp, 8, 16, table, 4, ctx, w, pos, st)
+    rs.rs_paged_attn(q, 512, 0, off, None, 1, 40, 4, 2, 128, kp, vp, 8, 16, table, 4, ctx, 0.09, out2, lse2, st, ws)
+    rs.rs_paged_weights(q, 512, 0, lse, off, 1, 40, 4, 2, 128, kp, 8, 16, table, 4, ctx, 0.09, w, st, ws)
+    rs.rs_paged_evict(kp, vp, 2, 128, 8, 16, table, 4, length, length, 1, 20, 3, w, pos, new, st, ws)
+g.replay()
+torch.cuda.synchronize()
+assert st.item() == 0 and new.item() == 20 and torch.equal(out, out2) and torch.equal(lse, lse2)
+assert abs(float(w[:, 48:64].sum()) + float(w[:, 16:20].sum())) > 0
+print("captured")
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST % (root, os.path.join(root, "tests"))], capture_output=True, text=True)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+def test_no_rows():
+    q, k, v = _qkv(0, 4, 2, 64)
+    out, lse, status = run_prompt(q, k, v, [0, 0, 0], rs.RS_BF16, 0.1)
+    assert status.tolist() == [0, 0]
+    pages, most, table, kp, vp = _cache([1, 1], [20, 30], 16)
+    w = torch.ones(2, pages * 16, device="cuda")
+    out, lse, status = run_paged(q, rs.RS_BF16, [0, 0, 0], None, kp, vp, 16, table, [20, 30], 0.1)
+    assert status.tolist() == [0, 0]
+    assert append(k, v, None, [0, 0, 0], kp, vp, 16, table, [20, 30]).tolist() == [0, 0]
+    assert weigh(q, rs.RS_BF16, lse, [0, 0, 0], kp, 16, table, [20, 30], 0.1, w).tolist() == [0, 0] and bool((w == 1).all())
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(5, 1), (48, 4), (33, 11), (96, 2), (64, 64)])
+def test_head_layouts(Hq, Hkv):
+    D, n, ctx, page = 64, [37, 150], [260, 5], 32
+    pages, most, table, kp, vp = _cache(n, ctx, page, Hkv, D)
+    off = _off(n)
+    q = _normal(1, off[-1], Hq, D, dtype=torch.bfloat16)
+    out, lse, status = run_paged(q, rs.RS_BF16, off, None, kp, vp, page, table, ctx, 0.125)
+    assert status.tolist() == [0, 0]
+    w = torch.zeros(Hkv, pages * page, device="cuda")
+    assert weigh(q, rs.RS_BF16, lse, off, kp, page, table, ctx, 0.125, w).tolist() == [0, 0]
+    for b in range(2):
+        a, e = off[b], off[b + 1]
+        at = slots(table, b, ctx[b] + n[b], page)
+        K, V, see = kp.view(-1, Hkv, D)[at], vp.view(-1, Hkv, D)[at], causal_mask(n[b], ctx[b])
+        o, z, o_tol, z_tol = attention(q[a:e], K, V, see, 0.125)
+        check(out[a:e], o, o_tol, "out")
+        check(lse[a:e], z, z_tol, "lse")
+        want, tol = ref_weights(q[a:e], K, lse[a:e], see, 0.125)
+        check(w[:, at], want, tol, "weights")
+
+
+def test_groups_of_heads_in_phases():
+    """More keys than L2 holds, read by several pairs of row tiles each: the KV heads are worked off in groups.  Some rows of
+    every head against the formula; the whole against a smaller call's bits."""
+    T, Hq, Hkv, D = 72000, 8, 8, 128
+    dt = torch.float16
+    q, k, v = _qkv(T, Hq, Hkv, D, dt)
+    out, lse, status = run_prompt(q, k, v, [0, T], rs.RS_F16, 0.09)
+    assert status.tolist() == [0]
+    for i in (0, 255, 256, 30000, 71999):
+        o, z, o_tol, z_tol = attention(q[i:i + 1], k[:i + 1], v[:i + 1], torch.ones(1, i + 1, dtype=torch.bool), 0.09)
+        check(out[i:i + 1], o, o_tol, "out of row %d" % i)
+        check(lse[i:i + 1], z, z_tol, "lse of row %d" % i)
+    rows = torch.arange(0, T, 977, device="cuda")
+    for h in (0, 3, 7):  # one head alone: another split, the same values within both roundings
+        o1, l1, _ = run_prompt(q[:, h:h + 1], k[:, h:h + 1], v[:, h:h + 1], [0, T], rs.RS_F16, 0.09)
+        assert float((lse[rows, h] - l1[rows, 0]).abs().max()) < 1e-4
+        assert float((out[rows, h].float() - o1[rows, 0].float()).abs().max()) < 2e-3

@@ -50,6 +50,7 @@ PAGED = ("rs_paged_append", "rs_paged_attn", "rs_paged_weights", "rs_paged_evict
     (dict(D=96), UNSUPPORTED, "96"), (dict(Hq=5), UNSUPPORTED, "Hq=5"), (dict(Hkv=0), UNSUPPORTED, "Hkv=0"), (dict(Hq=0), UNSUPPORTED, "Hq=0"),
     (dict(Hq=129, Hkv=1), UNSUPPORTED, "128"), (dict(dtype=2), INVALID, "dtype 2"), (dict(dtype=-1), INVALID, "dtype -1"),
     (dict(B=-1), INVALID, "negative"), (dict(T=-1), INVALID, "negative"), (dict(B=4097), INVALID, "4096"),
+    (dict(T=(1 << 30) + 1), INVALID, "2^30"),
     (dict(scale=0.0), INVALID, "scale"), (dict(scale=float("nan")), INVALID, "scale"), (dict(scale=float("inf")), INVALID, "scale"),
     (dict(off=None), INVALID, "null request"), (dict(status=None), INVALID, "null request"), (dict(q=None), INVALID, "null row"),
     (dict(lse=None), INVALID, "null row"), (dict(q=P + 8), INVALID, "aligned"), (dict(ws=P + 8), INVALID, "aligned"),
