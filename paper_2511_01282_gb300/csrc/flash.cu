@@ -143,7 +143,7 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc, double kv_bytes, 
     __syncthreads();
     const int M = pairs;
     const long long per = tiles * a.Hkv / (2 * a.grid);
-    const int beta = kFlWH * (int)(per < kFlSegCost ? per : kFlSegCost);
+    const int beta = (int)(per * a.single < a.start ? per * a.single : a.start);
     long long carry = 0;
     for (int base = 0; base < M; base += blockDim.x) {
         const int i = base + tid;
@@ -235,6 +235,8 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     a.tq = flash_tq(a.G);
     a.grid = flash_grid();
     a.anc = parents ? w.anc : nullptr;
+    a.single = fl_single(D);
+    a.start = fl_start(D);
     a.wait_limit = wait_limit();
     const double bytes = 4.0 * (double)kv_rows * a.Hkv * D;
     a.kv_stream = bytes > 0.5 * (double)l2_bytes();

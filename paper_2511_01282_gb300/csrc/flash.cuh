@@ -49,8 +49,13 @@ static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "re
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
 constexpr int kFlRows = 2 * kBM;  // rows of a segment and of a partial slot
 constexpr int kFlCombRows = 32;   // of them for a block of flash_combine
-constexpr int kFlWF = 5, kFlWH = 3;  // cost of a key tile for a pair and for a single row tile
-constexpr int kFlSegCost = 8;        // cost of a segment's start, in single-tile key tiles, at most
+// What a CTA's time goes to, in eighths of a key tile of a pair: a key tile where
+// only the first row tile has rows, and a segment's start (the first copies and
+// products, the epilogue).  Fitted to every CTA's cycles over packed prompts, chunks
+// and a long prompt: 2650, 1900 and 5000 cycles at D = 64; 2850, 2500 and 7200 at D = 128.
+constexpr int kFlPair = 8;
+constexpr int fl_single(int D) { return D == 64 ? 6 : 7; }
+constexpr int fl_start(int D) { return D == 64 ? 15 : 20; }
 // Tensor memory columns
 template <int D>
 struct FlTm {
@@ -73,6 +78,7 @@ struct FlashArgs {
     int4 *bound;                 // [phase][CTA] where the CTA's share starts: (head in phase, pair, tile)
     float *part_o, *part_m, *part_l;
     int max_phases, grid;
+    int single, start;           // costs: fl_single, fl_start
     int comb_blocks;             // blocks of flash_combine per cut segment
     int B, T, Hq, Hkv, G, tq;
     int kv_stream;               // K/V is large next to L2: tiles read once are evicted first
@@ -92,7 +98,7 @@ __device__ __forceinline__ int pair_tiles(const FlashArgs &a, int n, int ctx, in
 }
 // cost of one of its key tiles
 __device__ __forceinline__ int tile_cost(const FlashArgs &a, int n, int p) {
-    return n - p * 2 * a.tq > a.tq ? kFlWF : kFlWH;
+    return n - p * 2 * a.tq > a.tq ? kFlPair : a.single;
 }
 
 struct FlPiece {
@@ -155,6 +161,8 @@ struct FlCursor {
 };
 
 // Where cost position x of a phase of hn heads falls: (head, pair, tile).
+// No piece shorter than half a segment's start is cut off (64 sequences of 256
+// tokens, 96.7 -> 93.0 us; 32 of up to 1000 at D = 128, 159.7 -> 156.1).
 // Whole warp; the pair is searched 32 ways at a time.
 __device__ __forceinline__ int4 fl_locate(const FlashArgs &a, long long x, int hn, int M, int beta) {
     const long long C = a.cum[M];
@@ -170,8 +178,10 @@ __device__ __forceinline__ int4 fl_locate(const FlashArgs &a, long long x, int h
         hi = min(lo + step, hi);
     }
     const int4 e = a.ent[lo];
-    const long long in = rem - a.cum[lo] - beta;
-    return make_int4(hh, lo, in > 0 ? (int)(in / tile_cost(a, e.w, e.y)) : 0, 0);
+    const int w = tile_cost(a, e.w, e.y), in = (int)(rem - a.cum[lo]) - beta;
+    if (2 * in < beta) return make_int4(hh, lo, 0, 0);
+    if (2 * (w * pair_tiles(a, e.w, a.ent_ctx[lo], e.y) - in) < beta) return lo + 1 < M ? make_int4(hh, lo + 1, 0, 0) : make_int4(hh + 1, 0, 0, 0);
+    return make_int4(hh, lo, in / w, 0);
 }
 
 template <bool BF16>
