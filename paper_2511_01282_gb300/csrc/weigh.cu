@@ -12,11 +12,19 @@
 // tokens neither copy nor multiply rows they do not have.  The segments lie end
 // to end, a CTA takes an equal share of their cost, and the sums of a segment that
 // a share's end cuts are joined by weigh_combine in order (the same bits every time).
-// Bound: K and the weights, read once, for single tokens; the exponentials (16
-// cycles a warp for 32 keys x 4 columns) and the product (2 D flop) for long chunks.
+// Bound: K and the weights, read once, for single tokens (16 requests of up to 8191
+// keys, D = 64: 80 MB in 23 us).  Chunks: shared memory, which the products read at
+// its full rate (8 KB each 64 cycles) while Q tiles are written to it and each warp
+// reads the columns' lse; then the exponentials (4 cycles a warp for 32 keys).  Four
+// prompts of 1000-4000 tokens, D = 128: 116 us, 1060 TFLOP/s of the rows and keys that see each other.
 //
-// Warps: 0 MMA issue, 1 copies Q, 2 copies K, 3 reads the columns' lse, 4-7 and
-// 8-11 the two key tiles.  Tensor memory: two S buffers of 128 columns for each.
+// Warps: 0 and 1 issue the products of a key tile each (one warp for both spent as
+// long on waits as on products), 2 copies K, 3 copies Q and reads its columns' lse
+// (K and Q by one warp: single tokens 33 -> 36 us).  Four warpgroups sum, one for
+// each key tile and parity of the Q tiles, which is its S buffer of 128 columns of
+// tensor memory: with two, the waits of a tile's chain were not covered (129 us
+// against 116).  At a segment's end the two of a key tile join their sums in shared
+// memory in a fixed order.
 #include <math.h>
 
 #include <algorithm>
@@ -31,10 +39,12 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kWgThreads = 384;
-constexpr uint32_t kWgRegsSum = 208, kWgRegsCopy = 88;
-static_assert(2 * 128 * kWgRegsSum + 128 * kWgRegsCopy == kWgThreads * 168, "register split");
+constexpr int kWgThreads = 640;
 constexpr int kWgKeys = 2 * kBN;  // keys of a segment
+// A warpgroup hands its part of a segment's sums to the other of its key tile in one of
+// these places.  It can not get kNL + 1 segments ahead: the columns' lse of its tiles
+// would have to be there, for which the other has finished all but kNL tiles before.
+constexpr int kJoins = 8;
 constexpr int kWgBeta = 2;  // cost of a segment's start (its K tiles), in Q tiles
 
 struct WeighArgs {
@@ -207,42 +217,45 @@ struct WgSmem {
     static constexpr int kNK = D == 128 ? 2 : 4, kNQ = D == 128 ? 2 : 4, kNL = 4;  // key pairs, Q tiles, columns' lse
     static constexpr int kK = 0, kQ = kNK * 2 * kTile;
     static constexpr int kLse = kQ + kNQ * kTile;     // [kNL][128] floats: -lse in the log2 domain
-    static constexpr int kMask = kLse + kNL * 512;  // 16-byte aligned
-    static_assert(kMask % 16 == 0, "");
-       // [kNL][4] words: the columns that count
-    static constexpr int kBar = kMask + kNL * 16;
-    static constexpr int kNumBars = 2 * (kNK + kNQ + kNL + 4) + 1;
+    static constexpr int kMask = kLse + kNL * 512;    // [kNL][4] words: the columns that count
+    static_assert(kMask % 16 == 0, "16-byte reads");
+    static constexpr int kJoin = kMask + kNL * 16;  // [2][kJoins][128] floats: sums of a segment's other Q tiles
+    static constexpr int kBar = kJoin + 2 * kJoins * 512;
+    static constexpr int kNumBars = 2 * (kNK + kNQ + kNL + 4) + 2 * kJoins + 2;
     static constexpr int kMisc = kBar + kNumBars * 8;
     static constexpr int kBounds = (kMisc + 8 + 15) / 16 * 16;
     static constexpr int kTotal = kBounds + 32 + 1024;
     static_assert(kTotal <= 232448, "shared memory of one CTA");
 };
 
-// sum += 2^(c s_i + nl_i) over N columns, two at a time; the statements in an
+// sum += 2^(c s_i + nl_i) over 32 columns, two at a time; the statements in an
 // order that keeps the other work between the exponentials (see exp_pairs).
-template <int N>
-__device__ __forceinline__ void exp_sums(const uint32_t (&s0)[32], const uint32_t (&s1)[32], float2 c, const ulonglong2 *nl,
-                                         uint64_t (&sum)[4]) {
+__device__ __forceinline__ void exp_sums(const uint32_t (&s)[32], float2 c, uint32_t nl, uint64_t (&sum)[4]) {
     constexpr int kAhead = 4, kBehind = 4;  // pairs of columns
-    float2 d[N / 2], p[N / 2];
-    ulonglong2 l;
+    constexpr int kRead = 2;                // 16-byte reads of nl ahead of their use
+    float2 d[16], p[16];
+    ulonglong2 l[8];
+    auto read = [&](int i) {
+        if (i < 8) asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(l[i].x), "=l"(l[i].y) : "r"(nl + 16 * i));
+    };
     auto fma1 = [&](int e) {
-        if (e % 2 == 0) l = nl[e / 2];
-        const float2 v = e < 16 ? make_float2(__uint_as_float(s0[2 * e]), __uint_as_float(s0[2 * e + 1]))
-                                : make_float2(__uint_as_float(s1[2 * e - 32]), __uint_as_float(s1[2 * e - 31]));
+        if (e % 2 == 0) read(e / 2 + kRead);
+        const float2 v = make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
         uint64_t r;
-        asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_b64(v)), "l"(as_b64(c)), "l"(e % 2 ? l.y : l.x));
+        asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_b64(v)), "l"(as_b64(c)), "l"(e % 2 ? l[e / 2].y : l[e / 2].x));
         d[e] = as_float2(r);
     };
 #pragma unroll
+    for (int i = 0; i < kRead; ++i) read(i);
+#pragma unroll
     for (int e = 0; e < kAhead; ++e) fma1(e);
 #pragma unroll
-    for (int e = 0; e < N / 2 + kBehind; ++e) {
-        if (e < N / 2) {
+    for (int e = 0; e < 16 + kBehind; ++e) {
+        if (e < 16) {
             asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[e].x) : "f"(d[e].x));
             asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[e].y) : "f"(d[e].y));
         }
-        if (e + kAhead < N / 2) fma1(e + kAhead);
+        if (e + kAhead < 16) fma1(e + kAhead);
         if (e >= kBehind) asm volatile("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[e & 3]) : "l"(as_b64(p[e - kBehind])));
     }
 }
@@ -257,7 +270,7 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                                                             ~uintptr_t(1023));
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kBar);
     uint64_t *kfull = bars, *kempty = kfull + NK, *qfull = kempty + NK, *qempty = qfull + NQ;
-    uint64_t *lfull = qempty + NQ, *lempty = lfull + NL, *sfull = lempty + NL, *sempty = sfull + 4, *drain = sempty + 4;
+    uint64_t *lfull = qempty + NQ, *lempty = lfull + NL, *sfull = lempty + NL, *sempty = sfull + 4, *joined = sempty + 4, *drain = joined + 2 * kJoins;
     uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + S::kMisc);
     volatile int *s_abort = reinterpret_cast<volatile int *>(smem + S::kMisc + 4);
     int4 *s_bound = reinterpret_cast<int4 *>(smem + S::kBounds);
@@ -267,26 +280,28 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
     if (tid == 0) {
         for (uint32_t s = 0; s < NK; ++s) {
             mbar_init(&kfull[s], 1);
-            mbar_init(&kempty[s], 1);
+            mbar_init(&kempty[s], 2);  // a commit for each key tile
         }
         for (uint32_t s = 0; s < NQ; ++s) {
             mbar_init(&qfull[s], 1);
-            mbar_init(&qempty[s], 1);
+            mbar_init(&qempty[s], 2);
         }
         for (uint32_t s = 0; s < NL; ++s) {
             mbar_init(&lfull[s], 32);
             mbar_init(&lempty[s], 2 * kBM);
         }
-        for (int s = 0; s < 4; ++s) {  // buffer u of key tile x: 2 x + u
+        for (int s = 0; s < 4; ++s) {  // buffer y of key tile x: 2 x + y
             mbar_init(&sfull[s], 1);
             mbar_init(&sempty[s], kBM);
         }
-        mbar_init(drain, 1);
+        for (int s = 0; s < 2 * kJoins; ++s) mbar_init(&joined[s], kBM);
+        mbar_init(&drain[0], 1);
+        mbar_init(&drain[1], 1);
         *s_abort = 0;
         fence_mbar_init();
     }
     if (warp == 0) tmem_alloc(s_tmem, kTmemCols);
-    if (warp == 1 && lane == 0) {
+    if (warp == 3 && lane == 0) {
         prefetch_tmap(&tmq);
         prefetch_tmap(&tmk);
     }
@@ -311,81 +326,52 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
     bool ok = true;
 
     if (warp < 4) {
-        reg_dealloc<kWgRegsCopy>();
-        if (warp == 0) {
-            // ------------------------------------------------------ MMA issuer (whole warp, one lane issues)
+        if (warp < 2) {
+            // ------------------------------------------------------ products of key tile x (whole warp, one lane issues)
+            const uint32_t x = (uint32_t)warp;
             // columns in units of 16, the product's granularity
             const uint32_t id = (idesc_16_f32(BF16, kBN, 16, false) & ~(0x3fu << 17)) | ((uint32_t)((cols + 15) / 16 * 2) << 17);
             const uint64_t d0 = sdesc_sw128(smem_u32(smem + S::kK), 16, 1024);
             const uint32_t d_hi = (uint32_t)(d0 >> 32), k_lo0 = (uint32_t)d0;
             const uint32_t q_lo0 = (uint32_t)sdesc_sw128(smem_u32(smem + S::kQ), 16, 1024);
-            const uint32_t tm = uniform(tmem), idu = uniform(id);
+            const uint32_t tm = uniform(tmem + x * 256), idu = uniform(id);
             constexpr uint32_t kTileDesc = S::kTile >> 4;
-            uint32_t g = 0, g1 = 0, piece = 0;  // Q tiles, those with two key tiles, segments
+            uint32_t g = 0, piece = 0;  // Q tiles, segments
             auto wait = [&](uint64_t *b1, uint32_t p1, uint64_t *b2, uint32_t p2) -> bool {
                 return ok = quick_wait2(b1, p1 & 1, b2, p2 & 1, s_abort, a.wait_limit);
             };
             while (ok && cur.next(pc)) {
                 const uint32_t ks = piece % NK;
-                const bool two = pc.rq.z + pc.rq.y > pc.jt * kWgKeys + kBN;
+                const bool here = pc.rq.z + pc.rq.y > pc.jt * kWgKeys + (int)x * kBN;
+                const uint32_t k_lo = uniform(k_lo0 + (2 * ks + x) * kTileDesc);
                 if (!wait(&kfull[ks], piece / NK, &kfull[ks], piece / NK)) break;
                 for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
                     const uint32_t qs = g % NQ;
-                    if (!wait(&qfull[qs], g / NQ, &sempty[g & 1], (g >> 1) ^ 1)) break;
-                    if (two && !wait(&sempty[2 + (g1 & 1)], (g1 >> 1) ^ 1, &sempty[2 + (g1 & 1)], (g1 >> 1) ^ 1)) break;
+                    const uint32_t buf = 2 * x + (g & 1);
+                    if (!wait(&qfull[qs], g / NQ, &sempty[buf], (g >> 1) ^ 1)) break;
                     tc_fence_after();
-                    const uint32_t q_lo = uniform(q_lo0 + qs * kTileDesc);
-#pragma unroll 1
-                    for (uint32_t x = 0; x < (two ? 2u : 1u); ++x) {
-                        const uint32_t u = x ? g1 & 1 : g & 1;
-                        const uint32_t k_lo = uniform(k_lo0 + (2 * ks + x) * kTileDesc), d = uniform(tm + (2 * x + u) * 128);
-                        if (elect_one()) {
+                    const uint32_t q_lo = uniform(q_lo0 + qs * kTileDesc), d = uniform(tm + (g & 1) * 128);
+                    if (elect_one()) {
+                        if (here) {  // (else the commits alone arrive)
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk) {
                                 const uint32_t o = (uint32_t)(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4);
                                 umma_ss(d, desc_of(k_lo + o, d_hi), desc_of(q_lo + o, d_hi), idu, kk > 0);
                             }
-                            umma_commit(&sfull[2 * x + u]);
                         }
-                        __syncwarp();
-                    }
-                    if (elect_one()) {
+                        umma_commit(&sfull[buf]);
                         umma_commit(&qempty[qs]);
                         if (qt == pc.q1 - 1) umma_commit(&kempty[ks]);
                     }
                     __syncwarp();
-                    g1 += two;
                 }
                 ++piece;
             }
             if (!ok) {
-                if (elect_one()) umma_commit(drain);
+                if (elect_one()) umma_commit(&drain[x]);
                 __syncwarp();
                 volatile int no_abort = 0;
-                mbar_wait(drain, 0, &no_abort, kWaitLimit);
-            }
-        } else if (warp == 1) {
-            // ------------------------------------------------------ Q tiles
-            const uint32_t q_tx = (uint32_t)cols * D * 2;
-            uint32_t g = 0;
-            while (ok && cur.next(pc)) {
-                const int q_first = pc.q_first;
-                for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
-                    const uint32_t qs = g % NQ;
-                    if (!(ok = warp_wait(&qempty[qs], ((g / NQ) & 1) ^ 1, s_abort, a.wait_limit))) break;
-                    if (lane == 0) {
-                        mbar_expect_tx(&qfull[qs], q_tx);
-#pragma unroll
-                        for (int kb = 0; kb < kKB; ++kb)
-                            tma_load_3d(smem + S::kQ + qs * S::kTile + kb * 16384, &tmq, &qfull[qs], kb * 64, pc.kvh * a.G,
-                                        pc.rq.x + (q_first + qt) * a.tq);
-                    }
-                    __syncwarp();
-                }
-            }
-            if (!ok) {  // let the copies already issued land before the CTA exits
-                volatile int no_abort = 0;
-                for (uint32_t t = g >= NQ ? g - NQ : 0; t < g; ++t) mbar_wait(&qfull[t % NQ], (t / NQ) & 1, &no_abort, kWaitLimit);
+                mbar_wait(&drain[x], 0, &no_abort, kWaitLimit);
             }
         } else if (warp == 2) {
             // ------------------------------------------------------ key pairs; lane x copies page x
@@ -423,7 +409,8 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                 for (uint32_t t = piece >= NK ? piece - NK : 0; t < piece; ++t) mbar_wait(&kfull[t % NK], (t / NK) & 1, &no_abort, kWaitLimit);
             }
         } else {
-            // ------------------------------------------------------ the columns' lse
+            // ------------------------------------------------------ Q tiles, their columns' lse
+            const uint32_t q_tx = (uint32_t)cols * D * 2;
             uint32_t g = 0;
             int tk[4], hg[4];  // column c = 32 i + lane: token c / G of the tile, head c % G of the group
 #pragma unroll
@@ -444,7 +431,16 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                 float next[4];
                 read(pc.q0, next);
                 for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
-                    const uint32_t ls = g % NL;
+                    const uint32_t ls = g % NL, qs = g % NQ;
+                    if (!(ok = warp_wait(&qempty[qs], ((g / NQ) & 1) ^ 1, s_abort, a.wait_limit))) break;
+                    if (lane == 0) {
+                        mbar_expect_tx(&qfull[qs], q_tx);
+#pragma unroll
+                        for (int kb = 0; kb < kKB; ++kb)
+                            tma_load_3d(smem + S::kQ + qs * S::kTile + kb * 16384, &tmq, &qfull[qs], kb * 64, pc.kvh * a.G,
+                                        pc.rq.x + (q_first + qt) * a.tq);
+                    }
+                    __syncwarp();
                     float v[4];
                     uint32_t m[4];
 #pragma unroll
@@ -452,7 +448,10 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                     if (qt + 1 < pc.q1) read(qt + 1, next);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) m[i] = __ballot_sync(0xffffffffu, isfinite(v[i]));
-                    if (!(ok = warp_wait(&lempty[ls], ((g / NL) & 1) ^ 1, s_abort, a.wait_limit))) break;
+                    if (!(ok = warp_wait(&lempty[ls], ((g / NL) & 1) ^ 1, s_abort, a.wait_limit))) {
+                        ++g;  // its Q tile is under way
+                        break;
+                    }
                     float *nl = reinterpret_cast<float *>(smem + S::kLse) + ls * 128;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) nl[32 * i + lane] = isfinite(v[i]) ? v[i] * -1.4426950408889634f : 0.f;
@@ -461,75 +460,77 @@ weigh_kernel(WeighArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                     warp_arrive(&lfull[ls]);
                 }
             }
+            if (!ok) {  // let the copies already issued land before the CTA exits
+                volatile int no_abort = 0;
+                for (uint32_t t = g >= NQ ? g - NQ : 0; t < g; ++t) mbar_wait(&qfull[t % NQ], (t / NQ) & 1, &no_abort, kWaitLimit);
+            }
         }
     } else {
-        reg_alloc<kWgRegsSum>();
         // ---------------------------------------------------------- sums (a thread per key)
-        const int x = (warp - 4) >> 2, r = tid & (kBN - 1);
-        const uint32_t s_tm0 = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)x * 256;
+        // x: the key tile; y: Q tiles of this parity
+        const int x = (warp - 4) >> 3, r = tid & (kBN - 1);
+        const uint32_t y = (uint32_t)(warp >> 2) - 1 & 1, buf = 2 * x + y;
+        const uint32_t s_tm = tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 128;
         const float2 c2 = make_float2(a.scale * 1.4426950408889634f, a.scale * 1.4426950408889634f);
-        const int halves = (cols + 63) / 64;
-        uint32_t g = 0, u = 0;  // Q tiles; those of this key tile
+        const int chunks = (cols + 31) / 32;
+        uint32_t g = 0, joins = 0;  // Q tiles, segments of more than one
         while (ok && cur.next(pc)) {
-            const int key = pc.jt * kWgKeys + x * kBN + r, keys = pc.rq.z + pc.rq.y;
+            const int key = pc.jt * kWgKeys + x * kBN + r, keys = pc.rq.z + pc.rq.y, n = pc.q1 - pc.q0;
             const bool here = keys > pc.jt * kWgKeys + x * kBN;  // this key tile has keys
-            const int q_first = pc.q_first;
-            const long long slot = key < keys ? key_slot(a, pc.b, key) : -1;
+            const bool last = ((g + n - 1) & 1) == y;            // the segment's last Q tile is this warpgroup's
+            const long long slot = last && key < keys ? key_slot(a, pc.b, key) : -1;
+            const int rel = key - pc.rq.z - (pc.q_first + pc.q0) * a.tq;  // the key's token, counted from the first Q tile's
             uint64_t sum[4] = {0, 0, 0, 0};  // pairs of floats
 #pragma unroll 1
-            for (int qt = pc.q0; qt < pc.q1; ++qt, ++g) {
-                const uint32_t ls = g % NL;
-                if (!here) {
-                    if (!(ok = quick_wait(&lfull[ls], (g / NL) & 1, s_abort, a.wait_limit))) break;
-                    warp_arrive(&lempty[ls]);
-                    continue;
-                }
-                const uint32_t buf = 2 * x + (u & 1);
-                if (!(ok = quick_wait2(&lfull[ls], (g / NL) & 1, &sfull[buf], (u >> 1) & 1, s_abort, a.wait_limit))) break;
+            for (uint32_t t = g + ((g ^ y) & 1); t < g + n; t += 2) {
+                const uint32_t ls = t % NL;
+                if (!(ok = quick_wait2(&lfull[ls], (t / NL) & 1, &sfull[buf], (t >> 1) & 1, s_abort, a.wait_limit))) break;
                 tc_fence_after();
+                const uint32_t nl = smem_u32(smem + S::kLse) + ls * 512;
+                const uint32_t *mask = reinterpret_cast<const uint32_t *>(smem + S::kMask) + ls * 4;
                 // columns from lo on see the key: its token is cached or not later than theirs
-                const int lo = max(0, key - pc.rq.z - (q_first + qt) * a.tq) * a.G;
-                const ulonglong2 *nl = reinterpret_cast<const ulonglong2 *>(smem + S::kLse) + ls * 32;
-                const uint4 mask = reinterpret_cast<const uint4 *>(smem + S::kMask)[ls];
-                const bool open = __all_sync(0xffffffffu, lo == 0 && (mask.x & mask.y & mask.z & mask.w) == 0xffffffffu);
-                if (cols <= 32) {  // single tokens, short chunks
-                    uint32_t va[32];
-                    tmem_ld32(s_tm0 + (u & 1) * 128, va);
+                const int lo = max(0, rel - (int)(t - g) * a.tq) * a.G;
+                const uint4 m = *reinterpret_cast<const uint4 *>(mask);
+                const bool open = __all_sync(0xffffffffu, lo == 0 && (m.x & m.y & m.z & m.w) == 0xffffffffu);
+#pragma unroll 1
+                for (int ch = 0; ch < (here ? chunks : 0); ++ch) {
+                    uint32_t v[32];
+                    tmem_ld32(s_tm + ch * 32, v);
                     tmem_wait_ld();
-                    tmem_regs_ready(va);
+                    tmem_regs_ready(v);
+                    if (ch == chunks - 1) {
+                        tc_fence_before();
+                        warp_arrive(&sempty[buf]);
+                    }
+                    if (!open) {  // by selection: what is hidden may be NaN
+                        const int l = lo - ch * 32;
+                        hide(v, mask[ch] & (l <= 0 ? 0xffffffffu : l >= 32 ? 0u : ~((1u << l) - 1u)));
+                    }
+                    exp_sums(v, c2, nl + ch * 128, sum);
+                }
+                if (!here) {
                     tc_fence_before();
                     warp_arrive(&sempty[buf]);
-                    hide(va, mask.x & (lo <= 0 ? 0xffffffffu : lo >= 32 ? 0u : ~((1u << lo) - 1u)));
-                    exp_sums<32>(va, va, c2, nl, sum);
-                } else {
-#pragma unroll 1
-                    for (int hh = 0; hh < halves; ++hh) {
-                        uint32_t va[32], vb[32];
-                        const uint32_t s_tm = s_tm0 + (u & 1) * 128 + hh * 64;
-                        tmem_ld32(s_tm, va);
-                        tmem_ld32(s_tm + 32, vb);
-                        tmem_wait_ld();
-                        tmem_regs_ready(va);
-                        tmem_regs_ready(vb);
-                        if (hh == halves - 1) {
-                            tc_fence_before();
-                            warp_arrive(&sempty[buf]);
-                        }
-                        if (!open) {  // by selection: what is hidden may be NaN
-                            const int l0 = lo - hh * 64, l1 = l0 - 32;
-                            hide(va, (hh ? mask.z : mask.x) & (l0 <= 0 ? 0xffffffffu : l0 >= 32 ? 0u : ~((1u << l0) - 1u)));
-                            hide(vb, (hh ? mask.w : mask.y) & (l1 <= 0 ? 0xffffffffu : l1 >= 32 ? 0u : ~((1u << l1) - 1u)));
-                        }
-                        exp_sums<64>(va, vb, c2, nl + hh * 16, sum);
-                    }
                 }
                 warp_arrive(&lempty[ls]);
-                ++u;
             }
             if (!ok) break;
-            const float2 t = add2(add2(as_float2(sum[0]), as_float2(sum[1])), add2(as_float2(sum[2]), as_float2(sum[3])));
-            const float total = t.x + t.y;
-            if (key < keys) {
+            g += n;
+            const float2 t2 = add2(add2(as_float2(sum[0]), as_float2(sum[1])), add2(as_float2(sum[2]), as_float2(sum[3])));
+            float total = t2.x + t2.y;
+            if (n > 1) {  // join both warpgroups' sums
+                const uint32_t place = x * kJoins + joins % kJoins;
+                float *other = reinterpret_cast<float *>(smem + S::kJoin) + place * kBN + r;
+                if (!last) {
+                    *other = total;
+                    warp_arrive(&joined[place]);
+                } else {
+                    if (!(ok = quick_wait(&joined[place], (joins / kJoins) & 1, s_abort, a.wait_limit))) break;
+                    total += *other;
+                }
+                ++joins;
+            }
+            if (last && key < keys) {
                 if (pc.slot >= 0) a.part[pc.slot * kWgKeys + x * kBN + r] = total;
                 else if (slot < 0) atomicOr(&a.status[pc.b], RS_ST_BAD_PAGE);
                 else atomicAdd(&a.weights[((long long)pc.kvh * a.n_pages << a.page_log2) + slot], total);  // the key's only one
@@ -585,26 +586,19 @@ int weigh_grid() { return std::min(num_sms(), kAttnMaxGrid); }
 
 template <int D, bool BF16>
 rs_status weigh_launch(const WeighArgs &a, const CUtensorMap &tmq, const CUtensorMap &tmk, const char *what, cudaStream_t st) {
-    // per device: 0 not asked, 1 ready, -1 too few registers for the warpgroups' split
-    static std::atomic<int> ready[64];
+    static std::atomic<bool> ready[64];  // per device
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
         set_error("%s: no current device", what);
         return RS_ERR_CUDA;
     }
-    if (ready[dev].load() == 0) {
-        cudaFuncAttributes fa;
-        const cudaError_t e1 = cudaFuncGetAttributes(&fa, weigh_kernel<D, BF16>);
-        const cudaError_t e2 = cudaFuncSetAttribute(weigh_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, WgSmem<D>::kTotal);
-        if (e1 != cudaSuccess || e2 != cudaSuccess) {
-            set_error("%s: kernel attributes: %s", what, cudaGetErrorString(e1 != cudaSuccess ? e1 : e2));
+    if (!ready[dev].load()) {
+        const cudaError_t e = cudaFuncSetAttribute(weigh_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, WgSmem<D>::kTotal);
+        if (e != cudaSuccess) {
+            set_error("%s: kernel attributes: %s", what, cudaGetErrorString(e));
             return RS_ERR_CUDA;
         }
-        ready[dev].store(fa.numRegs * kWgThreads >= (int)(2 * 128 * kWgRegsSum + 128 * kWgRegsCopy) ? 1 : -1);
-    }
-    if (ready[dev].load() != 1) {
-        set_error("%s: kernel built with too few registers per thread", what);
-        return RS_ERR_CUDA;
+        ready[dev].store(true);
     }
     launch_pdl(weigh_plan, dim3(1), dim3(1024), 0, st, a);
     RS_CHECK_LAUNCH(what);
