@@ -433,7 +433,7 @@ rs_status rs_tree_sample(const float *logits, int R, int V, const int32_t *node_
  *            with its own distance between rows in elements (q_stride,
  *            k_stride, v_stride: at least heads x D, multiples of 8), so that
  *            they may be parts of one projection's rows; 16-byte aligned.
- *   seq_off  [B+1] int32; sequences may have no rows; B <= 4096.
+ *   seq_off  [B+1] int32; sequences may have no rows; B <= 4096, T <= 2^30.
  *   D in {64, 128}; Hq a multiple of Hkv, at most 128 times (query head h
  *   reads KV head h / (Hq / Hkv)); scale > 0.
  *   out      [T, Hq, D] of type dtype, 32-byte aligned;  lse [T, Hq] fp32;
@@ -476,7 +476,7 @@ rs_status rs_prompt_attn(const uint16_t *q, int64_t q_stride, const uint16_t *k,
  * of its pages, with weight 0 and position pos[row] (the slot number where
  * pos is NULL).
  *   k, v     [T, Hkv, D], k_stride / v_stride elements from row to row (at
- *            least Hkv x D, multiples of 8; 16-byte aligned).
+ *            least Hkv x D, multiples of 8; 16-byte aligned); T <= 2^30.
  *   new_off  [B+1] int32 (one that decreases anywhere rejects every request);
  *            ctx_len [B] int32: tokens cached before.
  *   weights, positions: NULL where the cache keeps none.
@@ -504,7 +504,7 @@ rs_status rs_paged_append(const uint16_t *k, int64_t k_stride, const uint16_t *v
  *   status   [B]: RS_ST_BAD_OFFSET, RS_ST_BAD_PAGE, RS_ST_BAD_TREE,
  *            RS_ST_TOO_LARGE (the request's rows are zeroed; those of a range
  *            that rs_prompt_attn rejects are left), RS_ST_TIMEOUT.
- * Types, arithmetic, B, head counts, alignment: as for rs_prompt_attn.  What
+ * Types, arithmetic, B, T, head counts, alignment: as for rs_prompt_attn.  What
  * slots behind a request's last token hold (NaN too) does not matter.
  */
 size_t rs_paged_attn_workspace_size(int B, int T, int Hq, int Hkv, int D);

@@ -101,6 +101,8 @@ extern "C" rs_status rs_paged_append(const uint16_t *k, int64_t k_stride, const 
     clear_error();
     const char *what = "rs_paged_append";
     RS_CHECK_ARG(B >= 0 && T >= 0, "%s: negative size", what);
+    RS_CHECK_ARG(T <= 1 << 30, "%s: T=%d above 2^30", what, T);  // a warp's next token stays an int
+    RS_CHECK_ARG(B <= 1 << 30, "%s: B=%d above 2^30", what, B);
     if (D != 64 && D != 128) {
         set_error("%s: head dim %d unsupported (64 or 128)", what, D);
         return RS_ERR_UNSUPPORTED;

@@ -82,7 +82,8 @@ def test_other_refusals(rs):
         ("rs_paged_attn", dict(out=P + 16), INVALID, "32-byte"), ("rs_paged_attn", dict(vp=None), INVALID, "null page"),
         ("rs_paged_attn", dict(ctx=None), INVALID, "null request"), ("rs_paged_append", dict(k_stride=8), INVALID, "rows of k and v"),
         ("rs_paged_append", dict(v=None), INVALID, "null row"), ("rs_paged_append", dict(Hkv=0), INVALID, "Hkv=0"),
-        ("rs_paged_append", dict(v=P + 4), INVALID, "aligned"), ("rs_paged_weights", dict(weights=None), INVALID, "null page"),
+        ("rs_paged_append", dict(v=P + 4), INVALID, "aligned"), ("rs_paged_append", dict(T=(1 << 30) + 1), INVALID, "2^30"),
+        ("rs_paged_append", dict(B=(1 << 30) + 1), INVALID, "2^30"), ("rs_paged_weights", dict(weights=None), INVALID, "null page"),
         ("rs_paged_evict", dict(budget=0), INVALID, "budget=0"), ("rs_paged_evict", dict(recent=9), INVALID, "recent=9"),
         ("rs_paged_evict", dict(recent=-1), INVALID, "recent=-1"), ("rs_paged_evict", dict(positions=None), INVALID, "null page"),
         ("rs_paged_evict", dict(B=4096, Hkv=16), INVALID, "65535"), ("rs_paged_evict", dict(nxt=None), INVALID, "null request"),
