@@ -3,7 +3,8 @@
 ``PagedCache`` holds the pages, the page table and, where eviction is wanted, every key's accumulated weight and position.
 A program appends the new tokens' keys and values, attends with their queries, and then says how many of them stay
 (``advance``); what was appended behind them is written over by the next ``append``.  ``prompt_attention`` is the pass over
-whole prompts that comes before.
+whole prompts that comes before.  ``append``, ``attend`` and ``weigh`` may be captured into a CUDA graph; the others copy from
+the host.
 """
 import torch
 
@@ -12,22 +13,43 @@ from . import respec as rs
 _CODES = {torch.bfloat16: rs.RS_BF16, torch.float16: rs.RS_F16}
 
 
-def _scratch(held, need, device):
-    """A buffer of at least `need` bytes: the one held where it is large enough."""
-    if held is None or held.numel() < need:
-        held = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
-    return held
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _heads(name, x, heads, D, dtype):
+    """x is [rows, heads, D] of the type; heads None: any number."""
+    _need(x.dim() == 3 and x.shape[2] == D and heads in (None, x.shape[1]) and x.dtype == dtype,
+          "%s: [rows, %s, %d] of %s expected, not %s of %s" % (name, heads or "heads", D, dtype, list(x.shape), x.dtype))
+
+
+def _ints(name, x, n):
+    _need(x.dtype == torch.int32 and x.dim() == 1 and x.numel() == n, "%s: %d values of int32 expected, not %s of %s"
+          % (name, n, list(x.shape), x.dtype))
+
+
+def _scratch(need, device):
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
 
 
 def prompt_attention(q, k, v, seq_off, scale, workspace=None):
     """Causal attention of packed prompts (rs_prompt_attn): q [T, Hq, D], k and v [T, Hkv, D] (rows may be parts of wider
-    ones), seq_off [B+1] int32 on the device.  Returns (out, lse, status, workspace)."""
+    ones), seq_off [B+1] int32 on the device.  Returns (out, lse, status, workspace); a workspace that is handed in again is used
+    where it is large enough."""
+    _need(q.dtype in _CODES and q.dim() == 3, "q: [rows, heads, D] of bfloat16 or float16 expected")
     T, Hq, D = q.shape
+    for name, x in (("k", k), ("v", v)):
+        _heads(name, x, k.shape[1] if x is v else None, D, q.dtype)
+        _need(x.shape[0] == T, "%s: %d rows expected, not %d" % (name, T, x.shape[0]))
     Hkv, B, dev = k.shape[1], seq_off.numel() - 1, q.device
+    _ints("seq_off", seq_off, B + 1)
     out = torch.empty((T, Hq, D), dtype=q.dtype, device=dev)
     lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
     status = torch.empty(B, dtype=torch.int32, device=dev)
-    workspace = _scratch(workspace, rs.rs_prompt_attn_workspace_size(B, T, Hq, Hkv, D), dev)
+    need = rs.rs_prompt_attn_workspace_size(B, T, Hq, Hkv, D)
+    if workspace is None or workspace.numel() < need:
+        workspace = _scratch(need, dev)
     rs.rs_prompt_attn(q, q.stride(0), k, k.stride(0), v, v.stride(0), _CODES[q.dtype], seq_off, B, T, Hq, Hkv, D, scale, out, lse,
                       status, workspace)
     return out, lse, status, workspace
@@ -50,32 +72,46 @@ class PagedCache:
         self.weights = z(Hkv, slots, dt=torch.float32) if track_weights else None
         self.positions = z(Hkv, slots, dt=torch.int32) if track_weights else None
         self.status = z(B, dt=torch.int32)
-        self._ws = None
 
     def _pages(self):
         return self.n_pages, self.page_size, self.table, self.max_pages
 
     def append(self, k, v, new_off, pos=None):
         """Keys and values [T, Hkv, D] of new tokens behind the cached ones; pos [T] their positions."""
-        rs.rs_paged_append(k, k.stride(0), v, v.stride(0), pos, new_off, self.B, k.shape[0], self.Hkv, self.D, self.k, self.v,
+        T = k.shape[0]
+        for name, x in (("k", k), ("v", v)):
+            _heads(name, x, self.Hkv, self.D, self.dtype)
+        _need(v.shape[0] == T, "v: %d rows expected, not %d" % (T, v.shape[0]))
+        _ints("new_off", new_off, self.B + 1)
+        if pos is not None:
+            _ints("pos", pos, T)
+        rs.rs_paged_append(k, k.stride(0), v, v.stride(0), pos, new_off, self.B, T, self.Hkv, self.D, self.k, self.v,
                            *self._pages(), self.length, self.weights, self.positions, self.status)
 
     def attend(self, q, new_off, scale, parents=None):
         """Attention of the appended tokens' queries [T, Hq, D]: (out, lse)."""
+        _heads("q", q, None, self.D, self.dtype)
         T, Hq, D = q.shape
+        _ints("new_off", new_off, self.B + 1)
+        if parents is not None:
+            _ints("parents", parents, T)
         out = torch.empty((T, Hq, D), dtype=q.dtype, device=self.device)
         lse = torch.empty((T, Hq), dtype=torch.float32, device=self.device)
-        self._ws = _scratch(self._ws, rs.rs_paged_attn_workspace_size(self.B, T, Hq, self.Hkv, D), self.device)
+        ws = _scratch(rs.rs_paged_attn_workspace_size(self.B, T, Hq, self.Hkv, D), self.device)
         rs.rs_paged_attn(q, q.stride(0), _CODES[q.dtype], new_off, parents, self.B, T, Hq, self.Hkv, D, self.k, self.v, *self._pages(),
-                         self.length, scale, out, lse, self.status, self._ws)
+                         self.length, scale, out, lse, self.status, ws)
         return out, lse
 
     def weigh(self, q, lse, new_off, scale):
         """Adds the weight that rows q [T, Hq, D] (causal, behind the cached tokens) give to every key they see."""
+        _heads("q", q, None, self.D, self.dtype)
         T, Hq, D = q.shape
-        self._ws = _scratch(self._ws, rs.rs_paged_weights_workspace_size(self.B, T, Hq, self.Hkv, D), self.device)
+        _need(lse.shape == (T, Hq) and lse.dtype == torch.float32, "lse: [%d, %d] of float32 expected" % (T, Hq))
+        _ints("new_off", new_off, self.B + 1)
+        self._tracked()
+        ws = _scratch(rs.rs_paged_weights_workspace_size(self.B, T, Hq, self.Hkv, D), self.device)
         rs.rs_paged_weights(q, q.stride(0), _CODES[q.dtype], lse, new_off, self.B, T, Hq, self.Hkv, D, self.k, *self._pages(),
-                            self.length, scale, self.weights, self.status, self._ws)
+                            self.length, scale, self.weights, self.status, ws)
 
     def rows(self, b, slots):
         """Pool rows of request b's slots (a device index tensor)."""
@@ -93,16 +129,23 @@ class PagedCache:
 
     def advance(self, counts):
         """The first counts[b] of the appended tokens stay."""
+        _need(len(counts) == self.B and all(c >= 0 and n + c <= self.max_pages * self.page_size for n, c in zip(self.lengths, counts)),
+              "counts: a number of tokens for each of %d requests, %d cached ones at most" % (self.B, self.max_pages * self.page_size))
         self._set([n + c for n, c in zip(self.lengths, counts)])
 
     def evict(self, next_pos, budget, recent):
         """Cuts every request to `budget` tokens per head; next_pos[b]: tokens that request b has seen."""
-        self._ws = _scratch(self._ws, rs.rs_paged_evict_workspace_size(self.B, self.Hkv, budget), self.device)
+        _need(len(next_pos) == self.B, "next_pos: a position for each of %d requests" % self.B)
+        self._tracked()
+        ws = _scratch(rs.rs_paged_evict_workspace_size(self.B, self.Hkv, budget), self.device)
         new = torch.empty_like(self.length)
         nxt = torch.tensor(next_pos, dtype=torch.int32, device=self.device)
         rs.rs_paged_evict(self.k, self.v, self.Hkv, self.D, *self._pages(), self.length, nxt, self.B, budget, recent, self.weights,
-                          self.positions, new, self.status, self._ws)
+                          self.positions, new, self.status, ws)
         self._set([min(n, budget) for n in self.lengths])
+
+    def _tracked(self):
+        _need(self.weights is not None, "a cache made with track_weights=True expected")
 
     def _set(self, lengths):
         self.lengths = list(lengths)

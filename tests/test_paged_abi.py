@@ -122,3 +122,29 @@ def test_rows_of_the_binding(rs):
         rs.rs_prompt_attn(torch.zeros(8, 4, 128, dtype=torch.bfloat16), *args[1:])
     with pytest.raises(C.ArgumentError):
         rs.rs_prompt_attn(*[1.5 if i == 1 else a for i, a in enumerate(args)])
+
+
+def test_refusals_of_the_cache():
+    """Tensors that do not fit the cache are refused before the library sees their addresses."""
+    from paper_2511_01282_gb300.paged import PagedCache, prompt_attention
+    c = PagedCache(2, 40, 16, 2, 64, device="cpu")
+    x = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)  # noqa: E731
+    off, off3 = x(3, dt=torch.int32), x(4, dt=torch.int32)
+    q, k, lse = x(5, 4, 64), x(5, 2, 64), x(5, 4, dt=torch.float32)
+    for f, word in [
+        (lambda: c.append(x(5, 2, 64, dt=torch.float16), k, off), "k:"), (lambda: c.append(k, x(5, 4, 64), off), "v:"),
+        (lambda: c.append(k, x(4, 2, 64), off), "v: 5 rows"), (lambda: c.append(x(5, 2, 128), k, off), "k:"),
+        (lambda: c.append(k, k, off3), "new_off"), (lambda: c.append(k, k, off.long()), "new_off"),
+        (lambda: c.append(k, k, off, x(4, dt=torch.int32)), "pos"), (lambda: c.attend(q.half(), off, 0.1), "q:"),
+        (lambda: c.attend(x(5, 4, 128), off, 0.1), "q:"), (lambda: c.attend(q, off, 0.1, x(6, dt=torch.int32)), "parents"),
+        (lambda: c.attend(q, off3, 0.1), "new_off"), (lambda: c.weigh(q, lse[:, :2], off, 0.1), "lse"),
+        (lambda: c.weigh(q, lse, off, 0.1), "track_weights"), (lambda: c.evict([1, 1], 8, 0), "track_weights"),
+        (lambda: c.evict([1], 8, 0), "next_pos"), (lambda: c.advance([1]), "counts"), (lambda: c.advance([0, -1]), "counts"),
+        (lambda: c.advance([49, 0]), "counts"), (lambda: prompt_attention(q, k.half(), k, off, 0.1), "k:"),
+        (lambda: prompt_attention(q, k, x(5, 4, 64), off, 0.1), "v:"), (lambda: prompt_attention(q, k[:4], k[:4], off, 0.1), "k: 5 rows"),
+        (lambda: prompt_attention(q, k, k, off.long(), 0.1), "seq_off"), (lambda: prompt_attention(q.float(), k, k, off, 0.1), "q:"),
+    ]:
+        with pytest.raises(ValueError, match=word):
+            f()
+    c.advance([48, 0])
+    assert c.lengths == [48, 0] and c.length.tolist() == [48, 0]
