@@ -237,6 +237,8 @@ class SpecLoop:
         # cache: "flat" (one row per token) or "paged", there with a budget of
         # tokens per KV head (None: nothing is evicted), the `recent` newest kept
         assert cache in ("flat", "paged") and (budget is None or cache == "paged")
+        if budget is not None and not 0 <= recent <= budget:
+            raise ValueError("recent=%d out of range (0 to the budget of %d tokens)" % (recent, budget))
         # with trace, every step appends host copies of each call's inputs and
         # outputs to self.trace (for checking a run call by call)
         self.trace = [] if trace else None
@@ -445,7 +447,9 @@ def main():
     args = ap.parse_args()
     if args.budget is not None and not args.paged:
         ap.error("--budget needs --paged")
-    cache = dict(cache="paged", budget=args.budget) if args.paged else {}
+    if args.budget is not None and args.budget < 1:
+        ap.error("--budget must be at least 1")
+    cache = dict(cache="paged", budget=args.budget, recent=min(64, args.budget or 64)) if args.paged else {}
     taus, ms = ([0.0, 1.0, 2.0, 3.0], [1, 2, 3]) if args.sweep else ([3.0], [2])
     for tau in taus:
         for m in ms:

@@ -87,3 +87,40 @@ def test_paged_cache_of_several_requests():
     assert c.lengths == [10, 7] and c.length.tolist() == [10, 7]
     pos = c.positions[:, c.rows(0, torch.arange(10, device="cuda"))]
     assert all(set(range(36, 40)) <= set(p) for p in pos.tolist())
+
+
+def test_captured_cache_calls_keep_their_scratch():
+    """A graph of a cache's calls is replayed after larger eager calls of the same cache, their memory in use again."""
+    from paper_2511_01282_gb300.paged import PagedCache
+    dt, Hq, Hkv, D = torch.bfloat16, 8, 2, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows = lambda n: torch.randn(n, Hq + 2 * Hkv, D, generator=g, device="cuda").to(dt)  # noqa: E731
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    c = PagedCache(2, 1024, 16, Hkv, D, dtype=dt, track_weights=True)
+    first, off = rows(600), i32(0, 400, 600)
+    c.append(first[:, Hq:Hq + Hkv], first[:, Hq + Hkv:], off)
+    c.advance([400, 200])
+    x, small = rows(2), i32(0, 1, 2)
+
+    def step():
+        c.append(x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], small)
+        out, lse = c.attend(x[:, :Hq], small, 0.09)
+        c.weigh(x[:, :Hq], lse, small, 0.09)
+        return out, lse
+
+    step()
+    weights = c.weights.clone()
+    c.weights.zero_()
+    want = [t.clone() for t in step()] + [c.weights.clone()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    big, big_off = rows(700), i32(0, 500, 700)
+    c.append(big[:, Hq:Hq + Hkv], big[:, Hq + Hkv:], big_off)
+    c.attend(big[:, :Hq], big_off, 0.09)
+    filler = [torch.full((1 << n,), 77, dtype=torch.uint8, device="cuda") for n in range(12, 27)]
+    c.weights.copy_(0 * weights)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(c.weights, want[2])
+    assert all(bool((f == 77).all()) for f in filler)

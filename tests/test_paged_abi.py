@@ -148,3 +148,10 @@ def test_refusals_of_the_cache():
             f()
     c.advance([48, 0])
     assert c.lengths == [48, 0] and c.length.tolist() == [48, 0]
+
+
+def test_refusals_of_the_loop():
+    from paper_2511_01282_gb300.e2e import SpecLoop
+    for budget, recent in ((32, 64), (8, -1)):
+        with pytest.raises(ValueError, match="recent=%d" % recent):
+            SpecLoop(None, None, None, None, cache="paged", budget=budget, recent=recent)
