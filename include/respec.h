@@ -10,6 +10,11 @@
  *   rs_tree_verify_attn tree attention of the verify pass   (Alg. 1 verification)
  *   rs_accept           Section 3.4 verification, Eq. 4-5  (Alg. 1 verify + EMA)
  *
+ * Around it: retrieval from an index (rs_match_index_*, rs_match_scan_indexed),
+ * sampling verification (rs_tree_sample), and the cache: whole prompts
+ * (rs_prompt_attn), a paged KV cache (rs_paged_append, rs_paged_attn) and its
+ * bound by attention weight (rs_paged_weights, rs_paged_evict).
+ *
  * General rules (every entry point):
  *   - All array arguments are DEVICE pointers owned by the caller, unless a
  *     comment says otherwise.  The library allocates nothing: scratch space
@@ -29,7 +34,7 @@
  *     0 when the request is fine) and the request's decision outputs are set
  *     to their empty values.
  *   - Offsets arrays are prefix sums with B+1 entries (offset[0] = 0).
- *   - bf16 tensors are passed as uint16_t bit patterns.
+ *   - bf16 and fp16 tensors are passed as uint16_t bit patterns.
  *   - Thread safety: calls are re-entrant; rs_last_error() is per thread.
  */
 #ifndef RESPEC_H

@@ -609,9 +609,9 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                     return true;
                 }
                 const uint32_t s_tm = s_tm0, p_tm = p_tm0;
-                // the row's maximum; 64 keys at a time, here and below, in loops that
-                // are not unrolled: tensor memory is read again at little cost, and the
-                // loop stays small enough for the instruction cache
+                // the row's maximum; 64 keys at a time, here and below: tensor memory is
+                // read again at little cost, and the exponentials' loop, which is not
+                // unrolled, stays small enough for the instruction cache
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
