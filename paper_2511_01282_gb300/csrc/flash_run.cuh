@@ -30,6 +30,7 @@ flash_combine(FlashArgs a) {
     const int4 *bound = a.bound + f * (a.grid + 1);
     const int c = min((int)blockIdx.x + 1, a.grid);
     const int4 start = bound[c], before = bound[c - 1];
+    const int4 p0 = bound[min(c - 1 + lane, a.grid)], q0 = bound[min(c + lane, a.grid)];
     const int blocks = gridDim.x * gridDim.y;
     for (int b = blockIdx.y * gridDim.x + blockIdx.x; b < a.B; b += blocks) {
         if (!(a.status[b] & ~RS_ST_TIMEOUT)) continue;
@@ -45,7 +46,7 @@ flash_combine(FlashArgs a) {
     const int x = y * kFlCombRows / kBM;  // row tile of the block's rows
     const int first = (e.y * 2 + x) * a.tq, r0 = y * kFlCombRows - x * kBM;
     if (r0 / a.G >= a.tq || first + r0 / a.G >= e.w) return;
-    if (a.status[e.x] & ~RS_ST_TIMEOUT) return;
+    const int bad = a.status[e.x] & ~RS_ST_TIMEOUT;
     const int kvh = f * a.Hkv / phases + start.x;
     constexpr int kC = D / 32;  // columns of a lane
 #pragma unroll 1
@@ -57,7 +58,11 @@ flash_combine(FlashArgs a) {
 #pragma unroll 1
         for (int c0 = c - 1;; c0 += 32) {  // 32 shares at a time; the first piece is the end of share c - 1
             const int c1 = c0 + lane;
-            const int4 p = bound[min(c1, a.grid)], q = bound[min(c1 + 1, a.grid)];
+            int4 p = p0, q = q0;
+            if (c0 >= c) {
+                p = bound[min(c1, a.grid)];
+                q = bound[min(c1 + 1, a.grid)];
+            }
             const bool head = c1 == c - 1;
             const bool in = head || (c1 < a.grid && same(p)), have = head || (in && !(same(q) && q.z == p.z));  // not an empty share
             const long long at = (long long)(2 * (f * a.grid + c1) + (head ? 1 : 0)) * kFlRows + row;
@@ -85,6 +90,7 @@ flash_combine(FlashArgs a) {
             }
             if (!__all_sync(0xffffffffu, in)) break;
         }
+        if (bad) break;
         const float fr = L > 0.f ? 1.f / L : L;  // no key with weight: 0; NaN stays
         const long long orow = (long long)(e.z + tok) * a.Hq + kvh * a.G + (r - t * a.G);
         uint32_t *d = reinterpret_cast<uint32_t *>(a.out + orow * D + lane * kC);
