@@ -6,9 +6,11 @@
 // slots behind the budget then move into the holes below it, both in ascending
 // order: the holes and the movers are disjoint, so all moves are independent,
 // and tokens that already lie below the budget are not touched.
-// Launches: evict_select (a CTA per (request, head): the list of moves) ->
-// evict_move.
-// Bound: weights and positions read once, the movers' rows read and written.
+// Launches: evict_select (a CTA or a cluster per (request, head): the list of
+// moves) -> evict_move.
+// Bound: weights and positions read once, the movers' rows read and written (4
+// caches of 32768 tokens to 4096, 8 heads, D = 128: select 24 us, a chain of passes
+// and barriers; move 24; 50 in a graph.  16 of 2112 to 2048: 16 us).
 #include <algorithm>
 #include <atomic>
 

@@ -23,7 +23,15 @@
 // what is cached and decides).  A segment cut by a share's end leaves partial (O, m, l),
 // which flash_combine joins in key order: no atomics, the same bits each run.
 //
-// Warps: 0 and 1 MMA issue for row tiles A and B, 2 and 3 TMA (K and Q, V), 4-7 softmax of tile A (thread = row), 8-11 of tile B.  Tensor memory (512 columns):
+// Bound: long prompts at D = 128, the tensor cores (16384 tokens, 32 heads on 8: 1.48
+// ms, 1480 TFLOP/s); at D = 64, whose products are half as long, the softmax warps
+// (issue slots 52 % full, each warp's chain of wait, maximum, exponentials and store;
+// 16 prompts of up to 4095 tokens: 522 us, 725 TFLOP/s, a tenth of it segments'
+// starts); single tokens, HBM (64 requests, 1.21 GB: 187 us, 6.5 TB/s); those of one
+// request, the latency of three launches (2048 keys: 19 us).
+//
+// Warps: 0 and 1 MMA issue for row tiles A and B, 2 and 3 TMA (K and Q, V), 4-7
+// softmax of tile A (thread = row), 8-11 of tile B.  Tensor memory (512 columns):
 //   D = 64: O_A O_B (64 each), S_A S_B (128 each), P_A P_B (64 each).  S of the
 //     next key tile is issued as soon as its softmax has read the last one, so
 //     that a softmax finds its next S ready and the exponentials bound the loop.

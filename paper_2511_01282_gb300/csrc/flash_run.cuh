@@ -18,7 +18,9 @@ namespace rs {
 // It also empties the rows of rejected requests (after the pieces' writers).
 // Bound: latency, of a handful of dependent loads and of the instructions, which
 // are fetched anew for every launch: the loop over the rows is not unrolled (four
-// rows at once in 600 instructions took 8 us for single tokens, this 6).
+// rows at once in 600 instructions took 8 us for single tokens, this 6), and the
+// bounds and the status are read before they are needed (one request's single
+// token as a whole 21.2 -> 19.4 us).
 constexpr int kFlCombThreads = 256;
 
 template <int D, bool BF16>
