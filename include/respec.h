@@ -532,7 +532,8 @@ rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtype, const in
  *   lse      [T, Hq] fp32;  weights [Hkv, n_pages * page_size] fp32 in/out.
  *   status   [B]: RS_ST_BAD_OFFSET (nothing of the request is added),
  *            RS_ST_BAD_PAGE (nothing is added in bad pages), RS_ST_TIMEOUT.
- * Sums are fp32, in a fixed order.
+ * Sums are fp32, in a fixed order; where requests share a page its weights gain
+ * what each of them gives, one after the other in no fixed order.
  */
 size_t rs_paged_weights_workspace_size(int B, int T, int Hq, int Hkv, int D);
 rs_status rs_paged_weights(const uint16_t *q, int64_t q_stride, int dtype, const float *lse,

@@ -170,3 +170,37 @@ def test_prompt_to_eviction_and_on():
             check(out[b:b + 1], o, o_tol, "out")
             check(lse[b:b + 1], z, z_tol, "lse")
         assert weigh(one[:, :Hq], code, lse, [0, 1, 2, 3], kp, page, table, ctx, scale, w).tolist() == [0] * B
+
+
+@pytest.mark.parametrize("n,ctx,D,t", [([64, 90, 33], [20000, 15001, 9000], 64, "f16"), ([50, 1, 70, 200], [12000, 9000, 14000, 100], 128, "bf16")])
+def test_weights_of_many_segments(n, ctx, D, t):
+    """Far more segments than CTAs, of one, two and more Q tiles."""
+    test_weights(n, ctx, 32, 8, D, t, 64)
+
+
+def test_requests_share_a_prefix():
+    """Three requests read one prefix's pages; what they append is their own, and the prefix gains all their weight."""
+    page, P, Hq, Hkv, D, t = 16, 320, 8, 2, 128, "bf16"
+    dt, code = DT[t]
+    n, ctx, scale = [1, 40, 3], [P, P, P + 5], D ** -0.5
+    pages, most, table, kp, vp = _pool(n, ctx, page, Hkv, D, dt, 3)
+    table[1:, :P // page] = table[0, :P // page]
+    S, off = pages * page, _off(n)
+    q, k, v = _normal(1, off[-1], Hq, D, dtype=dt), _normal(2, S, Hkv, D, dtype=dt), _normal(3, S, Hkv, D, dtype=dt)
+    kp.view(S, Hkv, D).copy_(k)
+    vp.view(S, Hkv, D).copy_(v)
+    out, lse, status = run_paged(q, code, off, None, kp, vp, page, table, ctx, scale)
+    w = torch.zeros(Hkv, S, device="cuda")
+    want, tol = torch.zeros(Hkv, S, dtype=torch.float64, device="cuda"), torch.zeros(Hkv, S, dtype=torch.float64, device="cuda")
+    for b in range(3):
+        a, e, see = off[b], off[b + 1], causal_mask(n[b], ctx[b])
+        at = slots(table, b, ctx[b] + n[b], page)
+        o, z, o_tol, z_tol = attention(q[a:e], k[at], v[at], see, scale)
+        check(out[a:e], o, o_tol, "out")
+        check(lse[a:e], z, z_tol, "lse")
+        got, t_b = ref_weights(q[a:e], k[at], lse[a:e], see, scale)
+        want[:, at] += got
+        tol[:, at] += t_b + 2.0 ** -23 * want[:, at]  # one more addition for each request
+    assert status.tolist() == [0] * 3
+    assert weigh(q, code, lse, off, kp, page, table, ctx, scale, w).tolist() == [0] * 3
+    check(w, want, tol, "weights")
