@@ -241,8 +241,9 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     const double bytes = 4.0 * (double)kv_rows * a.Hkv * D;
     a.kv_stream = bytes > 0.5 * (double)l2_bytes();
     a.max_phases = bytes > 1.5 * (double)l2_bytes() ? max_phases(a.B, a.T, a.Hkv, a.tq) : 1;
-    // a segment has no more rows than the call's tokens fill
-    a.comb_blocks = (a.T > a.tq ? kFlRows : std::max(a.T, 1) * a.G + kFlCombRows - 1) / kFlCombRows;
+    // rows of a segment, by the average request, and how many of them a block of eight warps joins
+    const int rows = std::min((a.T + a.B - 1) / a.B, 2 * a.tq) * a.G, each = 8 * ((long long)a.T * a.Hq <= 4096 ? 1 : 4);
+    a.comb_blocks = std::max((rows + each - 1) / each, 1);
     const int box = a.page_table ? std::min(1 << a.page_log2, kBN) : kBN;
     CUtensorMap tmq, tmk, tmv;
     if (!rows_map(&tmq, q, type, D, a.Hq, a.T, q_stride, a.G, a.tq) ||

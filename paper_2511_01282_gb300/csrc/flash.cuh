@@ -56,7 +56,6 @@ constexpr uint32_t kFlRegsSoft = 224, kFlRegsProd = 56;
 static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "register split");
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
 constexpr int kFlRows = 2 * kBM;  // rows of a segment and of a partial slot
-constexpr int kFlCombRows = 32;   // of them for a block of flash_combine
 // What a CTA's time goes to, in eighths of a key tile of a pair: a key tile where
 // only the first row tile has rows, and a segment's start (the first copies and
 // products, the epilogue).  Fitted to every CTA's cycles over packed prompts, chunks

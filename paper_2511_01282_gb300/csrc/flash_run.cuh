@@ -11,16 +11,19 @@
 namespace rs {
 
 // flash_combine: joins the pieces of the segments that the shares' ends cut.
-// Block (c, y) looks at where CTA c + 1's share of a phase starts; if that is
-// inside a segment, and the first cut of it, the block joins 32 of its rows,
-// a row to a warp at a time, its lanes the pieces' (m, l) first and then the columns:
+// Block (c, y) looks at where CTA c + 1's share of each phase starts; if that is
+// inside a segment, and the first cut of it, the block joins every gridDim.y-th
+// eight of its rows, a row to a warp, its lanes the pieces' (m, l) first and then
+// the columns:
 //     M = max m_p, L = sum 2^(m_p - M) l_p, O = sum 2^(m_p - M) O_p / L
 // It also empties the rows of rejected requests (after the pieces' writers).
 // Bound: latency, of a handful of dependent loads and of the instructions, which
 // are fetched anew for every launch: the loop over the rows is not unrolled (four
 // rows at once in 600 instructions took 8 us for single tokens, this 6), and the
 // bounds and the status are read before they are needed (one request's single
-// token as a whole 21.2 -> 19.4 us).
+// token as a whole 21.2 -> 19.4 us).  With few rows in all a warp takes one of a
+// segment (a tree of 65 nodes 34 -> 27 us), else four (16 such trees 124 us, with
+// one 136), by the average request: single tokens have a block, not eight.
 constexpr int kFlCombThreads = 256;
 
 template <int D, bool BF16>
@@ -28,11 +31,8 @@ __global__ void __launch_bounds__(kFlCombThreads)
 flash_combine(FlashArgs a) {
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int phases = a.n_pairs[2], f = blockIdx.y / a.comb_blocks, y = blockIdx.y % a.comb_blocks;
-    const int4 *bound = a.bound + f * (a.grid + 1);
+    constexpr int kWarps = kFlCombThreads / 32;
     const int c = min((int)blockIdx.x + 1, a.grid);
-    const int4 start = bound[c], before = bound[c - 1];
-    const int4 p0 = bound[min(c - 1 + lane, a.grid)], q0 = bound[min(c + lane, a.grid)];
     const int blocks = gridDim.x * gridDim.y;
     for (int b = blockIdx.y * gridDim.x + blockIdx.x; b < a.B; b += blocks) {
         if (!(a.status[b] & ~RS_ST_TIMEOUT)) continue;
@@ -42,65 +42,70 @@ flash_combine(FlashArgs a) {
         for (long long i = threadIdx.x; i < rows * (D / 8); i += kFlCombThreads) o[i] = make_uint4(0, 0, 0, 0);
         for (long long i = threadIdx.x; i < rows; i += kFlCombThreads) a.lse[(long long)rq.x * a.Hq + i] = 0.f;
     }
-    auto same = [&](int4 r) { return r.x == start.x && r.y == start.y && r.z > 0; };
-    if (f >= phases || c >= a.grid || start.z == 0 || same(before)) return;  // between segments, or not the first cut
-    const int4 e = a.ent[start.y];  // request, pair, first row, rows
-    const int x = y * kFlCombRows / kBM;  // row tile of the block's rows
-    const int first = (e.y * 2 + x) * a.tq, r0 = y * kFlCombRows - x * kBM;
-    if (r0 / a.G >= a.tq || first + r0 / a.G >= e.w) return;
-    const int bad = a.status[e.x] & ~RS_ST_TIMEOUT;
-    const int kvh = f * a.Hkv / phases + start.x;
-    constexpr int kC = D / 32;  // columns of a lane
+    if (c >= a.grid) return;
 #pragma unroll 1
-    for (int k = warp; k < kFlCombRows; k += kFlCombThreads / 32) {
-        const int r = r0 + k, t = r / a.G, tok = first + t;
-        if (t >= a.tq || tok >= e.w) break;
-        const long long row = x * kBM + r;
-        float M = -INFINITY, L = 0.f, acc[kC] = {};
+    for (int f = 0; f < a.max_phases && (f == 0 || f < a.n_pairs[2]); ++f) {
+        const int4 *bound = a.bound + f * (a.grid + 1);
+        const int4 start = bound[c], before = bound[c - 1];
+        const int4 p0 = bound[min(c - 1 + lane, a.grid)], q0 = bound[min(c + lane, a.grid)];
+        auto same = [&](int4 r) { return r.x == start.x && r.y == start.y && r.z > 0; };
+        if (start.z == 0 || same(before)) continue;  // between segments, or not the first cut
+        const int4 e = a.ent[start.y];  // request, pair, first row, rows
+        const int bad = a.status[e.x] & ~RS_ST_TIMEOUT;
+        const int kvh = (f > 0 ? f * a.Hkv / a.n_pairs[2] : 0) + start.x;
+        constexpr int kC = D / 32;  // columns of a lane
 #pragma unroll 1
-        for (int c0 = c - 1;; c0 += 32) {  // 32 shares at a time; the first piece is the end of share c - 1
-            const int c1 = c0 + lane;
-            int4 p = p0, q = q0;
-            if (c0 >= c) {
-                p = bound[min(c1, a.grid)];
-                q = bound[min(c1 + 1, a.grid)];
-            }
-            const bool head = c1 == c - 1;
-            const bool in = head || (c1 < a.grid && same(p)), have = head || (in && !(same(q) && q.z == p.z));  // not an empty share
-            const long long at = (long long)(2 * (f * a.grid + c1) + (head ? 1 : 0)) * kFlRows + row;
-            const float m = have ? a.part_m[at] : -INFINITY, l = have ? a.part_l[at] : 0.f;
-            const float Mn = fmaxf(M, warp_max(m));
-            const float old = Mn == -INFINITY ? 1.f : sm100::ex2(M - Mn);
-            const float w = Mn == -INFINITY ? (have ? 1.f : 0.f) : sm100::ex2(m - Mn);
-            L = L * old + warp_sum(have ? w * l : 0.f);
+        for (int k = blockIdx.y * kWarps + warp; k < kFlRows; k += gridDim.y * kWarps) {
+            const int x = k / kBM, r = k & (kBM - 1), t = r / a.G, tok = (e.y * 2 + x) * a.tq + t;
+            if (t >= a.tq) continue;
+            if (tok >= e.w) break;
+            const long long row = k;
+            float M = -INFINITY, L = 0.f, acc[kC] = {};
+#pragma unroll 1
+            for (int c0 = c - 1;; c0 += 32) {  // 32 shares at a time; the first piece is the end of share c - 1
+                const int c1 = c0 + lane;
+                int4 p = p0, q = q0;
+                if (c0 >= c) {
+                    p = bound[min(c1, a.grid)];
+                    q = bound[min(c1 + 1, a.grid)];
+                }
+                const bool head = c1 == c - 1;
+                const bool in = head || (c1 < a.grid && same(p)), have = head || (in && !(same(q) && q.z == p.z));  // not an empty share
+                const long long at = (long long)(2 * (f * a.grid + c1) + (head ? 1 : 0)) * kFlRows + row;
+                const float m = have ? a.part_m[at] : -INFINITY, l = have ? a.part_l[at] : 0.f;
+                const float Mn = fmaxf(M, warp_max(m));
+                const float old = Mn == -INFINITY ? 1.f : sm100::ex2(M - Mn);
+                const float w = Mn == -INFINITY ? (have ? 1.f : 0.f) : sm100::ex2(m - Mn);
+                L = L * old + warp_sum(have ? w * l : 0.f);
 #pragma unroll
-            for (int j = 0; j < kC; ++j) acc[j] *= old;
-            M = Mn;
-            const unsigned pieces = __ballot_sync(0xffffffffu, have);
-            const int cnt = 32 - __clz(pieces);  // 0 where the run ended with the last 32
-            const float *o = a.part_o + ((long long)(2 * (f * a.grid + c0)) * kFlRows + row) * D + lane * kC;
+                for (int j = 0; j < kC; ++j) acc[j] *= old;
+                M = Mn;
+                const unsigned pieces = __ballot_sync(0xffffffffu, have);
+                const int cnt = 32 - __clz(pieces);  // 0 where the run ended with the last 32
+                const float *o = a.part_o + ((long long)(2 * (f * a.grid + c0)) * kFlRows + row) * D + lane * kC;
 #pragma unroll 4
-            for (int k1 = 0; k1 < cnt; ++k1) {
-                const float wp = __shfl_sync(0xffffffffu, w, k1);
-                if (!((pieces >> k1) & 1u)) continue;
-                const float *src = o + (long long)(2 * k1 + (c0 + k1 == c - 1 ? 1 : 0)) * kFlRows * D;
-                float v[kC];
-                if constexpr (kC == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(src);
-                else *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
+                for (int k1 = 0; k1 < cnt; ++k1) {
+                    const float wp = __shfl_sync(0xffffffffu, w, k1);
+                    if (!((pieces >> k1) & 1u)) continue;
+                    const float *src = o + (long long)(2 * k1 + (c0 + k1 == c - 1 ? 1 : 0)) * kFlRows * D;
+                    float v[kC];
+                    if constexpr (kC == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(src);
+                    else *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
 #pragma unroll
-                for (int j = 0; j < kC; ++j) acc[j] = fmaf(wp, v[j], acc[j]);
+                    for (int j = 0; j < kC; ++j) acc[j] = fmaf(wp, v[j], acc[j]);
+                }
+                if (!__all_sync(0xffffffffu, in)) break;
             }
-            if (!__all_sync(0xffffffffu, in)) break;
+            if (bad) break;
+            const float fr = L > 0.f ? 1.f / L : L;  // no key with weight: 0; NaN stays
+            const long long orow = (long long)(e.z + tok) * a.Hq + kvh * a.G + (r - t * a.G);
+            uint32_t *d = reinterpret_cast<uint32_t *>(a.out + orow * D + lane * kC);
+            if constexpr (kC == 4)
+                *reinterpret_cast<uint2 *>(d) = make_uint2(pack16<BF16>(acc[0] * fr, acc[1] * fr), pack16<BF16>(acc[2] * fr, acc[3] * fr));
+            else
+                *d = pack16<BF16>(acc[0] * fr, acc[1] * fr);
+            if (lane == 0) a.lse[orow] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : (L == 0.f ? -INFINITY : L);
         }
-        if (bad) break;
-        const float fr = L > 0.f ? 1.f / L : L;  // no key with weight: 0; NaN stays
-        const long long orow = (long long)(e.z + tok) * a.Hq + kvh * a.G + (r - t * a.G);
-        uint32_t *d = reinterpret_cast<uint32_t *>(a.out + orow * D + lane * kC);
-        if constexpr (kC == 4)
-            *reinterpret_cast<uint2 *>(d) = make_uint2(pack16<BF16>(acc[0] * fr, acc[1] * fr), pack16<BF16>(acc[2] * fr, acc[3] * fr));
-        else
-            *d = pack16<BF16>(acc[0] * fr, acc[1] * fr);
-        if (lane == 0) a.lse[orow] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : (L == 0.f ? -INFINITY : L);
     }
 }
 
@@ -133,7 +138,7 @@ rs_status flash_launch_d(const FlashArgs &a, const CUtensorMap &tmq, const CUten
     }
     launch_pdl(flash_kernel<D, BF16>, dim3(a.grid), dim3(kFlThreads), FlSmem<D>::kTotal, st, a, tmq, tmk, tmv);
     RS_CHECK_LAUNCH(what);
-    launch_full(flash_combine<D, BF16>, dim3(std::max(a.grid - 1, 1), a.max_phases * a.comb_blocks), dim3(kFlCombThreads), 0, st, a);
+    launch_full(flash_combine<D, BF16>, dim3(std::max(a.grid - 1, 1), a.comb_blocks), dim3(kFlCombThreads), 0, st, a);
     RS_CHECK_LAUNCH(what);
     return RS_OK;
 }
