@@ -6,8 +6,8 @@
 // holds one key's scores of up to 128 (token, head) columns and its sum stays in
 // a register: no exchange between threads, and K, which is read once, stays in
 // shared memory while the Q tiles pass by.  A segment is (KV head, request, 256
-// keys): two key tiles, one per warpgroup, so that a Q tile serves 256 keys (with
-// one they would ask L2 for 12 TB/s).  Its units are the Q tiles of tq tokens
+// keys): two key tiles, so that a Q tile serves 256 keys (with one they would ask
+// L2 for 12 TB/s).  Its units are the Q tiles of tq tokens
 // that see the keys; tq follows the average chunk, up to 128 / G, so that single
 // tokens neither copy nor multiply rows they do not have.  The segments lie end
 // to end, a CTA takes an equal share of their cost, and the sums of a segment that
