@@ -204,3 +204,8 @@ def test_requests_share_a_prefix():
     assert status.tolist() == [0] * 3
     assert weigh(q, code, lse, off, kp, page, table, ctx, scale, w).tolist() == [0] * 3
     check(w, want, tol, "weights")
+
+
+@pytest.mark.parametrize("B", [33, 70, 1100])
+def test_weights_of_many_requests(B):
+    test_weights([i % 3 for i in range(B)], [i * 7 % 40 for i in range(B)], 2, 1, 64, "f16", 8)
