@@ -187,3 +187,15 @@ def test_append_then_attend(n, ctx, Hq, Hkv, D, t, page, tree):
         o, z, o_tol, z_tol = attention(q[a:e], K[b], V[b], see, scale)
         check(out[a:e], o, o_tol, "out of request %d" % b)
         check(lse[a:e], z, z_tol, "lse of request %d" % b)
+
+
+@pytest.mark.parametrize("B,D,t", [(33, 64, "f16"), (70, 128, "bf16"), (1100, 64, "bf16")])
+def test_many_requests(B, D, t):
+    """More requests than a warp, and than a block, has threads."""
+    test_prompt([i * 5 % 7 for i in range(B)], 2, 1, D, t)
+    test_append_then_attend([i % 3 for i in range(B)], [i * 7 % 40 for i in range(B)], 2, 1, D, t, 8, False)
+
+
+def test_many_pairs_of_row_tiles():
+    """One prompt of more pairs than a block has threads: 128 heads on one, one token to a row tile."""
+    test_prompt([2300], 128, 1, 64, "f16")
