@@ -13,7 +13,7 @@
 // to end, a CTA takes an equal share of their cost, and the sums of a segment that
 // a share's end cuts are joined by weigh_combine in order (the same bits every time).
 // Bound: K and the weights, read once, for single tokens (16 requests of up to 8191
-// keys, D = 64: 80 MB in 23 us).  Chunks: shared memory, which the products read at
+// keys, D = 64: 80 MB in 22 us).  Chunks: shared memory, which the products read at
 // its full rate (8 KB each 64 cycles) while Q tiles are written to it and each warp
 // reads the columns' lse; then the exponentials (4 cycles a warp for 32 keys).  Four
 // prompts of 1000-4000 tokens, D = 128: 116 us, 1060 TFLOP/s of the rows and keys that see each other.
