@@ -114,12 +114,16 @@ class PagedCache:
                             self.length, scale, self.weights, self.status, ws)
 
     def rows(self, b, slots):
-        """Pool rows of request b's slots (a device index tensor)."""
+        """Pool rows of request b's slots (a device index tensor; slots below the capacity: the lookup does not check)."""
         return self.table[b].long()[slots // self.page_size] * self.page_size + slots % self.page_size
 
     def keep(self, b, nodes):
         """Of the tokens appended behind request b's cached ones, `nodes` (ascending) come first: the accepted path of a tree."""
-        at = torch.as_tensor(nodes, dtype=torch.int64, device=self.device) + self.lengths[b]
+        nodes = torch.as_tensor(nodes, dtype=torch.int64).tolist()
+        _need(0 <= b < self.B, "request %d: there are %d" % (b, self.B))
+        _need(all(0 <= x < self.max_pages * self.page_size - self.lengths[b] for x in nodes),
+              "nodes: tokens behind the %d cached ones expected, %d slots in all" % (self.lengths[b], self.max_pages * self.page_size))
+        at = torch.tensor(nodes, dtype=torch.int64, device=self.device) + self.lengths[b]
         src, dst = self.rows(b, at), self.rows(b, torch.arange(len(nodes), device=self.device) + self.lengths[b])
         for x in (self.k, self.v):
             x = x.view(-1, self.Hkv, self.D)
