@@ -448,8 +448,11 @@ rs_status rs_tree_sample(const float *logits, int R, int V, const int32_t *node_
  *            RS_ST_TIMEOUT.
  * Products run on the tensor cores with fp32 accumulation; softmax statistics
  * are fp32; P is rounded to dtype for the second product.  A row whose scores
- * are all -inf gives zeros and lse -inf.  NaN or infinity in a row of K or V
- * reaches rows of its own sequence only (also earlier ones of the same 128).
+ * are all -inf gives zeros and lse -inf.  NaN or infinity in a row of K reaches
+ * the rows that see it.  In a row of V (weight 0 times NaN is NaN) it also
+ * reaches earlier rows of its sequence that share both the 128 keys and a row
+ * tile with one that sees those keys: row tiles are 128 / (Hq / Hkv) tokens,
+ * rounded down, and keys go by 128, both from the sequence's first.
  * The result does not depend on what else runs: the same bits every time.
  */
 size_t rs_prompt_attn_workspace_size(int B, int T, int Hq, int Hkv, int D);
@@ -509,8 +512,10 @@ rs_status rs_paged_append(const uint16_t *k, int64_t k_stride, const uint16_t *v
  *   status   [B]: RS_ST_BAD_OFFSET, RS_ST_BAD_PAGE, RS_ST_BAD_TREE,
  *            RS_ST_TOO_LARGE (the request's rows are zeroed; those of a range
  *            that rs_prompt_attn rejects are left), RS_ST_TIMEOUT.
- * Types, arithmetic, B, T, head counts, alignment: as for rs_prompt_attn.  What
- * slots behind a request's last token hold (NaN too) does not matter.
+ * Types, arithmetic, B, T, head counts, alignment: as for rs_prompt_attn, NaN in
+ * V too (keys by 128 slots, row tiles from the first new token; in a tree, of a
+ * new token, it reaches any row of the request).  What slots behind a request's
+ * last token hold (NaN too) does not matter.
  */
 size_t rs_paged_attn_workspace_size(int B, int T, int Hq, int Hkv, int D);
 rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtype, const int32_t *new_off,

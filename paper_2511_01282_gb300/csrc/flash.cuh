@@ -52,7 +52,9 @@ namespace rs {
 
 constexpr int kFlThreads = 384;
 constexpr int kFlMmaWarp = 0, kFlTmaWarp = 2, kFlSoftWarp = 4;  // two warps issue products, two copy
-constexpr uint32_t kFlRegsSoft = 224, kFlRegsProd = 56;
+// (at D = 128 the product warps store 84 bytes of spilled registers with 56, 12 with 88;
+// the softmax warps' code is the same from 200 up)
+constexpr uint32_t kFlRegsSoft = 208, kFlRegsProd = 88;
 static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "register split");
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
 constexpr int kFlRows = 2 * kBM;  // rows of a segment and of a partial slot
@@ -102,6 +104,11 @@ __device__ __forceinline__ int pair_keys(const FlashArgs &a, int n, int ctx, int
 }
 __device__ __forceinline__ int pair_tiles(const FlashArgs &a, int n, int ctx, int p) {
     return (pair_keys(a, n, ctx, p) + kBN - 1) / kBN;
+}
+// Key tiles that some row of row tile x of the pair sees.  The first row tile's may end
+// before the pair's (causal): P V is left out there, where P is 0 and V may hold NaN.
+__device__ __forceinline__ int row_tiles(const FlashArgs &a, int n, int ctx, int p, int x) {
+    return (ctx + (a.anc ? n : min(n, (2 * p + x + 1) * a.tq)) + kBN - 1) / kBN;
 }
 // cost of one of its key tiles
 __device__ __forceinline__ int tile_cost(const FlashArgs &a, int n, int p) {
@@ -473,39 +480,45 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             if (!wait(&kfull[g % NK], g / NK, &qfull[x], pieces)) break;
             if (kApart && done > 0 && !wait(&sfree[x], done - 1, &sfree[x], done - 1)) break;
             issue_s(g);
-#pragma unroll 1
-            for (int tl = 0; tl < n; ++tl, ++done) {
+            // of the piece's key tiles, those that some row of the row tile sees; the others go
+            // through without P V (a loop of their own: a condition in one loop cost a prompt
+            // of 16384 tokens 3 %)
+            const int seen = (int)uniform((uint32_t)min(n, row_tiles(a, pc.n, pc.ctx, pc.p, x) - pc.j0));
+            auto step = [&](auto seen_t, int tl) {
+                constexpr bool kSeen = decltype(seen_t)::value;
                 const uint32_t t = g + tl, st = t % NV;
                 const bool more = tl + 1 < n;
                 if (kApart) {  // S of the next tile goes ahead of this one's P V
                     if (more) {
-                        if (!wait(&kfull[(t + 1) % NK], (t + 1) / NK, &sfree[x], done)) break;
+                        if (!wait(&kfull[(t + 1) % NK], (t + 1) / NK, &sfree[x], done)) return;
                         issue_s(t + 1);
                     }
-                    if (!wait(&vfull[st], t / NV, &pfull[x], done)) break;
+                    if (!wait(&vfull[st], t / NV, &pfull[x], done)) return;
                 } else {
                     // what does not depend on the softmax first; then P and, where both row
                     // tiles are at work, the turn: they alternate, so that one's softmax
                     // runs beside the other's products
                     const uint32_t tn = t + 1;
-                    if (!wait(&vfull[st], t / NV, more ? &kfull[tn % NK] : &vfull[st], more ? tn / NK : t / NV)) break;
+                    if (!wait(&vfull[st], t / NV, more ? &kfull[tn % NK] : &vfull[st], more ? tn / NK : t / NV)) return;
                     const bool must = pc.full && (x == 1 || turns > 0);
-                    if (!wait(&pfull[x], done, must ? &turn[x] : &pfull[x], must ? turns - (x == 0 ? 1 : 0) : done)) break;
+                    if (!wait(&pfull[x], done, must ? &turn[x] : &pfull[x], must ? turns - (x == 0 ? 1 : 0) : done)) return;
                 }
-                if (tl == 0 && pieces > 0 && !wait(&ofree[x], pieces - 1, &ofree[x], pieces - 1)) break;
+                if (tl == 0 && pieces > 0 && !wait(&ofree[x], pieces - 1, &ofree[x], pieces - 1)) return;
                 tc_fence_after();
                 const uint32_t v_lo = uniform(v_lo0 + st * kTileDesc);
 #pragma unroll
                 for (int part = 0; part < kParts; ++part) {
                     if (part > 0) {
-                        if (!wait(&pfull2[x], done, &pfull2[x], done)) break;
+                        if (!wait(&pfull2[x], done, &pfull2[x], done)) return;
                         tc_fence_after();
                     }
                     if (elect_one()) {
+                        if constexpr (kSeen) {
 #pragma unroll
-                        for (int ks = part * 8 / kParts; ks < (part + 1) * 8 / kParts; ++ks)
-                            umma_ts(o_tm, p_tm + ks * 8, desc_of(v_lo + (uint32_t)((ks * 2048) >> 4), d_hi), idO,
-                                    (tl > 0 || ks > 0) ? 1u : 0u);
+                            for (int ks = part * 8 / kParts; ks < (part + 1) * 8 / kParts; ++ks)
+                                umma_ts(o_tm, p_tm + ks * 8, desc_of(v_lo + (uint32_t)((ks * 2048) >> 4), d_hi), idO,
+                                        (tl > 0 || ks > 0) ? 1u : 0u);
+                        }
                         if (part == kParts - 1) {
                             umma_commit(&pvdone[x]);
                             umma_commit(&vempty[st]);
@@ -516,7 +529,7 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                     }
                     __syncwarp();
                 }
-                if (!ok) break;
+                if (!ok) return;
                 if (!kApart) {
                     if (more) issue_s(t + 1);
                     if (pc.full) {
@@ -525,7 +538,12 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                         ++turns;
                     }
                 }
-            }
+            };
+            int tl = 0;
+#pragma unroll 1
+            for (; ok && tl < seen; ++tl, ++done) step(std::true_type(), tl);
+#pragma unroll 1
+            for (; ok && tl < n; ++tl, ++done) step(std::false_type(), tl);
             ++pieces;
             g += n;
         }
@@ -704,7 +722,9 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                 const long long orow = (long long)(pc.n0 + tok) * a.Hq + pc.kvh * G + rg;
                 const long long prow = (long long)pc.slot * kFlRows + x * kBM + r;
                 const bool final = pc.slot < 0;
-                const float f = l > 0.f ? 1.f / l : l;  // no key with weight: 0; NaN stays
+                const float f = l > 0.f ? 1.f / l : l;  // NaN stays
+                // no key with weight: zeros, whatever V held or, where the row tile sees none of
+                // the piece's keys, was in the columns
 #pragma unroll 1
                 for (int ch = 0; ch < D / 32; ++ch) {
                     uint32_t xo[32];
@@ -712,6 +732,10 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                     tmem_wait_ld();
                     tmem_regs_ready(xo);
                     if (!valid) continue;
+                    if (l == 0.f) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) xo[e] = 0u;
+                    }
                     if (final) {
                         uint32_t v[16];
 #pragma unroll
