@@ -259,7 +259,7 @@ struct FlSmem {
     static constexpr int kNK = D == 128 ? 3 : 4, kNV = D == 128 ? 2 : 4;  // stages of K and V
     static constexpr int kK = 0, kV = kNK * kTile, kQ = kV + kNV * kTile;
     static constexpr int kBar = kQ + 2 * kTile;
-    static constexpr int kNumBars = 2 * kNK + 2 * kNV + 22;
+    static constexpr int kNumBars = 2 * kNK + 2 * kNV + 20;
     static constexpr int kMisc = kBar + kNumBars * 8;    // tensor memory base, abort flag
     static constexpr int kBounds = (kMisc + 8 + 15) / 16 * 16;
     static constexpr int kBytes = kBounds + 2 * kFlMaxPhases * 16;
@@ -279,10 +279,10 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                                                             ~uintptr_t(1023));
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kBar);
     uint64_t *kfull = bars, *kempty = kfull + NK, *vfull = kempty + NK, *vempty = vfull + NV;
-    // per row tile: S there, S read (kApart), P there (its two halves), P V complete
-    // (its first half), Q there, Q read, O read, turn at the tensor core
+    // per row tile: S there, S read (kApart), P there (its two halves), P V complete,
+    // Q there, Q read, O read, turn at the tensor core
     uint64_t *sfull = vempty + NV, *sfree = sfull + 2, *pfull = sfree + 2, *pfull2 = pfull + 2, *pvdone = pfull2 + 2;
-    uint64_t *phalf = pvdone + 2, *qfull = phalf + 2, *qfree = qfull + 2, *ofree = qfree + 2, *turn = ofree + 2;
+    uint64_t *qfull = pvdone + 2, *qfree = qfull + 2, *ofree = qfree + 2, *turn = ofree + 2;
     uint64_t *drain = turn + 2;
     uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + S::kMisc);
     volatile int *s_abort = reinterpret_cast<volatile int *>(smem + S::kMisc + 4);
@@ -307,7 +307,6 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             mbar_init(&qfull[x], 1);
             mbar_init(&qfree[x], kBM);
             mbar_init(&ofree[x], kBM);
-            mbar_init(&phalf[x], 1);
             mbar_init(&turn[x], 1);
             mbar_init(&drain[x], 1);
         }
@@ -523,8 +522,6 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                             umma_commit(&pvdone[x]);
                             umma_commit(&vempty[st]);
                             if (!pc.full) umma_commit(&vempty[st]);
-                        } else {
-                            umma_commit(&phalf[x]);
                         }
                     }
                     __syncwarp();
