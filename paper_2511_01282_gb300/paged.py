@@ -4,7 +4,7 @@
 A program appends the new tokens' keys and values, attends with their queries, and then says how many of them stay
 (``advance``); what was appended behind them is written over by the next ``append``.  ``prompt_attention`` is the pass over
 whole prompts that comes before.  ``append``, ``attend`` and ``weigh`` may be captured into a CUDA graph; the others copy from
-the host.
+the host.  What the calls report about requests (bad pages, a time-out) is gathered on the device: ``check`` reads it and raises.
 """
 import torch
 
@@ -27,6 +27,17 @@ def _heads(name, x, heads, D, dtype):
 def _ints(name, x, n):
     _need(x.dtype == torch.int32 and x.dim() == 1 and x.numel() == n, "%s: %d values of int32 expected, not %s of %s"
           % (name, n, list(x.shape), x.dtype))
+
+
+_STATUS = [n for n in dir(rs) if n.startswith("RS_ST_")]
+
+
+def _flags(status):
+    return " ".join(n[6:] for n in _STATUS if status & getattr(rs, n)) or "status %d" % status
+
+
+def _raise(status):
+    raise RuntimeError("; ".join("request %d: %s" % (b, _flags(x)) for b, x in enumerate(status) if x))
 
 
 def _scratch(need, device):
@@ -71,7 +82,23 @@ class PagedCache:
         slots = self.n_pages * page_size
         self.weights = z(Hkv, slots, dt=torch.float32) if track_weights else None
         self.positions = z(Hkv, slots, dt=torch.int32) if track_weights else None
-        self.status = z(B, dt=torch.int32)
+        self.status = z(B, dt=torch.int32)  # RS_ST_* flags of all calls since the last check
+
+    def report(self, status):
+        """A call's status [B] joins those that `check` looks at (on the device: it may be captured)."""
+        self.status |= status
+
+    def check(self):
+        """Raises where a call since the last check has reported something about a request; waits for the calls."""
+        found = self.status.tolist()
+        if any(found):
+            self.status.zero_()
+            _raise(found)
+
+    def _reported(self, call, *args, workspace=()):
+        status = torch.empty_like(self.status)
+        call(*args, status, *workspace)
+        self.report(status)
 
     def _pages(self):
         return self.n_pages, self.page_size, self.table, self.max_pages
@@ -85,8 +112,8 @@ class PagedCache:
         _ints("new_off", new_off, self.B + 1)
         if pos is not None:
             _ints("pos", pos, T)
-        rs.rs_paged_append(k, k.stride(0), v, v.stride(0), pos, new_off, self.B, T, self.Hkv, self.D, self.k, self.v,
-                           *self._pages(), self.length, self.weights, self.positions, self.status)
+        self._reported(rs.rs_paged_append, k, k.stride(0), v, v.stride(0), pos, new_off, self.B, T, self.Hkv, self.D, self.k, self.v,
+                       *self._pages(), self.length, self.weights, self.positions)
 
     def attend(self, q, new_off, scale, parents=None):
         """Attention of the appended tokens' queries [T, Hq, D]: (out, lse)."""
@@ -98,8 +125,8 @@ class PagedCache:
         out = torch.empty((T, Hq, D), dtype=q.dtype, device=self.device)
         lse = torch.empty((T, Hq), dtype=torch.float32, device=self.device)
         ws = _scratch(rs.rs_paged_attn_workspace_size(self.B, T, Hq, self.Hkv, D), self.device)
-        rs.rs_paged_attn(q, q.stride(0), _CODES[q.dtype], new_off, parents, self.B, T, Hq, self.Hkv, D, self.k, self.v, *self._pages(),
-                         self.length, scale, out, lse, self.status, ws)
+        self._reported(rs.rs_paged_attn, q, q.stride(0), _CODES[q.dtype], new_off, parents, self.B, T, Hq, self.Hkv, D, self.k, self.v,
+                       *self._pages(), self.length, scale, out, lse, workspace=(ws,))
         return out, lse
 
     def weigh(self, q, lse, new_off, scale):
@@ -110,8 +137,8 @@ class PagedCache:
         _ints("new_off", new_off, self.B + 1)
         self._tracked()
         ws = _scratch(rs.rs_paged_weights_workspace_size(self.B, T, Hq, self.Hkv, D), self.device)
-        rs.rs_paged_weights(q, q.stride(0), _CODES[q.dtype], lse, new_off, self.B, T, Hq, self.Hkv, D, self.k, *self._pages(),
-                            self.length, scale, self.weights, self.status, ws)
+        self._reported(rs.rs_paged_weights, q, q.stride(0), _CODES[q.dtype], lse, new_off, self.B, T, Hq, self.Hkv, D, self.k,
+                       *self._pages(), self.length, scale, self.weights, workspace=(ws,))
 
     def rows(self, b, slots):
         """Pool rows of request b's slots (a device index tensor; slots below the capacity: the lookup does not check)."""
@@ -138,15 +165,20 @@ class PagedCache:
         self._set([n + c for n, c in zip(self.lengths, counts)])
 
     def evict(self, next_pos, budget, recent):
-        """Cuts every request to `budget` tokens per head; next_pos[b]: tokens that request b has seen."""
+        """Cuts every request to `budget` tokens per head; next_pos[b]: tokens that request b has seen.  A request that the call
+        rejects keeps its tokens, and this raises."""
         _need(len(next_pos) == self.B, "next_pos: a position for each of %d requests" % self.B)
         self._tracked()
         ws = _scratch(rs.rs_paged_evict_workspace_size(self.B, self.Hkv, budget), self.device)
-        new = torch.empty_like(self.length)
+        both = torch.empty((2, self.B), dtype=torch.int32, device=self.device)
+        new, status = both.unbind()
         nxt = torch.tensor(next_pos, dtype=torch.int32, device=self.device)
         rs.rs_paged_evict(self.k, self.v, self.Hkv, self.D, *self._pages(), self.length, nxt, self.B, budget, recent, self.weights,
-                          self.positions, new, self.status, ws)
-        self._set([min(n, budget) for n in self.lengths])
+                          self.positions, new, status, ws)
+        self.length.copy_(new)
+        self.lengths, found = both.tolist()
+        if any(found):
+            _raise(found)
 
     def _tracked(self):
         _need(self.weights is not None, "a cache made with track_weights=True expected")

@@ -27,3 +27,57 @@ def test_keep_takes_the_last_slot():
     c.keep(1, [])
     assert c.k.view(-1, 2, 64)[60:64, 0, 0].tolist() == [60, 63, 62, 63]
     assert c.k.view(-1, 2, 64)[64 + 3:64 + 6, 0, 0].tolist() == [64 + 5, 64 + 63, 64 + 5]
+
+
+def _stub(monkeypatch, name, status, also=None):
+    """rs.<name> leaves `status` in the tensor that follows what the call of the library has for it."""
+    def call(*args):
+        if also:
+            also(*args)
+        at = -1 if name == "rs_paged_append" else -2
+        args[at].copy_(torch.tensor(status, dtype=torch.int32))
+    monkeypatch.setattr(rs, name, call)
+    if hasattr(rs, name + "_workspace_size"):
+        monkeypatch.setattr(rs, name + "_workspace_size", lambda *a: 0)
+
+
+def _tracked(B=2, **kw):
+    return PagedCache(B, 64, 16, 2, 64, track_weights=True, device="cpu", **kw)
+
+
+def _x(n, h=2):
+    return torch.zeros(n, h, 64, dtype=torch.bfloat16)
+
+
+OFF = torch.tensor([0, 2, 5], dtype=torch.int32)
+
+
+def test_statuses_gather_until_they_are_looked_at(monkeypatch):
+    c, q, lse = _tracked(), _x(5, 4), torch.zeros(5, 4)
+    _stub(monkeypatch, "rs_paged_append", [0, rs.RS_ST_BAD_PAGE])
+    c.append(_x(5), _x(5), OFF)
+    _stub(monkeypatch, "rs_paged_append", [0, 0])
+    c.append(_x(5), _x(5), OFF)
+    _stub(monkeypatch, "rs_paged_attn", [0, rs.RS_ST_TIMEOUT])
+    c.attend(q, OFF, 0.1)
+    _stub(monkeypatch, "rs_paged_weights", [0, 0])
+    c.weigh(q, lse, OFF, 0.1)
+    with pytest.raises(RuntimeError, match="request 1: BAD_PAGE TIMEOUT$"):
+        c.check()
+    c.check()
+    c.report(torch.tensor([1024, 0], dtype=torch.int32))
+    with pytest.raises(RuntimeError, match="request 0: status 1024$"):
+        c.check()
+
+
+def test_an_eviction_takes_the_lengths_that_are_reported(monkeypatch):
+    c = _tracked()
+    c.advance([40, 30])
+
+    def lengths(*args):
+        args[-3].copy_(torch.tensor([40, 8], dtype=torch.int32))
+
+    _stub(monkeypatch, "rs_paged_evict", [rs.RS_ST_BAD_PAGE, 0], lengths)
+    with pytest.raises(RuntimeError, match="request 0: BAD_PAGE$"):
+        c.evict([40, 30], 8, 2)
+    assert c.lengths == [40, 8] and c.length.tolist() == [40, 8]
