@@ -107,7 +107,8 @@ class TinyLM:
         x = self.p["emb"][tokens]
         for i, layer in enumerate(cache["layers"]):
             q, k, v = self._qkv(x, i)
-            out, lse, _, cache["ws"] = prompt_attention(q, k, v, off, self.D ** -0.5, cache["ws"])
+            out, lse, status, cache["ws"] = prompt_attention(q, k, v, off, self.D ** -0.5, cache["ws"])
+            layer.report(status)
             layer.append(k, v, off)
             cache["rows"][i] = (q, lse)
             x = self._layer_end(x, out.float(), i)
@@ -147,6 +148,10 @@ class TinyLM:
                 layer.evict([cache["seen"]], cache["budget"], cache["recent"])
         if cache["budget"] is not None:
             cache["S"] = min(cache["S"], cache["budget"])
+        # what the calls since the last commit have reported, all layers' in one read
+        if bool(torch.stack([layer.status for layer in cache["layers"]]).any()):
+            for layer in cache["layers"]:
+                layer.check()
 
     def forward_tree(self, cache, tokens, parents, ws):
         """Logits [N, V] of a draft tree hanging after the cached prefix.
