@@ -77,8 +77,11 @@ class PagedCache:
         z = lambda *s, dt: torch.zeros(s, dtype=dt, device=self.device)  # noqa: E731
         self.k, self.v = z(self.n_pages, page_size, Hkv, D, dt=dtype), z(self.n_pages, page_size, Hkv, D, dt=dtype)
         self.table = torch.arange(self.n_pages, dtype=torch.int32, device=self.device).view(B, self.max_pages)
-        self.length = z(B, dt=torch.int32)  # cached tokens
-        self.lengths = [0] * B              # the same on the host
+        # cached tokens, and the position of the next one (behind an eviction it is the higher); the same on the host
+        self._counts = z(2, B, dt=torch.int32)
+        self.length, self.next = self._counts.unbind()
+        self.lengths, self.seen = [0] * B, [0] * B
+        self._numbered = False  # the last tokens came without positions
         slots = self.n_pages * page_size
         self.weights = z(Hkv, slots, dt=torch.float32) if track_weights else None
         self.positions = z(Hkv, slots, dt=torch.int32) if track_weights else None
@@ -104,16 +107,27 @@ class PagedCache:
         return self.n_pages, self.page_size, self.table, self.max_pages
 
     def append(self, k, v, new_off, pos=None):
-        """Keys and values [T, Hkv, D] of new tokens behind the cached ones; pos [T] their positions."""
+        """Keys and values [T, Hkv, D] of new tokens behind the cached ones; pos [T] their positions (where the cache keeps any):
+        without it they go on from the tokens that the request has seen."""
         T = k.shape[0]
         for name, x in (("k", k), ("v", v)):
             _heads(name, x, self.Hkv, self.D, self.dtype)
         _need(v.shape[0] == T, "v: %d rows expected, not %d" % (T, v.shape[0]))
         _ints("new_off", new_off, self.B + 1)
+        self._numbered = pos is None
         if pos is not None:
             _ints("pos", pos, T)
+        elif self.positions is not None and T > 0 and self.B > 0:
+            pos = self._numbers(T, new_off)
         self._reported(rs.rs_paged_append, k, k.stride(0), v, v.stride(0), pos, new_off, self.B, T, self.Hkv, self.D, self.k, self.v,
                        *self._pages(), self.length, self.weights, self.positions)
+
+    def _numbers(self, T, new_off):
+        """Row i of request b: next[b] + i, on the device (the library's own numbers are slots, which fall behind where tokens
+        have been evicted)."""
+        at = torch.arange(T, dtype=torch.int32, device=self.device)
+        b = torch.searchsorted(new_off[1:], at, right=True).clamp_(max=self.B - 1)
+        return self.next[b] + at - new_off[b]
 
     def attend(self, q, new_off, scale, parents=None):
         """Attention of the appended tokens' queries [T, Hq, D]: (out, lse)."""
@@ -145,7 +159,8 @@ class PagedCache:
         return self.table[b].long()[slots // self.page_size] * self.page_size + slots % self.page_size
 
     def keep(self, b, nodes):
-        """Of the tokens appended behind request b's cached ones, `nodes` (ascending) come first: the accepted path of a tree."""
+        """Of the tokens appended behind request b's cached ones, `nodes` (ascending) come first: the accepted path of a tree.
+        Positions that the append was given go with them; without any the path's tokens follow each other."""
         nodes = torch.as_tensor(nodes, dtype=torch.int64).tolist()
         _need(0 <= b < self.B, "request %d: there are %d" % (b, self.B))
         _need(all(0 <= x < self.max_pages * self.page_size - self.lengths[b] for x in nodes),
@@ -156,33 +171,37 @@ class PagedCache:
             x = x.view(-1, self.Hkv, self.D)
             x[dst] = x[src]
         if self.positions is not None:
-            self.positions[:, dst] = self.positions[:, src]
+            if self._numbered:
+                self.positions[:, dst] = torch.arange(len(nodes), dtype=torch.int32, device=self.device) + self.seen[b]
+            else:
+                self.positions[:, dst] = self.positions[:, src]
 
     def advance(self, counts):
         """The first counts[b] of the appended tokens stay."""
         _need(len(counts) == self.B and all(c >= 0 and n + c <= self.max_pages * self.page_size for n, c in zip(self.lengths, counts)),
               "counts: a number of tokens for each of %d requests, %d cached ones at most" % (self.B, self.max_pages * self.page_size))
-        self._set([n + c for n, c in zip(self.lengths, counts)])
+        self._set([n + c for n, c in zip(self.lengths, counts)], [n + c for n, c in zip(self.seen, counts)])
 
     def evict(self, next_pos, budget, recent):
-        """Cuts every request to `budget` tokens per head; next_pos[b]: tokens that request b has seen.  A request that the call
-        rejects keeps its tokens, and this raises."""
+        """Cuts every request to `budget` tokens per head; next_pos[b]: tokens that request b has seen (later ones are counted
+        on from there).  A request that the call rejects keeps its tokens, and this raises."""
         _need(len(next_pos) == self.B, "next_pos: a position for each of %d requests" % self.B)
         self._tracked()
         ws = _scratch(rs.rs_paged_evict_workspace_size(self.B, self.Hkv, budget), self.device)
         both = torch.empty((2, self.B), dtype=torch.int32, device=self.device)
         new, status = both.unbind()
-        nxt = torch.tensor(next_pos, dtype=torch.int32, device=self.device)
+        seen = [int(x) for x in next_pos]
+        nxt = torch.tensor(seen, dtype=torch.int32, device=self.device)
         rs.rs_paged_evict(self.k, self.v, self.Hkv, self.D, *self._pages(), self.length, nxt, self.B, budget, recent, self.weights,
                           self.positions, new, status, ws)
-        self.length.copy_(new)
-        self.lengths, found = both.tolist()
+        torch.stack((new, nxt), out=self._counts)
+        (self.lengths, found), self.seen = both.tolist(), seen
         if any(found):
             _raise(found)
 
     def _tracked(self):
         _need(self.weights is not None, "a cache made with track_weights=True expected")
 
-    def _set(self, lengths):
-        self.lengths = list(lengths)
-        self.length.copy_(torch.tensor(self.lengths, dtype=torch.int32))
+    def _set(self, lengths, seen):
+        self.lengths, self.seen = list(lengths), list(seen)
+        self._counts.copy_(torch.tensor([self.lengths, self.seen], dtype=torch.int32))

@@ -81,3 +81,64 @@ def test_an_eviction_takes_the_lengths_that_are_reported(monkeypatch):
     with pytest.raises(RuntimeError, match="request 0: BAD_PAGE$"):
         c.evict([40, 30], 8, 2)
     assert c.lengths == [40, 8] and c.length.tolist() == [40, 8]
+
+
+def test_tokens_without_positions_go_on_from_those_seen(monkeypatch):
+    c, got = _tracked(B=3), []
+
+    def evicted(*args):
+        args[-3].copy_(torch.tensor([8, 8, 3], dtype=torch.int32))
+
+    _stub(monkeypatch, "rs_paged_append", [0] * 3, lambda *a: got.append(a[4] if a[4] is None else a[4].tolist()))
+    _stub(monkeypatch, "rs_paged_evict", [0] * 3, evicted)
+    off = torch.tensor([0, 2, 2, 5], dtype=torch.int32)
+    c.append(_x(7), _x(7), off)  # two rows behind the last request
+    c.advance([40, 30, 3])
+    c.evict([40, 30, 3], 8, 2)
+    c.append(_x(5), _x(5), off)
+    c.advance([2, 0, 1])
+    c.append(_x(5), _x(5), off)
+    own = torch.arange(5, dtype=torch.int32)
+    c.append(_x(5), _x(5), off, own)
+    c.append(_x(0), _x(0), torch.zeros(4, dtype=torch.int32))
+    assert [x[:5] if x else x for x in got] == [[0, 1, 0, 1, 2], [40, 41, 3, 4, 5], [42, 43, 4, 5, 6], [0, 1, 2, 3, 4], None]
+    assert c.lengths == [10, 8, 4] and c.seen == [42, 30, 4]
+    assert c.length.tolist() == c.lengths and c.next.tolist() == c.seen
+    plain = PagedCache(3, 64, 16, 2, 64, device="cpu")  # no positions to keep: nothing is computed for them
+    plain.append(_x(5), _x(5), off)
+    assert got[-1] is None
+
+
+def test_offsets_that_decrease_number_nothing_out_of_range(monkeypatch):
+    c = _tracked()
+    _stub(monkeypatch, "rs_paged_append", [rs.RS_ST_BAD_OFFSET] * 2)
+    for off in ([0, 9, 4], [-3, 2, 5], [7, 7, 7], [5, 0, -9]):
+        c.append(_x(5), _x(5), torch.tensor(off, dtype=torch.int32))
+
+
+def test_the_accepted_path_follows_on(monkeypatch):
+    c = _tracked(B=1)
+    _stub(monkeypatch, "rs_paged_append", [0])
+    c.advance([20])
+    off = torch.tensor([0, 9], dtype=torch.int32)
+    c.append(_x(9), _x(9), off)
+    c.positions[:, 20:29] = torch.arange(20, 29, dtype=torch.int32)
+    c.keep(0, [0, 3, 8])
+    assert c.positions[0, 20:24].tolist() == [20, 21, 22, 23]
+    c.append(_x(9), _x(9), off, off.new_tensor(range(500, 509)))
+    c.positions[:, 20:29] = torch.arange(500, 509, dtype=torch.int32)
+    c.keep(0, [0, 3, 8])
+    assert c.positions[0, 20:24].tolist() == [500, 503, 508, 503]
+
+
+def test_a_refused_eviction_changes_nothing(monkeypatch):
+    c = _tracked()
+    c.advance([40, 30])
+
+    def refused(*args):
+        raise rs.RespecError(rs.RS_ERR_INVALID_ARG, "budget=0")
+
+    _stub(monkeypatch, "rs_paged_evict", [0, 0], refused)
+    with pytest.raises(rs.RespecError):
+        c.evict([90, 90], 0, 0)
+    assert (c.lengths, c.seen, c.length.tolist(), c.next.tolist()) == ([40, 30], [40, 30], [40, 30], [40, 30])
