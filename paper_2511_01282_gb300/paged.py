@@ -24,6 +24,11 @@ def _heads(name, x, heads, D, dtype):
           "%s: [rows, %s, %d] of %s expected, not %s of %s" % (name, heads or "heads", D, dtype, list(x.shape), x.dtype))
 
 
+def _apart(x):
+    """Elements from row to row of [rows, heads, D]; what a tensor has for a single row means nothing."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+
+
 def _ints(name, x, n):
     _need(x.dtype == torch.int32 and x.dim() == 1 and x.numel() == n, "%s: %d values of int32 expected, not %s of %s"
           % (name, n, list(x.shape), x.dtype))
@@ -61,7 +66,7 @@ def prompt_attention(q, k, v, seq_off, scale, workspace=None):
     need = rs.rs_prompt_attn_workspace_size(B, T, Hq, Hkv, D)
     if workspace is None or workspace.numel() < need:
         workspace = _scratch(need, dev)
-    rs.rs_prompt_attn(q, q.stride(0), k, k.stride(0), v, v.stride(0), _CODES[q.dtype], seq_off, B, T, Hq, Hkv, D, scale, out, lse,
+    rs.rs_prompt_attn(q, _apart(q), k, _apart(k), v, _apart(v), _CODES[q.dtype], seq_off, B, T, Hq, Hkv, D, scale, out, lse,
                       status, workspace)
     return out, lse, status, workspace
 
@@ -119,7 +124,7 @@ class PagedCache:
             _ints("pos", pos, T)
         elif self.positions is not None and T > 0 and self.B > 0:
             pos = self._numbers(T, new_off)
-        self._reported(rs.rs_paged_append, k, k.stride(0), v, v.stride(0), pos, new_off, self.B, T, self.Hkv, self.D, self.k, self.v,
+        self._reported(rs.rs_paged_append, k, _apart(k), v, _apart(v), pos, new_off, self.B, T, self.Hkv, self.D, self.k, self.v,
                        *self._pages(), self.length, self.weights, self.positions)
 
     def _numbers(self, T, new_off):
@@ -139,7 +144,7 @@ class PagedCache:
         out = torch.empty((T, Hq, D), dtype=q.dtype, device=self.device)
         lse = torch.empty((T, Hq), dtype=torch.float32, device=self.device)
         ws = _scratch(rs.rs_paged_attn_workspace_size(self.B, T, Hq, self.Hkv, D), self.device)
-        self._reported(rs.rs_paged_attn, q, q.stride(0), _CODES[q.dtype], new_off, parents, self.B, T, Hq, self.Hkv, D, self.k, self.v,
+        self._reported(rs.rs_paged_attn, q, _apart(q), _CODES[q.dtype], new_off, parents, self.B, T, Hq, self.Hkv, D, self.k, self.v,
                        *self._pages(), self.length, scale, out, lse, workspace=(ws,))
         return out, lse
 
@@ -151,7 +156,7 @@ class PagedCache:
         _ints("new_off", new_off, self.B + 1)
         self._tracked()
         ws = _scratch(rs.rs_paged_weights_workspace_size(self.B, T, Hq, self.Hkv, D), self.device)
-        self._reported(rs.rs_paged_weights, q, q.stride(0), _CODES[q.dtype], lse, new_off, self.B, T, Hq, self.Hkv, D, self.k,
+        self._reported(rs.rs_paged_weights, q, _apart(q), _CODES[q.dtype], lse, new_off, self.B, T, Hq, self.Hkv, D, self.k,
                        *self._pages(), self.length, scale, self.weights, workspace=(ws,))
 
     def rows(self, b, slots):

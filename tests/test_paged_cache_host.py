@@ -142,3 +142,25 @@ def test_a_refused_eviction_changes_nothing(monkeypatch):
     with pytest.raises(rs.RespecError):
         c.evict([90, 90], 0, 0)
     assert (c.lengths, c.seen, c.length.tolist(), c.next.tolist()) == ([40, 30], [40, 30], [40, 30], [40, 30])
+
+
+def test_a_single_row_has_no_distance_to_the_next(monkeypatch):
+    """What a tensor says of the stride of a dimension of one row is anything: a token's heads taken from [heads, 1, D] say D."""
+    from paper_2511_01282_gb300 import paged
+    got = []
+    c = PagedCache(1, 64, 16, 2, 64, device="cpu", track_weights=True)
+    q, k = (torch.zeros(h, 1, 64, dtype=torch.bfloat16).transpose(0, 1) for h in (4, 2))
+    assert q.stride(0) == 64 and q.is_contiguous()
+    off = torch.tensor([0, 1], dtype=torch.int32)
+    _stub(monkeypatch, "rs_paged_append", [0], lambda *a: got.append((a[1], a[3])))
+    _stub(monkeypatch, "rs_paged_attn", [0], lambda *a: got.append(a[1]))
+    _stub(monkeypatch, "rs_paged_weights", [0], lambda *a: got.append(a[1]))
+    _stub(monkeypatch, "rs_prompt_attn", [0], lambda *a: got.append((a[1], a[3], a[5])))
+    c.append(k, k, off, off[:1])
+    out, lse = c.attend(q, off, 0.1)
+    c.weigh(q, lse, off, 0.1)
+    paged.prompt_attention(q, k, k, off, 0.1)
+    assert got == [(128, 128), 256, 256, (256, 128, 128)]
+    wide = torch.zeros(3, 8, 64, dtype=torch.bfloat16)
+    c.append(wide[:, :2], wide[:, 2:4], torch.tensor([0, 3], dtype=torch.int32), torch.arange(3, dtype=torch.int32))
+    assert got[-1] == (512, 512)
