@@ -72,9 +72,14 @@ def prompt_attention(q, k, v, seq_off, scale, workspace=None):
 
 
 class PagedCache:
-    """B requests with `tokens` slots each, in pages of `page_size` tokens."""
+    """B requests with `tokens` slots each, in pages of `page_size` tokens.  Every request owns its pages for good: an eviction bounds
+    what the calls read, not the memory.  (The library's calls take any page table.)"""
 
     def __init__(self, B, tokens, page_size, Hkv, D, dtype=torch.bfloat16, track_weights=False, device="cuda"):
+        _need(dtype in _CODES and D in (64, 128), "dtype=%s, D=%d: bfloat16 or float16, 64 or 128 expected" % (dtype, D))
+        _need(8 <= page_size <= 65536 and page_size & (page_size - 1) == 0, "page_size=%d: a power of two from 8 to 65536 expected" % page_size)
+        _need(B >= 0 and tokens >= 0 and Hkv >= 1, "B=%d, tokens=%d, Hkv=%d: out of range" % (B, tokens, Hkv))
+        _need(B * -(-tokens // page_size) * page_size < (1 << 31) - 65536, "%d requests of %d tokens: 2^31 slots or more" % (B, tokens))
         self.B, self.page_size, self.Hkv, self.D, self.dtype = B, page_size, Hkv, D, dtype
         self.max_pages = -(-tokens // page_size)
         self.n_pages = B * self.max_pages

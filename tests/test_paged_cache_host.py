@@ -164,3 +164,14 @@ def test_a_single_row_has_no_distance_to_the_next(monkeypatch):
     wide = torch.zeros(3, 8, 64, dtype=torch.bfloat16)
     c.append(wide[:, :2], wide[:, 2:4], torch.tensor([0, 3], dtype=torch.int32), torch.arange(3, dtype=torch.int32))
     assert got[-1] == (512, 512)
+
+
+@pytest.mark.parametrize("bad,word", [
+    (dict(dtype=torch.float32), "dtype"), (dict(D=96), "96"), (dict(page_size=24), "page_size=24"), (dict(page_size=4), "page_size=4"),
+    (dict(page_size=0), "page_size=0"), (dict(page_size=1 << 17), "page_size=131072"), (dict(Hkv=0), "Hkv=0"), (dict(B=-1), "B=-1"),
+    (dict(tokens=-1), "tokens=-1"), (dict(tokens=1 << 31), "slots"),
+])
+def test_a_cache_that_no_call_would_take_is_refused(bad, word):
+    args = dict(dict(B=2, tokens=40, page_size=16, Hkv=2, D=64, dtype=torch.bfloat16, device="meta"), **bad)
+    with pytest.raises(ValueError, match=word):
+        PagedCache(**args)
