@@ -551,8 +551,9 @@ rs_status rs_paged_weights(const uint16_t *q, int64_t q_stride, int dtype, const
 /* ===================================================== rs_paged_evict ====
  * Cuts every request's cache down to `budget` tokens per KV head.  Of the
  * slots s < cache_len[b] of a head those stay that come first in the order:
- * recent ones (position >= next_pos[b] - recent), then higher weight (NaN
- * last), then lower slot.  Kept tokens behind slot `budget` move into the
+ * recent ones (position >= next_pos[b] - recent), the lower slot first whatever
+ * their weight (where positions make more of them than the budget holds); then
+ * the others, higher weight first (NaN last), then lower slot.  Kept tokens behind slot `budget` move into the
  * slots below it that are given up, both in ascending order: K, V, weight and
  * position; everything else below the budget stays where it is, and what lies
  * behind it is left as it is.  A request of at most `budget` tokens is not

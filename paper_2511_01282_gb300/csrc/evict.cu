@@ -2,7 +2,7 @@
 // tokens per KV head, by accumulated attention weight.
 //
 // Of the slots s < len of one (request, head) the first `budget` in the order
-// (recent ones, then weight descending, then slot ascending) stay.  The kept
+// (recent ones by slot, then the others by weight descending and slot ascending) stay.  The kept
 // slots behind the budget then move into the holes below it, both in ascending
 // order: the holes and the movers are disjoint, so all moves are independent,
 // and tokens that already lie below the budget are not touched.
