@@ -196,7 +196,8 @@ struct Work {
     uint32_t *anc;
     size_t bytes;
 };
-Work carve(void *base, int B, int T, int Hq, int Hkv, int D) {
+// trees: rows may be draft trees' (their ancestor sets)
+Work carve(void *base, int B, int T, int Hq, int Hkv, int D, bool trees) {
     Work w{};
     const int tq = flash_tq(Hq / Hkv);
     const size_t grid = (size_t)flash_grid(), F = (size_t)max_phases(B, T, Hkv, tq);
@@ -209,7 +210,7 @@ Work carve(void *base, int B, int T, int Hq, int Hkv, int D) {
     a.ent_ctx = cv.take<int>(pairs);
     a.n_pairs = cv.take<int>(3);
     a.bound = cv.take<int4>(F * (grid + 1));
-    w.anc = cv.take<uint32_t>((size_t)T * kAncWords);
+    if (trees) w.anc = cv.take<uint32_t>((size_t)T * kAncWords);
     a.part_m = cv.take<float>(2 * grid * F * kFlRows);
     a.part_l = cv.take<float>(2 * grid * F * kFlRows);
     a.part_o = cv.take<float>(2 * grid * F * kFlRows * (size_t)D);
@@ -221,8 +222,8 @@ bool sizes_ok(int B, int T, int Hq, int Hkv, int D) {
     return B >= 0 && T >= 0 && Hkv >= 1 && Hq >= 1 && Hq % Hkv == 0 && Hq / Hkv <= kBM && (D == 64 || D == 128) && B <= kBatchMax;
 }
 
-size_t workspace_size(int B, int T, int Hq, int Hkv, int D) {
-    return sizes_ok(B, T, Hq, Hkv, D) ? carve(nullptr, B, T, Hq, Hkv, D).bytes : 0;
+size_t workspace_size(int B, int T, int Hq, int Hkv, int D, bool trees) {
+    return sizes_ok(B, T, Hq, Hkv, D) ? carve(nullptr, B, T, Hq, Hkv, D, trees).bytes : 0;
 }
 
 // The launches of both calls.  a: everything but what comes out of the sizes.
@@ -267,7 +268,7 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
 using namespace rs;
 
 extern "C" size_t rs_prompt_attn_workspace_size(int B, int T, int Hq, int Hkv, int D) {
-    return workspace_size(B, T, Hq, Hkv, D);
+    return workspace_size(B, T, Hq, Hkv, D, false);
 }
 
 extern "C" rs_status rs_prompt_attn(const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride,
@@ -285,7 +286,7 @@ extern "C" rs_status rs_prompt_attn(const uint16_t *q, int64_t q_stride, const u
     if ((st = check_stride(what, "v", v, v_stride, Hkv, D)) != RS_OK) return st;
     RS_CHECK_ARG((((uintptr_t)out | (uintptr_t)workspace) & 31) == 0, "%s: out and workspace must be 32-byte aligned", what);
     if (B == 0) return RS_OK;
-    Work w = carve(workspace, B, T, Hq, Hkv, D);
+    Work w = carve(workspace, B, T, Hq, Hkv, D, false);
     if (workspace_bytes < w.bytes || !workspace) {
         set_error("%s: workspace %zu bytes < %zu required", what, workspace_bytes, w.bytes);
         return RS_ERR_CAPACITY;
@@ -307,7 +308,7 @@ extern "C" rs_status rs_prompt_attn(const uint16_t *q, int64_t q_stride, const u
 }
 
 extern "C" size_t rs_paged_attn_workspace_size(int B, int T, int Hq, int Hkv, int D) {
-    return workspace_size(B, T, Hq, Hkv, D);
+    return workspace_size(B, T, Hq, Hkv, D, true);
 }
 
 extern "C" rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtype, const int32_t *new_off,
@@ -327,7 +328,7 @@ extern "C" rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtyp
     RS_CHECK_ARG((((uintptr_t)k_pages | (uintptr_t)v_pages) & 15) == 0, "%s: pages must be 16-byte aligned", what);
     RS_CHECK_ARG((((uintptr_t)out | (uintptr_t)workspace) & 31) == 0, "%s: out and workspace must be 32-byte aligned", what);
     if (B == 0) return RS_OK;
-    Work w = carve(workspace, B, T, Hq, Hkv, D);
+    Work w = carve(workspace, B, T, Hq, Hkv, D, true);
     if (workspace_bytes < w.bytes || !workspace) {
         set_error("%s: workspace %zu bytes < %zu required", what, workspace_bytes, w.bytes);
         return RS_ERR_CAPACITY;
