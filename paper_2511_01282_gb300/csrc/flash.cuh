@@ -52,8 +52,8 @@ namespace rs {
 
 constexpr int kFlThreads = 384;
 constexpr int kFlMmaWarp = 0, kFlTmaWarp = 2, kFlSoftWarp = 4;  // two warps issue products, two copy
-// (at D = 128 the product warps store 84 bytes of spilled registers with 56, 12 with 88;
-// the softmax warps' code is the same from 200 up)
+// (with 56 registers the product warps spill: 56 bytes at D = 128, with 88 12, and packed
+// prompts take 525 us for 518; the softmax warps' code is the same from 200 up)
 constexpr uint32_t kFlRegsSoft = 208, kFlRegsProd = 88;
 static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "register split");
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
@@ -480,44 +480,42 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             if (kApart && done > 0 && !wait(&sfree[x], done - 1, &sfree[x], done - 1)) break;
             issue_s(g);
             // of the piece's key tiles, those that some row of the row tile sees; the others go
-            // through without P V (a loop of their own: a condition in one loop cost a prompt
-            // of 16384 tokens 3 %)
+            // through without P V (by a predicate: a branch around it cost a prompt of 16384
+            // tokens 3 %)
             const int seen = (int)uniform((uint32_t)min(n, row_tiles(a, pc.n, pc.ctx, pc.p, x) - pc.j0));
-            auto step = [&](auto seen_t, int tl) {
-                constexpr bool kSeen = decltype(seen_t)::value;
+#pragma unroll 1
+            for (int tl = 0; tl < n; ++tl, ++done) {
                 const uint32_t t = g + tl, st = t % NV;
                 const bool more = tl + 1 < n;
                 if (kApart) {  // S of the next tile goes ahead of this one's P V
                     if (more) {
-                        if (!wait(&kfull[(t + 1) % NK], (t + 1) / NK, &sfree[x], done)) return;
+                        if (!wait(&kfull[(t + 1) % NK], (t + 1) / NK, &sfree[x], done)) break;
                         issue_s(t + 1);
                     }
-                    if (!wait(&vfull[st], t / NV, &pfull[x], done)) return;
+                    if (!wait(&vfull[st], t / NV, &pfull[x], done)) break;
                 } else {
                     // what does not depend on the softmax first; then P and, where both row
                     // tiles are at work, the turn: they alternate, so that one's softmax
                     // runs beside the other's products
                     const uint32_t tn = t + 1;
-                    if (!wait(&vfull[st], t / NV, more ? &kfull[tn % NK] : &vfull[st], more ? tn / NK : t / NV)) return;
+                    if (!wait(&vfull[st], t / NV, more ? &kfull[tn % NK] : &vfull[st], more ? tn / NK : t / NV)) break;
                     const bool must = pc.full && (x == 1 || turns > 0);
-                    if (!wait(&pfull[x], done, must ? &turn[x] : &pfull[x], must ? turns - (x == 0 ? 1 : 0) : done)) return;
+                    if (!wait(&pfull[x], done, must ? &turn[x] : &pfull[x], must ? turns - (x == 0 ? 1 : 0) : done)) break;
                 }
-                if (tl == 0 && pieces > 0 && !wait(&ofree[x], pieces - 1, &ofree[x], pieces - 1)) return;
+                if (tl == 0 && pieces > 0 && !wait(&ofree[x], pieces - 1, &ofree[x], pieces - 1)) break;
                 tc_fence_after();
                 const uint32_t v_lo = uniform(v_lo0 + st * kTileDesc);
 #pragma unroll
                 for (int part = 0; part < kParts; ++part) {
                     if (part > 0) {
-                        if (!wait(&pfull2[x], done, &pfull2[x], done)) return;
+                        if (!wait(&pfull2[x], done, &pfull2[x], done)) break;
                         tc_fence_after();
                     }
                     if (elect_one()) {
-                        if constexpr (kSeen) {
 #pragma unroll
-                            for (int ks = part * 8 / kParts; ks < (part + 1) * 8 / kParts; ++ks)
-                                umma_ts(o_tm, p_tm + ks * 8, desc_of(v_lo + (uint32_t)((ks * 2048) >> 4), d_hi), idO,
-                                        (tl > 0 || ks > 0) ? 1u : 0u);
-                        }
+                        for (int ks = part * 8 / kParts; ks < (part + 1) * 8 / kParts; ++ks)
+                            umma_ts_if(tl < seen, o_tm, p_tm + ks * 8, desc_of(v_lo + (uint32_t)((ks * 2048) >> 4), d_hi), idO,
+                                       (tl > 0 || ks > 0) ? 1u : 0u);
                         if (part == kParts - 1) {
                             umma_commit(&pvdone[x]);
                             umma_commit(&vempty[st]);
@@ -526,7 +524,7 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                     }
                     __syncwarp();
                 }
-                if (!ok) return;
+                if (!ok) break;
                 if (!kApart) {
                     if (more) issue_s(t + 1);
                     if (pc.full) {
@@ -535,12 +533,7 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                         ++turns;
                     }
                 }
-            };
-            int tl = 0;
-#pragma unroll 1
-            for (; ok && tl < seen; ++tl, ++done) step(std::true_type(), tl);
-#pragma unroll 1
-            for (; ok && tl < n; ++tl, ++done) step(std::false_type(), tl);
+            }
             ++pieces;
             g += n;
         }
