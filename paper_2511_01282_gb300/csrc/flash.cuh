@@ -26,7 +26,7 @@
 // Bound: long prompts at D = 128, the tensor cores (16384 tokens, 32 heads on 8: 1.48
 // ms, 1480 TFLOP/s); at D = 64, whose products are half as long, the softmax warps
 // (issue slots 52 % full, each warp's chain of wait, maximum, exponentials and store;
-// 16 prompts of up to 4095 tokens: 522 us, 725 TFLOP/s, a tenth of it segments'
+// 16 prompts of up to 4095 tokens: 518 us, 732 TFLOP/s, a tenth of it segments'
 // starts); single tokens, HBM (64 requests, 1.21 GB: 187 us, 6.5 TB/s); those of one
 // request, the latency of three launches (2048 keys: 19 us).
 //
