@@ -2,8 +2,8 @@
 
 A case is one call:
 
-  append8  ``rs_paged_append8``: keys and values of new tokens into e4m3 pages, an exponent of two for each 16 tokens and head
-  attend8  ``rs_paged_attn8``: a chunk of new tokens (a single one, a piece of a prompt, a draft tree) against those pages
+  append8  ``rs_coded_append``: keys and values of new tokens into e4m3 pages, an exponent of two for each 16 tokens and head
+  attend8  ``rs_coded_attn``: a chunk of new tokens (a single one, a piece of a prompt, a draft tree) against those pages
   rotary   ``rs_rotary``: queries and keys turned by their positions, or turned back (the gradient)
   copy     ``rs_pages_copy``: pages copied by a list of pairs, with all that the cache keeps about them
   compact  ``rs_pages_compact``: a pool's used pages moved below its free ones, page tables and reference counts renumbered
@@ -283,12 +283,12 @@ def _run_own(st):
         return dict(_pool(st, st["status"]), table=table, refs=refs, new_id=st["new_id"])
     cache = (st["kp"], st["vp"], st["ke"], st["ve"], st["pages"], c["page"], st["table"], st["most"], st["ctx"])
     if op == "append8":
-        rs.rs_paged_append8(st["k"], Hkv * D, st["v"], Hkv * D, dt, st["off"], c["B"], st["T"], Hkv, D, *cache, st["status"])
+        rs.rs_coded_append(st["k"], Hkv * D, st["v"], Hkv * D, dt, st["off"], c["B"], st["T"], Hkv, D, *cache, st["status"])
         return _pool(st, st["status"])
     Hq = c["Hq"]
     if "ws" not in st:
-        st["ws"] = torch.empty(rs.rs_paged_attn8_workspace_size(c["B"], st["T"], st["n_max"], Hq, Hkv, D), dtype=torch.uint8, device="cuda")
-    rs.rs_paged_attn8(st["q"], Hq * D, dt, st["off"], st["parents"], c["B"], st["T"], st["n_max"], Hq, Hkv, D, *cache, st["scale"], st["out"],
+        st["ws"] = torch.empty(rs.rs_coded_attn_workspace_size(c["B"], st["T"], st["n_max"], Hq, Hkv, D), dtype=torch.uint8, device="cuda")
+    rs.rs_coded_attn(st["q"], Hq * D, dt, st["off"], st["parents"], c["B"], st["T"], st["n_max"], Hq, Hkv, D, *cache, st["scale"], st["out"],
                       st["lse"], st["status"], st["ws"])
     return dict(out=st["out"], lse=st["lse"], status=st["status"])
 
