@@ -13,7 +13,9 @@
  * Around it: retrieval from an index (rs_match_index_*, rs_match_scan_indexed),
  * sampling verification (rs_tree_sample), and the cache: whole prompts
  * (rs_prompt_attn), a paged KV cache (rs_paged_append, rs_paged_attn) and its
- * bound by attention weight (rs_paged_weights, rs_paged_evict).
+ * bound by attention weight (rs_paged_weights, rs_paged_evict), the same cache in
+ * 8 bits (rs_coded_append, rs_coded_attn), rotary positions (rs_rotary), and its
+ * pages copied and closed up (rs_pages_copy, rs_pages_compact).
  *
  * General rules (every entry point):
  *   - All array arguments are DEVICE pointers owned by the caller, unless a
@@ -90,6 +92,10 @@ typedef enum {
 /* type of a 16-bit tensor (uint16_t bit patterns) */
 #define RS_BF16 0
 #define RS_F16  1
+
+/* which values of a head make a pair (rs_rotary), rot of them in all */
+#define RS_ROTARY_HALF        0  /* i and i + rot / 2 */
+#define RS_ROTARY_INTERLEAVED 1  /* 2 i and 2 i + 1   */
 
 /* -------------------------------------------------------------- parameters */
 /* Hyper-parameters of Algorithm 1 (its inputs), Eq. 6-7 and Section 3.4.
@@ -573,6 +579,114 @@ rs_status rs_paged_evict(uint16_t *k_pages, uint16_t *v_pages, int Hkv, int D, i
                          const int32_t *cache_len, const int32_t *next_pos, int B, int budget,
                          int recent, float *weights, int32_t *positions, int32_t *new_len,
                          int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ================================================= the cache in 8 bits ====
+ * k_codes and v_codes [n_pages, page_size, Hkv, D] hold e4m3 codes (16-byte
+ * aligned), k_exps and v_exps [n_pages, page_size / 16, Hkv] int8 an exponent for
+ * each block of 16 slots and head: value = code x 2^exponent.  page_size is a power
+ * of two from 16 to 65536; the page table, ctx_len and new_off are those of the
+ * cache in 16 bits.  Weights and positions are not kept: rs_paged_weights and
+ * rs_paged_evict take the cache in 16 bits only.
+ *
+ * Exponents lie within -117 .. 120 in a cache of bf16 values and within -15 .. 8 in
+ * one of fp16 values (outside, they count as the nearest of these): there code x
+ * 2^exponent is exact in that type (fp16 at exponent 8: codes up to 240).  A cache
+ * is read with the type that it was appended with.
+ */
+
+/* ==================================================== rs_coded_append ====
+ * New tokens enter the cache: row i of request b goes to slot ctx_len[b] + i.
+ * Per block of 16 slots and head, K and V each by themselves:
+ *     e    = the least exponent of the type's range with max |x| <= 448 x 2^e over
+ *            the block's new finite values; where slots of the block lie below
+ *            ctx_len[b] (their tokens stay), at least the block's exponent so far;
+ *     code = e4m3(x / 2^e), to nearest even; infinities and NaN become NaN; fp16 at
+ *            e = 8 stops at 240.
+ * Codes that stay in a block whose exponent grows become e4m3(code / 2^(growth)):
+ * exact, but for results below 2^-6, which round to steps of 2^-9.
+ *   k, v, strides, new_off, B, T, status: as for rs_paged_append (B <= 2^28);
+ *            dtype RS_BF16 or RS_F16.
+ */
+rs_status rs_coded_append(const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride, int dtype,
+                          const int32_t *new_off, int B, int T, int Hkv, int D, uint8_t *k_codes, uint8_t *v_codes,
+                          int8_t *k_exps, int8_t *v_exps, int n_pages, int page_size, const int32_t *page_table,
+                          int max_pages, const int32_t *ctx_len, int32_t *status, void *stream);
+
+/* ====================================================== rs_coded_attn ====
+ * rs_paged_attn over the cache in 8 bits: keys and values are code x 2^exponent,
+ * exactly.
+ *   max_new  no request has more new tokens than this (1 for single tokens): the
+ *            work is laid out by it.  A request that has more is rejected with
+ *            RS_ST_TOO_LARGE.  T where nothing better is known.
+ *   the rest as for rs_paged_attn.  Size the workspace with the same six sizes.
+ * Where max_new x Hq / Hkv <= 32, P is rounded to fp16 (2^-12 relative) and NaN in V
+ * of a key that a row does not see reaches it only within a block of 16 slots that
+ * it sees a part of; else as rs_paged_attn.  The result does not depend on what
+ * else runs: the same bits every time.
+ */
+size_t rs_coded_attn_workspace_size(int B, int T, int max_new, int Hq, int Hkv, int D);
+rs_status rs_coded_attn(const uint16_t *q, int64_t q_stride, int dtype, const int32_t *new_off,
+                        const int32_t *parents, int B, int T, int max_new, int Hq, int Hkv, int D,
+                        const uint8_t *k_codes, const uint8_t *v_codes, const int8_t *k_exps, const int8_t *v_exps,
+                        int n_pages, int page_size, const int32_t *page_table, int max_pages, const int32_t *ctx_len,
+                        float scale, uint16_t *out, float *lse, int32_t *status, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/* ========================================================== rs_rotary ====
+ * Rotary positions: every pair (x, y) of the first rot values of a head becomes
+ *     scale (x cos a - y sin a),  scale (y cos a + x sin a),  a = pos[row] f_i,
+ * for pair i = 0 .. rot / 2 - 1; the values behind rot are copied.  inverse != 0
+ * turns by -a: with the same scale that is the gradient.
+ *   q, q_out [T, Hq, D] and k, k_out [T, Hkv, D] of type dtype, each with its own
+ *            distance between rows (at least heads x D, a multiple of 8; 16-byte
+ *            aligned).  An output may be its input, with the same stride; other
+ *            overlaps are not allowed.  Hq or Hkv may be 0 (its pointers NULL).
+ *   D        a multiple of 8, up to 512; rot even, 2 .. D; layout RS_ROTARY_*.
+ *   pos      [T] int32, any values.
+ *   turns    [rot / 2] uint64: f_i / (2 pi) as a fraction of 2^64 (whole turns fall
+ *            away), so that pos x turns mod 2^64 is the angle without rounding.
+ *   scale    a magnitude (1 usually), finite.
+ * Computed in fp32 (the angle is off by 2^-24 of at most half a turn), rounded once.
+ */
+rs_status rs_rotary(const uint16_t *q, int64_t q_stride, uint16_t *q_out, int64_t q_out_stride, const uint16_t *k,
+                    int64_t k_stride, uint16_t *k_out, int64_t k_out_stride, int dtype, const int32_t *pos, int T,
+                    int Hq, int Hkv, int D, int rot, int layout, const uint64_t *turns, float scale, int inverse,
+                    void *stream);
+
+/* ====================================================== rs_pages_copy ====
+ * Pages of a pool copied: pairs [n, 2] int32 (from, to), 8-byte aligned.
+ *   bits     16: k_pages and v_pages as for rs_paged_append, k_exps and v_exps NULL;
+ *            8: codes and exponents as for rs_coded_append.
+ *   weights, positions: [Hkv, n_pages * page_size], or NULL.
+ *   status   [1]: RS_ST_BAD_PAGE where a pair names a page outside the pool: that
+ *            pair is left out.
+ * A page is the destination of one pair at most and of none that it is the source
+ * of (but of the pair of itself, which does nothing): else what such a page holds
+ * afterwards is not defined, nothing else.
+ */
+rs_status rs_pages_copy(void *k_pages, void *v_pages, int8_t *k_exps, int8_t *v_exps, float *weights, int32_t *positions,
+                        int bits, int Hkv, int D, int n_pages, int page_size, const int32_t *pairs, int n,
+                        int32_t *status, void *stream);
+
+/* =================================================== rs_pages_compact ====
+ * A pool closed up: its U used pages (refs > 0) come to lie in pages 0 .. U - 1.
+ * The r-th used page at U or above moves to the r-th free one below U; all others
+ * stay, and what pages from U on hold is left.
+ *   arrays, bits: as for rs_pages_copy.
+ *   page_table [B, max_pages] in/out: the first held[b] entries of request b get
+ *            their pages' new numbers.
+ *   refs     [n_pages] int32 in/out: how many table entries name the page; moves
+ *            with it (a page that has moved leaves 0).
+ *   new_id   [n_pages] int32 out: where each page is now, -1 for free ones.
+ *   status   [B]: RS_ST_BAD_OFFSET (held[b] outside 0 .. max_pages: its entries
+ *            stay), RS_ST_BAD_PAGE (an entry outside the pool or of a free page:
+ *            it stays, the others change).
+ */
+size_t rs_pages_compact_workspace_size(int n_pages);
+rs_status rs_pages_compact(void *k_pages, void *v_pages, int8_t *k_exps, int8_t *v_exps, float *weights,
+                           int32_t *positions, int bits, int Hkv, int D, int n_pages, int page_size, int32_t *page_table,
+                           int max_pages, const int32_t *held, int B, int32_t *refs, int32_t *new_id, int32_t *status,
+                           void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

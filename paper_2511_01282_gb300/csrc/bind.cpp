@@ -26,7 +26,7 @@
 #define RS_ENTRIES(X)                                                                                            \
     X(entropy_gate) X(entropy_gate_noalloc) X(entropy_gate_rows) X(match_scan) X(tree_verify_attn) X(accept)     \
     X(match_index_build) X(match_index_append) X(match_scan_indexed) X(tree_sample) X(prompt_attn) X(paged_append)  \
-    X(paged_attn) X(paged_weights) X(paged_evict)
+    X(paged_attn) X(paged_weights) X(paged_evict) X(coded_append) X(coded_attn) X(rotary) X(pages_copy) X(pages_compact)
 
 namespace {
 
@@ -587,6 +587,120 @@ RS_BIND(paged_evict) {
         return [=] {
             return lib.paged_evict(kp, vp, Hkv, D, pages, size, table, most, len, next, B, budget, recent, weights, positions, new_len,
                                    status, ws, wb, st);
+        };
+    });
+}
+
+// The arrays of a pool of pages, as the two calls below take them.
+struct PoolArgs {
+    void *k, *v;
+    int8_t *ke, *ve;
+    float *weights;
+    int32_t *positions;
+    int bits, Hkv, D, pages, size;
+    explicit PoolArgs(Args &a)
+        : k(a.ptr<void>()), v(a.ptr<void>()), ke(a.ptr<int8_t>()), ve(a.ptr<int8_t>()), weights(a.ptr<float>()),
+          positions(a.ptr<int32_t>()), bits(a.i32()), Hkv(a.i32()), D(a.i32()), pages(a.i32()), size(a.i32()) {}
+};
+
+RS_BIND(coded_append) {
+    return guarded(v, n, [](Args &a) {
+        int64_t ks, vs;
+        auto *k = a.rows(&ks), *vv = a.rows(&vs);
+        const int dtype = a.i32();
+        auto *off = a.ptr<const int32_t>();
+        const int B = a.i32(), T = a.i32(), Hkv = a.i32(), D = a.i32();
+        auto *kp = a.ptr<uint8_t>(), *vp = a.ptr<uint8_t>();
+        auto *ke = a.ptr<int8_t>(), *ve = a.ptr<int8_t>();
+        const int pages = a.i32(), size = a.i32();
+        auto *table = a.ptr<const int32_t>();
+        const int most = a.i32();
+        auto *ctx = a.ptr<const int32_t>();
+        auto *status = a.ptr<int32_t>();
+        void *st = a.stream();
+        a.on_current_device();
+        return [=] {
+            return lib.coded_append(k, ks, vv, vs, dtype, off, B, T, Hkv, D, kp, vp, ke, ve, pages, size, table, most, ctx, status, st);
+        };
+    });
+}
+
+RS_BIND(coded_attn) {
+    return guarded(v, n, [](Args &a) {
+        int64_t qs;
+        auto *q = a.rows(&qs);
+        const int dtype = a.i32();
+        auto *off = a.ptr<const int32_t>(), *parents = a.ptr<const int32_t>();
+        const int B = a.i32(), T = a.i32(), max_new = a.i32(), Hq = a.i32(), Hkv = a.i32(), D = a.i32();
+        auto *kp = a.ptr<const uint8_t>(), *vp = a.ptr<const uint8_t>();
+        auto *ke = a.ptr<const int8_t>(), *ve = a.ptr<const int8_t>();
+        const int pages = a.i32(), size = a.i32();
+        auto *table = a.ptr<const int32_t>();
+        const int most = a.i32();
+        auto *ctx = a.ptr<const int32_t>();
+        const float scale = a.f32();
+        auto *out = a.ptr<uint16_t>();
+        auto *lse = a.ptr<float>();
+        auto *status = a.ptr<int32_t>();
+        size_t wb;
+        void *ws = a.sized(&wb, true), *st = a.stream();
+        a.on_current_device();
+        return [=] {
+            return lib.coded_attn(q, qs, dtype, off, parents, B, T, max_new, Hq, Hkv, D, kp, vp, ke, ve, pages, size, table, most, ctx,
+                                  scale, out, lse, status, ws, wb, st);
+        };
+    });
+}
+
+RS_BIND(rotary) {
+    return guarded(v, n, [](Args &a) {
+        int64_t qs, qos, ks, kos;
+        auto *q = a.rows(&qs);
+        auto *qo = const_cast<uint16_t *>(a.rows(&qos));
+        auto *k = a.rows(&ks);
+        auto *ko = const_cast<uint16_t *>(a.rows(&kos));
+        const int dtype = a.i32();
+        auto *pos = a.ptr<const int32_t>();
+        const int T = a.i32(), Hq = a.i32(), Hkv = a.i32(), D = a.i32(), rot = a.i32(), layout = a.i32();
+        auto *turns = a.ptr<const uint64_t>();
+        const float scale = a.f32();
+        const int inverse = a.i32();
+        void *st = a.stream();
+        a.on_current_device();
+        return [=] {
+            return lib.rotary(q, qs, qo, qos, k, ks, ko, kos, dtype, pos, T, Hq, Hkv, D, rot, layout, turns, scale, inverse, st);
+        };
+    });
+}
+
+RS_BIND(pages_copy) {
+    return guarded(v, n, [](Args &a) {
+        const PoolArgs p(a);
+        auto *pairs = a.ptr<const int32_t>();
+        const int count = a.i32();
+        auto *status = a.ptr<int32_t>();
+        void *st = a.stream();
+        a.on_current_device();
+        return [=] {
+            return lib.pages_copy(p.k, p.v, p.ke, p.ve, p.weights, p.positions, p.bits, p.Hkv, p.D, p.pages, p.size, pairs, count, status, st);
+        };
+    });
+}
+
+RS_BIND(pages_compact) {
+    return guarded(v, n, [](Args &a) {
+        const PoolArgs p(a);
+        auto *table = a.ptr<int32_t>();
+        const int most = a.i32();
+        auto *held = a.ptr<const int32_t>();
+        const int B = a.i32();
+        auto *refs = a.ptr<int32_t>(), *new_id = a.ptr<int32_t>(), *status = a.ptr<int32_t>();
+        size_t wb;
+        void *ws = a.sized(&wb, true), *st = a.stream();
+        a.on_current_device();
+        return [=] {
+            return lib.pages_compact(p.k, p.v, p.ke, p.ve, p.weights, p.positions, p.bits, p.Hkv, p.D, p.pages, p.size, table, most, held, B,
+                                     refs, new_id, status, ws, wb, st);
         };
     });
 }

@@ -1,0 +1,58 @@
+// coded.cuh -- the 8-bit KV cache's number format: e4m3 codes with an exponent
+// of two for each block of 16 tokens and KV head, value = code 2^e.
+//
+// A power of two and not any scale: codes of a floating type lose nothing by it
+// (their step is relative to the value), code 2^e is exact in bf16 and, within the
+// exponents that an fp16 cache has, in fp16, so that products take the values as
+// they are; and when a later token raises a block's exponent the codes that are
+// there shift without rounding, but for those that fall among the subnormals.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace rs {
+
+constexpr int kCodeBlock = 16, kCodeBlockLog2 = 4;  // tokens that share an exponent
+
+// Exponents that values of a type get: 2^e x code has to be representable, from the
+// smallest step (2^-9 x 2^e) on.  An fp16 cache at e = 8 stops at code 240 (61440; a
+// larger one, 256 = 65536, is above fp16's largest value).
+__host__ __device__ constexpr int code_exp_min(bool bf16) { return bf16 ? -117 : -15; }
+__host__ __device__ constexpr int code_exp_max(bool bf16) { return bf16 ? 120 : 8; }
+__device__ __forceinline__ int code_exp(int e, bool bf16) { return min(max(e, code_exp_min(bf16)), code_exp_max(bf16)); }
+
+// 2^e for -126 <= e <= 127
+__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// two codes (the low 16 bits) -> fp16, exact; NaN stays NaN
+__device__ __forceinline__ uint32_t decode2(uint32_t two) {
+    uint32_t h;
+    asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(h) : "r"(two));
+    return h;
+}
+// the low and the high two of four codes
+__device__ __forceinline__ void decode4(uint32_t four, uint32_t &lo, uint32_t &hi) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(four));
+}
+// (lo, hi) -> two codes, to nearest even; NaN -> NaN
+__device__ __forceinline__ uint32_t encode2(float lo, float hi) {
+    uint32_t c;
+    asm("{\n\t.reg .b16 c;\n\tcvt.rn.satfinite.e4m3x2.f32 c, %1, %2;\n\tcvt.u32.u16 %0, c;\n\t}" : "=r"(c) : "f"(hi), "f"(lo));
+    return c;
+}
+
+// The pool and its page table.  Codes [n_pages, page_size, Hkv, D]; exponents
+// [n_pages, page_size / 16, Hkv].
+struct CodedPool {
+    uint8_t *k, *v;
+    int8_t *ke, *ve;
+    const int32_t *table, *ctx;
+    int n_pages, page_log2, max_pages;
+};
+
+}  // namespace rs

@@ -1,5 +1,5 @@
-// flash.cu -- rs_prompt_attn and rs_paged_attn: the plan of the work and the
-// host side of the attention core (flash.cuh).
+// flash.cu -- rs_prompt_attn and rs_paged_attn (and rs_coded_attn's long chunks): the
+// plan of the work and the host side of the attention core (flash.cuh).
 // Launches: flash_plan (one CTA, and one per request for draft trees) ->
 // flash_kernel (a CTA per SM) -> flash_combine.
 #include <cudaTypedefs.h>
@@ -10,6 +10,7 @@
 
 #include "common.cuh"
 #include "flash.cuh"
+#include "flash_coded.h"
 #include "tmap.cuh"
 
 namespace rs {
@@ -58,7 +59,7 @@ __device__ __forceinline__ int check_rows(const FlashArgs &a, int b, int4 &rq) {
     if (n0 < 0 || n1 < n0 || n1 > a.T) return RS_ST_BAD_OFFSET;
     rq = make_int4(n0, 0, 0, n1 - n0);
     if (ctx < 0 || (a.page_table && (long long)ctx + (n1 - n0) > ((long long)a.max_pages << a.page_log2))) return RS_ST_BAD_OFFSET;
-    if (a.anc && n1 - n0 > RS_MAX_NODES) return RS_ST_TOO_LARGE;
+    if (n1 - n0 > a.max_new || (a.anc && n1 - n0 > RS_MAX_NODES)) return RS_ST_TOO_LARGE;
     rq = make_int4(n0, n1 - n0, ctx, n1 - n0);
     return 0;
 }
@@ -226,11 +227,13 @@ size_t workspace_size(int B, int T, int Hq, int Hkv, int D, bool trees) {
     return sizes_ok(B, T, Hq, Hkv, D) ? carve(nullptr, B, T, Hq, Hkv, D, trees).bytes : 0;
 }
 
-// The launches of both calls.  a: everything but what comes out of the sizes.
+// The launches of the calls.  a: everything but what comes out of the sizes.  k and v
+// null: the cache in 8 bits.
 rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, int64_t q_stride, const void *k,
                     int64_t k_stride, const void *v, int64_t v_stride, long long kv_rows, const int32_t *parents,
                     cudaStream_t st) {
     FlashArgs &a = w.a;
+    const bool coded = !k;
     const int type = dtype == RS_BF16;
     a.G = a.Hq / a.Hkv;
     a.tq = flash_tq(a.G);
@@ -239,7 +242,8 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     a.single = fl_single(D);
     a.start = fl_start(D);
     a.wait_limit = wait_limit();
-    const double bytes = 4.0 * (double)kv_rows * a.Hkv * D;
+    const double token = (coded ? 2.0 : 4.0) * a.Hkv * D;  // bytes
+    const double bytes = token * (double)kv_rows;
     a.kv_stream = bytes > 0.5 * (double)l2_bytes();
     a.max_phases = bytes > 1.5 * (double)l2_bytes() ? max_phases(a.B, a.T, a.Hkv, a.tq) : 1;
     // rows of a segment, by the average request, and how many of them a block of eight warps joins
@@ -248,21 +252,48 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     const int box = a.page_table ? std::min(1 << a.page_log2, kBN) : kBN;
     CUtensorMap tmq, tmk, tmv;
     if (!rows_map(&tmq, q, type, D, a.Hq, a.T, q_stride, a.G, a.tq) ||
-        !rows_map(&tmk, k, type, D, a.Hkv, kv_rows, k_stride, 1, box) ||
-        !rows_map(&tmv, v, type, D, a.Hkv, kv_rows, v_stride, 1, box)) {
+        (!coded && (!rows_map(&tmk, k, type, D, a.Hkv, kv_rows, k_stride, 1, box) ||
+                    !rows_map(&tmv, v, type, D, a.Hkv, kv_rows, v_stride, 1, box)))) {
         set_error("%s: cuTensorMapEncodeTiled failed", what);
         return RS_ERR_CUDA;
     }
     // a thread per request and per pair, as far as a block goes (fewer warps, shorter barriers)
     const int wide = std::max(a.B, a.T / (2 * a.tq) + a.B);
     const int threads = std::min(std::max((wide + 31) / 32 * 32, parents ? RS_MAX_NODES : 32), kPlanThreads);
-    launch_pdl(flash_plan, dim3(1 + (parents ? a.B : 0)), dim3(threads), 0, st, a, parents, w.anc, 4.0 * a.Hkv * D,
+    launch_pdl(flash_plan, dim3(1 + (parents ? a.B : 0)), dim3(threads), 0, st, a, parents, w.anc, token,
                (double)l2_bytes());
     RS_CHECK_LAUNCH(what);
+    if (coded) return type ? flash_launch_coded<true>(a, D, tmq, what, st) : flash_launch_coded<false>(a, D, tmq, what, st);
     return type ? flash_launch<true>(a, D, tmq, tmk, tmv, what, st) : flash_launch<false>(a, D, tmq, tmk, tmv, what, st);
 }
 
 }  // namespace
+
+size_t flash_coded_workspace(int B, int T, int Hq, int Hkv, int D) { return workspace_size(B, T, Hq, Hkv, D, true); }
+
+rs_status flash_coded(const char *what, const FlashCoded &f, const CodedPool &pool, cudaStream_t st) {
+    Work w = carve(f.workspace, f.B, f.T, f.Hq, f.Hkv, f.D, true);
+    FlashArgs &a = w.a;
+    a.off = f.off;
+    a.ctx = pool.ctx;
+    a.page_table = pool.table;
+    a.max_pages = pool.max_pages;
+    a.n_pages = pool.n_pages;
+    a.page_log2 = pool.page_log2;
+    a.coded = pool;
+    a.B = f.B;
+    a.T = f.T;
+    a.max_new = f.max_new;
+    a.Hq = f.Hq;
+    a.Hkv = f.Hkv;
+    a.scale = f.scale;
+    a.out = f.out;
+    a.lse = f.lse;
+    a.status = f.status;
+    return flash_run(what, w, f.dtype, f.D, f.T ? f.q : f.workspace, f.q_stride, nullptr, 0, nullptr, 0,
+                     (long long)pool.n_pages << pool.page_log2, f.parents, st);
+}
+
 }  // namespace rs
 
 using namespace rs;
@@ -295,6 +326,7 @@ extern "C" rs_status rs_prompt_attn(const uint16_t *q, int64_t q_stride, const u
     a.off = seq_off;
     a.B = B;
     a.T = T;
+    a.max_new = T;
     a.Hq = Hq;
     a.Hkv = Hkv;
     a.scale = scale;
@@ -343,6 +375,7 @@ extern "C" rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtyp
     a.page_log2 = page_log2(page_size);
     a.B = B;
     a.T = T;
+    a.max_new = T;
     a.Hq = Hq;
     a.Hkv = Hkv;
     a.scale = scale;

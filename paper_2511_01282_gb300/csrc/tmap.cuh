@@ -91,6 +91,15 @@ inline rs_status check_pages(const char *what, int n_pages, int page_size, int m
     return RS_OK;
 }
 
+// The same of an 8-bit cache: a page holds whole blocks of 16 tokens.
+inline rs_status check_coded_pages(const char *what, int n_pages, int page_size, int max_pages) {
+    if (page_size == 8) {
+        set_error("%s: page size 8 unsupported (a power of two, 16 to 65536)", what);
+        return RS_ERR_UNSUPPORTED;
+    }
+    return check_pages(what, n_pages, page_size, max_pages);
+}
+
 // Clock cycles a pipeline wait may take; RS_DEBUG_WAIT_LIMIT (a test hook)
 // shortens it so that the time-out path can be exercised.
 inline long long wait_limit() {

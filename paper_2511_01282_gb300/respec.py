@@ -23,6 +23,7 @@ RS_OK, RS_ERR_INVALID_ARG, RS_ERR_UNSUPPORTED, RS_ERR_CAPACITY, RS_ERR_CUDA = ra
 RS_ST_BAD_TREE, RS_ST_TRUNCATED, RS_ST_BAD_POS, RS_ST_TOO_LARGE, RS_ST_TIMEOUT = 1, 2, 4, 8, 16
 RS_ST_BAD_OFFSET, RS_ST_BAD_PAGE = 32, 64
 RS_BF16, RS_F16 = 0, 1
+RS_ROTARY_HALF, RS_ROTARY_INTERLEAVED = 0, 1
 RS_MAX_L, RS_MAX_TOPC, RS_MAX_SPAN, RS_MAX_BETA, RS_MAX_NODES = 8, 8, 256, 16, 256
 
 
@@ -94,6 +95,15 @@ _SIGS = {
     "rs_paged_evict": (C.c_int, [_P] * 2 + [C.c_int] * 4 + [_P, C.c_int] + [_P] * 2 + [C.c_int] * 3 + [_P] * 5
                        + [C.c_size_t, _P]),
     "rs_entropy_gate_rows": (C.c_int, [_P, _P, _P, C.c_int, rs_params, _P, _P, _P, _P, _P, _P]),
+    "rs_coded_append": (C.c_int, [_P, C.c_int64] * 2 + [C.c_int, _P] + [C.c_int] * 4 + [_P] * 4 + [C.c_int] * 2
+                        + [_P, C.c_int] + [_P] * 3),
+    "rs_coded_attn_workspace_size": (C.c_size_t, [C.c_int] * 6),
+    "rs_coded_attn": (C.c_int, [_P, C.c_int64, C.c_int] + [_P] * 2 + [C.c_int] * 6 + [_P] * 4 + [C.c_int] * 2
+                      + [_P, C.c_int, _P, C.c_float] + [_P] * 4 + [C.c_size_t, _P]),
+    "rs_rotary": (C.c_int, [_P, C.c_int64] * 4 + [C.c_int, _P] + [C.c_int] * 6 + [_P, C.c_float, C.c_int, _P]),
+    "rs_pages_copy": (C.c_int, [_P] * 6 + [C.c_int] * 5 + [_P, C.c_int] + [_P] * 2),
+    "rs_pages_compact_workspace_size": (C.c_size_t, [C.c_int]),
+    "rs_pages_compact": (C.c_int, [_P] * 6 + [C.c_int] * 5 + [_P, C.c_int, _P, C.c_int] + [_P] * 4 + [C.c_size_t, _P]),
 }
 
 
@@ -296,3 +306,45 @@ def rs_paged_evict(k_pages, v_pages, Hkv, D, n_pages, page_size, page_table, max
     _check((_bind or _native()).rs_paged_evict(k_pages, v_pages, Hkv, D, n_pages, page_size, page_table,
                                                max_pages, cache_len, next_pos, B, budget, recent, weights,
                                                positions, new_len, status, workspace, stream))
+
+
+def rs_coded_append(k, k_stride, v, v_stride, dtype, new_off, B, T, Hkv, D, k_codes, v_codes, k_exps, v_exps, n_pages, page_size,
+                    page_table, max_pages, ctx_len, status, stream=None):
+    _check((_bind or _native()).rs_coded_append(k, k_stride, v, v_stride, dtype, new_off, B, T, Hkv, D, k_codes, v_codes,
+                                                k_exps, v_exps, n_pages, page_size, page_table, max_pages, ctx_len, status,
+                                                stream))
+
+
+def rs_coded_attn_workspace_size(B, T, max_new, Hq, Hkv, D):
+    return int(lib().rs_coded_attn_workspace_size(B, T, max_new, Hq, Hkv, D))
+
+
+def rs_coded_attn(q, q_stride, dtype, new_off, parents, B, T, max_new, Hq, Hkv, D, k_codes, v_codes, k_exps, v_exps, n_pages,
+                  page_size, page_table, max_pages, ctx_len, scale, out, lse, status, workspace, stream=None):
+    _check((_bind or _native()).rs_coded_attn(q, q_stride, dtype, new_off, parents, B, T, max_new, Hq, Hkv, D, k_codes,
+                                              v_codes, k_exps, v_exps, n_pages, page_size, page_table, max_pages, ctx_len,
+                                              scale, out, lse, status, workspace, stream))
+
+
+def rs_rotary(q, q_stride, q_out, q_out_stride, k, k_stride, k_out, k_out_stride, dtype, pos, T, Hq, Hkv, D, rot, layout, turns,
+              scale, inverse, stream=None):
+    """q, k and the outputs may be parts of wider rows, as for rs_prompt_attn; turns holds 64-bit words (int64 will do)."""
+    _check((_bind or _native()).rs_rotary(q, q_stride, q_out, q_out_stride, k, k_stride, k_out, k_out_stride, dtype, pos, T,
+                                          Hq, Hkv, D, rot, layout, turns, scale, inverse, stream))
+
+
+def rs_pages_copy(k_pages, v_pages, k_exps, v_exps, weights, positions, bits, Hkv, D, n_pages, page_size, pairs, n, status,
+                  stream=None):
+    _check((_bind or _native()).rs_pages_copy(k_pages, v_pages, k_exps, v_exps, weights, positions, bits, Hkv, D, n_pages,
+                                              page_size, pairs, n, status, stream))
+
+
+def rs_pages_compact_workspace_size(n_pages):
+    return int(lib().rs_pages_compact_workspace_size(n_pages))
+
+
+def rs_pages_compact(k_pages, v_pages, k_exps, v_exps, weights, positions, bits, Hkv, D, n_pages, page_size, page_table,
+                     max_pages, held, B, refs, new_id, status, workspace, stream=None):
+    _check((_bind or _native()).rs_pages_compact(k_pages, v_pages, k_exps, v_exps, weights, positions, bits, Hkv, D, n_pages,
+                                                 page_size, page_table, max_pages, held, B, refs, new_id, status, workspace,
+                                                 stream))
