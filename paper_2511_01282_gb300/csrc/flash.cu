@@ -227,13 +227,12 @@ size_t workspace_size(int B, int T, int Hq, int Hkv, int D, bool trees) {
     return sizes_ok(B, T, Hq, Hkv, D) ? carve(nullptr, B, T, Hq, Hkv, D, trees).bytes : 0;
 }
 
-// The launches of the calls.  a: everything but what comes out of the sizes.  k and v
-// null: the cache in 8 bits.
+// The launches of the calls.  a: everything but what comes out of the sizes (coded: of
+// the cache in 8 bits, k and v its codes).
 rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, int64_t q_stride, const void *k,
                     int64_t k_stride, const void *v, int64_t v_stride, long long kv_rows, const int32_t *parents,
-                    cudaStream_t st) {
+                    bool coded, cudaStream_t st) {
     FlashArgs &a = w.a;
-    const bool coded = !k;
     const int type = dtype == RS_BF16;
     a.G = a.Hq / a.Hkv;
     a.tq = flash_tq(a.G);
@@ -252,8 +251,8 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     const int box = a.page_table ? std::min(1 << a.page_log2, kBN) : kBN;
     CUtensorMap tmq, tmk, tmv;
     if (!rows_map(&tmq, q, type, D, a.Hq, a.T, q_stride, a.G, a.tq) ||
-        (!coded && (!rows_map(&tmk, k, type, D, a.Hkv, kv_rows, k_stride, 1, box) ||
-                    !rows_map(&tmv, v, type, D, a.Hkv, kv_rows, v_stride, 1, box)))) {
+        !(coded ? codes_map(&tmk, k, D, a.Hkv, kv_rows, box) : rows_map(&tmk, k, type, D, a.Hkv, kv_rows, k_stride, 1, box)) ||
+        !(coded ? codes_map(&tmv, v, D, a.Hkv, kv_rows, box) : rows_map(&tmv, v, type, D, a.Hkv, kv_rows, v_stride, 1, box))) {
         set_error("%s: cuTensorMapEncodeTiled failed", what);
         return RS_ERR_CUDA;
     }
@@ -263,7 +262,7 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     launch_pdl(flash_plan, dim3(1 + (parents ? a.B : 0)), dim3(threads), 0, st, a, parents, w.anc, token,
                (double)l2_bytes());
     RS_CHECK_LAUNCH(what);
-    if (coded) return type ? flash_launch_coded<true>(a, D, tmq, what, st) : flash_launch_coded<false>(a, D, tmq, what, st);
+    if (coded) return type ? flash_launch_coded<true>(a, D, tmq, tmk, tmv, what, st) : flash_launch_coded<false>(a, D, tmq, tmk, tmv, what, st);
     return type ? flash_launch<true>(a, D, tmq, tmk, tmv, what, st) : flash_launch<false>(a, D, tmq, tmk, tmv, what, st);
 }
 
@@ -290,8 +289,8 @@ rs_status flash_coded(const char *what, const FlashCoded &f, const CodedPool &po
     a.out = f.out;
     a.lse = f.lse;
     a.status = f.status;
-    return flash_run(what, w, f.dtype, f.D, f.T ? f.q : f.workspace, f.q_stride, nullptr, 0, nullptr, 0,
-                     (long long)pool.n_pages << pool.page_log2, f.parents, st);
+    return flash_run(what, w, f.dtype, f.D, f.T ? f.q : f.workspace, f.q_stride, pool.n_pages ? pool.k : f.workspace, 0,
+                     pool.n_pages ? pool.v : f.workspace, 0, (long long)pool.n_pages << pool.page_log2, f.parents, true, st);
 }
 
 }  // namespace rs
@@ -336,7 +335,7 @@ extern "C" rs_status rs_prompt_attn(const uint16_t *q, int64_t q_stride, const u
     // no rows: nothing is read, the maps only need some address
     const void *any = workspace;
     return flash_run(what, w, dtype, D, T ? q : any, q_stride, T ? k : any, k_stride, T ? v : any, v_stride, T, nullptr,
-                     (cudaStream_t)stream);
+                     false, (cudaStream_t)stream);
 }
 
 extern "C" size_t rs_paged_attn_workspace_size(int B, int T, int Hq, int Hkv, int D) {
@@ -385,5 +384,5 @@ extern "C" rs_status rs_paged_attn(const uint16_t *q, int64_t q_stride, int dtyp
     const void *any = workspace;
     const int64_t row = (int64_t)Hkv * D;
     return flash_run(what, w, dtype, D, T ? q : any, q_stride, n_pages ? k_pages : any, row, n_pages ? v_pages : any, row,
-                     (long long)n_pages * page_size, parents, (cudaStream_t)stream);
+                     (long long)n_pages * page_size, parents, false, (cudaStream_t)stream);
 }

@@ -57,10 +57,6 @@ constexpr int kFlMmaWarp = 0, kFlTmaWarp = 2, kFlSoftWarp = 4;  // two warps iss
 // prompts take 525 us for 518; the softmax warps' code is the same from 200 up)
 constexpr uint32_t kFlRegsSoft = 208, kFlRegsProd = 88;
 static_assert(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd == kFlThreads * 168, "register split");
-// over a cache in 8 bits four more warps turn codes into the 16-bit tiles
-constexpr int kFlCodedThreads = 512, kFlDecodeWarp = 12;
-constexpr uint32_t kFlCodedSoft = 168, kFlCodedProd = 64, kFlCodedDecode = 112;
-static_assert(2 * 128 * kFlCodedSoft + 128 * (kFlCodedProd + kFlCodedDecode) == kFlCodedThreads * 128, "register split");
 constexpr int kFlMaxPhases = 4;   // groups of KV heads
 constexpr int kFlRows = 2 * kBM;  // rows of a segment and of a partial slot
 // What a CTA's time goes to, in eighths of a key tile of a pair: a key tile where
@@ -274,39 +270,8 @@ struct FlSmem {
     static_assert(kTotal <= 232448, "shared memory of one CTA");
 };
 
-// Four codes (values c 2^e, e in both halves of `two_e`, 16 bits) as four 16-bit
-// values; exact.
-template <bool BF16>
-__device__ __forceinline__ uint2 decode16(uint32_t four, uint32_t two_e) {
-    uint2 h;
-    decode4(four, h.x, h.y);
-    if (BF16) {
-        const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&h.x));
-        const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&h.y));
-        h.x = pack_bf16x2(a.x, a.y);
-        h.y = pack_bf16x2(b.x, b.y);
-        asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(h.x) : "r"(two_e));
-        asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(h.y) : "r"(two_e));
-    } else {
-        asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h.x) : "r"(two_e));
-        asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h.y) : "r"(two_e));
-    }
-    return h;
-}
-// 2^e as a 16-bit value, in both halves
-template <bool BF16>
-__device__ __forceinline__ uint32_t two_to(int e) {
-    const uint32_t h = BF16 ? (uint32_t)(e + 127) << 7 : (e >= -14 ? (uint32_t)(e + 15) << 10 : 0x200u);  // (2^-15: subnormal)
-    return h | h << 16;
-}
-__device__ __forceinline__ uint4 load_once(const uint8_t *p) {
-    uint4 r;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
-    return r;
-}
-
-template <int D, bool BF16, bool CODED>
-__global__ void __launch_bounds__(CODED ? kFlCodedThreads : kFlThreads, 1)
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kFlThreads, 1)
 flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_constant__ CUtensorMap tmk,
              const __grid_constant__ CUtensorMap tmv) {
     using namespace sm100;
@@ -329,11 +294,11 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         for (int s = 0; s < (int)NK; ++s) {
-            mbar_init(&kfull[s], CODED ? 128 : 1);
+            mbar_init(&kfull[s], 1);
             mbar_init(&kempty[s], 2);  // one for each row tile
         }
         for (int s = 0; s < (int)NV; ++s) {
-            mbar_init(&vfull[s], CODED ? 128 : 1);
+            mbar_init(&vfull[s], 1);
             mbar_init(&vempty[s], 2);
         }
         for (int x = 0; x < 2; ++x) {
@@ -354,10 +319,8 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
     if (warp == kFlMmaWarp) tmem_alloc(s_tmem, kTmemCols);
     if (warp == kFlTmaWarp && lane == 0) {
         prefetch_tmap(&tmq);
-        if (!CODED) {
-            prefetch_tmap(&tmk);
-            prefetch_tmap(&tmv);
-        }
+        prefetch_tmap(&tmk);
+        prefetch_tmap(&tmv);
     }
     pdl_wait_prev();
     pdl_launch_next();
@@ -385,32 +348,8 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
     FlPiece pc;
 
     if (warp < kFlSoftWarp) {
-      reg_dealloc<CODED ? kFlCodedProd : kFlRegsProd>();
-      if (CODED && warp >= kFlTmaWarp) {
-        // ---------------------------------------------------------- Q tiles alone
-        const uint32_t q_tx = (uint32_t)(tq * G) * D * 2;
-        uint32_t quse[2] = {0, 0};
-        bool ok = warp == kFlTmaWarp;
-        while (ok && cur.next(pc)) {
-            for (int x = 0; x < (pc.full ? 2 : 1); ++x) {
-                if (quse[x] > 0 && !(ok = warp_wait(&qfree[x], (quse[x] - 1) & 1, s_abort, a.wait_limit))) break;
-                ++quse[x];
-                if (lane == 0) {
-                    mbar_expect_tx(&qfull[x], q_tx);
-#pragma unroll
-                    for (int kb = 0; kb < kKB; ++kb)
-                        tma_load_3d(smem + S::kQ + x * S::kTile + kb * 16384, &tmq, &qfull[x], kb * 64, pc.kvh * G,
-                                    pc.n0 + (pc.p * 2 + x) * tq);
-                }
-                __syncwarp();
-            }
-        }
-        if (!ok && warp == kFlTmaWarp) {  // let the copies already issued land before the CTA exits
-            volatile int no_abort = 0;
-            for (int x = 0; x < 2; ++x)
-                if (quse[x] > 0) mbar_wait(&qfull[x], (quse[x] - 1) & 1, &no_abort, kWaitLimit);
-        }
-      } else if (warp >= kFlTmaWarp) {
+      reg_dealloc<kFlRegsProd>();
+      if (warp >= kFlTmaWarp) {
         // ---------------------------------------------------------- TMA producers
         // One warp for K (and Q), one for V.  Whole warps: in a paged cache lane x
         // copies page x of the tile (a copy takes a warp some 75 cycles to issue, and
@@ -617,8 +556,8 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             mbar_wait(&drain[x], 0, &no_abort, kWaitLimit);
         }
       }
-    } else if (!CODED || warp < kFlDecodeWarp) {
-        reg_alloc<CODED ? kFlCodedSoft : kFlRegsSoft>();
+    } else {
+        reg_alloc<kFlRegsSoft>();
         // ---------------------------------------------------------- softmax / epilogue (rows)
         const int x = (warp - kFlSoftWarp) >> 2;  // row tile of this warpgroup
         const int r = tid & (kBM - 1);  // row of the tile == tensor memory lane
@@ -666,7 +605,7 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
                 tc_fence_after();
                 // the piece's last S has read Q: its buffer is free
                 if (tl == n - 1) warp_arrive(&qfree[x]);
-                if (!CODED && key0 + kBN > pc.keys) {
+                if (key0 + kBN > pc.keys) {
                     // slots behind the last key hold anything, NaN too: their V rows are zeroed (by
                     // each row tile for its own product)
                     if (!(ok = quick_wait(&vfull[t % NV], (t / NV) & 1, s_abort, a.wait_limit))) return false;
@@ -821,92 +760,6 @@ flash_kernel(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_
             warp_arrive(&ofree[x]);
             g += n;
         }
-    } else {
-        reg_dealloc<kFlCodedDecode>();
-        // ---------------------------------------------------------- codes to tiles
-        // The four warps decode a K tile, then a V tile, each a quarter of its rows; the next
-        // tile's codes are on the way meanwhile.  A lane has 16 codes of a row (32 bytes of the
-        // tile); step i of a warp lies in one block of 16 slots, whose number in the pool and
-        // exponents lane i looks up a tile ahead.
-        constexpr int kRowLanes = D / 16, kRowsStep = 128 / kRowLanes, kLoads = kBN / kRowsStep;
-        const int ci = tid - kFlDecodeWarp * 32, part = ci % kRowLanes, row0 = ci / kRowLanes;
-        const CodedPool &pool = a.coded;
-        const int page_mask = (1 << (a.page_log2 - kCodeBlockLog2)) - 1;
-        const int stride = a.Hkv * D;
-        uint32_t kst = 0, kph = 0, vst = 0, vph = 0;
-        bool ok = true;
-        while (ok && cur.next(pc)) {
-            const int32_t *table = a.page_table + (long long)pc.b * a.max_pages;
-            const int row_block = row0 / kCodeBlock;  // of a step's blocks, this warp's
-            // block (lane: step) of tile jt in the pool, -1: no keys or a bad page; its exponents
-            auto look = [&](int jt, int &exps) -> int {
-                const int j = jt * (kBN / kCodeBlock) + lane * (kRowsStep / kCodeBlock) + row_block;
-                exps = 0;
-                if (lane >= kLoads || jt >= pc.j1 || j * kCodeBlock >= pc.keys) return -1;
-                const int id = table[j >> (a.page_log2 - kCodeBlockLog2)];
-                if (id < 0 || id >= a.n_pages) {  // nothing outside the pool is read: zeros
-                    atomicOr(&a.status[pc.b], RS_ST_BAD_PAGE);
-                    return -1;
-                }
-                const int blk = (id << (a.page_log2 - kCodeBlockLog2)) + (j & page_mask);
-                const long long at = (long long)blk * a.Hkv + pc.kvh;
-                exps = (int)(uint8_t)pool.ke[at] | (int)(uint8_t)pool.ve[at] << 8;
-                return blk;
-            };
-            auto load = [&](const uint8_t *codes, int jt, int blk, uint4 (&x)[kLoads]) {
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    const int at = __shfl_sync(0xffffffffu, blk, i);
-                    x[i] = make_uint4(0, 0, 0, 0);
-                    if (at >= 0 && jt * kBN + i * kRowsStep + row0 < pc.keys)
-                        x[i] = load_once(codes + ((long long)at * kCodeBlock + row0 % kCodeBlock) * stride + pc.kvh * D + part * 16);
-                }
-            };
-            auto decode = [&](unsigned char *tile, int exps, bool v, const uint4 (&x)[kLoads]) {
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    const int e2 = __shfl_sync(0xffffffffu, exps, i);
-                    const uint32_t two_e = two_to<BF16>(code_exp((int)(int8_t)(v ? e2 >> 8 : e2 & 255), BF16));
-                    const uint2 c0 = decode16<BF16>(x[i].x, two_e), c1 = decode16<BF16>(x[i].y, two_e);
-                    const uint2 c2 = decode16<BF16>(x[i].z, two_e), c3 = decode16<BF16>(x[i].w, two_e);
-                    const uint4 lo = make_uint4(c0.x, c0.y, c1.x, c1.y), hi = make_uint4(c2.x, c2.y, c3.x, c3.y);
-                    // 128-byte swizzle: 16-byte word w of row r at w ^ (r & 7).  Lanes of the second 64
-                    // columns write their second word first: another set of banks
-                    const int row = i * kRowsStep + row0, kb = part / 4, w = part % 4 * 2;
-                    unsigned char *dst = tile + kb * 16384 + row * 128;
-                    *reinterpret_cast<uint4 *>(dst + ((w + kb) ^ (row & 7)) * 16) = kb ? hi : lo;
-                    *reinterpret_cast<uint4 *>(dst + ((w + 1 - kb) ^ (row & 7)) * 16) = kb ? lo : hi;
-                }
-                fence_async_smem();
-            };
-            uint4 kx[kLoads], vx[kLoads];
-            int exps, exps1;
-            int blk = look(pc.j0, exps);
-            load(pool.k, pc.j0, blk, kx);
-            load(pool.v, pc.j0, blk, vx);
-            int blk1 = look(pc.j0 + 1, exps1);
-#pragma unroll 1
-            for (int jt = pc.j0; jt < pc.j1; ++jt) {
-                if (!(ok = quick_wait(&kempty[kst], kph ^ 1, s_abort, a.wait_limit))) break;
-                decode(smem + S::kK + kst * S::kTile, exps, false, kx);
-                warp_arrive(&kfull[kst]);
-                if (++kst == NK) {
-                    kst = 0;
-                    kph ^= 1;
-                }
-                load(pool.k, jt + 1, blk1, kx);
-                if (!(ok = quick_wait(&vempty[vst], vph ^ 1, s_abort, a.wait_limit))) break;
-                decode(smem + S::kV + vst * S::kTile, exps, true, vx);
-                warp_arrive(&vfull[vst]);
-                if (++vst == NV) {
-                    vst = 0;
-                    vph ^= 1;
-                }
-                load(pool.v, jt + 1, blk1, vx);
-                exps = exps1;
-                blk1 = look(jt + 2, exps1);
-            }
-        }
     }
     __syncthreads();
     if (warp == kFlMmaWarp) {
@@ -924,6 +777,7 @@ rs_status flash_launch(const FlashArgs &a, int D, const CUtensorMap &tmq, const 
                        const char *what, cudaStream_t st);
 // over the cache in 8 bits
 template <bool BF16>
-rs_status flash_launch_coded(const FlashArgs &a, int D, const CUtensorMap &tmq, const char *what, cudaStream_t st);
+rs_status flash_launch_coded(const FlashArgs &a, int D, const CUtensorMap &tmq, const CUtensorMap &tmk, const CUtensorMap &tmv,
+                             const char *what, cudaStream_t st);
 
 }  // namespace rs

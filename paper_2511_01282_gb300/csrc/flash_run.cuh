@@ -109,12 +109,11 @@ flash_combine(FlashArgs a) {
     }
 }
 
-template <int D, bool BF16, bool CODED>
+template <int D, bool BF16>
 rs_status flash_launch_d(const FlashArgs &a, const CUtensorMap &tmq, const CUtensorMap &tmk, const CUtensorMap &tmv,
                          const char *what, cudaStream_t st) {
     // per device: 0 not asked, 1 ready, -1 built with too few registers for the
     // warpgroups' split (a raise that cannot be granted would wait for ever)
-    constexpr int kThreads = CODED ? kFlCodedThreads : kFlThreads;
     static std::atomic<int> ready[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
@@ -123,21 +122,21 @@ rs_status flash_launch_d(const FlashArgs &a, const CUtensorMap &tmq, const CUten
     }
     if (ready[dev].load() == 0) {
         cudaFuncAttributes fa;
-        const cudaError_t e1 = cudaFuncGetAttributes(&fa, flash_kernel<D, BF16, CODED>);
-        const cudaError_t e2 = cudaFuncSetAttribute(flash_kernel<D, BF16, CODED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        const cudaError_t e1 = cudaFuncGetAttributes(&fa, flash_kernel<D, BF16>);
+        const cudaError_t e2 = cudaFuncSetAttribute(flash_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                     FlSmem<D>::kTotal);
         if (e1 != cudaSuccess || e2 != cudaSuccess) {
             set_error("%s: kernel attributes: %s", what, cudaGetErrorString(e1 != cudaSuccess ? e1 : e2));
             return RS_ERR_CUDA;
         }
-        const int need = CODED ? kFlCodedThreads * 128 : (int)(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd);
-        ready[dev].store(fa.numRegs * kThreads >= need ? 1 : -1);
+        const int need = (int)(2 * 128 * kFlRegsSoft + 128 * kFlRegsProd);
+        ready[dev].store(fa.numRegs * kFlThreads >= need ? 1 : -1);
     }
     if (ready[dev].load() != 1) {
         set_error("%s: attention kernel built with too few registers per thread", what);
         return RS_ERR_CUDA;
     }
-    launch_pdl(flash_kernel<D, BF16, CODED>, dim3(a.grid), dim3(kThreads), FlSmem<D>::kTotal, st, a, tmq, tmk, tmv);
+    launch_pdl(flash_kernel<D, BF16>, dim3(a.grid), dim3(kFlThreads), FlSmem<D>::kTotal, st, a, tmq, tmk, tmv);
     RS_CHECK_LAUNCH(what);
     launch_full(flash_combine<D, BF16>, dim3(std::max(a.grid - 1, 1), a.comb_blocks), dim3(kFlCombThreads), 0, st, a);
     RS_CHECK_LAUNCH(what);
@@ -147,14 +146,8 @@ rs_status flash_launch_d(const FlashArgs &a, const CUtensorMap &tmq, const CUten
 template <bool BF16>
 rs_status flash_launch(const FlashArgs &a, int D, const CUtensorMap &tmq, const CUtensorMap &tmk, const CUtensorMap &tmv,
                        const char *what, cudaStream_t st) {
-    return D == 128 ? flash_launch_d<128, BF16, false>(a, tmq, tmk, tmv, what, st)
-                    : flash_launch_d<64, BF16, false>(a, tmq, tmk, tmv, what, st);
-}
-
-template <bool BF16>
-rs_status flash_launch_coded(const FlashArgs &a, int D, const CUtensorMap &tmq, const char *what, cudaStream_t st) {
-    return D == 128 ? flash_launch_d<128, BF16, true>(a, tmq, tmq, tmq, what, st)
-                    : flash_launch_d<64, BF16, true>(a, tmq, tmq, tmq, what, st);
+    return D == 128 ? flash_launch_d<128, BF16>(a, tmq, tmk, tmv, what, st)
+                    : flash_launch_d<64, BF16>(a, tmq, tmk, tmv, what, st);
 }
 
 }  // namespace rs

@@ -44,6 +44,20 @@ inline bool rows_map(CUtensorMap *m, const void *base, bool bf16, int D, int hea
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Rows of `heads` heads of D one-byte codes, viewed as (D, heads, rows); boxes of a head
+// x box_rows, as they are, zeros past the rows.
+inline bool codes_map(CUtensorMap *m, const void *base, int D, int heads, long long rows, int box_rows) {
+    auto fn = tmap_encode();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)std::max(rows, 1ll)};
+    cuuint64_t strides[2] = {(cuuint64_t)D, (cuuint64_t)D * heads};
+    cuuint32_t box[3] = {(cuuint32_t)D, 1, (cuuint32_t)box_rows};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 inline int page_log2(int page_size) {
     int l = 0;
     while ((1 << l) < page_size) ++l;
