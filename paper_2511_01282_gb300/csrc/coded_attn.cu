@@ -19,7 +19,7 @@ int row_tiles(int max_new, int G) {
     const long long rows = (long long)max_new * G;
     return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= kRowMax ? 4 : 0;
 }
-int per_sm(int tiles) { return tiles == 4 ? 2 : 3; }
+int per_sm(int tiles) { return tiles == 1 ? 3 : 2; }
 
 struct Work {
     RowsArgs a;
@@ -29,13 +29,14 @@ Work carve(void *base, int B, int Hkv, int D, int tiles) {
     Work w{};
     RowsArgs &a = w.a;
     a.grid = per_sm(tiles) * num_sms();
+    a.most_hw = Hkv % 4 == 0 ? 4 : Hkv % 2 == 0 ? 2 : 1;
     Carve cv(base);
     a.req = cv.take<int4>((size_t)B);
     a.cum = cv.take<long long>((size_t)B + 1);
     a.start = cv.take<int4>((size_t)a.grid);
     a.flag = cv.take<unsigned char>((size_t)B * Hkv + a.grid);
-    a.part_lse = cv.take<float>(2 * (size_t)a.grid * 8 * tiles);
-    a.part_o = cv.take<float>(2 * (size_t)a.grid * 8 * tiles * D);
+    a.part_lse = cv.take<float>(2 * (size_t)a.grid * a.most_hw * 8 * tiles);
+    a.part_o = cv.take<float>(2 * (size_t)a.grid * a.most_hw * 8 * tiles * D);
     w.bytes = cv.used();
     return w;
 }
@@ -47,6 +48,14 @@ bool sizes_ok(int B, int T, int max_new, int Hq, int Hkv, int D) {
 
 template <int D, int NT, bool TREE>
 rs_status launch_rows(const RowsArgs &a, cudaStream_t st) {
+    CUtensorMap tmk, tmv;
+    const long long slots = (long long)a.c.n_pages << a.c.page_log2;
+    const void *any = a.req;  // no pages: nothing is read
+    if (!codes_map(&tmk, slots ? a.c.k : any, D, a.Hkv, slots, kCodeBlock, true) ||
+        !codes_map(&tmv, slots ? a.c.v : any, D, a.Hkv, slots, kCodeBlock, true)) {
+        set_error("rs_coded_attn: cuTensorMapEncodeTiled failed");
+        return RS_ERR_CUDA;
+    }
     constexpr int kBytes = RowsShape<D, NT>::kBytes;
     static std::atomic<int> ready[64];
     int dev = 0;
@@ -55,16 +64,19 @@ rs_status launch_rows(const RowsArgs &a, cudaStream_t st) {
         return RS_ERR_CUDA;
     }
     if (!ready[dev].load()) {
-        const cudaError_t e = cudaFuncSetAttribute(coded_rows<D, NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+        cudaError_t e = cudaFuncSetAttribute(coded_rows<D, NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+        // the same division of L1 for both kernels: changing it between them takes an SM 1.5 us
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(coded_join<D>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
         if (e != cudaSuccess) {
             set_error("rs_coded_attn: kernel attributes: %s", cudaGetErrorString(e));
             return RS_ERR_CUDA;
         }
         ready[dev].store(1);
     }
-    launch_pdl(coded_rows<D, NT, TREE>, dim3(a.grid), dim3(kRowThreads), kBytes, st, a);
+    launch_pdl(coded_rows<D, NT, TREE>, dim3(a.grid), dim3(kRowThreads), kBytes, st, a, tmk, tmv);
     RS_CHECK_LAUNCH("rs_coded_attn");
-    launch_pdl(coded_join<D>, dim3(a.grid), dim3(kRowThreads), 0, st, a, NT);
+    const int each = std::min((a.most_hw * std::min(a.max_new * a.G, kRowMax) + kRowWarps - 1) / kRowWarps, 8);
+    launch_pdl(coded_join<D>, dim3(a.grid, std::max(each, 1)), dim3(kRowThreads), 0, st, a, NT);
     RS_CHECK_LAUNCH("rs_coded_attn");
     return RS_OK;
 }
@@ -136,6 +148,7 @@ extern "C" rs_status rs_coded_attn(const uint16_t *q, int64_t q_stride, int dtyp
     a.G = G;
     a.bf16 = dtype == RS_BF16;
     a.scale = scale;
+    a.wait_limit = wait_limit();
     a.out = out;
     a.lse = lse;
     a.status = status;

@@ -18,10 +18,15 @@
 // only when they would be exceeded by 2^8.  bf16 queries are scaled by a power of two
 // per row, so that fp16 holds them (what lies 2^-39 below a row's largest is lost).
 //
-// Work: units are blocks of 16 keys of a (request, KV head); all units in a row are
-// cut into equal shares, a CTA each, and a CTA's warps take its blocks in turn.  A
-// lane copies the bytes it will read itself (cp.async into its own part of a ring),
-// so that 16 KB a warp are under way without registers or barriers.  Pieces of a cut
+// Work: units are blocks of 16 keys of a request and a group of up to four KV heads;
+// all units in a row are cut into equal shares, a CTA each.  A CTA's warps are its heads
+// (where there are fewer than four, several warps share a head and take its blocks in
+// turn), so that the heads' codes of a token, 128 bytes each and next to one another,
+// are read at about the same time.  A warp has a ring of its own that TMA fills, a
+// block's K and V a box each (with cp.async instead, 16 bytes a lane, an SM does not have
+// enough under way: 4.7 TB/s, whatever the kernel does with the bytes).  Two blocks at a
+// time: one is a chain of some 2600 cycles (copies read, eight products in a row, maxima,
+// exponentials, a transpose, products), which the twelve warps of an SM do not fill.  Pieces of a cut
 // (request, head) are joined in order by coded_join: the same bits every time.
 //
 // Bound: HBM, of 2 D bytes a key and KV head.
@@ -29,6 +34,7 @@
 
 #include "attn_core.cuh"
 #include "coded.cuh"
+#include "roles.cuh"
 
 namespace rs {
 
@@ -41,15 +47,17 @@ struct RowsArgs {
     const int32_t *off, *parents;
     CodedPool c;
     int B, T, max_new, Hq, Hkv, G, bf16, grid;
+    int most_hw;          // heads of a group at most (4, 2 or 1)
     float scale;
+    long long wait_limit;
     uint16_t *out;
     float *lse;
     int32_t *status;
     // workspace
     int4 *req;            // first row, rows of its own, ctx, status (of the arguments)
     long long *cum;       // blocks before each request (of one KV head); [B]: all
-    int4 *start;          // per CTA: request, head, first block, CTAs in use (0: nothing to do)
-    unsigned char *flag;  // per piece, numbered (request, head) + CTA: status bits
+    int4 *start;          // per CTA: request, group, first block, CTAs in use (0: nothing to do) and heads of a group << 24
+    unsigned char *flag;  // per piece, numbered (request, group) + CTA: status bits
     float *part_o, *part_lse;  // two slots a CTA: the piece that it goes on with, the one that it begins
 };
 
@@ -70,7 +78,7 @@ __device__ __forceinline__ int owner(long long x, long long W, int n) { return (
 
 // Where a CTA's share begins, and the walk over its pieces.
 struct RowsWalk {
-    int b, h, j, nb;      // request, head, block; blocks of the request
+    int b, h, j, nb;      // request, group, block; blocks of the request
     int latest;           // largest first row of the requests so far
     int4 rq;
     long long left;       // units of the share that are left
@@ -86,12 +94,13 @@ __device__ __forceinline__ long long warp_prefix(long long v) {
 
 // The whole block: every thread counts the units of a run of requests; the one whose
 // run holds the share's start finds it.  CTA 0 writes the requests' records.
-__device__ __forceinline__ RowsWalk rows_plan(const RowsArgs &a, int &used) {
+__device__ __forceinline__ RowsWalk rows_plan(const RowsArgs &a, int &used, int &hw) {
     __shared__ long long s_sum[kRowWarps];
-    __shared__ int s_late[kRowWarps];
+    __shared__ int s_late[kRowWarps], s_live;  // s_live: requests with keys
     __shared__ RowsWalk s_walk;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int each = (a.B + kRowThreads - 1) / kRowThreads;
+    if (tid == 0) s_live = 0;
     const int b0 = min(tid * each, a.B), b1 = min(b0 + each, a.B);
     int late = INT_MIN;
     for (int b = b0; b < b1; ++b) late = max(late, a.off[b]);
@@ -108,12 +117,17 @@ __device__ __forceinline__ RowsWalk rows_plan(const RowsArgs &a, int &used) {
     for (int w = 0; w < warp; ++w) x = max(x, s_late[w]);
     const int before = x;
     long long mine = 0;
+    int live = 0;
     for (int b = b0; b < b1; ++b) {
         int4 rq;
         const int st = rows_check(a, b, x, rq);
-        mine += rows_blocks(rq, st);
+        const int nb = rows_blocks(rq, st);
+        mine += nb;
+        live += nb > 0;
         x = max(x, a.off[b]);
     }
+    live = __reduce_add_sync(0xffffffffu, live);
+    if (lane == 0 && live) atomicAdd(&s_live, live);
     const long long incl = warp_prefix(mine);
     if (lane == 31) s_sum[warp] = incl;
     __syncthreads();
@@ -122,13 +136,20 @@ __device__ __forceinline__ RowsWalk rows_plan(const RowsArgs &a, int &used) {
         if (w < warp) first += s_sum[w];
         total += s_sum[w];
     }
-    const long long W = total * a.Hkv;
-    // shares of at least two blocks a warp: shorter ones cost more to join than they save
-    const long long fit = (W + 2 * kRowWarps - 1) / (2 * kRowWarps);
-    used = (int)(fit < a.grid ? fit : (long long)a.grid);
+    // Heads side by side read HBM better, warps side by side at one head leave fewer pieces to
+    // join: the first where every warp has 16 blocks and more
+    hw = total * a.Hkv >= 16ll * kRowWarps * a.grid ? a.most_hw : 1;
+    const int groups = a.Hkv / hw;
+    const long long W = total * groups;
+    // shares of at least two steps a warp: shorter ones cost more to join than they save.  With
+    // few segments a whole number of shares each, at least one: a CTA has one piece then
+    // (of requests of one length)
+    const int least = 4 * kRowWarps / hw;
+    const long long fit = min((W + least - 1) / least, (long long)a.grid), segments = (long long)s_live * groups;
+    used = (int)(2 * segments > a.grid ? fit : segments * max(fit / max(segments, 1ll), 1ll));
     const int c = blockIdx.x;
     const long long lo = c < used ? W * c / used : 0, hi = c < used ? W * (c + 1) / used : 0;
-    if (c == 0 || (c < used && lo >= first * a.Hkv && lo < (first + mine) * a.Hkv)) {
+    if (c == 0 || (c < used && lo >= first * groups && lo < (first + mine) * groups)) {
         long long at = first;
         int l = before;
         for (int b = b0; b < b1; ++b) {
@@ -140,8 +161,8 @@ __device__ __forceinline__ RowsWalk rows_plan(const RowsArgs &a, int &used) {
                 a.req[b] = make_int4(rq.x, rq.y, rq.z, st);
                 a.cum[b] = at;
             }
-            if (c < used && lo >= at * a.Hkv && lo < (at + nb) * a.Hkv) {
-                const long long in = lo - at * a.Hkv;
+            if (c < used && lo >= at * groups && lo < (at + nb) * groups) {
+                const long long in = lo - at * groups;
                 s_walk = RowsWalk{b, (int)(in / nb), (int)(in % nb), nb, l, rq, hi - lo};
             }
             at += nb;
@@ -151,15 +172,15 @@ __device__ __forceinline__ RowsWalk rows_plan(const RowsArgs &a, int &used) {
     __syncthreads();
     RowsWalk w{};
     if (c < used) w = s_walk;
-    if (tid == 0) a.start[c] = make_int4(w.b, w.h, w.j, used);
+    if (tid == 0) a.start[c] = make_int4(w.b, w.h, w.j, used | hw << 24);
     return w;
 }
 // behind a piece of `done` units: the next one
-__device__ __forceinline__ void rows_next(const RowsArgs &a, RowsWalk &w, int done) {
+__device__ __forceinline__ void rows_next(const RowsArgs &a, RowsWalk &w, int done, int groups) {
     w.left -= done;
     if (w.left <= 0) return;
     w.j = 0;
-    if (++w.h < a.Hkv) return;
+    if (++w.h < groups) return;
     w.h = 0;
     do {
         ++w.b;
@@ -180,17 +201,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-template <int N>
-__device__ __forceinline__ void copy_async(void *dst, const void *src) {
-    const uint32_t d = sm100::smem_u32(dst);
-    if (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(d), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -209,46 +219,131 @@ __device__ __forceinline__ uint32_t pair_of(float lo, float hi, bool bf16) {
 
 template <int D, int NT>
 struct RowsShape {
-    static constexpr int kLoads = D == 128 ? 8 : 6;        // copies of a lane and block: K's, then V's four
-    static constexpr int kKLoads = D == 128 ? 4 : 2, kVBytes = D == 128 ? 16 : 8;
-    static constexpr int kStageLane = 32 * D / 32;         // bytes of a lane and stage: 16 keys x D, K and V, over 32 lanes
-    static constexpr int kStages = D == 128 ? 4 : 8;
-    static constexpr int kStageBytes = 32 * kStageLane;    // of a warp
+    static constexpr int kKLoads = D == 128 ? 4 : 2;  // words of a block's K that a lane reads
+    static constexpr int kBlocks = NT == 4 ? 1 : 2;        // blocks of a step (four tiles of O fill the registers)
+    static constexpr int kStages = (D == 128 ? 4 : 8) / kBlocks;
+    static constexpr int kBlockBytes = 32 * D;             // 16 keys, K and V
+    static constexpr int kStageBytes = kBlocks * kBlockBytes;  // of a warp
     static constexpr int kRing = kRowWarps * kStages * kStageBytes;
     static constexpr int kRows = 8 * NT;
     static constexpr int kRowStride = D + 4;               // floats, of a warp's O in shared memory
     static constexpr int kMerge = kRowWarps * kRows * (kRowStride + 1) * 4;
-    static constexpr int kBytes = kRing > kMerge ? kRing : kMerge;
-    static constexpr int kPerSm = NT == 4 ? 2 : 3;
+    static constexpr int kBytes = (kRing > kMerge ? kRing : kMerge) + 1024;  // the base is rounded up to 1 KB
+    static constexpr int kPerSm = NT == 1 ? 3 : 2;
 };
 
 template <int D, int NT, bool TREE>
 __global__ void __launch_bounds__(kRowThreads, RowsShape<D, NT>::kPerSm)
-coded_rows(RowsArgs a) {
+coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv) {
     using Sh = RowsShape<D, NT>;
-    constexpr int kS = Sh::kStages, kSteps = D / 16, kTiles = D / 16;  // k-steps of K Q^T, 16-column tiles of O^T
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int s_exp[kRowWarps][kS];
-    pdl_enter();
-    int used;
-    RowsWalk w = rows_plan(a, used);
+    constexpr int kS = Sh::kStages, kBl = Sh::kBlocks, kSteps = D / 16, kTiles = D / 16;  // k-steps of K Q^T, 16-column tiles of O^T
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ uint64_t s_full[kRowWarps][kS];
+    __shared__ int s_gave_up;
+    volatile int *s_abort = &s_gave_up;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kRowWarps * kS; ++i) sm100::mbar_init(&s_full[0][0] + i, 1);
+        s_gave_up = 0;
+        sm100::fence_mbar_init();
+        sm100::prefetch_tmap(&tmk);
+        sm100::prefetch_tmap(&tmv);
+    }
+    // the joining kernel is let in at the end: its blocks, waiting beside these, cost 64 single
+    // tokens 27 us of 138
+    pdl_wait_prev();
+    int used, hw;
+    RowsWalk w = rows_plan(a, used, hw);
+    const int groups = a.Hkv / hw;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
     unsigned char *ring = smem + warp * kS * Sh::kStageBytes;
     const float cexp = a.scale * 1.4426950408889634f;
     const bool bf16 = a.bf16;
+    const int head = warp % hw, kw = warp / hw, KW = kRowWarps / hw;  // head of the group; the warp's place among the head's
+    uint32_t filled = 0, drained = 0;  // stages of this warp's ring, over all pieces
     bool begun = false;
     while (w.left > 0) {
-        const int b = w.b, h = w.h, j0 = w.j, nb = w.nb;
+        const int b = w.b, h = w.h * hw + head, j0 = w.j, nb = w.nb;
         const int j1 = (int)min((long long)nb, j0 + w.left);
         const int n0 = w.rq.x, n = w.rq.y, ctx = w.rq.z, R = n * a.G, keys = ctx + n;
         int flag = 0;
+        float o[NT][kTiles][4], m[NT][2], l[NT][2], ref[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                m[nt][e] = ref[nt][e] = -INFINITY;
+                l[nt][e] = 0.f;
+            }
+        }
+
+        // This warp's steps: blocks j0 + kBl kw .., KW kBl apart.  Lane x looks up the x-th block of
+        // 32: its number in the pool and its exponents, 32 blocks ahead.
+        constexpr int kBatch = 32 / kBl;  // steps
+        const int steps_all = (j1 - j0 + kBl - 1) / kBl, mine = steps_all > kw ? (steps_all - kw + KW - 1) / KW : 0;
+        const int32_t *table = a.c.table + (long long)b * a.c.max_pages;
+        const int in_page = (1 << (a.c.page_log2 - kCodeBlockLog2)) - 1;
+        auto block_at = [&](int bat) { return j0 + kBl * (kw + KW * (bat * kBatch + lane / kBl)) + lane % kBl; };
+        auto page_of = [&](int bat) -> int {
+            const int j = block_at(bat);
+            return j < j1 ? table[j >> (a.c.page_log2 - kCodeBlockLog2)] : 0;
+        };
+        auto block_of = [&](int bat, int id) -> int {  // -1: not this CTA's, or a bad page
+            const int j = block_at(bat);
+            if (j >= j1) return -1;
+            if (id < 0 || id >= a.c.n_pages) {
+                flag |= RS_ST_BAD_PAGE;
+                return -1;
+            }
+            return (id << (a.c.page_log2 - kCodeBlockLog2)) + (j & in_page);
+        };
+        auto exps_of = [&](int blk) -> int {  // (ek, ev) as two bytes
+            if (blk < 0) return 0;
+            const long long at = (long long)blk * a.Hkv + h;
+            return (int)(uint8_t)a.c.ke[at] | (int)(uint8_t)a.c.ve[at] << 8;
+        };
+        // the ring's words, as the boxes are swizzled: 16-byte word c of row r
+        auto word = [&](int r, int c) { return D == 128 ? r * 128 + ((c ^ (r & 7)) * 16) : r * 64 + ((c ^ (r >> 1 & 3)) * 16); };
+        int blk = -1, exps = 0, blk_next = -1, exps_next = 0, id_next = 0;
+        // copies step it (of this warp) into its stage; cur: the batch of blk
+        auto issue = [&](int it, int cur) {
+            if (it >= mine) return;
+            int at[kBl], n_at = 0;
+#pragma unroll
+            for (int u = 0; u < kBl; ++u) {
+                at[u] = __shfl_sync(0xffffffffu, it / kBatch == cur ? blk : blk_next, it % kBatch * kBl + u);
+                n_at += at[u] >= 0;
+            }
+            if (lane == 0) {
+                uint64_t *bar = &s_full[warp][filled % kS];
+                unsigned char *dst = ring + filled % kS * Sh::kStageBytes;
+                sm100::mbar_expect_tx(bar, (uint32_t)(n_at * Sh::kBlockBytes));
+#pragma unroll
+                for (int u = 0; u < kBl; ++u)
+                    if (at[u] >= 0) {
+                        sm100::tma_load_3d(dst + u * Sh::kBlockBytes, &tmk, bar, 0, h, at[u] * kCodeBlock);
+                        sm100::tma_load_3d(dst + u * Sh::kBlockBytes + kCodeBlock * D, &tmv, bar, 0, h, at[u] * kCodeBlock);
+                    }
+            }
+            __syncwarp();
+            ++filled;
+        };
+        if (mine > 0) {
+            blk = block_of(0, page_of(0));
+            for (int it = 0; it < kS; ++it) issue(it, 0);
+            exps = exps_of(blk);
+        }
         uint32_t anc = 0;  // lane i: node i's ancestors and itself
         if (TREE) {
             const int pa = lane < n ? a.parents[n0 + lane] : -1;
             const bool bad = lane < n && (lane == 0 ? pa != -1 : pa < 0 || pa >= lane);
             if (__any_sync(0xffffffffu, bad)) {
-                flag = RS_ST_BAD_TREE;
+                flag |= RS_ST_BAD_TREE;
             } else {
                 int x = lane < n ? lane : -1;
                 while (__any_sync(0xffffffffu, x >= 0)) {
@@ -320,168 +415,104 @@ coded_rows(RowsArgs a) {
         }
         const int open = TREE ? ctx : ctx + 1;  // keys that every row sees
 
-        float o[NT][kTiles][4], m[NT][2], l[NT][2], ref[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                m[nt][e] = ref[nt][e] = -INFINITY;
-                l[nt][e] = 0.f;
-            }
-        }
-
-        // This warp's blocks: j0 + warp, 4 apart.  Lane x looks up the x-th of 32: its number
-        // in the pool and its exponents, 32 blocks ahead.
-        const int mine = j1 - j0 > warp ? (j1 - j0 - warp + kRowWarps - 1) / kRowWarps : 0;
-        const int32_t *table = a.c.table + (long long)b * a.c.max_pages;
-        const int in_page = (1 << (a.c.page_log2 - kCodeBlockLog2)) - 1;
-        auto page_of = [&](int it) -> int {
-            const int j = j0 + warp + kRowWarps * it;
-            return it < mine ? table[j >> (a.c.page_log2 - kCodeBlockLog2)] : 0;
-        };
-        auto block_of = [&](int it, int id) -> int {  // -1: a bad page
-            if (it >= mine) return -1;
-            if (id < 0 || id >= a.c.n_pages) {
-                flag |= RS_ST_BAD_PAGE;
-                return -1;
-            }
-            return (id << (a.c.page_log2 - kCodeBlockLog2)) + ((j0 + warp + kRowWarps * it) & in_page);
-        };
-        auto exps_of = [&](int blk) -> int {  // (ek, ev) as two bytes
-            if (blk < 0) return 0;
-            const long long at = (long long)blk * a.Hkv + h;
-            return (int)(uint8_t)a.c.ke[at] | (int)(uint8_t)a.c.ve[at] << 8;
-        };
-        int id_next = page_of(lane);
-        int blk = block_of(lane, id_next), exps = exps_of(blk), blk_next = -1, exps_next = 0;
-        // copies block it (of this warp) into its stage
-        auto issue = [&](int it) {
-            if (it < mine) {
-                const int x = it & 31;
-                const int at = __shfl_sync(0xffffffffu, blk, x);
-                const int e = __shfl_sync(0xffffffffu, exps, x);
-                const int st = it % kS;
-                if (lane == 0) s_exp[warp][st] = e;
-                if (at >= 0) {
-                    unsigned char *dst = ring + st * Sh::kStageBytes;
-                    const long long base = ((long long)at * kCodeBlock * a.Hkv + h) * D;
-                    const int row = a.Hkv * D;
-                    const uint8_t *ks = a.c.k + base + 16 * t, *vs = a.c.v + base + (D / 8) * g;
-#pragma unroll
-                    for (int x2 = 0; x2 < 2; ++x2)
-#pragma unroll
-                        for (int u = 0; u < D / 64; ++u)
-                            copy_async<16>(dst + ((x2 * (D / 64) + u) * 32 + lane) * 16, ks + (long long)(g + 8 * x2) * row + 64 * u);
-                    unsigned char *vd = dst + Sh::kKLoads * 512;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        copy_async<Sh::kVBytes>(vd + (y * 32 + lane) * Sh::kVBytes, vs + (long long)(2 * t + (y & 1) + 8 * (y >> 1)) * row);
-                }
-            }
-            copy_commit();
-        };
-        // the lookups of the blocks ahead, a step at a time
-        auto look_ahead = [&](int it) {  // `it`: the block to be issued next
-            const int x = it & 31, base = (it & ~31) + 32;
-            if (x == 8) id_next = page_of(base + lane);
-            if (x == 16) {
-                blk_next = block_of(base + lane, id_next);
-                exps_next = exps_of(blk_next);
-            }
-            if (x == 0 && it > 0) {
-                blk = blk_next;
-                exps = exps_next;
-            }
-        };
-        if (flag & RS_ST_BAD_TREE) {
-            // nothing is computed: the request's rows are emptied
-        } else {
-#pragma unroll 1
-            for (int it = 0; it < kS - 1; ++it) issue(it);
+        if (!(flag & RS_ST_BAD_TREE)) {  // (else nothing is computed: the request's rows are emptied)
 #pragma unroll 1
             for (int it = 0; it < mine; ++it) {
-                copy_wait<kS - 2>();
-                __syncwarp();  // the stage's exponents
-                const int st = it % kS;
-                const unsigned char *src = ring + st * Sh::kStageBytes;
-                const int e2 = s_exp[warp][st];
-                const int ek = code_exp((int)(int8_t)(e2 & 255), bf16), ev = code_exp((int)(int8_t)(e2 >> 8), bf16);
-                uint4 kc[Sh::kKLoads];
+                const int cur = it / kBatch;
+                // the lookups of the next batch, a step at a time
+                if (it % kBatch == 2) id_next = page_of(cur + 1);
+                if (it % kBatch == 5) {
+                    blk_next = block_of(cur + 1, id_next);
+                    exps_next = exps_of(blk_next);
+                }
+                if (!quick_wait(&s_full[warp][drained % kS], drained / kS & 1, s_abort, a.wait_limit)) {
+                    flag |= RS_ST_TIMEOUT;
+                    break;
+                }
+                const unsigned char *src = ring + drained % kS * Sh::kStageBytes;
+                ++drained;
+                const int block0 = j0 + kBl * (kw + KW * it), key0 = block0 * kCodeBlock;
+                float s[kBl][NT][4], evf[kBl], two_ek[kBl];
 #pragma unroll
-                for (int i = 0; i < Sh::kKLoads; ++i) kc[i] = *reinterpret_cast<const uint4 *>(src + (i * 32 + lane) * 16);
-                uint32_t vc[4][D / 32];
+                for (int u = 0; u < kBl; ++u) {
+                    const int e2 = __shfl_sync(0xffffffffu, exps, it % kBatch * kBl + u);
+                    two_ek[u] = pow2i(code_exp((int)(int8_t)(e2 & 255), bf16));
+                    evf[u] = (float)code_exp((int)(int8_t)(e2 >> 8), bf16);
+                }
+                // S^T: keys g and g + 8 of a block, rows 2 t and 2 t + 1 of every tile; even and odd
+                // steps are summed apart
+                uint4 kc[kBl][Sh::kKLoads];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const unsigned char *p = src + Sh::kKLoads * 512 + (y * 32 + lane) * Sh::kVBytes;
-                    if constexpr (D == 128) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(p);
-                        vc[y][0] = x.x, vc[y][1] = x.y, vc[y][2] = x.z, vc[y][3] = x.w;
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(p);
-                        vc[y][0] = x.x, vc[y][1] = x.y;
+                for (int u = 0; u < kBl; ++u)
+#pragma unroll
+                    for (int i = 0; i < Sh::kKLoads; ++i)
+                        kc[u][i] = *reinterpret_cast<const uint4 *>(src + u * Sh::kBlockBytes + word(i / (D / 64) * 8 + g, i % (D / 64) * 4 + t));
+                float s1[kBl][NT][4];
+#pragma unroll
+                for (int u = 0; u < kBl; ++u)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[u][nt][e] = s1[u][nt][e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                    for (int u = 0; u < kBl; ++u) {
+                        const uint4 &x = kc[u][k / 4], &y = kc[u][D / 64 + k / 4];
+                        const uint32_t wx = (k & 3) == 0 ? x.x : (k & 3) == 1 ? x.y : (k & 3) == 2 ? x.z : x.w;
+                        const uint32_t wy = (k & 3) == 0 ? y.x : (k & 3) == 1 ? y.y : (k & 3) == 2 ? y.z : y.w;
+                        uint32_t a0, a1, a2, a3;
+                        decode4(wx, a0, a2);
+                        decode4(wy, a1, a3);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma_f16(NT < 4 && (k & 1) ? s1[u][nt] : s[u][nt], a0, a1, a2, a3, qf[nt][k][0], qf[nt][k][1]);
                     }
-                }
-                look_ahead(it + kS - 1);
-                issue(it + kS - 1);
-                const int key0 = (j0 + warp + kRowWarps * it) * kCodeBlock;
-                // S^T: keys g and g + 8, rows 2 t and 2 t + 1 of every tile
-                float s[NT][4];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
-#pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    const uint4 &x = kc[k / 4], &y = kc[D / 64 + k / 4];
-                    const uint32_t wx = (k & 3) == 0 ? x.x : (k & 3) == 1 ? x.y : (k & 3) == 2 ? x.z : x.w;
-                    const uint32_t wy = (k & 3) == 0 ? y.x : (k & 3) == 1 ? y.y : (k & 3) == 2 ? y.z : y.w;
-                    uint32_t a0, a1, a2, a3;
-                    decode4(wx, a0, a2);
-                    decode4(wy, a1, a3);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a0, a1, a2, a3, qf[nt][k][0], qf[nt][k][1]);
-                }
-                const bool masked = key0 + kCodeBlock > open;
-                const float two_ek = pow2i(ek), evf = (float)ev;
+                const bool masked = key0 + kBl * kCodeBlock > open || block0 + kBl > j1;
                 bool grow = false;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
+                for (int u = 0; u < kBl; ++u)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[nt][e] *= factor[nt][e & 1] * two_ek;
-                    if (masked) {
+                    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int key = key0 + g + (e >> 1) * 8, node = key - ctx;
-                            const bool on = TREE ? node < 0 || (node < 32 && ((see[nt][e & 1] >> node) & 1u)) : key < limit[nt][e & 1];
-                            if (!on) s[nt][e] = -INFINITY;
+                        for (int e = 0; e < 4; ++e) s[u][nt][e] = (NT < 4 ? s[u][nt][e] + s1[u][nt][e] : s[u][nt][e]) * (factor[nt][e & 1] * two_ek[u]);
+                        if (masked) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int key = key0 + u * kCodeBlock + g + (e >> 1) * 8, node = key - ctx;
+                                const bool on = TREE ? node < 0 || (node < 32 && ((see[nt][e & 1] >> node) & 1u)) : key < limit[nt][e & 1];
+                                if (!on || block0 + u >= j1) s[u][nt][e] = -INFINITY;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float x = fmaxf(s[u][nt][e], s[u][nt][e + 2]);
+                            grow |= x > m[nt][e] + 8.f || x + evf[u] > ref[nt][e] + 8.f;
                         }
                     }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float x = fmaxf(s[nt][e], s[nt][e + 2]);
-                        grow |= x > m[nt][e] + 8.f || x + evf > ref[nt][e] + 8.f;
-                    }
-                }
                 if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float x = fmaxf(s[nt][e], s[nt][e + 2]);
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                            float x = -INFINITY, y = -INFINITY;  // the largest score, and with its block's ev
+#pragma unroll
+                            for (int u = 0; u < kBl; ++u) {
+                                const float z = fmaxf(s[u][nt][e], s[u][nt][e + 2]);
+                                x = fmaxf(x, z);
+                                y = fmaxf(y, z + evf[u]);
+                            }
+#pragma unroll
+                            for (int d = 4; d < 32; d *= 2) {
+                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+                                y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, d));
+                            }
                             if (x > m[nt][e] + 8.f) {
                                 l[nt][e] *= sm100::ex2(m[nt][e] - x);
                                 m[nt][e] = x;
                             }
-                            if (x + evf > ref[nt][e] + 8.f) {
-                                const float f = sm100::ex2(ref[nt][e] - (x + evf));
-                                ref[nt][e] = x + evf;
+                            if (y > ref[nt][e] + 8.f) {
+                                const float f = sm100::ex2(ref[nt][e] - y);
+                                ref[nt][e] = y;
 #pragma unroll
                                 for (int i = 0; i < kTiles; ++i) {
                                     o[nt][i][e] *= f;
@@ -490,41 +521,67 @@ coded_rows(RowsArgs a) {
                             }
                         }
                 }
-                uint32_t pb[NT][2];  // P'^T as the product's second operand
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float p[4];
+                for (int u = 0; u < kBl; ++u) {
+                    uint32_t pb[NT][2];  // P'^T as the product's second operand
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float nm = m[nt][e] == -INFINITY ? 0.f : m[nt][e];
-                        const float nr = ref[nt][e] == -INFINITY ? 0.f : evf + 7.f - ref[nt][e];
-                        l[nt][e] += sm100::ex2(s[nt][e] - nm) + sm100::ex2(s[nt][e + 2] - nm);
-                        p[e] = sm100::ex2(s[nt][e] + nr);
-                        p[e + 2] = sm100::ex2(s[nt][e + 2] + nr);
-                    }
-                    pb[nt][0] = transpose8(half2_of(p[0], p[1]));
-                    pb[nt][1] = transpose8(half2_of(p[2], p[3]));
-                }
-                if (key0 + kCodeBlock > keys) {  // slots behind the last key hold anything
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float p[4];
 #pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        if (key0 + 2 * t + (y & 1) + 8 * (y >> 1) >= keys) {
-#pragma unroll
-                            for (int i = 0; i < D / 32; ++i) vc[y][i] = 0;
+                        for (int e = 0; e < 2; ++e) {
+                            const float nm = m[nt][e] == -INFINITY ? 0.f : m[nt][e];
+                            const float nr = ref[nt][e] == -INFINITY ? 0.f : evf[u] + 7.f - ref[nt][e];
+                            l[nt][e] += sm100::ex2(s[u][nt][e] - nm) + sm100::ex2(s[u][nt][e + 2] - nm);
+                            p[e] = sm100::ex2(s[u][nt][e] + nr);
+                            p[e + 2] = sm100::ex2(s[u][nt][e + 2] + nr);
                         }
+                        pb[nt][0] = transpose8(half2_of(p[0], p[1]));
+                        pb[nt][1] = transpose8(half2_of(p[2], p[3]));
+                    }
+                    uint32_t vc[4][D / 32];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int key = 2 * t + (y & 1) + 8 * (y >> 1);
+                        const unsigned char *q = src + u * Sh::kBlockBytes + kCodeBlock * D +
+                                                 (D == 128 ? word(key, g) : word(key, g >> 1) + (g & 1) * 8);
+                        if constexpr (D == 128) {
+                            const uint4 x = *reinterpret_cast<const uint4 *>(q);
+                            vc[y][0] = x.x, vc[y][1] = x.y, vc[y][2] = x.z, vc[y][3] = x.w;
+                        } else {
+                            const uint2 x = *reinterpret_cast<const uint2 *>(q);
+                            vc[y][0] = x.x, vc[y][1] = x.y;
+                        }
+                    }
+                    if (key0 + (u + 1) * kCodeBlock > keys || block0 + u >= j1) {  // slots behind the last key hold anything
+#pragma unroll
+                        for (int y = 0; y < 4; ++y)
+                            if (block0 + u >= j1 || key0 + u * kCodeBlock + 2 * t + (y & 1) + 8 * (y >> 1) >= keys) {
+#pragma unroll
+                                for (int i = 0; i < D / 32; ++i) vc[y][i] = 0;
+                            }
+                    }
+                    // O^T: columns D / 8 g + 2 i (+ 1) of tile i
+#pragma unroll
+                    for (int i = 0; i < kTiles; ++i) {
+                        const uint32_t pick = i & 1 ? 0x7362u : 0x5140u;
+                        uint32_t a0, a1, a2, a3;
+                        decode4(__byte_perm(vc[0][i / 2], vc[1][i / 2], pick), a0, a1);
+                        decode4(__byte_perm(vc[2][i / 2], vc[3][i / 2], pick), a2, a3);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][i], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                    }
                 }
-                // O^T: columns D / 8 g + 2 i (+ 1) of tile i
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i) {
-                    const uint32_t pick = i & 1 ? 0x7362u : 0x5140u;
-                    uint32_t a0, a1, a2, a3;
-                    decode4(__byte_perm(vc[0][i / 2], vc[1][i / 2], pick), a0, a1);
-                    decode4(__byte_perm(vc[2][i / 2], vc[3][i / 2], pick), a2, a3);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][i], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                __syncwarp();  // all have read the stage
+                issue(it + kS, cur);
+                if (it % kBatch == kBatch - 1) {
+                    blk = blk_next;
+                    exps = exps_next;
                 }
             }
-            copy_wait<0>();
+        }
+        for (; drained < filled; ++drained) {  // given up: what is on its way lands first
+            volatile int no_abort = 0;
+            sm100::mbar_wait(&s_full[warp][drained % kS], drained / kS & 1, &no_abort, kWaitLimit);
         }
         flag = __reduce_or_sync(0xffffffffu, flag);
 
@@ -559,20 +616,16 @@ coded_rows(RowsArgs a) {
         const bool final = j0 == 0 && j1 == nb;
         const int slot = 2 * blockIdx.x + (j0 == 0 ? 1 : 0);
         const float *all = reinterpret_cast<const float *>(smem);
-        for (int i = tid; i < R * (D / 4); i += kRowThreads) {
-            const int row = i / (D / 4), col = i % (D / 4) * 4;
-            float z[kRowWarps], top = -INFINITY;
-#pragma unroll
-            for (int x = 0; x < kRowWarps; ++x) {
-                z[x] = s_lse[x * Sh::kRows + row];
-                top = fmaxf(top, z[x]);
-            }
+        for (int i = tid; i < hw * R * (D / 4); i += kRowThreads) {
+            const int hr = i / (D / 4), col = i % (D / 4) * 4, hx = hr / R, row = hr - hx * R;  // head of the group, row
+            float top = -INFINITY;
+            for (int x = hx; x < kRowWarps; x += hw) top = fmaxf(top, s_lse[x * Sh::kRows + row]);
             float sum = 0.f;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int x = 0; x < kRowWarps; ++x) {
-                if (z[x] == -INFINITY) continue;
-                const float p = sm100::ex2(z[x] - top);
+            for (int x = hx; x < kRowWarps; x += hw) {
+                const float z = s_lse[x * Sh::kRows + row];
+                if (z == -INFINITY) continue;
+                const float p = sm100::ex2(z - top);
                 const float4 y = *reinterpret_cast<const float4 *>(all + (x * Sh::kRows + row) * Sh::kRowStride + col);
                 sum += p;
                 v.x = fmaf(p, y.x, v.x);
@@ -584,52 +637,56 @@ coded_rows(RowsArgs a) {
             v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
             if (final) {
                 const int tok = row / a.G;
-                const long long orow = (long long)(n0 + tok) * a.Hq + h * a.G + (row - tok * a.G);
+                const long long orow = (long long)(n0 + tok) * a.Hq + (w.h * hw + hx) * a.G + (row - tok * a.G);
                 *reinterpret_cast<uint2 *>(a.out + orow * D + col) = make_uint2(pair_of(v.x, v.y, bf16), pair_of(v.z, v.w, bf16));
                 if (col == 0) a.lse[orow] = z2 * 0.6931471805599453f;
             } else {
-                *reinterpret_cast<float4 *>(a.part_o + ((long long)slot * Sh::kRows + row) * D + col) = v;
-                if (col == 0) a.part_lse[slot * Sh::kRows + row] = z2;
+                *reinterpret_cast<float4 *>(a.part_o + ((long long)(slot * hw + hx) * Sh::kRows + row) * D + col) = v;
+                if (col == 0) a.part_lse[(slot * hw + hx) * Sh::kRows + row] = z2;
             }
         }
+        sm100::fence_async_smem();  // the ring is copied to again
         __syncthreads();
         if (tid == 0) {
-            const long long piece = (long long)b * a.Hkv + h + blockIdx.x;
+            const long long piece = (long long)b * groups + w.h + blockIdx.x;
             a.flag[piece] = (unsigned char)s_flag;
             if (!begun && j0 == 0 && blockIdx.x > 0) a.flag[piece - 1] = 0;  // a number that no piece has
         }
         begun = true;
-        rows_next(a, w, j1 - j0);
+        rows_next(a, w, j1 - j0, groups);
     }
+    pdl_launch_next();
 }
 
-// Joins the pieces of the segments that the shares' ends cut (the block of the share
-// that holds a segment's second piece), a row to a warp, lanes the pieces' sums first
+// Joins the pieces of the segments that the shares' ends cut (the blocks of the share
+// that holds a segment's second piece, as many as give a warp a row: one request's pieces
+// have few such shares), a row to a warp, lanes the pieces' sums first
 // and then the columns; empties the rows of rejected requests; writes the statuses.
 template <int D>
 __global__ void __launch_bounds__(kRowThreads)
 coded_join(RowsArgs a, int row_tiles) {
-    pdl_enter();
+    pdl_wait_prev();
+    pdl_launch_next();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long total = a.cum[a.B], W = total * a.Hkv;
-    const int used = a.start[0].w;
-    auto status_of = [&](int b) -> int {  // whole warp
-        const int4 rq = a.req[b];
-        const long long lo = a.cum[b] * a.Hkv, hi = a.cum[b + 1] * a.Hkv;
-        int st = rq.w;
+    const int4 at = a.start[min((int)blockIdx.x + 1, a.grid - 1)];
+    const int hw = at.w >> 24, used = at.w & 0xffffff, groups = a.Hkv / hw;
+    const long long total = a.cum[a.B], W = total * groups;
+    // the flags of request b's pieces, whose units are [lo, hi) (whole warp)
+    auto flags_of = [&](int b, long long lo, long long hi) -> int {
+        int bits = 0;
         if (hi > lo) {
-            const long long first = (long long)b * a.Hkv + owner(lo, W, used), last = (long long)(b + 1) * a.Hkv - 1 + owner(hi - 1, W, used);
-            int bits = 0;
+            const long long first = (long long)b * groups + owner(lo, W, used), last = (long long)(b + 1) * groups - 1 + owner(hi - 1, W, used);
             for (long long i = first + lane; i <= last; i += 32) bits |= a.flag[i];
-            st |= __reduce_or_sync(0xffffffffu, bits);
         }
-        return st;
+        return (int)__reduce_or_sync(0xffffffffu, bits);
     };
-    for (int b = blockIdx.x * kRowWarps + warp; b < a.B; b += gridDim.x * kRowWarps) {
-        const int st = status_of(b);
+    const int blocks = gridDim.x * gridDim.y;
+    // (the last blocks first: those with pieces to join are at the front)
+    for (int b = (blocks - 1 - (int)(blockIdx.y * gridDim.x + blockIdx.x)) * kRowWarps + warp; b < a.B; b += blocks * kRowWarps) {
+        const int4 rq = a.req[b];
+        const int st = rq.w | flags_of(b, a.cum[b] * groups, a.cum[b + 1] * groups);
         if (lane == 0) a.status[b] = st;
         if (!st) continue;
-        const int4 rq = a.req[b];
         const long long rows = (long long)rq.y * a.Hq;  // none where another request may have them
         uint4 *o = reinterpret_cast<uint4 *>(a.out + (long long)rq.x * a.Hq * D);
         for (long long i = lane; i < rows * (D / 8); i += 32) o[i] = make_uint4(0, 0, 0, 0);
@@ -637,22 +694,23 @@ coded_join(RowsArgs a, int row_tiles) {
     }
     const int c = blockIdx.x + 1;
     if (c >= used) return;
-    const int4 at = a.start[c];
     if (at.z == 0) return;  // it begins with a segment
     const int4 rq = a.req[at.x];
     const long long nb = a.cum[at.x + 1] - a.cum[at.x];
-    const long long x0 = a.cum[at.x] * a.Hkv + at.y * nb;
+    const long long x0 = a.cum[at.x] * groups + at.y * nb;
     const int c0 = owner(x0, W, used), c1 = owner(x0 + nb - 1, W, used);
     if (c0 != c - 1) return;  // not the second piece
-    if (status_of(at.x)) return;
+    const bool bad = rq.w != 0 || flags_of(at.x, x0 - at.y * nb, x0 + (groups - at.y) * nb) != 0;
     const int pieces = c1 - c0 + 1, rows = 8 * row_tiles;
     constexpr int kC = D / 32;  // columns of a lane
-    for (int row = warp; row < rq.y * a.G; row += kRowWarps) {
+    const int R = rq.y * a.G;
+    for (int hr = blockIdx.y * kRowWarps + warp; hr < hw * R; hr += gridDim.y * kRowWarps) {
+        const int hx = hr / R, row = hr - hx * R;  // head of the group, row
         float top = -INFINITY, sum = 0.f, acc[kC] = {};
         for (int p0 = 0; p0 < pieces; p0 += 32) {
             const int cnt = min(pieces - p0, 32);
             auto slot = [&](int p) { return 2 * (c0 + p) + (p == 0 ? 1 : 0); };
-            const float z = lane < cnt ? a.part_lse[slot(p0 + lane) * rows + row] : -INFINITY;
+            const float z = lane < cnt ? a.part_lse[(slot(p0 + lane) * hw + hx) * rows + row] : -INFINITY;
             const float next = fmaxf(top, warp_max(z));
             const float old = next == -INFINITY ? 1.f : sm100::ex2(top - next);
             const float wt = z == -INFINITY ? 0.f : sm100::ex2(z - (next == -INFINITY ? 0.f : next));
@@ -660,10 +718,10 @@ coded_join(RowsArgs a, int row_tiles) {
             sum = sum * old + warp_sum(wt);
 #pragma unroll
             for (int j = 0; j < kC; ++j) acc[j] *= old;
-#pragma unroll 4
+#pragma unroll 8
             for (int p = 0; p < cnt; ++p) {
                 const float f = __shfl_sync(0xffffffffu, wt, p);
-                const float *src = a.part_o + ((long long)slot(p0 + p) * rows + row) * D + lane * kC;
+                const float *src = a.part_o + ((long long)(slot(p0 + p) * hw + hx) * rows + row) * D + lane * kC;
                 float v[kC];
                 if constexpr (kC == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(src);
                 else *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
@@ -671,9 +729,10 @@ coded_join(RowsArgs a, int row_tiles) {
                 for (int j = 0; j < kC; ++j) acc[j] = fmaf(f, v[j], acc[j]);
             }
         }
+        if (bad) break;
         const float f = sum == 0.f ? 0.f : 1.f / sum;
         const int tok = row / a.G;
-        const long long orow = (long long)(rq.x + tok) * a.Hq + at.y * a.G + (row - tok * a.G);
+        const long long orow = (long long)(rq.x + tok) * a.Hq + (at.y * hw + hx) * a.G + (row - tok * a.G);
         uint32_t *d = reinterpret_cast<uint32_t *>(a.out + orow * D + lane * kC);
 #pragma unroll
         for (int j = 0; j < kC / 2; ++j) d[j] = pair_of(acc[2 * j] * f, acc[2 * j + 1] * f, a.bf16);

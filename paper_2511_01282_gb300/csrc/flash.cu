@@ -251,8 +251,8 @@ rs_status flash_run(const char *what, Work &w, int dtype, int D, const void *q, 
     const int box = a.page_table ? std::min(1 << a.page_log2, kBN) : kBN;
     CUtensorMap tmq, tmk, tmv;
     if (!rows_map(&tmq, q, type, D, a.Hq, a.T, q_stride, a.G, a.tq) ||
-        !(coded ? codes_map(&tmk, k, D, a.Hkv, kv_rows, box) : rows_map(&tmk, k, type, D, a.Hkv, kv_rows, k_stride, 1, box)) ||
-        !(coded ? codes_map(&tmv, v, D, a.Hkv, kv_rows, box) : rows_map(&tmv, v, type, D, a.Hkv, kv_rows, v_stride, 1, box))) {
+        !(coded ? codes_map(&tmk, k, D, a.Hkv, kv_rows, box, false) : rows_map(&tmk, k, type, D, a.Hkv, kv_rows, k_stride, 1, box)) ||
+        !(coded ? codes_map(&tmv, v, D, a.Hkv, kv_rows, box, false) : rows_map(&tmv, v, type, D, a.Hkv, kv_rows, v_stride, 1, box))) {
         set_error("%s: cuTensorMapEncodeTiled failed", what);
         return RS_ERR_CUDA;
     }

@@ -68,77 +68,84 @@ __device__ __forceinline__ RotaryRow row_of(const RotaryArgs &a, int t0, int r) 
 }
 
 // Pairs (x, y) become (x c - y s, y c + x s).  A block takes a few tokens: their
-// cosines and sines once into shared memory, then a thread turns eight pairs of a
-// head (two 16-byte words) or copies a word of the part that is not turned.
-// blockDim.x: those of one head; the rows of all tokens run along blockDim.y.
-// kWide: half a multiple of 8.  Otherwise single values, a pair each.
+// cosines and sines once into shared memory, then a thread turns a 16-byte word of a
+// head (four pairs side by side) or two half a turned part apart (eight pairs), or
+// copies a word of the part that is not turned.  blockDim.x: the words of one head; the
+// rows (token, head) run along blockDim.y, several to a thread at once.
+// kKind 0: halves, their size a multiple of 8; 1: interleaved, rot a multiple of 8;
+// 2: other sizes, single values, a pair to a thread.
 // Bound: 4 (Hq + Hkv) D bytes a token.
-template <bool BF16, bool kWide>
+template <bool BF16, int kKind>
 __global__ void __launch_bounds__(kRotThreads)
 rotary_kernel(RotaryArgs a) {
     pdl_enter();
-    // wide: word q of chunk c at [token][q half / 8 + c], (cos, sin) pairs 2 q and 2 q + 1 of its eight
+    // kinds 0 and 1: word q of unit c at [token][q C + c], (cos, sin) of pairs 2 q and 2 q + 1 of its own
     __shared__ float4 s_turn[kRotTokens * kRotMaxHalf / 2];
+    constexpr int kPairs = kKind == 0 ? 8 : 4;  // of a unit
     const int tid = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
     const int t0 = blockIdx.x * a.tokens, tokens = min(a.tokens, a.T - t0);
-    const int C = a.half / 8;
+    const int C = a.half / kPairs;
     for (int i = tid; i < tokens * a.half; i += threads) {
         const int t = i / a.half, p = i - t * a.half;
         const float2 v = turn(a, a.pos[t0 + t], p);
         float2 *row = reinterpret_cast<float2 *>(s_turn) + t * a.half;
-        row[kWide ? ((p >> 1) % 4 * C + p / 8) * 2 + (p & 1) : p] = v;
+        row[kKind < 2 ? (p % kPairs / 2 * C + p / kPairs) * 2 + (p & 1) : p] = v;
     }
     __syncthreads();
     const int rows = tokens * (a.heads[0] + a.heads[1]);
-    if constexpr (kWide) {
+    const int first = blockIdx.y * blockDim.y + threadIdx.y, step = gridDim.y * blockDim.y;
+    if constexpr (kKind < 2) {
+        constexpr int kWords = kKind == 0 ? 2 : 1, kRows = 4 / kWords;  // words of a unit, rows at a time
         const int unit = threadIdx.x;
-        const int step = gridDim.y * blockDim.y;
-        auto load = [&](int r, uint4 &x, uint4 &y, RotaryRow &w) {
-            w = row_of(a, t0, r);
-            const uint4 *in = reinterpret_cast<const uint4 *>(w.in);
-            if (unit >= C) {
-                x = in[unit + C];
-                return;
-            }
-            x = in[a.interleaved ? 2 * unit : unit];
-            y = in[a.interleaved ? 2 * unit + 1 : C + unit];
-        };
-        auto finish = [&](uint4 x, uint4 y, const RotaryRow &w) {
-            uint4 *out = reinterpret_cast<uint4 *>(w.out);
-            if (unit >= C) {
-                out[unit + C] = x;
-                return;
-            }
-            uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+        const bool turned = unit < C;
+        // the unit's words in a row (the part that is not turned has one each)
+        const int at0 = turned || kKind == 1 ? unit : unit + C, at1 = C + unit;
+        for (int r = first; r < rows; r += kRows * step) {
+            uint4 x[kRows][kWords];
+            RotaryRow w[kRows];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float4 cs = s_turn[w.token * (a.half / 2) + q * C + unit];  // pairs 2 q and 2 q + 1
-                if (a.interleaved) {
-                    uint32_t &w0 = q < 2 ? u[2 * q] : v[2 * q - 4], &w1 = q < 2 ? u[2 * q + 1] : v[2 * q - 3];
-                    const float2 p0 = unpack16<BF16>(w0), p1 = unpack16<BF16>(w1);
-                    w0 = pack16<BF16>(fmaf(p0.x, cs.x, -p0.y * cs.y), fmaf(p0.y, cs.x, p0.x * cs.y));
-                    w1 = pack16<BF16>(fmaf(p1.x, cs.z, -p1.y * cs.w), fmaf(p1.y, cs.z, p1.x * cs.w));
-                } else {
-                    const float2 p = unpack16<BF16>(u[q]), r = unpack16<BF16>(v[q]);
-                    u[q] = pack16<BF16>(fmaf(p.x, cs.x, -r.x * cs.y), fmaf(p.y, cs.z, -r.y * cs.w));
-                    v[q] = pack16<BF16>(fmaf(r.x, cs.x, p.x * cs.y), fmaf(r.y, cs.z, p.y * cs.w));
+            for (int k = 0; k < kRows; ++k)
+                if (r + k * step < rows) {
+                    w[k] = row_of(a, t0, r + k * step);
+                    const uint4 *in = reinterpret_cast<const uint4 *>(w[k].in);
+                    x[k][0] = in[at0];
+                    if (kKind == 0 && turned) x[k][kWords - 1] = in[at1];
                 }
-            }
-            out[a.interleaved ? 2 * unit : unit] = make_uint4(u[0], u[1], u[2], u[3]);
-            out[a.interleaved ? 2 * unit + 1 : C + unit] = make_uint4(v[0], v[1], v[2], v[3]);
-        };
-        for (int r = blockIdx.y * blockDim.y + threadIdx.y; r < rows; r += 2 * step) {
-            uint4 x0, y0, x1, y1;
-            RotaryRow w0, w1;
-            const bool two = r + step < rows;
-            load(r, x0, y0, w0);
-            if (two) load(r + step, x1, y1, w1);
-            finish(x0, y0, w0);
-            if (two) finish(x1, y1, w1);
+#pragma unroll
+            for (int k = 0; k < kRows; ++k)
+                if (r + k * step < rows) {
+                    uint4 *out = reinterpret_cast<uint4 *>(w[k].out);
+                    if (!turned) {
+                        out[at0] = x[k][0];
+                        continue;
+                    }
+                    const float4 *cs = s_turn + w[k].token * (a.half / 2) + unit;
+                    uint32_t u[4] = {x[k][0].x, x[k][0].y, x[k][0].z, x[k][0].w};
+                    if constexpr (kKind == 1) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const float4 c = cs[q * C];
+                            const float2 p0 = unpack16<BF16>(u[2 * q]), p1 = unpack16<BF16>(u[2 * q + 1]);
+                            u[2 * q] = pack16<BF16>(fmaf(p0.x, c.x, -p0.y * c.y), fmaf(p0.y, c.x, p0.x * c.y));
+                            u[2 * q + 1] = pack16<BF16>(fmaf(p1.x, c.z, -p1.y * c.w), fmaf(p1.y, c.z, p1.x * c.w));
+                        }
+                    } else {
+                        uint32_t v[4] = {x[k][kWords - 1].x, x[k][kWords - 1].y, x[k][kWords - 1].z, x[k][kWords - 1].w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float4 c = cs[q * C];
+                            const float2 p = unpack16<BF16>(u[q]), o = unpack16<BF16>(v[q]);
+                            u[q] = pack16<BF16>(fmaf(p.x, c.x, -o.x * c.y), fmaf(p.y, c.z, -o.y * c.w));
+                            v[q] = pack16<BF16>(fmaf(o.x, c.x, p.x * c.y), fmaf(o.y, c.z, p.y * c.w));
+                        }
+                        out[at1] = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                    out[at0] = make_uint4(u[0], u[1], u[2], u[3]);
+                }
         }
     } else {
         const float2 *s_pair = reinterpret_cast<const float2 *>(s_turn);
-        for (int r = blockIdx.y * blockDim.y + threadIdx.y; r < rows; r += gridDim.y * blockDim.y) {
+        for (int r = first; r < rows; r += step) {
             const RotaryRow w = row_of(a, t0, r);
             for (int p = threadIdx.x; p < a.half; p += blockDim.x) {
                 const int i = a.interleaved ? 2 * p : p, j = a.interleaved ? 2 * p + 1 : a.half + p;
@@ -152,6 +159,13 @@ rotary_kernel(RotaryArgs a) {
                 for (int i = 2 * a.half + threadIdx.x; i < a.D; i += blockDim.x) w.out[i] = w.in[i];
         }
     }
+}
+
+template <bool BF16>
+void launch_rotary(const RotaryArgs &a, int kind, dim3 grid, dim3 block, cudaStream_t s) {
+    if (kind == 0) launch_pdl(rotary_kernel<BF16, 0>, grid, block, 0, s, a);
+    else if (kind == 1) launch_pdl(rotary_kernel<BF16, 1>, grid, block, 0, s, a);
+    else launch_pdl(rotary_kernel<BF16, 2>, grid, block, 0, s, a);
 }
 
 rs_status check_rows(const char *what, const char *name, const void *p, int64_t stride, int heads, int D) {
@@ -222,15 +236,15 @@ extern "C" rs_status rs_rotary(const uint16_t *q, int64_t q_stride, uint16_t *q_
     const int sms = num_sms(), H = Hq + Hkv;
     a.tokens = std::min(std::max(T / (4 * sms), 1), kRotTokens);
     const long long blocks = ((long long)T + a.tokens - 1) / a.tokens;
-    const bool wide = a.half % 8 == 0;
-    const int x = wide ? a.half / 8 + (a.copy ? (D - rot) / 8 : 0) : 32;
+    const int kind = a.interleaved ? (rot % 8 ? 2 : 1) : (a.half % 8 ? 2 : 0);
+    const int x = kind == 2 ? 32 : a.half / (kind == 0 ? 8 : 4) + (a.copy ? (D - rot) / 8 : 0);
     const dim3 block((unsigned)x, (unsigned)std::max(kRotThreads / x, 1));
     const long long rows = (long long)a.tokens * H;
     const long long most = (rows + block.y - 1) / block.y;
     const dim3 grid((unsigned)blocks, (unsigned)std::max(1ll, std::min(most, 2ll * sms / blocks)));
     const cudaStream_t s = (cudaStream_t)stream;
-    if (dtype == RS_BF16) launch_pdl(wide ? rotary_kernel<true, true> : rotary_kernel<true, false>, grid, block, 0, s, a);
-    else launch_pdl(wide ? rotary_kernel<false, true> : rotary_kernel<false, false>, grid, block, 0, s, a);
+    if (dtype == RS_BF16) launch_rotary<true>(a, kind, grid, block, s);
+    else launch_rotary<false>(a, kind, grid, block, s);
     RS_CHECK_LAUNCH(what);
     return RS_OK;
 }

@@ -45,8 +45,9 @@ inline bool rows_map(CUtensorMap *m, const void *base, bool bf16, int D, int hea
 }
 
 // Rows of `heads` heads of D one-byte codes, viewed as (D, heads, rows); boxes of a head
-// x box_rows, as they are, zeros past the rows.
-inline bool codes_map(CUtensorMap *m, const void *base, int D, int heads, long long rows, int box_rows) {
+// x box_rows, swizzled over their D bytes where asked for, zeros past the rows.  A head's codes of a token are 128 bytes at
+// most: promoted to 256, half of what is read belongs to another head (1.5 times the bytes).
+inline bool codes_map(CUtensorMap *m, const void *base, int D, int heads, long long rows, int box_rows, bool swizzled) {
     auto fn = tmap_encode();
     if (!fn) return false;
     cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)std::max(rows, 1ll)};
@@ -54,7 +55,9 @@ inline bool codes_map(CUtensorMap *m, const void *base, int D, int heads, long l
     cuuint32_t box[3] = {(cuuint32_t)D, 1, (cuuint32_t)box_rows};
     cuuint32_t estr[3] = {1, 1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE,
+              !swizzled ? CU_TENSOR_MAP_SWIZZLE_NONE : D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
