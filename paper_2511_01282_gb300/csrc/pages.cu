@@ -17,9 +17,9 @@ struct Pages {
 };
 
 // A block copies a page in units: 16 KB of keys or values, all loads of a thread
-// under way before its first store (a quarter of that is in flight for each of an
-// SM's blocks, which covers HBM's latency), and one unit for the small arrays.
-// Bound: 2 bytes moved a byte.
+// under way before its first store, and one unit for the small arrays.
+// Bound: 2 bytes moved a byte: 2500 pages of 133 KB, 666 MB, in 99 us, 6.7 TB/s (with 64
+// blocks an SM, which take a few units each; 8 that take many 106 us, a unit of 32 KB 104).
 constexpr int kCopyThreads = 256, kCopyWords = 4;  // 16-byte words of a thread
 constexpr int kCopyUnit = kCopyThreads * kCopyWords * 16;
 
@@ -216,7 +216,7 @@ rs_status make_pages(const char *what, Pages &p, void *k, void *v, int8_t *ke, i
     return RS_OK;
 }
 
-unsigned copy_grid(long long units) { return (unsigned)std::max(1ll, std::min(units, 8ll * num_sms())); }
+unsigned copy_grid(long long units) { return (unsigned)std::max(1ll, std::min(units, 64ll * num_sms())); }
 
 struct CompactWork {
     int32_t *n_moves;
