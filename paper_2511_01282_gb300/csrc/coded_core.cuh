@@ -2,15 +2,17 @@
 // draft trees.  Plan, pieces and joining are flash.cuh's; so is the arithmetic, but
 // for what the codes change:
 //
-// Products take codes as they are, exact in fp16 (a conversion of two codes is one
-// instruction; with the exponents multiplied in and bf16 tiles it was five, and the
-// converting warps bound the loop: trees of 65 nodes over 32768 keys 1356 us).  The
-// exponents go into the softmax, where 16 keys share a factor and an offset:
-//     S_rj = q_r.K_j,  s_rj = c 2^(ek) S_rj,  P'_rj = 2^(s_rj + ev - R_r + 7),
-//     O'_r = sum P'_rj V_j,  l_r = sum 2^(s_rj - m_r) = sum_blocks 2^(R_r - 7 - ev - m_r) sum P'_rj
-// with m_r and R_r running bounds of s and of s + ev, moved only when they are exceeded
+// Products take codes as fp16, times 2^(e - E) with E the largest exponent of the tile's
+// eight blocks: exact while they lie within 15 of each other, and where they do not (values
+// of very different sizes side by side) the codes as they are, with a factor and an offset
+// for each block in the softmax.  (With code 2^e in bf16 tiles, five instructions for two
+// codes instead of two, the converting warps bound the loop: trees of 65 nodes over 32768
+// keys 1356 us.)  The tile's exponents go into the softmax:
+//     S_rj = q_r.K_j,  s_rj = c 2^(Ek) S_rj,  P'_rj = 2^(s_rj + Ev - R_r + 7),
+//     O'_r = sum P'_rj V_j,  l_r = sum 2^(s_rj - m_r) = sum_tiles 2^(R_r - 7 - Ev - m_r) sum P'_rj
+// with m_r and R_r running bounds of s and of s + Ev, moved only when they are exceeded
 // by 2^8 (P' <= 2^15 in fp16, weights down to 2^-32 of the largest stay above its
-// subnormals).  Where ev is so far below R - m that P' would vanish in fp32 while the
+// subnormals).  Where Ev is so far below R - m that P' would vanish in fp32 while the
 // weight counts, l is summed from its own exponentials.  bf16 queries are scaled by a
 // power of two per row into fp16 (what lies 2^-39 below a row's largest is lost).
 //
@@ -26,7 +28,10 @@
 // what is on its way (4.2 us a key tile).  K and V tiles share one ring, K a tile ahead:
 // K0 K1 V0 K2 V1 ... V(n-1).
 //
-// Bound: trees HBM, chunks the softmax warps.
+// Measured: four trees of 65 nodes over 32768 keys (40 / 8 heads of 128, bf16) 460 us, bound by
+// the converting warps (an instruction in two cycles for each two codes, and 400 cycles of waits and
+// fences a tile); 512 new tokens behind 8192 (four requests, 32 / 8 heads of 64, fp16) 515 us, bound by
+// the softmax warps (2600 cycles of exponentials a key tile and row tile).
 #pragma once
 
 #include "coded.cuh"
@@ -43,16 +48,19 @@ struct CoSmem {
     static constexpr int kTile = kBN * D * 2;
     static constexpr int kNR = D == 128 ? 3 : 8;             // stages of fp16 tiles
     static constexpr int kNC = D == 128 ? 4 : 6;             // stages of codes
-    // tiles whose exponents are kept: the copying warp is at most kNC / 2 + kNR / 2 + 1 tiles ahead of
-    // the products, and those one or two ahead of a softmax that still reads
-    static constexpr int kExps = 16;
+    // Tiles whose exponents are kept.  They are written for up to four tiles when the first one's K is
+    // about to be copied, so when K of kNC / 2 tiles before is in the ring, so when position kNR before
+    // that one is free: at kNR = 3 the products of tile t - 5 are done (and t + 3 takes its place), at
+    // 8 S of tile t - 7, whose softmax reads on.
+    static constexpr int kExps = D == 128 ? 8 : 16;
     static constexpr int kRing = 0, kQ = kNR * kTile, kCodes = kQ + 2 * kTile;
     static constexpr int kBar = kCodes + kNC * kBN * D;
     static constexpr int kNumBars = 2 * kNR + 2 * kNC + 23;
     static constexpr int kMisc = kBar + kNumBars * 8;        // tensor memory base, abort flag
     static constexpr int kBounds = (kMisc + 8 + 15) / 16 * 16;
-    static constexpr int kExp = kBounds + 2 * kFlMaxPhases * 16;  // (ek + 127, ev + 128) as two bytes [tile][block]
-    static constexpr int kShift = kExp + kExps * 16;         // int8 [row tile][row]
+    // [tile]: (ek + 127, ev + 128) of its eight blocks, two bytes each; then those of the tile, and whether they hold
+    static constexpr int kExp = kBounds + 2 * kFlMaxPhases * 16;
+    static constexpr int kShift = kExp + kExps * 32;         // int8 [row tile][row]
     static constexpr int kStat = kShift + 2 * kBM;           // float2 [row]: the second warpgroup's sums
     static constexpr int kBytes = kStat + kBM * 8;
     static constexpr int kTotal = kBytes + 1024;             // the base is rounded up to 1 KB
@@ -65,40 +73,10 @@ __device__ __forceinline__ int v_at(int tl, int n) { return tl == n - 1 ? 2 * n 
 __device__ __forceinline__ bool is_v(int pos, int n) { return pos == 2 * n - 1 || (pos > 0 && !(pos & 1)); }
 __device__ __forceinline__ int tile_at(int pos, int n) { return pos == 2 * n - 1 ? n - 1 : pos == 0 ? 0 : (pos & 1) ? (pos + 1) / 2 : pos / 2 - 1; }
 
-// 64 weights of a row, four blocks: xp = 2^(c s + nb) in fp16, each block's fp32 sum in two parts.
-// (exp_pairs of flash.cuh, with a factor and an offset to a block.)
-__device__ __forceinline__ void exp_blocks(const uint32_t (&s0)[32], const uint32_t (&s1)[32], const float (&c)[4], const float (&nb)[4],
-                                           float (&sum)[4][2], uint32_t (&xp)[32]) {
-    constexpr int kAhead = 4, kBehind = 4;  // pairs
-    float d[64], p[64];
-    auto fma1 = [&](int i) {
-        const float v = __uint_as_float(i < 32 ? s0[i] : s1[i - 32]);
-        asm volatile("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d[i]) : "f"(v), "f"(c[i / 16]), "f"(nb[i / 16]));
-    };
-#pragma unroll
-    for (int i = 0; i < 2 * kAhead; ++i) fma1(i);
-#pragma unroll
-    for (int e = 0; e < 32 + kBehind; ++e) {
-        if (e < 32) {
-            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[2 * e]) : "f"(d[2 * e]));
-            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[2 * e + 1]) : "f"(d[2 * e + 1]));
-        }
-        if (e + kAhead < 32) {
-            fma1(2 * (e + kAhead));
-            fma1(2 * (e + kAhead) + 1);
-        }
-        if (e >= kBehind) {
-            const int q = e - kBehind;
-            if (q % 8 == 0) {
-                sum[q / 8][0] = p[2 * q];
-                sum[q / 8][1] = p[2 * q + 1];
-            } else {
-                asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(sum[q / 8][0]) : "f"(p[2 * q]));
-                asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(sum[q / 8][1]) : "f"(p[2 * q + 1]));
-            }
-            asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(xp[q]) : "f"(p[2 * q + 1]), "f"(p[2 * q]));
-        }
-    }
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
 template <int D, bool BF16>
@@ -109,8 +87,9 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
     using S = CoSmem<D>;
     constexpr uint32_t NR = S::kNR, NC = S::kNC;
     extern __shared__ unsigned char smem_raw[];
-    unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                                            ~uintptr_t(1023));
+    // (an offset and not a rounded address: the compiler then knows it for shared memory, whose
+    // loads and stores are several times as fast as generic ones)
+    unsigned char *smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kBar);
     uint64_t *full = bars, *empty = full + NR, *cfull = empty + NR, *cempty = cfull + NC;  // tiles, codes
     // per softmax: S there, S read (kApart), P there (its two halves), P V complete, Q copied,
@@ -215,9 +194,12 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
         }
       } else if (warp == kCoCopyWarp) {
         // ---------------------------------------------------------- codes and exponents
-        // Lane x copies page x of a tile, and looks up its block x's exponents.
+        // Lane x copies page x of a tile.  The pages and the exponents of four tiles' 32 blocks are looked
+        // up by a lane each, four tiles ahead and in three steps, as each waits for the one before
+        // (looked up a tile ahead in one go they took 1.6 us a tile, and bound trees).
         const int page = 1 << a.page_log2, box = page < kBN ? page : kBN;  // keys per copy
         const int in_page = (page >> kCodeBlockLog2) - 1;
+        constexpr int kBlocks = kBN / kCodeBlock, kBatch = 32 / kBlocks;   // of a tile; tiles of a batch
         const CodedPool &pool = a.coded;
         const uint64_t once = l2_evict_first_policy();
         uint32_t c = 0, used = 0, g = 0;  // positions copied; stages in use (at most all)
@@ -226,51 +208,67 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
             const int n = pc.j1 - pc.j0;
             const int32_t *table = a.page_table + (long long)pc.b * a.max_pages;
             const bool evict = a.kv_stream && pc.n <= 2 * tq;
-            // row of the pool where lane x's copy of tile tl starts, -1: none
-            auto row_of = [&](int tl) -> int {
-                const int key = (pc.j0 + tl) * kBN + lane * box;
-                if (tl >= n || lane * box >= kBN || key >= pc.keys) return -1;
-                const int id = table[key >> a.page_log2];
-                if (id < 0 || id >= a.n_pages) {  // nothing outside the pool is read: the copy fills zeros
-                    atomicOr(&a.status[pc.b], RS_ST_BAD_PAGE);
-                    return a.n_pages << a.page_log2;
-                }
-                return (id << a.page_log2) + (key & (page - 1));
+            // this lane's block of batch `bat`; its page: -1 none, -2 a bad one
+            auto block_at = [&](int bat) { return (pc.j0 + bat * kBatch) * kBlocks + lane; };
+            auto there = [&](int bat) { return bat * kBatch + lane / kBlocks < n && (long long)block_at(bat) * kCodeBlock < pc.keys; };
+            auto page_of = [&](int bat) { return there(bat) ? table[block_at(bat) >> (a.page_log2 - kCodeBlockLog2)] : -1; };
+            auto checked = [&](int bat, int id) -> int {
+                if (!there(bat)) return -1;
+                if (id >= 0 && id < a.n_pages) return id;
+                atomicOr(&a.status[pc.b], RS_ST_BAD_PAGE);  // nothing outside the pool is read: the copy fills zeros
+                return -2;
             };
-            // exponents of lane x's block of tile tl, as the softmax takes them
-            auto exps_of = [&](int tl) -> int {
-                const int j = (pc.j0 + tl) * (kBN / kCodeBlock) + lane;
-                int ek = 0, ev = 0;
-                if (tl < n && lane < kBN / kCodeBlock && (long long)j * kCodeBlock < pc.keys) {
-                    const int id = table[j >> (a.page_log2 - kCodeBlockLog2)];
-                    if (id >= 0 && id < a.n_pages) {
-                        const long long at = (((long long)id << (a.page_log2 - kCodeBlockLog2)) + (j & in_page)) * a.Hkv + pc.kvh;
-                        ek = pool.ke[at];
-                        ev = pool.ve[at];
-                    }
-                }
-                return (code_exp(ek, BF16) + 127) | (code_exp(ev, BF16) + 128) << 8;
-            };
-            int row = row_of(0), last = -1, exps = exps_of(0), next_row = -1, next_exps = 0;
+            auto exp_at = [&](int bat, int id) { return (((long long)id << (a.page_log2 - kCodeBlockLog2)) + (block_at(bat) & in_page)) * a.Hkv + pc.kvh; };
+            auto packed = [&](int id, int ek, int ev) { return id < 0 ? 0 : (code_exp(ek, BF16) + 127) | (code_exp(ev, BF16) + 128) << 8; };
+            int id = checked(0, page_of(0)), id1 = -1, ek1 = 0, ev1 = 0;
+            int exps = packed(id, id >= 0 ? pool.ke[exp_at(0, id)] : 0, id >= 0 ? pool.ve[exp_at(0, id)] : 0);
+            int row = -1, last = -1;
             for (int pos = 0; pos < 2 * n; ++pos, ++c) {
                 const bool v = is_v(pos, n);
                 const int tl = tile_at(pos, n);
-                if (!v) {  // the lookups of the next tile
-                    if (pos > 0) {
-                        last = row;
-                        row = next_row;
-                        exps = next_exps;
+                if (!v) {
+                    const int bat = tl / kBatch, q = tl % kBatch;
+                    if (q == 0 && tl > 0) {
+                        id = id1;
+                        exps = packed(id, ek1, ev1);
                     }
-                    next_row = row_of(tl + 1);
-                    next_exps = exps_of(tl + 1);
+                    // row of the pool where lane x's copy of the tile starts, -1: none
+                    last = row;
+                    const int from = __shfl_sync(0xffffffffu, id, q * kBlocks + min(lane * (box >> kCodeBlockLog2), kBlocks - 1));
+                    row = lane * box >= kBN || from == -1 ? -1
+                          : from < 0 ? a.n_pages << a.page_log2 : (from << a.page_log2) + (((pc.j0 + tl) * kBN + lane * box) & (page - 1));
+                    if (q == 0) id1 = page_of(bat + 1);
+                    if (q == 1) {
+                        id1 = checked(bat + 1, id1);
+                        if (id1 >= 0) {
+                            const long long at = exp_at(bat + 1, id1);
+                            ek1 = pool.ke[at];
+                            ev1 = pool.ve[at];
+                        }
+                    }
                 }
-                // (V of the tile before, but for the last one, which follows its own K's successor)
-                const int from = v ? (pos == 2 * n - 1 ? row : last) : row;
+                // (V of the tile before, but for the last one, which follows its own K)
+                const int from = v && pos < 2 * n - 1 ? last : row;
                 const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, from >= 0)) * (uint32_t)(box * D);
                 const uint32_t st = c % NC;
                 if (!(ok = warp_wait(&cempty[st], (c / NC & 1) ^ 1, s_abort, a.wait_limit))) break;
-                if (!v && lane < kBN / kCodeBlock)
-                    *reinterpret_cast<unsigned short *>(s_exp + ((g + tl) % S::kExps) * 16 + lane * 2) = (unsigned short)exps;
+                if (!v && tl % kBatch == 0) {
+                    // the batch's exponents, and the largest of each tile's eight blocks, which lie side by side
+                    const int ek = exps & 255, ev = exps >> 8;
+                    int top_k = ek, low_k = exps ? ek : 255, top_v = ev, low_v = exps ? ev : 255;
+#pragma unroll
+                    for (int d = 1; d < kBlocks; d *= 2) {
+                        top_k = max(top_k, __shfl_xor_sync(0xffffffffu, top_k, d));
+                        low_k = min(low_k, __shfl_xor_sync(0xffffffffu, low_k, d));
+                        top_v = max(top_v, __shfl_xor_sync(0xffffffffu, top_v, d));
+                        low_v = min(low_v, __shfl_xor_sync(0xffffffffu, low_v, d));
+                    }
+                    unsigned char *to = s_exp + ((g + tl + lane / kBlocks) % S::kExps) * 32;
+                    // (a block without keys or of a bad page: any exponent, as its codes are 0)
+                    *reinterpret_cast<unsigned short *>(to + lane % kBlocks * 2) = (unsigned short)(exps ? exps : top_k | top_v << 8);
+                    if (lane % kBlocks == 0)
+                        *reinterpret_cast<int *>(to + 16) = top_k | top_v << 8 | (top_k - low_k <= 15 && top_v - low_v <= 15 ? 1 << 16 : 0);
+                }
                 __syncwarp();
                 if (lane == 0) mbar_expect_tx(&cfull[st], tx);
                 __syncwarp();
@@ -446,9 +444,9 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
             const int open = pc.ctx + (a.anc ? 0 : tok0 + 1);  // keys that every row of the tile sees
             const int seen = pc.ctx + tok + 1;                 // causal: keys this row sees
             float m = -INFINITY, ref = -INFINITY, l = 0.f, rowf = cexp;
-            // One key tile; masked: some row does not see all of the keys.
-            auto tile = [&](auto masked_t, int tl) -> bool {
-                constexpr bool masked = decltype(masked_t)::value;
+            // One key tile; masked: some row does not see all of the keys.  (Code that runs once a tile and
+            // not twice: the kernel's roles share an instruction cache.)
+            auto tile = [&](bool masked, int tl) -> bool {
                 const uint32_t t = g + tl;
                 const int key0 = (pc.j0 + tl) * kBN;
                 uint32_t mk[4] = {};                    // the keys this row sees
@@ -488,16 +486,14 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                     ++done;
                     return true;
                 }
-                const uint4 exps = *reinterpret_cast<const uint4 *>(s_exp + (t % S::kExps) * 16);
-                auto pair = [&](int b) { return b < 2 ? exps.x : b < 4 ? exps.y : b < 6 ? exps.z : exps.w; };
-                auto two_ek = [&](int b) { return __uint_as_float(__byte_perm(pair(b), 0, b & 1 ? 0x4442 : 0x4440) << 23); };
-                auto ev_of = [&](int b) { return __uint_as_float(__byte_perm(pair(b), 0x4b000000u, b & 1 ? 0x7443 : 0x7441)) - 8388736.f; };
-                auto factor = [&](int b) { return fmaxf(rowf * two_ek(b), 0x1p-126f); };  // not 0: hidden scores stay -inf
-                // the row's maxima, 64 keys at a time
-                float mt = -INFINITY, rmax = -INFINITY, ev_min = INFINITY;
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    uint32_t va[32], vb[32];
+                const unsigned char *exps = s_exp + (t % S::kExps) * 32;
+                const int head = *reinterpret_cast<const int *>(exps + 16);
+                const bool same = head >> 16 & 1;  // one exponent for all of the tile's K, one for its V
+                // (factors are not 0: hidden scores stay -inf)
+                auto factor = [&](int e2) { return fmaxf(rowf * __uint_as_float((uint32_t)(e2 & 255) << 23), 0x1p-126f); };
+                auto offset = [&](int e2) { return (float)((e2 >> 8 & 255) - 128); };
+                auto block = [&](int b) { return (int)*reinterpret_cast<const unsigned short *>(exps + 2 * b); };
+                auto load64 = [&](int hh, uint32_t (&va)[32], uint32_t (&vb)[32]) {
                     tmem_ld32(s_tm + hh * 64, va);
                     tmem_ld32(s_tm + hh * 64 + 32, vb);
                     tmem_wait_ld();
@@ -507,18 +503,45 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                         hide(va, hh ? mk[2] : mk[0]);
                         hide(vb, hh ? mk[3] : mk[1]);
                     }
+                };
+                auto scores = [&](int b, uint32_t (&va)[16]) {  // of block b
+                    tmem_ld16(s_tm + b * 16, va);
+                    tmem_wait_ld16(va);
+                    if (masked) {
+                        const uint32_t see = (b < 2 ? mk[0] : b < 4 ? mk[1] : b < 6 ? mk[2] : mk[3]) >> (b & 1 ? 16 : 0);
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        float m0 = -INFINITY, m1 = -INFINITY;
+                        for (int e = 0; e < 16; ++e)
+                            if (!((see >> e) & 1u)) va[e] = 0xff800000u;
+                    }
+                };
+                const float c_all = factor(head), ev_all = offset(head);
+                // the row's maxima, 64 keys at a time
+                float mt, rmax, ev_min = ev_all;
+                if (same) {
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const int i = b * 16 + e;
-                            m0 = fmaxf(m0, __uint_as_float(i < 32 ? va[i & 31] : vb[i & 31]));
-                            m1 = fmaxf(m1, __uint_as_float(i < 32 ? va[(i + 1) & 31] : vb[(i + 1) & 31]));
-                        }
-                        const float xb = fmaxf(m0, m1) * factor(hh * 4 + b), ev = ev_of(hh * 4 + b);
-                        mt = fmaxf(mt, xb);
-                        rmax = fmaxf(rmax, xb + ev);
+                    for (int hh = 0; hh < 2; ++hh) {
+                        uint32_t va[32], vb[32];
+                        load64(hh, va, vb);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            mx[e & 3] = fmaxf(mx[e & 3], fmaxf(__uint_as_float(va[e]), __uint_as_float(vb[e])));
+                    }
+                    mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c_all;
+                    rmax = mt + ev_all;
+                } else {
+                    mt = rmax = -INFINITY;
+#pragma unroll 1
+                    for (int b = 0; b < 8; ++b) {
+                        uint32_t va[16];
+                        scores(b, va);
+                        float x = -INFINITY;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x = fmaxf(x, __uint_as_float(va[e]));
+                        const float ev = offset(block(b));
+                        x *= factor(block(b));
+                        mt = fmaxf(mt, x);
+                        rmax = fmaxf(rmax, x + ev);
                         ev_min = fminf(ev_min, ev);
                     }
                 }
@@ -545,65 +568,63 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                     }
                 }
                 const float mn = m == -INFINITY ? 0.f : m, up = ref == -INFINITY ? 0.f : 7.f - ref;
-                // P' of a block may vanish in fp32 while its keys count for l (values 2^90 below
-                // others'): then l is summed by itself
-                const bool apart = __any_sync(0xffffffffu, -up - ev_min - mn > 90.f);
+                // P' may vanish in fp32 while its keys count for l (values 2^90 below others'): then l is
+                // summed by itself; so it is where the blocks' exponents differ too much
+                const bool apart = !same || __any_sync(0xffffffffu, -up - ev_min - mn > 90.f);
                 if (apart) {
-#pragma unroll
-                    for (int ch = 0; ch < 4; ++ch) {
-                        uint32_t va[32];
-                        tmem_ld32(s_tm + ch * 32, va);
-                        tmem_wait_ld();
-                        tmem_regs_ready(va);
-                        if (masked) hide(va, mk[ch]);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) l += ex2(fmaf(__uint_as_float(va[e]), factor(ch * 2 + e / 16), -mn));
-                    }
-                }
 #pragma unroll 1
-                for (int hh = 0; hh < 2; ++hh) {
-                    uint32_t va[32], vb[32], xp[32];
-                    tmem_ld32(s_tm + hh * 64, va);
-                    tmem_ld32(s_tm + hh * 64 + 32, vb);
-                    float c[4], nb[4], sum[4][2];
+                    for (int b = 0; b < 8; ++b) {
+                        uint32_t va[16];
+                        scores(b, va);
+                        const float c = same ? c_all : factor(block(b));
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        c[b] = hh ? factor(4 + b) : factor(b);
-                        nb[b] = (hh ? ev_of(4 + b) : ev_of(b)) + up;
-                    }
-                    tmem_wait_ld();
-                    tmem_regs_ready(va);
-                    tmem_regs_ready(vb);
-                    if (masked) {
-                        hide(va, hh ? mk[2] : mk[0]);
-                        hide(vb, hh ? mk[3] : mk[1]);
-                    }
-                    if (kApart && hh) {  // S has been read: the next one may be written
-                        tc_fence_before();
-                        warp_arrive(&sfree[x]);
-                    }
-                    exp_blocks(va, vb, c, nb, sum, xp);
-                    if (!apart) {
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) l = fmaf(sum[b][0] + sum[b][1], ex2(-nb[b] - mn), l);
-                    }
-                    if (kApart && !hh && !wait_idle()) return false;
-                    tmem_st32(p_tm + hh * 32, xp);
-                    if (!kApart || hh) {
-                        tmem_wait_st();
-                        tc_fence_before();
-                        warp_arrive(kApart || !hh ? &pfull[x] : &pfull2[x]);
+                        for (int e = 0; e < 16; ++e) l += ex2(fmaf(__uint_as_float(va[e]), c, -mn));
                     }
                 }
+                float sum4[4] = {0.f, 0.f, 0.f, 0.f};
+                if (same) {
+#pragma unroll 1
+                    for (int hh = 0; hh < 2; ++hh) {
+                        uint32_t va[32], vb[32], xp[32];
+                        load64(hh, va, vb);
+                        if (kApart && hh) {  // S has been read: the next one may be written
+                            tc_fence_before();
+                            warp_arrive(&sfree[x]);
+                        }
+                        exp_pairs<false>(va, vb, c_all, ev_all + up, sum4, xp);
+                        if (kApart && !hh && !wait_idle()) return false;
+                        tmem_st32(p_tm + hh * 32, xp);
+                        if (!kApart || hh) {
+                            tmem_wait_st();
+                            tc_fence_before();
+                            warp_arrive(kApart || !hh ? &pfull[x] : &pfull2[x]);
+                        }
+                    }
+                } else {
+                    if (kApart && !wait_idle()) return false;
+#pragma unroll 1
+                    for (int b = 0; b < 8; ++b) {  // (P over S: of columns that have been read)
+                        uint32_t va[16], xp[8];
+                        scores(b, va);
+                        const float c = factor(block(b)), nb = offset(block(b)) + up;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            xp[e] = pack16<false>(ex2(fmaf(__uint_as_float(va[2 * e]), c, nb)), ex2(fmaf(__uint_as_float(va[2 * e + 1]), c, nb)));
+                        tmem_st8(p_tm + b * 8, xp);
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    if (kApart) warp_arrive(&sfree[x]);
+                    warp_arrive(&pfull[x]);
+                    if (!kApart) warp_arrive(&pfull2[x]);
+                }
+                if (!apart) l = fmaf((sum4[0] + sum4[1]) + (sum4[2] + sum4[3]), ex2(-up - ev_all - mn), l);
                 ++done;
                 return true;
             };
-            int tl = first;
             const int n_open = min(n, open / kBN - pc.j0);
 #pragma unroll 1
-            for (; ok && tl < n_open; tl += step) tile(std::false_type(), tl);
-#pragma unroll 1
-            for (; ok && tl < n; tl += step) tile(std::true_type(), tl);
+            for (int tl = first; ok && tl < n; tl += step) tile(tl >= n_open, tl);
             if (!ok || !(ok = quick_wait(&pvdone[x], (done - 1) & 1, s_abort, a.wait_limit))) break;
             tc_fence_after();
             // log2 of the sum of the weights, and what O' has to be multiplied with, as a power of two
@@ -679,78 +700,105 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
     } else {
         reg_dealloc<kCoRegsDecode>();
         // ---------------------------------------------------------- codes to tiles
-        // The four warps turn one copied tile after the other into fp16, each a quarter of its
-        // rows; a lane has 16 codes of a row, 32 bytes of the tile.
+        // Four warps turn a copied tile into fp16, each a quarter of its rows; a lane has 16 codes of
+        // a row, 32 bytes of the tile.  (Two groups of four that take turns need registers that the
+        // softmax warps miss more.)
         constexpr int kRowLanes = D / 16, kRowsStep = 128 / kRowLanes, kLoads = kBN / kRowsStep;
-        const int ci = tid - kCoDecodeWarp * 32, part = ci % kRowLanes, row0 = ci / kRowLanes;
-        uint32_t c = 0, quse[2] = {0, 0};  // positions done
+        const int ci = tid & 127, part = ci % kRowLanes, row0 = ci / kRowLanes;
+        uint32_t before = 0, quse[2] = {0, 0};  // positions of earlier pieces; Q tiles
         bool ok = true;
         while (ok && cur.next(pc)) {
             const int n = pc.j1 - pc.j0;
 #pragma unroll 1
-            for (int pos = 0; pos < 2 * n; ++pos, ++c) {
-                const uint32_t cst = c % NC, st = c % NR;
-                const int keys = pc.keys - (pc.j0 + tile_at(pos, n)) * kBN;  // of the tile; behind them anything, NaN too
+            for (int pos = 0; pos < 2 * n; ++pos) {
+                const uint32_t c = before + pos, cst = c % NC, st = c % NR;
+                const int keys = pc.keys - (pc.j0 + tile_at(pos, n)) * kBN;  // of the tile
                 if (!(ok = quick_wait2(&cfull[cst], c / NC & 1, &empty[st], (c / NR & 1) ^ 1, s_abort, a.wait_limit))) break;
-                const unsigned char *codes = smem + S::kCodes + cst * (kBN * D) + ci * 16;
+                const unsigned char *codes = smem + S::kCodes + cst * (kBN * D);
                 unsigned char *tile = smem + S::kRing + st * S::kTile;
+                const bool v_tile = is_v(pos, n);
+                const unsigned char *exps = s_exp + ((before / 2 + tile_at(pos, n)) % S::kExps) * 32;
+                const int head = *reinterpret_cast<const int *>(exps + 16);
+                const int top = head >> (v_tile ? 8 : 0) & 255;
+                const bool scaled = head >> 16 & 1;
+                const unsigned char *exp = exps + (v_tile ? 1 : 0) + row0 / kCodeBlock * 2;
+                // A lane's 16 codes are two words of eight: at D = 128 one of each 64 columns (of odd rows the
+                // second first), at D = 64 side by side.  All go to other banks that way, there and here.
+                const unsigned char *const from = codes + row0 * D + (D == 128 ? (row0 & 1) * 64 + part * 8 : part * 16);
+                const int step = D == 128 ? (row0 & 1 ? -64 : 64) : 8;
+                // 128-byte swizzle: 16-byte word w of row r at w ^ (r & 7)
+                unsigned char *const to = tile + row0 * 128;
+                const int at0 = D == 128 ? (row0 & 1) * 16384 + ((part ^ (row0 & 7)) * 16) : ((2 * part) ^ (row0 & 7)) * 16;
+                const int at1 = D == 128 ? at0 ^ 16384 : ((2 * part + 1) ^ (row0 & 7)) * 16;
+#pragma unroll 1
+                for (int i0 = 0; i0 < kLoads; i0 += 4) {
+                    uint2 x[4], y[4];  // (all loads before the first store, which the compiler does not move them over)
+                    uint32_t f[4];
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    const int row = i * kRowsStep + row0, kb = part / 4, w = part % 4 * 2;
-                    uint4 v = *reinterpret_cast<const uint4 *>(codes + i * 2048);
-                    if (row >= keys) v = make_uint4(0, 0, 0, 0);
-                    uint4 lo, hi;
-                    decode4(v.x, lo.x, lo.y);
-                    decode4(v.y, lo.z, lo.w);
-                    decode4(v.z, hi.x, hi.y);
-                    decode4(v.w, hi.z, hi.w);
-                    // 128-byte swizzle: 16-byte word w of row r at w ^ (r & 7).  Lanes of the second 64
-                    // columns write their second word first: another set of banks
-                    unsigned char *dst = tile + kb * 16384 + row * 128;
-                    *reinterpret_cast<uint4 *>(dst + ((w + kb) ^ (row & 7)) * 16) = kb ? hi : lo;
-                    *reinterpret_cast<uint4 *>(dst + ((w + 1 - kb) ^ (row & 7)) * 16) = kb ? lo : hi;
+                    for (int i = 0; i < 4; ++i) {
+                        x[i] = *reinterpret_cast<const uint2 *>(from + (i0 + i) * 2048);
+                        y[i] = *reinterpret_cast<const uint2 *>(from + (i0 + i) * 2048 + step);
+                        const int down = scaled ? top - exp[(i0 + i) * (kRowsStep / kCodeBlock) * 2] : 0;
+                        f[i] = down < 15 ? (uint32_t)(15 - down) * 0x04000400u : 0x02000200u;  // 2^-down, twice
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint4 lo, hi;
+                        decode4(x[i].x, lo.x, lo.y);
+                        decode4(x[i].y, lo.z, lo.w);
+                        decode4(y[i].x, hi.x, hi.y);
+                        decode4(y[i].y, hi.z, hi.w);
+                        lo = make_uint4(mul_f16x2(lo.x, f[i]), mul_f16x2(lo.y, f[i]), mul_f16x2(lo.z, f[i]), mul_f16x2(lo.w, f[i]));
+                        hi = make_uint4(mul_f16x2(hi.x, f[i]), mul_f16x2(hi.y, f[i]), mul_f16x2(hi.z, f[i]), mul_f16x2(hi.w, f[i]));
+                        *reinterpret_cast<uint4 *>(to + at0 + (i0 + i) * kRowsStep * 128) = lo;
+                        *reinterpret_cast<uint4 *>(to + at1 + (i0 + i) * kRowsStep * 128) = hi;
+                    }
                 }
+                if (keys < kBN)  // behind the last key anything was copied, NaN too
+#pragma unroll 1
+                    for (int i = 0; i < kLoads; ++i)
+                        if (i * kRowsStep + row0 >= keys) {
+                            *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
+                        }
                 fence_async_smem();
                 warp_arrive(&full[st]);
                 warp_arrive(&cempty[cst]);
-                if (BF16 && pos == 0) {
-                    // Q to fp16 in place, a row to a thread, by a power of two that brings its largest
-                    // value to 2^14 .. 2^15
-                    for (int x = 0; x < 2; ++x) {
-                        if (!takes_part(x)) continue;
-                        if (!(ok = quick_wait(&qfull[x], quse[x] & 1, s_abort, a.wait_limit))) break;
-                        ++quse[x];
-                        unsigned char *row = smem + S::kQ + x * S::kTile + ci * 128;
-                        uint32_t most = 0;
-#pragma unroll 4
-                        for (int i = 0; i < 8 * kKB; ++i) {
-                            const uint4 v = *reinterpret_cast<const uint4 *>(row + (i >> 3) * 16384 + ((i + ci) & 7) * 16);
-                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                if (const int x = pos; BF16 && pos < 2 && takes_part(x)) {
+                    // Q tile x to fp16 in place, a row to a thread, by a power of two that brings its largest value
+                    // to 2^14 .. 2^15
+                    if (!(ok = quick_wait(&qfull[x], quse[x] & 1, s_abort, a.wait_limit))) break;
+                    ++quse[x];
+                    unsigned char *row = smem + S::kQ + x * S::kTile + ci * 128;
+                    uint32_t most = 0;
+#pragma unroll 2
+                    for (int i = 0; i < 8 * kKB; ++i) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(row + (i >> 3) * 16384 + ((i + ci) & 7) * 16);
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const uint32_t lo = (w[e] << 16) & 0x7fffffffu, hi = w[e] & 0x7fff0000u;
-                                most = max(most, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
-                            }
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t lo = (w[e] << 16) & 0x7fffffffu, hi = w[e] & 0x7fff0000u;
+                            most = max(most, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
                         }
-                        const int shift = most ? max((int)(most >> 23) - 127 - 14, -112) : 0;
-                        const float down = pow2i(-shift);
-#pragma unroll 4
-                        for (int i = 0; i < 8 * kKB; ++i) {
-                            uint4 *p = reinterpret_cast<uint4 *>(row + (i >> 3) * 16384 + ((i + ci) & 7) * 16);
-                            uint4 v = *p;
-                            uint32_t *w = &v.x;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                w[e] = pack16<false>(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xffff0000u) * down);
-                            *p = v;
-                        }
-                        s_shift[x * kBM + ci] = (int8_t)shift;
-                        fence_async_smem();
-                        warp_arrive(&qready[x]);
                     }
-                    if (!ok) break;
+                    const int shift = most ? max((int)(most >> 23) - 127 - 14, -112) : 0;
+                    const float down = pow2i(-shift);
+#pragma unroll 2
+                    for (int i = 0; i < 8 * kKB; ++i) {
+                        uint4 *p = reinterpret_cast<uint4 *>(row + (i >> 3) * 16384 + ((i + ci) & 7) * 16);
+                        uint4 v = *p;
+                        uint32_t *w = &v.x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = pack16<false>(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xffff0000u) * down);
+                        *p = v;
+                    }
+                    s_shift[x * kBM + ci] = (int8_t)shift;
+                    fence_async_smem();
+                    warp_arrive(&qready[x]);
                 }
             }
+            before += 2 * n;
         }
     }
     __syncthreads();

@@ -238,7 +238,8 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
     using Sh = RowsShape<D, NT>;
     constexpr int kS = Sh::kStages, kBl = Sh::kBlocks, kSteps = D / 16, kTiles = D / 16;  // k-steps of K Q^T, 16-column tiles of O^T
     extern __shared__ unsigned char smem_raw[];
-    unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    // (an offset and not a rounded address, which would make all loads generic ones)
+    unsigned char *smem = smem_raw + (-sm100::smem_u32(smem_raw) & 1023u);
     __shared__ uint64_t s_full[kRowWarps][kS];
     __shared__ int s_gave_up;
     volatile int *s_abort = &s_gave_up;

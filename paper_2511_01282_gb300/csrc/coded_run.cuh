@@ -26,7 +26,7 @@ rs_status coded_launch_d(const FlashArgs &a, const CUtensorMap &tmq, const CUten
             set_error("%s: kernel attributes: %s", what, cudaGetErrorString(e1 != cudaSuccess ? e1 : e2));
             return RS_ERR_CUDA;
         }
-        const int need = (int)(2 * 128 * kCoRegsSoft + 128 * (kCoRegsProd + kCoRegsDecode));
+        const int need = kCoThreads * 128;
         ready[dev].store(fa.numRegs * kCoThreads >= need ? 1 : -1);
     }
     if (ready[dev].load() != 1) {
