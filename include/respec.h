@@ -590,7 +590,7 @@ rs_status rs_paged_evict(uint16_t *k_pages, uint16_t *v_pages, int Hkv, int D, i
  *
  * Exponents lie within -117 .. 120 in a cache of bf16 values and within -15 .. 8 in
  * one of fp16 values (outside, they count as the nearest of these): there code x
- * 2^exponent is exact in that type (fp16 at exponent 8: codes up to 240).  A cache
+ * 2^exponent is exact in that type (at the largest exponent: codes up to 240).  A cache
  * is read with the type that it was appended with.
  */
 
@@ -600,8 +600,8 @@ rs_status rs_paged_evict(uint16_t *k_pages, uint16_t *v_pages, int Hkv, int D, i
  *     e    = the least exponent of the type's range with max |x| <= 448 x 2^e over
  *            the block's new finite values; where slots of the block lie below
  *            ctx_len[b] (their tokens stay), at least the block's exponent so far;
- *     code = e4m3(x / 2^e), to nearest even; infinities and NaN become NaN; fp16 at
- *            e = 8 stops at 240.
+ *     code = e4m3(x / 2^e), to nearest even; infinities and NaN become NaN; at
+ *            the largest exponent it stops at 240 (values up to 1/16 above it become it).
  * Codes that stay in a block whose exponent grows become e4m3(code / 2^(growth)):
  * exact, but for results below 2^-6, which round to steps of 2^-9.
  *   k, v, strides, new_off, B, T, status: as for rs_paged_append (B <= 2^28);
@@ -619,9 +619,11 @@ rs_status rs_coded_append(const uint16_t *k, int64_t k_stride, const uint16_t *v
  *            work is laid out by it.  A request that has more is rejected with
  *            RS_ST_TOO_LARGE.  T where nothing better is known.
  *   the rest as for rs_paged_attn.  Size the workspace with the same six sizes.
- * Where max_new x Hq / Hkv <= 32, P is rounded to fp16 (2^-12 relative) and NaN in V
- * of a key that a row does not see reaches it only within a block of 16 slots that
- * it sees a part of; else as rs_paged_attn.  The result does not depend on what
+ * P is rounded to fp16 (2^-12 relative; weights below 2^-32 of a row's largest may
+ * vanish); bf16 queries are taken times a power of two as fp16 (elements below 2^-39
+ * of a row's largest may vanish).  NaN in V of a key that a row does not see reaches
+ * it only where it sees another key of the same 16 slots (max_new x Hq / Hkv <= 32) or
+ * another row of its 128-row tile sees it (else).  The result does not depend on what
  * else runs: the same bits every time.
  */
 size_t rs_coded_attn_workspace_size(int B, int T, int max_new, int Hq, int Hkv, int D);

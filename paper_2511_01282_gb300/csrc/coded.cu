@@ -106,7 +106,7 @@ __device__ __forceinline__ void code_block(const uint4 (&x)[kSteps], uint8_t *co
             e = before;
         }
     }
-    if (odd || (!BF16 && e == code_exp_max(false))) {  // not finite: NaN; fp16 at the largest exponent: no code above 240
+    if (odd || e == code_exp_max(BF16)) {  // not finite: NaN; at the largest exponent: no code above 240
         const float f = pow2i(-e);
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
@@ -118,7 +118,7 @@ __device__ __forceinline__ void code_block(const uint4 (&x)[kSteps], uint8_t *co
                 float2 g = unpack16<BF16>(pick(x[u], i));
                 g.x = fabsf(g.x) == INFINITY ? NAN : g.x * f;
                 g.y = fabsf(g.y) == INFINITY ? NAN : g.y * f;
-                if (!BF16 && e == code_exp_max(false)) {
+                if (e == code_exp_max(BF16)) {
                     if (fabsf(g.x) > 240.f) g.x = copysignf(240.f, g.x);
                     if (fabsf(g.y) > 240.f) g.y = copysignf(240.f, g.y);
                 }

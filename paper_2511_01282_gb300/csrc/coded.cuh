@@ -18,8 +18,8 @@ namespace rs {
 constexpr int kCodeBlock = 16, kCodeBlockLog2 = 4;  // tokens that share an exponent
 
 // Exponents that values of a type get: 2^e x code has to be representable, from the
-// smallest step (2^-9 x 2^e) on.  An fp16 cache at e = 8 stops at code 240 (61440; a
-// larger one, 256 = 65536, is above fp16's largest value).
+// smallest step (2^-9 x 2^e) on.  At the largest exponent the codes stop at 240: the
+// next one, 256 x 2^e, is above the type's largest value (2^16 and 2^128).
 __host__ __device__ constexpr int code_exp_min(bool bf16) { return bf16 ? -117 : -15; }
 __host__ __device__ constexpr int code_exp_max(bool bf16) { return bf16 ? 120 : 8; }
 __device__ __forceinline__ int code_exp(int e, bool bf16) { return min(max(e, code_exp_min(bf16)), code_exp_max(bf16)); }

@@ -47,7 +47,7 @@ def exponent(values, dtype):
 def block_codes(x, e, dtype):
     """Codes of new values x (a tensor) at exponent e."""
     x = torch.where(x.to(F64).isinf(), math.nan, x.to(F64)) * 2.0 ** -e
-    if dtype == torch.float16 and e == RANGE[dtype][1]:
+    if e == RANGE[dtype][1]:
         x = torch.where(x.abs() > 240.0, torch.copysign(torch.full_like(x, 240.0), x), x)
     return encode(x)
 

@@ -22,3 +22,5 @@ def test_exponents():
         assert cr.exponent([448.0, -1.0], dt) == 0 and cr.exponent([-448.5], dt) == 1 and cr.exponent([224.0], dt) == -1
         assert cr.exponent([torch.finfo(dt).max], dt) == hi
     assert cr.decode(cr.block_codes(torch.tensor([65504.0, -65504.0, 61000.0]).half(), 8, torch.float16)).tolist() == [240.0, -240.0, 240.0]
+    most = torch.finfo(torch.bfloat16).max
+    assert cr.decode(cr.block_codes(torch.tensor([most, -most]).bfloat16(), 120, torch.bfloat16)).tolist() == [240.0, -240.0]
