@@ -3,6 +3,8 @@
 ``respec``   -- binding of the C ABI in ``include/respec.h``
 ``pipeline`` -- ``VerifyStep``: device buffers + the four calls of one step
 ``paged``    -- ``PagedCache``: a paged KV cache and its calls; prompt attention
+``shared``   -- ``SharedCache``: requests that share the pages of one pool
+``rotary``   -- ``Rotary``: rotary positions of queries and keys
 ``build``    -- in-tree nvcc build of ``librespec.so``
 """
 from . import respec  # noqa: F401

@@ -1,7 +1,7 @@
 """Synthetic end-to-end loop of Algorithm 1 over many decoding steps.
 
-A random-weight decoder-only transformer (GQA, head dim 64, no positional
-encoding, RMSNorm, SwiGLU MLP, an untied output head scaled to logits of
+A random-weight decoder-only transformer (GQA, head dim 64, rotary positions
+on request, RMSNorm, SwiGLU MLP, an untied output head scaled to logits of
 standard deviation ~6, which gives rows a median entropy of ~1.8 nats) plays
 the target model; the
 same architecture with perturbed weights plays the draft model.  Both run
@@ -27,7 +27,14 @@ With ``cache="paged"`` both models keep their keys and values in pages
 (``rs_prompt_attn``, ``rs_paged_append``), trees are verified by
 ``rs_paged_attn``, and with a ``budget`` every commit adds the committed rows'
 attention weights to the keys they see (``rs_paged_weights``) and a cache
-that has outgrown the budget is cut back to it (``rs_paged_evict``).
+that has outgrown the budget is cut back to it (``rs_paged_evict``).  With
+``bits=8`` the pages hold 8 bits a value (``rs_coded_append``,
+``rs_coded_attn``); the tokens are then those of the rounded cache, not
+exactly the target's.
+
+With ``rotary=True`` queries and keys are turned by their positions
+(``rs_rotary``) before the cache takes them; a tree's node lies at the prefix's
+end plus its depth.
 
 With tau = 0 the relaxed check accepts only argmax tokens, so the loop must
 reproduce the target's plain greedy decoding token for token
@@ -47,6 +54,7 @@ import torch
 
 from . import respec as rs
 from .paged import PagedCache, prompt_attention
+from .rotary import Rotary
 
 
 def _rms(x, eps=1e-6):
@@ -57,7 +65,7 @@ class TinyLM:
     """Random-weight GQA decoder; attention through rs_tree_verify_attn."""
 
     def __init__(self, V=4096, d=256, L=2, Hq=4, Hkv=2, D=64, ffn=512, seed=0, logit_std=6.0,
-                 base=None, noise=0.0, device="cuda"):
+                 base=None, noise=0.0, device="cuda", rotary=False):
         self.V, self.d, self.L, self.Hq, self.Hkv, self.D = V, d, L, Hq, Hkv, D
         self.logit_scale = logit_std / math.sqrt(d)  # unit-RMS state, unit-variance head
         self.device = torch.device(device)
@@ -77,22 +85,36 @@ class TinyLM:
             if base is not None:
                 t = base.p[n].cpu() + noise * torch.randn(t.shape, generator=g) * t.std()
             self.p[n] = t.to(self.device)
+        self.rotary = Rotary(D, device=self.device) if rotary else None
 
     # ------------------------------------------------------------ KV cache
     def new_cache(self, cap):
         z = lambda: torch.zeros((cap, self.Hkv, self.D), dtype=torch.bfloat16, device=self.device)  # noqa: E731
         return dict(K=[z() for _ in range(self.L)], V=[z() for _ in range(self.L)], cap=cap, S=0)
 
-    def new_paged_cache(self, cap, page_size=32, budget=None, recent=0):
+    def new_paged_cache(self, cap, page_size=32, budget=None, recent=0, bits=16):
         """The same in pages; with a budget it is cut back to that many tokens whenever it has more after a commit."""
-        layers = [PagedCache(1, cap, page_size, self.Hkv, self.D, track_weights=budget is not None, device=self.device)
+        layers = [PagedCache(1, cap, page_size, self.Hkv, self.D, track_weights=budget is not None, device=self.device, bits=bits)
                   for _ in range(self.L)]
         return dict(layers=layers, cap=cap, S=0, seen=0, budget=budget, recent=recent, rows=[None] * self.L, ws=None)
 
-    def _qkv(self, x, i):
+    def _qkv(self, x, i, pos):
+        """bf16 queries, keys and values of layer i; pos [N] int32 their positions, None without rotary ones."""
         h, N = _rms(x), x.shape[0]
         heads = lambda w, n: (h @ self.p["%s.%d" % (w, i)]).view(N, n, self.D).to(torch.bfloat16)  # noqa: E731
-        return heads("wq", self.Hq), heads("wk", self.Hkv), heads("wv", self.Hkv)
+        q, k, v = heads("wq", self.Hq), heads("wk", self.Hkv), heads("wv", self.Hkv)
+        if pos is not None:
+            self.rotary(q, k, pos, out=(q, k))
+        return q, k, v
+
+    def _positions(self, first, parents):
+        """A tree's positions: its root's is first, a node's its parent's plus one."""
+        if self.rotary is None:
+            return None
+        depth, at = (parents >= 0).int(), parents.clamp(min=0).long()
+        for _ in range(8):  # 2^8 nodes at most
+            depth, at = depth + depth[at], at[at]
+        return depth + first
 
     def _layer_end(self, x, out, i):
         x = x + out.reshape(x.shape[0], self.Hq * self.D) @ self.p["wo.%d" % i]
@@ -104,9 +126,10 @@ class TinyLM:
         N = tokens.numel()
         assert cache["S"] == 0 and N <= cache["cap"]
         off = torch.tensor([0, N], dtype=torch.int32, device=self.device)
+        pos = torch.arange(N, dtype=torch.int32, device=self.device) if self.rotary else None
         x = self.p["emb"][tokens]
         for i, layer in enumerate(cache["layers"]):
-            q, k, v = self._qkv(x, i)
+            q, k, v = self._qkv(x, i, pos)
             out, lse, status, cache["ws"] = prompt_attention(q, k, v, off, self.D ** -0.5, cache["ws"])
             layer.report(status)
             layer.append(k, v, off)
@@ -120,9 +143,10 @@ class TinyLM:
         dev = self.device
         off = torch.tensor([0, N], dtype=torch.int32, device=dev)
         pos = torch.arange(cache["seen"], cache["seen"] + N, dtype=torch.int32, device=dev)
+        turned = self._positions(cache["seen"], parents)
         x = self.p["emb"][tokens]
         for i, layer in enumerate(cache["layers"]):
-            q, k, v = self._qkv(x, i)
+            q, k, v = self._qkv(x, i, turned)
             layer.append(k, v, off, pos)
             out, lse = layer.attend(q, off, self.D ** -0.5, parents)
             cache["rows"][i] = (q, lse)
@@ -169,12 +193,10 @@ class TinyLM:
         out = torch.empty((N, self.Hq, self.D), dtype=torch.float32, device=dev)
         lse = torch.empty((N, self.Hq), dtype=torch.float32, device=dev)
         status = torch.empty(1, dtype=torch.int32, device=dev)
+        pos = self._positions(S, parents)
         x = self.p["emb"][tokens]
         for i in range(self.L):
-            h = _rms(x)
-            q = (h @ self.p["wq.%d" % i]).view(N, self.Hq, self.D).to(torch.bfloat16).contiguous()
-            cache["K"][i][S:S + N] = (h @ self.p["wk.%d" % i]).view(N, self.Hkv, self.D).to(torch.bfloat16)
-            cache["V"][i][S:S + N] = (h @ self.p["wv.%d" % i]).view(N, self.Hkv, self.D).to(torch.bfloat16)
+            q, cache["K"][i][S:S + N], cache["V"][i][S:S + N] = self._qkv(x, i, pos)
             rs.rs_tree_verify_attn(q, cache["K"][i], cache["V"][i], cache["cap"], kv_off, ctx, node_off,
                                    parents, 1, N, self.Hq, self.Hkv, self.D, self.D ** -0.5, out, lse,
                                    status, ws)
@@ -197,6 +219,13 @@ class TinyLM:
                 cache["V"][i][S:S + n] = cache["V"][i][src]
         cache["S"] = S + n
 
+    def _turned(self, x):
+        """Rows 0, 1, ... of x turned, in 64 bits, rounded as in the cache."""
+        a = (torch.arange(x.shape[0]).double()[:, None] * self.rotary.freq).to(self.device)[:, None]
+        lo, hi = x.double().chunk(2, -1)
+        out = torch.cat([lo * a.cos() - hi * a.sin(), hi * a.cos() + lo * a.sin()], -1)
+        return out.to(torch.bfloat16).float()
+
     def dense_logits(self, tokens):
         """Plain causal attention over a whole sequence (bf16-rounded Q, K, V
         as in the cache, fp32 softmax): the independent greedy reference."""
@@ -209,6 +238,8 @@ class TinyLM:
             q = (h @ self.p["wq.%d" % i]).view(T, self.Hq, self.D).to(torch.bfloat16).float()
             k = (h @ self.p["wk.%d" % i]).view(T, self.Hkv, self.D).to(torch.bfloat16).float()
             v = (h @ self.p["wv.%d" % i]).view(T, self.Hkv, self.D).to(torch.bfloat16).float()
+            if self.rotary:
+                q, k = self._turned(q), self._turned(k)
             k, v = k.repeat_interleave(G, dim=1), v.repeat_interleave(G, dim=1)
             s = torch.einsum("qhd,khd->hqk", q, k) * self.D ** -0.5
             s = s.masked_fill(~mask, float("-inf"))
@@ -232,7 +263,7 @@ class SpecLoop:
     """One request decoded by the full step of Algorithm 1 (B = 1)."""
 
     def __init__(self, target, draft, prompt, p, widths=(4, 3, 2), cap=4096, acc_cap=64, trace=False,
-                 retrieval="scan", cache="flat", page_size=32, budget=None, recent=64):
+                 retrieval="scan", cache="flat", page_size=32, budget=None, recent=64, bits=16):
         self.t, self.dr, self.p = target, draft, p
         # retrieval: "scan" (rs_match_scan over the buffer) or "index" (an
         # index built over the prompt, the committed tokens appended to it
@@ -240,8 +271,11 @@ class SpecLoop:
         assert retrieval in ("scan", "index")
         self.retrieval = retrieval
         # cache: "flat" (one row per token) or "paged", there with a budget of
-        # tokens per KV head (None: nothing is evicted), the `recent` newest kept
+        # tokens per KV head (None: nothing is evicted), the `recent` newest kept,
+        # or with 8 bits a value
         assert cache in ("flat", "paged") and (budget is None or cache == "paged")
+        if bits == 8 and (cache != "paged" or budget is not None):
+            raise ValueError("bits=8: a paged cache without a budget expected")
         if budget is not None and not 0 <= recent <= budget:
             raise ValueError("recent=%d out of range (0 to the budget of %d tokens)" % (recent, budget))
         # with trace, every step appends host copies of each call's inputs and
@@ -262,7 +296,7 @@ class SpecLoop:
         self.h_best = torch.zeros(1, dtype=torch.float32, device=dev)
         self.ok = torch.zeros(1, dtype=torch.uint8, device=dev)
         if cache == "paged":
-            self.tc, self.dc = (m.new_paged_cache(cap, page_size, budget, recent) for m in (target, draft))
+            self.tc, self.dc = (m.new_paged_cache(cap, page_size, budget, recent, bits) for m in (target, draft))
         else:
             self.tc, self.dc = target.new_cache(cap), draft.new_cache(cap)
         self.ws_attn = torch.empty(max(rs.rs_tree_verify_attn_workspace_size(1, 256, target.Hq, target.Hkv,
@@ -430,9 +464,9 @@ def model_prompt(model, n, seed=0):
     return np.concatenate([start, greedy_reference(model, start, n - 16)]).astype(np.int32)
 
 
-def run(tau, m, n_new=256, prompt_len=512, seed=0, noise=0.1, **cache):
-    target = TinyLM(seed=seed)
-    draft = TinyLM(seed=seed + 1, base=target, noise=noise)
+def run(tau, m, n_new=256, prompt_len=512, seed=0, noise=0.1, rotary=False, **cache):
+    target = TinyLM(seed=seed, rotary=rotary)
+    draft = TinyLM(seed=seed + 1, base=target, noise=noise, rotary=rotary)
     p = rs.params(tau=tau, m=m, span_len=8)
     loop = SpecLoop(target, draft, model_prompt(target, prompt_len, seed), p, **cache)
     loop.generate(n_new)
@@ -449,16 +483,20 @@ def main():
     ap.add_argument("--seeds", type=int, default=1)
     ap.add_argument("--paged", action="store_true", help="keep the caches in pages")
     ap.add_argument("--budget", type=int, default=None, help="tokens a paged cache keeps per KV head")
+    ap.add_argument("--bits", type=int, choices=(8, 16), default=16, help="bits a value of a paged cache")
+    ap.add_argument("--rotary", action="store_true", help="models with rotary positions")
     args = ap.parse_args()
+    if args.bits == 8 and (not args.paged or args.budget is not None):
+        ap.error("--bits 8 needs --paged and no --budget")
     if args.budget is not None and not args.paged:
         ap.error("--budget needs --paged")
     if args.budget is not None and args.budget < 1:
         ap.error("--budget must be at least 1")
-    cache = dict(cache="paged", budget=args.budget, recent=min(64, args.budget or 64)) if args.paged else {}
+    cache = dict(cache="paged", budget=args.budget, recent=min(64, args.budget or 64), bits=args.bits) if args.paged else {}
     taus, ms = ([0.0, 1.0, 2.0, 3.0], [1, 2, 3]) if args.sweep else ([3.0], [2])
     for tau in taus:
         for m in ms:
-            runs = [run(tau, m, n_new=args.tokens, seed=s, **cache) for s in range(args.seeds)]
+            runs = [run(tau, m, n_new=args.tokens, seed=s, rotary=args.rotary, **cache) for s in range(args.seeds)]
             steps = sum(r["steps"] for r in runs)
             row = dict(tau=tau, m=m, seeds=args.seeds, tokens=args.tokens * args.seeds, steps=steps,
                        mean_tokens_per_step=round(sum(r["mean_tokens_per_step"] * r["steps"] for r in runs) / steps, 3),
