@@ -1,0 +1,150 @@
+"""Attention over the cache in 8 bits where single calls of ordinary sizes do not go: caches so long that KV heads are read side by
+side, waits that run out, two calls at once, sizes that reject one of many requests."""
+import random
+
+import pytest
+import torch
+
+from paged_ref import slots
+from test_gpu_coded import Pool, attend, check_attention, fill, i32, rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def rs():
+    from paper_2511_01282_gb300 import respec
+    return respec
+
+
+# The few-row kernel takes several KV heads of a block side by side from 64 blocks and heads a CTA on: with 152 SMs of three
+# CTAs (two from nine rows on), 29184 (19456) of them, so with 4 heads 117000 tokens, with 2 at a time of 6 heads 78000.
+@pytest.mark.parametrize("Hq,Hkv,D,page,n,tree,dt", [
+    (16, 4, 64, 64, 1, False, torch.float16), (12, 6, 64, 16, 3, False, torch.bfloat16), (8, 4, 128, 128, 4, True, torch.bfloat16),
+    (16, 8, 64, 32, 8, True, torch.float16), (12, 6, 128, 256, 16, False, torch.bfloat16)])
+def test_long_caches_with_heads_side_by_side(rs, Hq, Hkv, D, page, n, tree, dt):
+    rows_ = n * Hq // Hkv
+    need = 64 * (456 if rows_ <= 8 else 304) // Hkv * 16
+    ctx = [0, need // 2, 5, 31, need // 4 + 3, 1000, need // 4 + 900, 0]
+    ns = [n, n, 1, 0, max(n - 1, 1), n, n, 1]
+    off = [0]
+    for x in ns:
+        off.append(off[-1] + x)
+    lens = [c + x for c, x in zip(ctx, ns)]
+    assert sum(-(-x // 16) for x, k in zip(lens, ns) if k) * Hkv >= 64 * (456 if rows_ <= 8 else 304)
+    pool = Pool(lens, page, Hkv, D, 5)
+    fill(rs, pool, lens, dt, 21)
+    q = rows(off[-1] + 2, Hq, D, dt, 23)
+    g = random.Random(7)
+    parents = i32([-1 if i == 0 else g.randrange(i) for x in ns for i in range(x)] + [0, 0]) if tree else None
+    got = attend(rs, pool, q, off, ctx, n, D ** -0.5, parents)
+    check_attention(pool, q, off, ctx, D ** -0.5, got, parents)
+    assert (got[0][-2:] == 7).all() and (got[1][-2:] == 7).all()
+    again = attend(rs, pool, q, off, ctx, n, D ** -0.5, parents)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+    # a bad page in the middle of a long request: that one is emptied, the others keep their bits
+    pool.table[4, (need // 8) // page] = pool.n
+    bad = attend(rs, pool, q, off, ctx, n, D ** -0.5, parents)
+    assert bad[2].tolist() == [rs.RS_ST_BAD_PAGE if b == 4 else 0 for b in range(8)]
+    a, e = off[4], off[5]
+    assert (bad[0][a:e] == 0).all() and (bad[1][a:e] == 0).all()
+    for x, y in zip(bad[:2], got[:2]):
+        assert torch.equal(x[:a], y[:a]) and torch.equal(x[e:], y[e:])
+
+
+@pytest.mark.parametrize("n", [1, 300])
+def test_waits_that_run_out_report_it(rs, n, monkeypatch):
+    """A limit of one cycle: the pipelines give up, say so, and the next call works.  (A try to pass a barrier itself waits for some
+    microseconds, so there is enough to do for one to fail.)"""
+    dt, D, Hkv, B = torch.bfloat16, 128, 8, 8
+    lens = [20000 + n] * B
+    pool = Pool(lens, 64, Hkv, D, 6)
+    fill(rs, pool, lens, dt, 71)
+    ctx, off = [20000] * B, [i * n for i in range(B + 1)]
+    q = rows(B * n, 32, D, dt, 73)
+    want = attend(rs, pool, q, off, ctx, n, 0.09)
+    assert want[2].tolist() == [0] * B
+    monkeypatch.setenv("RS_DEBUG_WAIT_LIMIT", "1")
+    short = attend(rs, pool, q, off, ctx, n, 0.09)
+    torch.cuda.synchronize()
+    assert set(short[2].tolist()) <= {0, rs.RS_ST_TIMEOUT}
+    for b, st in enumerate(short[2].tolist()):  # a request that reports nothing has its results
+        if st == 0:
+            assert torch.equal(short[0][off[b]:off[b + 1]], want[0][off[b]:off[b + 1]])
+    monkeypatch.delenv("RS_DEBUG_WAIT_LIMIT")
+    again = attend(rs, pool, q, off, ctx, n, 0.09)
+    assert all(torch.equal(a, b) for a, b in zip(want, again))
+
+
+def test_calls_at_once_with_workspaces_of_their_own(rs):
+    dt, D, Hkv = torch.float16, 64, 2
+    lens = [5000, 700]
+    pool = Pool(lens, 32, Hkv, D, 6)
+    fill(rs, pool, lens, dt, 71)
+    calls = []
+    for i, n in enumerate((1, 4, 60, 300)):
+        off, ctx = [0, n, 2 * n], [5000 - n, 700 - n]
+        calls.append((rows(2 * n, 8, D, dt, 80 + i), off, ctx, n, torch.cuda.Stream()))
+    alone = [attend(rs, pool, q, off, ctx, n, 0.1) for q, off, ctx, n, _ in calls]
+    bufs = []
+    for q, off, ctx, n, _ in calls:
+        need = rs.rs_coded_attn_workspace_size(2, 2 * n, n, 8, Hkv, D)
+        bufs.append((torch.empty_like(q), torch.empty(2 * n, 8, device="cuda"), i32([-1, -1]),
+                     torch.empty(need, dtype=torch.uint8, device="cuda"), i32(off), pool.args(i32(ctx))))
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for (q, off, ctx, n, s), (out, lse, st, ws, offs, args) in zip(calls, bufs):
+            rs.rs_coded_attn(q, 8 * D, rs.RS_F16, offs, None, 2, 2 * n, n, 8, Hkv, D, *args, 0.1, out, lse, st, ws, stream=s)
+    torch.cuda.synchronize()
+    for (out, lse, st, *_), want in zip(bufs, alone):
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]) and st.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("n", [1, 2, 40])
+def test_a_request_with_too_many_tokens_among_others(rs, n):
+    dt, D, Hkv = torch.bfloat16, 128, 2
+    ns = [n, n + 1, 0, n]
+    off = [0]
+    for x in ns:
+        off.append(off[-1] + x)
+    ctx = [200, 300, 5, 0]
+    pool = Pool([c + x for c, x in zip(ctx, ns)], 16, Hkv, D, 6)
+    fill(rs, pool, [c + x for c, x in zip(ctx, ns)], dt, 71)
+    q = rows(off[-1], 8, D, dt, 73)
+    got = attend(rs, pool, q, off, ctx, n, 0.09)
+    assert got[2].tolist() == [0, rs.RS_ST_TOO_LARGE, 0, 0]
+    check_attention(pool, q, off, ctx, 0.09, got, skip=[1])
+    assert (got[0][off[1]:off[2]] == 0).all() and (got[1][off[1]:off[2]] == 0).all()
+
+
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_scores_of_minus_infinity_and_infinite_queries(rs, n, dt):
+    """An infinite query element makes its row's scores infinite of either sign or NaN: that row is not a number, no other changes."""
+    D, Hkv = 64, 2
+    pool = Pool([90 + n], 16, Hkv, D, 6)
+    fill(rs, pool, [90 + n], dt, 71)
+    q = rows(n, 4, D, dt, 73)
+    want = attend(rs, pool, q, [0, n], [90], n, 0.1)
+    q[n - 1, 2, 7] = float("inf")
+    got = attend(rs, pool, q, [0, n], [90], n, 0.1)
+    assert got[2].tolist() == [0]
+    same = torch.ones(n, 4, dtype=torch.bool, device="cuda")
+    same[n - 1, 2] = False
+    assert torch.equal(got[0][same], want[0][same]) and torch.equal(got[1][same], want[1][same])
+    assert got[0][n - 1, 2].isnan().all() and not got[1][n - 1, 2].isfinite()
+
+
+@pytest.mark.parametrize("n,most", [(1, 1), (3, 3), (40, 40)])
+def test_zero_queries_and_a_scale_that_makes_one_key_all(rs, n, most):
+    """Equal weights on every key; and scores so far apart that the largest takes all."""
+    dt, D, Hkv = torch.bfloat16, 128, 1
+    pool = Pool([500 + n], 32, Hkv, D, 6)
+    fill(rs, pool, [500 + n], dt, 71, 0.0)
+    q = rows(n, 2, D, dt, 73)
+    got = attend(rs, pool, q * 0, [0, n], [500], most, 0.1)
+    check_attention(pool, q * 0, [0, n], [500], 0.1, got)
+    got = attend(rs, pool, q, [0, n], [500], most, 30.0)
+    check_attention(pool, q, [0, n], [500], 30.0, got)
+    at = slots(pool.table, 0, 501, 32)
+    assert len(set(at.tolist())) == 501
