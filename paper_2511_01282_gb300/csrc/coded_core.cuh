@@ -2,19 +2,18 @@
 // draft trees.  Plan, pieces and joining are flash.cuh's; so is the arithmetic, but
 // for what the codes change:
 //
-// Products take codes as fp16, times 2^(e - E) with E the largest exponent of the tile's
-// eight blocks: exact while they lie within 15 of each other, and where they do not (values
-// of very different sizes side by side) the codes as they are, with a factor and an offset
-// for each block in the softmax.  (With code 2^e in bf16 tiles, five instructions for two
-// codes instead of two, the converting warps bound the loop: trees of 65 nodes over 32768
-// keys 1356 us.)  The tile's exponents go into the softmax:
-//     S_rj = q_r.K_j,  s_rj = c 2^(Ek) S_rj,  P'_rj = 2^(s_rj + Ev - R_r + 7),
-//     O'_r = sum P'_rj V_j,  l_r = sum 2^(s_rj - m_r) = sum_tiles 2^(R_r - 7 - Ev - m_r) sum P'_rj
-// with m_r and R_r running bounds of s and of s + Ev, moved only when they are exceeded
-// by 2^8 (P' <= 2^15 in fp16, weights down to 2^-32 of the largest stay above its
-// subnormals).  Where Ev is so far below R - m that P' would vanish in fp32 while the
+// Products take codes as fp16, which holds them exactly; the exponents, one for 16 keys,
+// go into the softmax:
+//     S_rj = q_r.K_j,  s_rj = c 2^(ek) S_rj,  P'_rj = 2^(s_rj + ev - R_r + 7),
+//     O'_r = sum P'_rj V_j,  l_r = sum 2^(s_rj - m_r) = sum_blocks 2^(R_r - 7 - ev - m_r) sum P'_rj
+// with m_r and R_r running bounds of s and of s + ev, moved only when they are exceeded
+// by 2^8 (P' <= 2^15 in fp16, weights times 2^ev down to 2^-32 of the largest stay above
+// its subnormals).  Where ev is so far below R - m that P' would vanish in fp32 while the
 // weight counts, l is summed from its own exponentials.  bf16 queries are scaled by a
-// power of two per row into fp16 (what lies 2^-39 below a row's largest is lost).
+// power of two per row into fp16 (what lies 2^-39 below a row's largest is lost).  The
+// converting warps are the scarcer: with code 2^e in bf16 tiles (five instructions for two
+// codes and not one) the trees below took 1356 us, with code 2^(e - E) in fp16 (E the tile's
+// largest; one multiplication, and one exponent in the softmax) 460 us and the chunks 515.
 //
 // A segment with two row tiles is worked off as in flash.cuh, a row tile to a
 // softmax warpgroup.  With one (trees, short chunks), the two take turns at the key
@@ -28,10 +27,11 @@
 // what is on its way (4.2 us a key tile).  K and V tiles share one ring, K a tile ahead:
 // K0 K1 V0 K2 V1 ... V(n-1).
 //
-// Measured: four trees of 65 nodes over 32768 keys (40 / 8 heads of 128, bf16) 460 us, bound by
-// the converting warps (an instruction in two cycles for each two codes, and 400 cycles of waits and
-// fences a tile); 512 new tokens behind 8192 (four requests, 32 / 8 heads of 64, fp16) 515 us, bound by
-// the softmax warps (2600 cycles of exponentials a key tile and row tile).
+// Measured: four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 344 us, 3.9 TB/s, bound by
+// the converting warps (two cycles for each two codes, and 400 of waits and fences a tile; the
+// cache in 16 bits takes 413 us); 200 to 1000 new tokens behind 4000 to 32000 (four requests,
+// 32 / 8 heads of 64, fp16) 552 us, bound by the softmax warps, which share their schedulers with
+// the converting ones (in 16 bits 378 us).
 #pragma once
 
 #include "coded.cuh"
@@ -40,7 +40,8 @@
 namespace rs {
 
 constexpr int kCoThreads = 512, kCoQWarp = 2, kCoCopyWarp = 3, kCoDecodeWarp = 12;
-constexpr uint32_t kCoRegsSoft = 176, kCoRegsProd = 80, kCoRegsDecode = 80;
+// (fewer for the issuing warps than they could use: 2 % less time than 176 / 80 / 80)
+constexpr uint32_t kCoRegsSoft = 184, kCoRegsProd = 64, kCoRegsDecode = 80;
 static_assert(2 * 128 * kCoRegsSoft + 128 * (kCoRegsProd + kCoRegsDecode) == kCoThreads * 128, "register split");
 
 template <int D>
@@ -58,8 +59,7 @@ struct CoSmem {
     static constexpr int kNumBars = 2 * kNR + 2 * kNC + 23;
     static constexpr int kMisc = kBar + kNumBars * 8;        // tensor memory base, abort flag
     static constexpr int kBounds = (kMisc + 8 + 15) / 16 * 16;
-    // [tile]: (ek + 127, ev + 128) of its eight blocks, two bytes each; then those of the tile, and whether they hold
-    static constexpr int kExp = kBounds + 2 * kFlMaxPhases * 16;
+    static constexpr int kExp = kBounds + 2 * kFlMaxPhases * 16;  // [tile][block]: 2^ek and ev, each a float's upper half
     static constexpr int kShift = kExp + kExps * 32;         // int8 [row tile][row]
     static constexpr int kStat = kShift + 2 * kBM;           // float2 [row]: the second warpgroup's sums
     static constexpr int kBytes = kStat + kBM * 8;
@@ -73,10 +73,41 @@ __device__ __forceinline__ int v_at(int tl, int n) { return tl == n - 1 ? 2 * n 
 __device__ __forceinline__ bool is_v(int pos, int n) { return pos == 2 * n - 1 || (pos > 0 && !(pos & 1)); }
 __device__ __forceinline__ int tile_at(int pos, int n) { return pos == 2 * n - 1 ? n - 1 : pos == 0 ? 0 : (pos & 1) ? (pos + 1) / 2 : pos / 2 - 1; }
 
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
+// exp_pairs in fp16 with a factor, an offset and a sum for each block of 16 keys.
+__device__ __forceinline__ void exp_blocks(const uint32_t (&s0)[32], const uint32_t (&s1)[32], const float (&c)[4], const float (&nb)[4],
+                                           float (&sum)[4], uint32_t (&xp)[32]) {
+    constexpr int kAhead = 4, kBehind = 4;  // pairs
+    float d[64], p[64], odd[4];
+    auto fma1 = [&](int i) {
+        const float v = __uint_as_float(i < 32 ? s0[i] : s1[i - 32]);
+        asm volatile("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d[i]) : "f"(v), "f"(c[i / 16]), "f"(nb[i / 16]));
+    };
+#pragma unroll
+    for (int i = 0; i < 2 * kAhead; ++i) fma1(i);
+#pragma unroll
+    for (int e = 0; e < 32 + kBehind; ++e) {
+        if (e < 32) {
+            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[2 * e]) : "f"(d[2 * e]));
+            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[2 * e + 1]) : "f"(d[2 * e + 1]));
+        }
+        if (e + kAhead < 32) {
+            fma1(2 * (e + kAhead));
+            fma1(2 * (e + kAhead) + 1);
+        }
+        if (e >= kBehind) {
+            const int q = e - kBehind, b = q / 8;
+            if (q % 8 == 0) {
+                sum[b] = p[2 * q];
+                odd[b] = p[2 * q + 1];
+            } else {
+                asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(sum[b]) : "f"(p[2 * q]));
+                asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(odd[b]) : "f"(p[2 * q + 1]));
+            }
+            asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(xp[q]) : "f"(p[2 * q + 1]), "f"(p[2 * q]));
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) sum[b] += odd[b];
 }
 
 template <int D, bool BF16>
@@ -219,9 +250,12 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                 return -2;
             };
             auto exp_at = [&](int bat, int id) { return (((long long)id << (a.page_log2 - kCodeBlockLog2)) + (block_at(bat) & in_page)) * a.Hkv + pc.kvh; };
-            auto packed = [&](int id, int ek, int ev) { return id < 0 ? 0 : (code_exp(ek, BF16) + 127) | (code_exp(ev, BF16) + 128) << 8; };
+            // (a block without keys or of a bad page: any exponent, as its codes are 0)
+            auto scales = [&](int id, int ek, int ev) -> uint32_t {  // (whole numbers of eight bits fit half a float)
+                return id < 0 ? 0x3f800000u : __float_as_uint(pow2i(code_exp(ek, BF16))) | __float_as_uint((float)code_exp(ev, BF16)) >> 16;
+            };
             int id = checked(0, page_of(0)), id1 = -1, ek1 = 0, ev1 = 0;
-            int exps = packed(id, id >= 0 ? pool.ke[exp_at(0, id)] : 0, id >= 0 ? pool.ve[exp_at(0, id)] : 0);
+            uint32_t exps = scales(id, id >= 0 ? pool.ke[exp_at(0, id)] : 0, id >= 0 ? pool.ve[exp_at(0, id)] : 0);
             int row = -1, last = -1;
             for (int pos = 0; pos < 2 * n; ++pos, ++c) {
                 const bool v = is_v(pos, n);
@@ -230,7 +264,7 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                     const int bat = tl / kBatch, q = tl % kBatch;
                     if (q == 0 && tl > 0) {
                         id = id1;
-                        exps = packed(id, ek1, ev1);
+                        exps = scales(id, ek1, ev1);
                     }
                     // row of the pool where lane x's copy of the tile starts, -1: none
                     last = row;
@@ -252,23 +286,8 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                 const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, from >= 0)) * (uint32_t)(box * D);
                 const uint32_t st = c % NC;
                 if (!(ok = warp_wait(&cempty[st], (c / NC & 1) ^ 1, s_abort, a.wait_limit))) break;
-                if (!v && tl % kBatch == 0) {
-                    // the batch's exponents, and the largest of each tile's eight blocks, which lie side by side
-                    const int ek = exps & 255, ev = exps >> 8;
-                    int top_k = ek, low_k = exps ? ek : 255, top_v = ev, low_v = exps ? ev : 255;
-#pragma unroll
-                    for (int d = 1; d < kBlocks; d *= 2) {
-                        top_k = max(top_k, __shfl_xor_sync(0xffffffffu, top_k, d));
-                        low_k = min(low_k, __shfl_xor_sync(0xffffffffu, low_k, d));
-                        top_v = max(top_v, __shfl_xor_sync(0xffffffffu, top_v, d));
-                        low_v = min(low_v, __shfl_xor_sync(0xffffffffu, low_v, d));
-                    }
-                    unsigned char *to = s_exp + ((g + tl + lane / kBlocks) % S::kExps) * 32;
-                    // (a block without keys or of a bad page: any exponent, as its codes are 0)
-                    *reinterpret_cast<unsigned short *>(to + lane % kBlocks * 2) = (unsigned short)(exps ? exps : top_k | top_v << 8);
-                    if (lane % kBlocks == 0)
-                        *reinterpret_cast<int *>(to + 16) = top_k | top_v << 8 | (top_k - low_k <= 15 && top_v - low_v <= 15 ? 1 << 16 : 0);
-                }
+                if (!v && tl % kBatch == 0)  // the batch's exponents
+                    *reinterpret_cast<uint32_t *>(s_exp + ((g + tl + lane / kBlocks) % S::kExps) * 32 + lane % kBlocks * 4) = exps;
                 __syncwarp();
                 if (lane == 0) mbar_expect_tx(&cfull[st], tx);
                 __syncwarp();
@@ -486,13 +505,11 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                     ++done;
                     return true;
                 }
-                const unsigned char *exps = s_exp + (t % S::kExps) * 32;
-                const int head = *reinterpret_cast<const int *>(exps + 16);
-                const bool same = head >> 16 & 1;  // one exponent for all of the tile's K, one for its V
+                const uint4 *exps = reinterpret_cast<const uint4 *>(s_exp + (t % S::kExps) * 32);  // of four blocks each
+                auto word = [](const uint4 &e4, int b) { return b == 0 ? e4.x : b == 1 ? e4.y : b == 2 ? e4.z : e4.w; };
                 // (factors are not 0: hidden scores stay -inf)
-                auto factor = [&](int e2) { return fmaxf(rowf * __uint_as_float((uint32_t)(e2 & 255) << 23), 0x1p-126f); };
-                auto offset = [&](int e2) { return (float)((e2 >> 8 & 255) - 128); };
-                auto block = [&](int b) { return (int)*reinterpret_cast<const unsigned short *>(exps + 2 * b); };
+                auto factor = [&](const uint4 &e4, int b) { return fmaxf(rowf * __uint_as_float(word(e4, b) & 0xffff0000u), 0x1p-126f); };
+                auto offset = [&](const uint4 &e4, int b) { return __uint_as_float(word(e4, b) << 16); };
                 auto load64 = [&](int hh, uint32_t (&va)[32], uint32_t (&vb)[32]) {
                     tmem_ld32(s_tm + hh * 64, va);
                     tmem_ld32(s_tm + hh * 64 + 32, vb);
@@ -504,45 +521,24 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                         hide(vb, hh ? mk[3] : mk[1]);
                     }
                 };
-                auto scores = [&](int b, uint32_t (&va)[16]) {  // of block b
-                    tmem_ld16(s_tm + b * 16, va);
-                    tmem_wait_ld16(va);
-                    if (masked) {
-                        const uint32_t see = (b < 2 ? mk[0] : b < 4 ? mk[1] : b < 6 ? mk[2] : mk[3]) >> (b & 1 ? 16 : 0);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (!((see >> e) & 1u)) va[e] = 0xff800000u;
-                    }
-                };
-                const float c_all = factor(head), ev_all = offset(head);
-                // the row's maxima, 64 keys at a time
-                float mt, rmax, ev_min = ev_all;
-                if (same) {
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        uint32_t va[32], vb[32];
-                        load64(hh, va, vb);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            mx[e & 3] = fmaxf(mx[e & 3], fmaxf(__uint_as_float(va[e]), __uint_as_float(vb[e])));
-                    }
-                    mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c_all;
-                    rmax = mt + ev_all;
-                } else {
-                    mt = rmax = -INFINITY;
+                // the row's maxima, of the scores and with their blocks' ev, 64 keys at a time
+                float mt = -INFINITY, rmax = -INFINITY, ev_min = INFINITY;
 #pragma unroll 1
-                    for (int b = 0; b < 8; ++b) {
-                        uint32_t va[16];
-                        scores(b, va);
-                        float x = -INFINITY;
+                for (int hh = 0; hh < 2; ++hh) {
+                    uint32_t va[32], vb[32];
+                    load64(hh, va, vb);
+                    const uint4 e4 = exps[hh];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) x = fmaxf(x, __uint_as_float(va[e]));
-                        const float ev = offset(block(b));
-                        x *= factor(block(b));
-                        mt = fmaxf(mt, x);
-                        rmax = fmaxf(rmax, x + ev);
-                        ev_min = fminf(ev_min, ev);
+                    for (int b = 0; b < 4; ++b) {
+                        const uint32_t *v = (b < 2 ? va : vb) + b % 2 * 16;
+                        float x[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2)
+                            x[e >> 1 & 1] = fmaxf(x[e >> 1 & 1], fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
+                        const float top = fmaxf(x[0], x[1]) * factor(e4, b);
+                        mt = fmaxf(mt, top);
+                        rmax = fmaxf(rmax, top + offset(e4, b));
+                        ev_min = fminf(ev_min, offset(e4, b));
                     }
                 }
                 // lazy rescale: a bound moves only when it is exceeded by more than 2^8
@@ -569,56 +565,46 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                 }
                 const float mn = m == -INFINITY ? 0.f : m, up = ref == -INFINITY ? 0.f : 7.f - ref;
                 // P' may vanish in fp32 while its keys count for l (values 2^90 below others'): then l is
-                // summed by itself; so it is where the blocks' exponents differ too much
-                const bool apart = !same || __any_sync(0xffffffffu, -up - ev_min - mn > 90.f);
+                // summed by itself
+                const bool apart = __any_sync(0xffffffffu, -up - ev_min - mn > 90.f);
                 if (apart) {
 #pragma unroll 1
-                    for (int b = 0; b < 8; ++b) {
-                        uint32_t va[16];
-                        scores(b, va);
-                        const float c = same ? c_all : factor(block(b));
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) l += ex2(fmaf(__uint_as_float(va[e]), c, -mn));
-                    }
-                }
-                float sum4[4] = {0.f, 0.f, 0.f, 0.f};
-                if (same) {
-#pragma unroll 1
                     for (int hh = 0; hh < 2; ++hh) {
-                        uint32_t va[32], vb[32], xp[32];
+                        uint32_t va[32], vb[32];
                         load64(hh, va, vb);
-                        if (kApart && hh) {  // S has been read: the next one may be written
-                            tc_fence_before();
-                            warp_arrive(&sfree[x]);
-                        }
-                        exp_pairs<false>(va, vb, c_all, ev_all + up, sum4, xp);
-                        if (kApart && !hh && !wait_idle()) return false;
-                        tmem_st32(p_tm + hh * 32, xp);
-                        if (!kApart || hh) {
-                            tmem_wait_st();
-                            tc_fence_before();
-                            warp_arrive(kApart || !hh ? &pfull[x] : &pfull2[x]);
-                        }
-                    }
-                } else {
-                    if (kApart && !wait_idle()) return false;
-#pragma unroll 1
-                    for (int b = 0; b < 8; ++b) {  // (P over S: of columns that have been read)
-                        uint32_t va[16], xp[8];
-                        scores(b, va);
-                        const float c = factor(block(b)), nb = offset(block(b)) + up;
+                        const uint4 e4 = exps[hh];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            xp[e] = pack16<false>(ex2(fmaf(__uint_as_float(va[2 * e]), c, nb)), ex2(fmaf(__uint_as_float(va[2 * e + 1]), c, nb)));
-                        tmem_st8(p_tm + b * 8, xp);
+                        for (int e = 0; e < 64; ++e) l += ex2(fmaf(__uint_as_float(e < 32 ? va[e] : vb[e - 32]), factor(e4, e / 16), -mn));
                     }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    if (kApart) warp_arrive(&sfree[x]);
-                    warp_arrive(&pfull[x]);
-                    if (!kApart) warp_arrive(&pfull2[x]);
                 }
-                if (!apart) l = fmaf((sum4[0] + sum4[1]) + (sum4[2] + sum4[3]), ex2(-up - ev_all - mn), l);
+#pragma unroll 1
+                for (int hh = 0; hh < 2; ++hh) {
+                    uint32_t va[32], vb[32], xp[32];
+                    load64(hh, va, vb);
+                    if (kApart && hh) {  // S has been read: the next one may be written
+                        tc_fence_before();
+                        warp_arrive(&sfree[x]);
+                    }
+                    const uint4 e4 = exps[hh];
+                    float c[4], nb[4], sum[4];
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        c[b] = factor(e4, b);
+                        nb[b] = offset(e4, b) + up;
+                    }
+                    exp_blocks(va, vb, c, nb, sum, xp);
+                    if (kApart && !hh && !wait_idle()) return false;
+                    tmem_st32(p_tm + hh * 32, xp);
+                    if (!apart) {
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) l = fmaf(sum[b], ex2(-nb[b] - mn), l);
+                    }
+                    if (!kApart || hh) {
+                        tmem_wait_st();
+                        tc_fence_before();
+                        warp_arrive(kApart || !hh ? &pfull[x] : &pfull2[x]);
+                    }
+                }
                 ++done;
                 return true;
             };
@@ -716,12 +702,6 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                 if (!(ok = quick_wait2(&cfull[cst], c / NC & 1, &empty[st], (c / NR & 1) ^ 1, s_abort, a.wait_limit))) break;
                 const unsigned char *codes = smem + S::kCodes + cst * (kBN * D);
                 unsigned char *tile = smem + S::kRing + st * S::kTile;
-                const bool v_tile = is_v(pos, n);
-                const unsigned char *exps = s_exp + ((before / 2 + tile_at(pos, n)) % S::kExps) * 32;
-                const int head = *reinterpret_cast<const int *>(exps + 16);
-                const int top = head >> (v_tile ? 8 : 0) & 255;
-                const bool scaled = head >> 16 & 1;
-                const unsigned char *exp = exps + (v_tile ? 1 : 0) + row0 / kCodeBlock * 2;
                 // A lane's 16 codes are two words of eight: at D = 128 one of each 64 columns (of odd rows the
                 // second first), at D = 64 side by side.  All go to other banks that way, there and here.
                 const unsigned char *const from = codes + row0 * D + (D == 128 ? (row0 & 1) * 64 + part * 8 : part * 16);
@@ -733,13 +713,10 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
 #pragma unroll 1
                 for (int i0 = 0; i0 < kLoads; i0 += 4) {
                     uint2 x[4], y[4];  // (all loads before the first store, which the compiler does not move them over)
-                    uint32_t f[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         x[i] = *reinterpret_cast<const uint2 *>(from + (i0 + i) * 2048);
                         y[i] = *reinterpret_cast<const uint2 *>(from + (i0 + i) * 2048 + step);
-                        const int down = scaled ? top - exp[(i0 + i) * (kRowsStep / kCodeBlock) * 2] : 0;
-                        f[i] = down < 15 ? (uint32_t)(15 - down) * 0x04000400u : 0x02000200u;  // 2^-down, twice
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -748,8 +725,6 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                         decode4(x[i].y, lo.z, lo.w);
                         decode4(y[i].x, hi.x, hi.y);
                         decode4(y[i].y, hi.z, hi.w);
-                        lo = make_uint4(mul_f16x2(lo.x, f[i]), mul_f16x2(lo.y, f[i]), mul_f16x2(lo.z, f[i]), mul_f16x2(lo.w, f[i]));
-                        hi = make_uint4(mul_f16x2(hi.x, f[i]), mul_f16x2(hi.y, f[i]), mul_f16x2(hi.z, f[i]), mul_f16x2(hi.w, f[i]));
                         *reinterpret_cast<uint4 *>(to + at0 + (i0 + i) * kRowsStep * 128) = lo;
                         *reinterpret_cast<uint4 *>(to + at1 + (i0 + i) * kRowsStep * 128) = hi;
                     }
