@@ -82,7 +82,7 @@ pages_copy(Pages p, const int2 *pairs, int n, int32_t *status) {
 // r-th free one below U.  One block; a warp takes runs of 512 pages, whose counts and
 // places within the run are votes' bits.
 // Bound: latency, of two passes over the counts and one over the moves: 16384 pages
-// 9 us (25 with 16 pages in a row to a thread, whose loads and stores are 32 lines each).
+// 10 us (25 with 16 pages in a row to a thread, whose loads and stores are 32 lines each).
 constexpr int kPlanThreads = 1024, kPlanEach = 16, kPlanRound = kPlanThreads * kPlanEach;
 static_assert(kPlanRound < 1 << 16, "two counts in a word");
 __global__ void __launch_bounds__(kPlanThreads)
