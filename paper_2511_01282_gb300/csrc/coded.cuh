@@ -27,13 +27,7 @@ __device__ __forceinline__ int code_exp(int e, bool bf16) { return min(max(e, co
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// two codes (the low 16 bits) -> fp16, exact; NaN stays NaN
-__device__ __forceinline__ uint32_t decode2(uint32_t two) {
-    uint32_t h;
-    asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(h) : "r"(two));
-    return h;
-}
-// the low and the high two of four codes
+// four codes -> fp16, exact (NaN stays NaN): the low and the high two
 __device__ __forceinline__ void decode4(uint32_t four, uint32_t &lo, uint32_t &hi) {
     asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
         : "=r"(lo), "=r"(hi)

@@ -30,7 +30,7 @@
 // Measured: four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 344 us, 3.9 TB/s, bound by
 // the converting warps (two cycles for each two codes, and 400 of waits and fences a tile; the
 // cache in 16 bits takes 413 us); 200 to 1000 new tokens behind 4000 to 32000 (four requests,
-// 32 / 8 heads of 64, fp16) 552 us, bound by the softmax warps, which share their schedulers with
+// 32 / 8 heads of 64, fp16) 541 us, bound by the softmax warps, which share their schedulers with
 // the converting ones (in 16 bits 378 us).
 #pragma once
 
@@ -70,7 +70,6 @@ struct CoSmem {
 // The n key tiles of a piece in the ring's order: positions 0 .. 2 n - 1.
 __device__ __forceinline__ int k_at(int tl) { return tl == 0 ? 0 : 2 * tl - 1; }
 __device__ __forceinline__ int v_at(int tl, int n) { return tl == n - 1 ? 2 * n - 1 : 2 * tl + 2; }
-__device__ __forceinline__ bool is_v(int pos, int n) { return pos == 2 * n - 1 || (pos > 0 && !(pos & 1)); }
 __device__ __forceinline__ int tile_at(int pos, int n) { return pos == 2 * n - 1 ? n - 1 : pos == 0 ? 0 : (pos & 1) ? (pos + 1) / 2 : pos / 2 - 1; }
 
 // exp_pairs in fp16 with a factor, an offset and a sum for each block of 16 keys.
@@ -233,8 +232,10 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
         constexpr int kBlocks = kBN / kCodeBlock, kBatch = 32 / kBlocks;   // of a tile; tiles of a batch
         const CodedPool &pool = a.coded;
         const uint64_t once = l2_evict_first_policy();
-        uint32_t c = 0, used = 0, g = 0;  // positions copied; stages in use (at most all)
+        const int lane_block = min(lane * (box >> kCodeBlockLog2), kBlocks - 1);  // of a tile: where the lane's copy starts
+        uint32_t c = 0, g = 0, st = 0, phase = 0;  // positions copied; the next one's stage, and which use of it
         bool ok = true;
+        auto free_stage = [&]() -> bool { return ok = quick_wait(&cempty[st], phase ^ 1, s_abort, a.wait_limit); };
         while (ok && cur.next(pc)) {
             const int n = pc.j1 - pc.j0;
             const int32_t *table = a.page_table + (long long)pc.b * a.max_pages;
@@ -256,21 +257,36 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
             };
             int id = checked(0, page_of(0)), id1 = -1, ek1 = 0, ev1 = 0;
             uint32_t exps = scales(id, id >= 0 ? pool.ke[exp_at(0, id)] : 0, id >= 0 ? pool.ve[exp_at(0, id)] : 0);
-            int row = -1, last = -1;
-            for (int pos = 0; pos < 2 * n; ++pos, ++c) {
-                const bool v = is_v(pos, n);
-                const int tl = tile_at(pos, n);
-                if (!v) {
+            auto copy = [&](const CUtensorMap *map, int from, uint32_t tx) {
+                if (lane == 0) mbar_expect_tx(&cfull[st], tx);
+                __syncwarp();
+                if (from >= 0) {
+                    unsigned char *dst = smem + S::kCodes + st * (kBN * D) + lane * box * D;
+                    if (evict) tma_load_3d_hint(dst, map, &cfull[st], 0, pc.kvh, from, once);
+                    else tma_load_3d(dst, map, &cfull[st], 0, pc.kvh, from);
+                }
+                ++c;
+                if (++st == NC) {
+                    st = 0;
+                    phase ^= 1;
+                }
+            };
+            // row of the pool where the lane's copy of the tile starts (-1: none), bytes of all copies
+            int row = -1;
+            uint32_t tx = 0;
+            for (int tl = 0; tl <= n; ++tl) {  // K of tile tl, V of the one before
+                const int last = row;
+                const uint32_t last_tx = tx;
+                if (tl < n) {
                     const int bat = tl / kBatch, q = tl % kBatch;
                     if (q == 0 && tl > 0) {
                         id = id1;
                         exps = scales(id, ek1, ev1);
                     }
-                    // row of the pool where lane x's copy of the tile starts, -1: none
-                    last = row;
-                    const int from = __shfl_sync(0xffffffffu, id, q * kBlocks + min(lane * (box >> kCodeBlockLog2), kBlocks - 1));
+                    const int from = __shfl_sync(0xffffffffu, id, q * kBlocks + lane_block);
                     row = lane * box >= kBN || from == -1 ? -1
-                          : from < 0 ? a.n_pages << a.page_log2 : (from << a.page_log2) + (((pc.j0 + tl) * kBN + lane * box) & (page - 1));
+                          : from < 0 ? a.n_pages << a.page_log2 : (from << a.page_log2) + (((pc.j0 + tl) * kBN) & (page - 1));
+                    tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, row >= 0)) * (uint32_t)(box * D);
                     if (q == 0) id1 = page_of(bat + 1);
                     if (q == 1) {
                         id1 = checked(bat + 1, id1);
@@ -280,30 +296,22 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                             ev1 = pool.ve[at];
                         }
                     }
+                    if (!free_stage()) break;
+                    if (q == 0)  // the batch's exponents
+                        *reinterpret_cast<uint32_t *>(s_exp + ((g + tl + lane / kBlocks) % S::kExps) * 32 + lane % kBlocks * 4) = exps;
+                    __syncwarp();
+                    copy(&tmk, row, tx);
                 }
-                // (V of the tile before, but for the last one, which follows its own K)
-                const int from = v && pos < 2 * n - 1 ? last : row;
-                const uint32_t tx = (uint32_t)__popc(__ballot_sync(0xffffffffu, from >= 0)) * (uint32_t)(box * D);
-                const uint32_t st = c % NC;
-                if (!(ok = warp_wait(&cempty[st], (c / NC & 1) ^ 1, s_abort, a.wait_limit))) break;
-                if (!v && tl % kBatch == 0)  // the batch's exponents
-                    *reinterpret_cast<uint32_t *>(s_exp + ((g + tl + lane / kBlocks) % S::kExps) * 32 + lane % kBlocks * 4) = exps;
-                __syncwarp();
-                if (lane == 0) mbar_expect_tx(&cfull[st], tx);
-                __syncwarp();
-                if (from >= 0) {
-                    unsigned char *dst = smem + S::kCodes + st * (kBN * D) + lane * box * D;
-                    if (evict) tma_load_3d_hint(dst, v ? &tmv : &tmk, &cfull[st], 0, pc.kvh, from, once);
-                    else tma_load_3d(dst, v ? &tmv : &tmk, &cfull[st], 0, pc.kvh, from);
+                if (tl > 0) {
+                    if (!free_stage()) break;
+                    copy(&tmv, last, last_tx);
                 }
-                __syncwarp();
-                used = min(used + 1, NC);
             }
             g += n;
         }
         if (!ok) {  // let the copies already issued land before the CTA exits
             volatile int no_abort = 0;
-            for (uint32_t u = 0; u < used; ++u) {
+            for (uint32_t u = min(c, NC); u > 0; --u) {
                 --c;
                 mbar_wait(&cfull[c % NC], c / NC & 1, &no_abort, kWaitLimit);
             }
@@ -691,15 +699,14 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
         // softmax warps miss more.)
         constexpr int kRowLanes = D / 16, kRowsStep = 128 / kRowLanes, kLoads = kBN / kRowsStep;
         const int ci = tid & 127, part = ci % kRowLanes, row0 = ci / kRowLanes;
-        uint32_t before = 0, quse[2] = {0, 0};  // positions of earlier pieces; Q tiles
+        uint32_t st = 0, phase = 0, cst = 0, cphase = 0;  // stages of tiles and codes, and which use of them
+        uint32_t quse[2] = {0, 0};                        // Q tiles
         bool ok = true;
         while (ok && cur.next(pc)) {
-            const int n = pc.j1 - pc.j0;
+            const int n = pc.j1 - pc.j0, tail = pc.keys - (pc.j1 - 1) * kBN;  // keys of the last tile
 #pragma unroll 1
             for (int pos = 0; pos < 2 * n; ++pos) {
-                const uint32_t c = before + pos, cst = c % NC, st = c % NR;
-                const int keys = pc.keys - (pc.j0 + tile_at(pos, n)) * kBN;  // of the tile
-                if (!(ok = quick_wait2(&cfull[cst], c / NC & 1, &empty[st], (c / NR & 1) ^ 1, s_abort, a.wait_limit))) break;
+                if (!(ok = quick_wait2(&cfull[cst], cphase, &empty[st], phase ^ 1, s_abort, a.wait_limit))) break;
                 const unsigned char *codes = smem + S::kCodes + cst * (kBN * D);
                 unsigned char *tile = smem + S::kRing + st * S::kTile;
                 // A lane's 16 codes are two words of eight: at D = 128 one of each 64 columns (of odd rows the
@@ -729,16 +736,24 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                         *reinterpret_cast<uint4 *>(to + at1 + (i0 + i) * kRowsStep * 128) = hi;
                     }
                 }
-                if (keys < kBN)  // behind the last key anything was copied, NaN too
+                if (tail < kBN && tile_at(pos, n) == n - 1)  // behind the last key anything was copied, NaN too
 #pragma unroll 1
                     for (int i = 0; i < kLoads; ++i)
-                        if (i * kRowsStep + row0 >= keys) {
+                        if (i * kRowsStep + row0 >= tail) {
                             *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
                             *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
                         }
                 fence_async_smem();
                 warp_arrive(&full[st]);
                 warp_arrive(&cempty[cst]);
+                if (++st == NR) {
+                    st = 0;
+                    phase ^= 1;
+                }
+                if (++cst == NC) {
+                    cst = 0;
+                    cphase ^= 1;
+                }
                 if (const int x = pos; BF16 && pos < 2 && takes_part(x)) {
                     // Q tile x to fp16 in place, a row to a thread, by a power of two that brings its largest value
                     // to 2^14 .. 2^15
@@ -773,7 +788,6 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                     warp_arrive(&qready[x]);
                 }
             }
-            before += 2 * n;
         }
     }
     __syncthreads();
