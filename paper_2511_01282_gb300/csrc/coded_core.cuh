@@ -27,11 +27,11 @@
 // what is on its way (4.2 us a key tile).  K and V tiles share one ring, K a tile ahead:
 // K0 K1 V0 K2 V1 ... V(n-1).
 //
-// Measured: four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 344 us, 3.9 TB/s, bound by
-// the converting warps (two cycles for each two codes, and 400 of waits and fences a tile; the
-// cache in 16 bits takes 413 us); 200 to 1000 new tokens behind 4000 to 32000 (four requests,
-// 32 / 8 heads of 64, fp16) 541 us, bound by the softmax warps, which share their schedulers with
-// the converting ones (in 16 bits 378 us).
+// Measured: four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 313 us, 4.3 TB/s (the
+// cache in 16 bits takes 403): a chain a key tile of one softmax warpgroup, product, softmax, product, with two
+// of them at work, beside 1000 cycles of conversion; 200 to 1000 new tokens behind 4000 to 32000
+// (four requests, 32 / 8 heads of 64, fp16) 436 us, bound by the softmax warps, which share their
+// schedulers with the converting ones (in 16 bits 378 us).
 #pragma once
 
 #include "coded.cuh"
@@ -72,41 +72,38 @@ __device__ __forceinline__ int k_at(int tl) { return tl == 0 ? 0 : 2 * tl - 1; }
 __device__ __forceinline__ int v_at(int tl, int n) { return tl == n - 1 ? 2 * n - 1 : 2 * tl + 2; }
 __device__ __forceinline__ int tile_at(int pos, int n) { return pos == 2 * n - 1 ? n - 1 : pos == 0 ? 0 : (pos & 1) ? (pos + 1) / 2 : pos / 2 - 1; }
 
-// exp_pairs in fp16 with a factor, an offset and a sum for each block of 16 keys.
+// 64 weights of a row as exp_pairs gives them, in fp16, with a factor, an offset and a sum for each block
+// of 16 keys; arguments and sums two to an instruction.
 __device__ __forceinline__ void exp_blocks(const uint32_t (&s0)[32], const uint32_t (&s1)[32], const float (&c)[4], const float (&nb)[4],
                                            float (&sum)[4], uint32_t (&xp)[32]) {
     constexpr int kAhead = 4, kBehind = 4;  // pairs
-    float d[64], p[64], odd[4];
+    float2 d[32], p[32];
+    uint64_t both[4];
     auto fma1 = [&](int i) {
-        const float v = __uint_as_float(i < 32 ? s0[i] : s1[i - 32]);
-        asm volatile("fma.rn.f32 %0, %1, %2, %3;" : "=f"(d[i]) : "f"(v), "f"(c[i / 16]), "f"(nb[i / 16]));
+        const float2 v = i < 16 ? make_float2(__uint_as_float(s0[2 * i]), __uint_as_float(s0[2 * i + 1]))
+                                : make_float2(__uint_as_float(s1[2 * i - 32]), __uint_as_float(s1[2 * i - 31]));
+        uint64_t r;
+        asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_b64(v)), "l"(as_b64(make_float2(c[i / 8], c[i / 8]))), "l"(as_b64(make_float2(nb[i / 8], nb[i / 8]))));
+        d[i] = as_float2(r);
     };
 #pragma unroll
-    for (int i = 0; i < 2 * kAhead; ++i) fma1(i);
+    for (int i = 0; i < kAhead; ++i) fma1(i);
 #pragma unroll
     for (int e = 0; e < 32 + kBehind; ++e) {
         if (e < 32) {
-            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[2 * e]) : "f"(d[2 * e]));
-            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[2 * e + 1]) : "f"(d[2 * e + 1]));
+            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[e].x) : "f"(d[e].x));
+            asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(p[e].y) : "f"(d[e].y));
         }
-        if (e + kAhead < 32) {
-            fma1(2 * (e + kAhead));
-            fma1(2 * (e + kAhead) + 1);
-        }
+        if (e + kAhead < 32) fma1(e + kAhead);
         if (e >= kBehind) {
             const int q = e - kBehind, b = q / 8;
-            if (q % 8 == 0) {
-                sum[b] = p[2 * q];
-                odd[b] = p[2 * q + 1];
-            } else {
-                asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(sum[b]) : "f"(p[2 * q]));
-                asm volatile("add.rn.f32 %0, %0, %1;" : "+f"(odd[b]) : "f"(p[2 * q + 1]));
-            }
-            asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(xp[q]) : "f"(p[2 * q + 1]), "f"(p[2 * q]));
+            if (q % 8 == 0) both[b] = as_b64(p[q]);
+            else asm volatile("add.rn.f32x2 %0, %0, %1;" : "+l"(both[b]) : "l"(as_b64(p[q])));
+            asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(xp[q]) : "f"(p[q].y), "f"(p[q].x));
         }
     }
 #pragma unroll
-    for (int b = 0; b < 4; ++b) sum[b] += odd[b];
+    for (int b = 0; b < 4; ++b) sum[b] = as_float2(both[b]).x + as_float2(both[b]).y;
 }
 
 template <int D, bool BF16>
@@ -471,27 +468,12 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
             const int open = pc.ctx + (a.anc ? 0 : tok0 + 1);  // keys that every row of the tile sees
             const int seen = pc.ctx + tok + 1;                 // causal: keys this row sees
             float m = -INFINITY, ref = -INFINITY, l = 0.f, rowf = cexp;
-            // One key tile; masked: some row does not see all of the keys.  (Code that runs once a tile and
-            // not twice: the kernel's roles share an instruction cache.)
+            // One key tile; masked: some row does not see all of the keys.  The kernel's roles share an
+            // instruction cache: what is rare is one small loop, and nothing is compiled twice (masks within
+            // the loads and sums of their own in registers took the chunks 523 us and not 464).
             auto tile = [&](bool masked, int tl) -> bool {
                 const uint32_t t = g + tl;
                 const int key0 = (pc.j0 + tl) * kBN;
-                uint32_t mk[4] = {};                    // the keys this row sees
-                if (masked) {
-                    if (a.anc) {
-                        uint32_t anc[kAncWords];
-#pragma unroll
-                        for (int w = 0; w < kAncWords; ++w) anc[w] = valid ? a.anc[(long long)(pc.n0 + tok) * kAncWords + w] : 0u;
-#pragma unroll
-                        for (int ch = 0; ch < 4; ++ch) mk[ch] = tree_window(anc, key0 + ch * 32 - pc.ctx);
-                    } else {
-#pragma unroll
-                        for (int ch = 0; ch < 4; ++ch) {
-                            const int c = seen - key0 - ch * 32;
-                            mk[ch] = c >= 32 ? 0xffffffffu : c <= 0 ? 0u : (1u << c) - 1u;
-                        }
-                    }
-                }
                 if (!(ok = quick_wait(&sfull[x], done & 1, s_abort, a.wait_limit))) return false;
                 tc_fence_after();
                 if (BF16 && tl == first) rowf = cexp * pow2i(s_shift[x * kBM + r]);
@@ -513,6 +495,24 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                     ++done;
                     return true;
                 }
+                if (masked) {  // hidden scores are replaced where they are: what follows knows nothing of them
+                    uint32_t anc[kAncWords];
+                    if (a.anc)
+#pragma unroll
+                        for (int w = 0; w < kAncWords; ++w) anc[w] = valid ? a.anc[(long long)(pc.n0 + tok) * kAncWords + w] : 0u;
+#pragma unroll 1
+                    for (int k0 = 0; k0 < kBN; k0 += 32) {
+                        uint32_t va[32];
+                        const int c = seen - key0 - k0;
+                        const uint32_t mk = a.anc ? tree_window(anc, key0 + k0 - pc.ctx) : c >= 32 ? 0xffffffffu : c <= 0 ? 0u : (1u << c) - 1u;
+                        tmem_ld32(s_tm + k0, va);
+                        tmem_wait_ld();
+                        tmem_regs_ready(va);
+                        hide(va, mk);
+                        tmem_st32(s_tm + k0, va);
+                    }
+                    tmem_wait_st();
+                }
                 const uint4 *exps = reinterpret_cast<const uint4 *>(s_exp + (t % S::kExps) * 32);  // of four blocks each
                 auto word = [](const uint4 &e4, int b) { return b == 0 ? e4.x : b == 1 ? e4.y : b == 2 ? e4.z : e4.w; };
                 // (factors are not 0: hidden scores stay -inf)
@@ -524,14 +524,10 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                     tmem_wait_ld();
                     tmem_regs_ready(va);
                     tmem_regs_ready(vb);
-                    if (masked) {
-                        hide(va, hh ? mk[2] : mk[0]);
-                        hide(vb, hh ? mk[3] : mk[1]);
-                    }
                 };
                 // the row's maxima, of the scores and with their blocks' ev, 64 keys at a time
                 float mt = -INFINITY, rmax = -INFINITY, ev_min = INFINITY;
-#pragma unroll 1
+#pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                     uint32_t va[32], vb[32];
                     load64(hh, va, vb);
@@ -542,7 +538,7 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                         float x[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                         for (int e = 0; e < 16; e += 2)
-                            x[e >> 1 & 1] = fmaxf(x[e >> 1 & 1], fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
+                            asm("max.f32 %0, %0, %1, %2;" : "+f"(x[e >> 1 & 1]) : "f"(__uint_as_float(v[e])), "f"(__uint_as_float(v[e + 1])));
                         const float top = fmaxf(x[0], x[1]) * factor(e4, b);
                         mt = fmaxf(mt, top);
                         rmax = fmaxf(rmax, top + offset(e4, b));
@@ -577,15 +573,18 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                 const bool apart = __any_sync(0xffffffffu, -up - ev_min - mn > 90.f);
                 if (apart) {
 #pragma unroll 1
-                    for (int hh = 0; hh < 2; ++hh) {
-                        uint32_t va[32], vb[32];
-                        load64(hh, va, vb);
-                        const uint4 e4 = exps[hh];
+                    for (int k0 = 0; k0 < kBN; k0 += 32) {
+                        uint32_t va[32];
+                        tmem_ld32(s_tm + k0, va);
+                        tmem_wait_ld();
+                        tmem_regs_ready(va);
+                        const uint4 e4 = exps[k0 / 64];
+                        const float c0 = factor(e4, k0 & 32 ? 2 : 0), c1 = factor(e4, k0 & 32 ? 3 : 1);
 #pragma unroll
-                        for (int e = 0; e < 64; ++e) l += ex2(fmaf(__uint_as_float(e < 32 ? va[e] : vb[e - 32]), factor(e4, e / 16), -mn));
+                        for (int e = 0; e < 32; ++e) l += ex2(fmaf(__uint_as_float(va[e]), e < 16 ? c0 : c1, -mn));
                     }
                 }
-#pragma unroll 1
+#pragma unroll(kApart ? 2 : 1)
                 for (int hh = 0; hh < 2; ++hh) {
                     uint32_t va[32], vb[32], xp[32];
                     load64(hh, va, vb);
