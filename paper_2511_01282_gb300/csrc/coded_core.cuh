@@ -27,11 +27,11 @@
 // what is on its way (4.2 us a key tile).  K and V tiles share one ring, K a tile ahead:
 // K0 K1 V0 K2 V1 ... V(n-1).
 //
-// Measured: four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 313 us, 4.3 TB/s (the
-// cache in 16 bits takes 403): a chain a key tile of one softmax warpgroup, product, softmax, product, with two
-// of them at work, beside 1000 cycles of conversion; 200 to 1000 new tokens behind 4000 to 32000
-// (four requests, 32 / 8 heads of 64, fp16) 436 us, bound by the softmax warps, which share their
-// schedulers with the converting ones (in 16 bits 378 us).
+// Measured: four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 310 us, 4.3 TB/s (the
+// cache in 16 bits takes 403), near what shared memory passes: 224 KB a key tile (products 96, tiles
+// written 64, codes read and written 64) in 2170 cycles; 200 to 1000 new tokens behind 4000 to
+// 32000 (four requests, 32 / 8 heads of 64, fp16) 440 us, bound by the softmax warps, which share
+// their schedulers with the converting ones (in 16 bits 378 us).
 #pragma once
 
 #include "coded.cuh"
@@ -699,92 +699,100 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
         constexpr int kRowLanes = D / 16, kRowsStep = 128 / kRowLanes, kLoads = kBN / kRowsStep;
         const int ci = tid & 127, part = ci % kRowLanes, row0 = ci / kRowLanes;
         uint32_t st = 0, phase = 0, cst = 0, cphase = 0;  // stages of tiles and codes, and which use of them
-        uint32_t quse[2] = {0, 0};                        // Q tiles
+        uint32_t qphase = 0;                              // bit x: of Q tile x
         bool ok = true;
         while (ok && cur.next(pc)) {
             const int n = pc.j1 - pc.j0, tail = pc.keys - (pc.j1 - 1) * kBN;  // keys of the last tile
+            // (the queries behind two positions, and not between the loop's statements: a jump over so much
+            // took 200 cycles a position)
 #pragma unroll 1
-            for (int pos = 0; pos < 2 * n; ++pos) {
-                if (!(ok = quick_wait2(&cfull[cst], cphase, &empty[st], phase ^ 1, s_abort, a.wait_limit))) break;
-                const unsigned char *codes = smem + S::kCodes + cst * (kBN * D);
-                unsigned char *tile = smem + S::kRing + st * S::kTile;
-                // A lane's 16 codes are two words of eight: at D = 128 one of each 64 columns (of odd rows the
-                // second first), at D = 64 side by side.  All go to other banks that way, there and here.
-                const unsigned char *const from = codes + row0 * D + (D == 128 ? (row0 & 1) * 64 + part * 8 : part * 16);
-                const int step = D == 128 ? (row0 & 1 ? -64 : 64) : 8;
-                // 128-byte swizzle: 16-byte word w of row r at w ^ (r & 7)
-                unsigned char *const to = tile + row0 * 128;
-                const int at0 = D == 128 ? (row0 & 1) * 16384 + ((part ^ (row0 & 7)) * 16) : ((2 * part) ^ (row0 & 7)) * 16;
-                const int at1 = D == 128 ? at0 ^ 16384 : ((2 * part + 1) ^ (row0 & 7)) * 16;
+            for (int half = BF16 ? 0 : 1; ok && half < 2; ++half) {
+                if (BF16 && half) {
 #pragma unroll 1
-                for (int i0 = 0; i0 < kLoads; i0 += 4) {
-                    uint2 x[4], y[4];  // (all loads before the first store, which the compiler does not move them over)
+                    for (int x = 0; x < 2; ++x) {
+                        if (!takes_part(x)) continue;
+                        // Q tile x to fp16 in place, a row to a thread, by a power of two that brings its largest value
+                        // to 2^14 .. 2^15
+                        if (!(ok = quick_wait(&qfull[x], qphase >> x & 1, s_abort, a.wait_limit))) break;
+                        qphase ^= 1u << x;
+                        unsigned char *row = smem + S::kQ + x * S::kTile + ci * 128;
+                        uint32_t most = 0;
+#pragma unroll 2
+                        for (int i = 0; i < 8 * kKB; ++i) {
+                            const uint4 v = *reinterpret_cast<const uint4 *>(row + (i >> 3) * 16384 + ((i + ci) & 7) * 16);
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[i] = *reinterpret_cast<const uint2 *>(from + (i0 + i) * 2048);
-                        y[i] = *reinterpret_cast<const uint2 *>(from + (i0 + i) * 2048 + step);
+                            for (int e = 0; e < 4; ++e) {
+                                const uint32_t lo = (w[e] << 16) & 0x7fffffffu, hi = w[e] & 0x7fff0000u;
+                                most = max(most, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+                            }
+                        }
+                        const int shift = most ? max((int)(most >> 23) - 127 - 14, -112) : 0;
+                        const float down = pow2i(-shift);
+#pragma unroll 2
+                        for (int i = 0; i < 8 * kKB; ++i) {
+                            uint4 *p = reinterpret_cast<uint4 *>(row + (i >> 3) * 16384 + ((i + ci) & 7) * 16);
+                            uint4 v = *p;
+                            uint32_t *w = &v.x;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                w[e] = pack16<false>(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xffff0000u) * down);
+                            *p = v;
+                        }
+                        s_shift[x * kBM + ci] = (int8_t)shift;
+                        fence_async_smem();
+                        warp_arrive(&qready[x]);
+                    }
+                    if (!ok) break;
+                }
+                const int end = half ? 2 * n : 2;
+#pragma unroll 1
+                for (int pos = BF16 && half ? 2 : 0; pos < end; ++pos) {
+                    if (!(ok = quick_wait2(&cfull[cst], cphase, &empty[st], phase ^ 1, s_abort, a.wait_limit))) break;
+                    const unsigned char *codes = smem + S::kCodes + cst * (kBN * D);
+                    unsigned char *tile = smem + S::kRing + st * S::kTile;
+                    // A lane's 16 codes are two words of eight: at D = 128 one of each 64 columns (of odd rows the
+                    // second first), at D = 64 side by side.  All go to other banks that way, there and here.
+                    const unsigned char *const from = codes + row0 * D + (D == 128 ? (row0 & 1) * 64 + part * 8 : part * 16);
+                    const int step = D == 128 ? (row0 & 1 ? -64 : 64) : 8;
+                    // 128-byte swizzle: 16-byte word w of row r at w ^ (r & 7)
+                    unsigned char *const to = tile + row0 * 128;
+                    const int at0 = D == 128 ? (row0 & 1) * 16384 + ((part ^ (row0 & 7)) * 16) : ((2 * part) ^ (row0 & 7)) * 16;
+                    const int at1 = D == 128 ? at0 ^ 16384 : ((2 * part + 1) ^ (row0 & 7)) * 16;
+                    uint2 x[kLoads], y[kLoads];  // (all loads before the first store, which the compiler does not move them over)
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) {
+                        x[i] = *reinterpret_cast<const uint2 *>(from + i * 2048);
+                        y[i] = *reinterpret_cast<const uint2 *>(from + i * 2048 + step);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < kLoads; ++i) {
                         uint4 lo, hi;
                         decode4(x[i].x, lo.x, lo.y);
                         decode4(x[i].y, lo.z, lo.w);
                         decode4(y[i].x, hi.x, hi.y);
                         decode4(y[i].y, hi.z, hi.w);
-                        *reinterpret_cast<uint4 *>(to + at0 + (i0 + i) * kRowsStep * 128) = lo;
-                        *reinterpret_cast<uint4 *>(to + at1 + (i0 + i) * kRowsStep * 128) = hi;
+                        *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = lo;
+                        *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = hi;
                     }
-                }
-                if (tail < kBN && tile_at(pos, n) == n - 1)  // behind the last key anything was copied, NaN too
+                    if (tail < kBN && tile_at(pos, n) == n - 1)  // behind the last key anything was copied, NaN too
 #pragma unroll 1
-                    for (int i = 0; i < kLoads; ++i)
-                        if (i * kRowsStep + row0 >= tail) {
-                            *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
-                            *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
-                        }
-                fence_async_smem();
-                warp_arrive(&full[st]);
-                warp_arrive(&cempty[cst]);
-                if (++st == NR) {
-                    st = 0;
-                    phase ^= 1;
-                }
-                if (++cst == NC) {
-                    cst = 0;
-                    cphase ^= 1;
-                }
-                if (const int x = pos; BF16 && pos < 2 && takes_part(x)) {
-                    // Q tile x to fp16 in place, a row to a thread, by a power of two that brings its largest value
-                    // to 2^14 .. 2^15
-                    if (!(ok = quick_wait(&qfull[x], quse[x] & 1, s_abort, a.wait_limit))) break;
-                    ++quse[x];
-                    unsigned char *row = smem + S::kQ + x * S::kTile + ci * 128;
-                    uint32_t most = 0;
-#pragma unroll 2
-                    for (int i = 0; i < 8 * kKB; ++i) {
-                        const uint4 v = *reinterpret_cast<const uint4 *>(row + (i >> 3) * 16384 + ((i + ci) & 7) * 16);
-                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t lo = (w[e] << 16) & 0x7fffffffu, hi = w[e] & 0x7fff0000u;
-                            most = max(most, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
-                        }
-                    }
-                    const int shift = most ? max((int)(most >> 23) - 127 - 14, -112) : 0;
-                    const float down = pow2i(-shift);
-#pragma unroll 2
-                    for (int i = 0; i < 8 * kKB; ++i) {
-                        uint4 *p = reinterpret_cast<uint4 *>(row + (i >> 3) * 16384 + ((i + ci) & 7) * 16);
-                        uint4 v = *p;
-                        uint32_t *w = &v.x;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[e] = pack16<false>(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xffff0000u) * down);
-                        *p = v;
-                    }
-                    s_shift[x * kBM + ci] = (int8_t)shift;
+                        for (int i = 0; i < kLoads; ++i)
+                            if (i * kRowsStep + row0 >= tail) {
+                                *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
+                                *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
+                            }
                     fence_async_smem();
-                    warp_arrive(&qready[x]);
+                    warp_arrive(&full[st]);
+                    warp_arrive(&cempty[cst]);
+                    if (++st == NR) {
+                        st = 0;
+                        phase ^= 1;
+                    }
+                    if (++cst == NC) {
+                        cst = 0;
+                        cphase ^= 1;
+                    }
                 }
             }
         }
