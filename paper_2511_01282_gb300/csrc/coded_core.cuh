@@ -29,7 +29,7 @@
 //
 // Measured: four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 310 us, 4.3 TB/s (the
 // cache in 16 bits takes 403), near what shared memory passes: 224 KB a key tile (products 96, tiles
-// written 64, codes read and written 64) in 2170 cycles; 200 to 1000 new tokens behind 4000 to
+// written 64, codes written and read 64) in 2200 cycles; 200 to 1000 new tokens behind 4000 to
 // 32000 (four requests, 32 / 8 heads of 64, fp16) 440 us, bound by the softmax warps, which share
 // their schedulers with the converting ones (in 16 bits 378 us).
 #pragma once
