@@ -250,8 +250,10 @@ extern "C" rs_status rs_coded_append(const uint16_t *k, int64_t k_stride, const 
                       CodedPool{k_codes, v_codes, k_exps, v_exps, page_table, ctx_len, n_pages, page_log2(page_size), n_pages ? max_pages : 0},
                       status, B, T, Hkv};
     const long long items = (T >> kCodeBlockLog2) + 2ll * B, blocks = (items + kCodeThreads / 32 - 1) / (kCodeThreads / 32);
-    // several times the warps that the SMs hold at a time (32 each), by heads where the blocks are few
-    const long long most = 12ll * num_sms();
+    // Several times the warps that the SMs hold at a time (32 each), by heads where the blocks are few; as many
+    // as they hold where those would be all: a second wave costs more than a second head (44 requests of a
+    // token or two, 40 heads: 9.0 us in two)
+    const long long most = 2 * blocks * Hkv <= 12ll * num_sms() ? 4ll * num_sms() : 12ll * num_sms();
     const unsigned x = (unsigned)std::min(blocks, most), y = (unsigned)std::min(std::max(most / (2ll * x), 1ll), (long long)Hkv);
     const dim3 grid(x, y, 2);
     const cudaStream_t s = (cudaStream_t)stream;

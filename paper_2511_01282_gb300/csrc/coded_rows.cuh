@@ -137,15 +137,18 @@ __device__ __forceinline__ RowsWalk rows_plan(const RowsArgs &a, int &used, int 
         total += s_sum[w];
     }
     // Heads side by side read HBM better, warps side by side at one head leave fewer pieces to
-    // join: the first where every warp has 16 blocks and more
-    hw = total * a.Hkv >= 16ll * kRowWarps * a.grid ? a.most_hw : 1;
+    // join: the first where every warp has 16 blocks and more, and where requests are so short (four
+    // blocks on average) that a head leaves most warps without any
+    hw = total * a.Hkv >= 16ll * kRowWarps * a.grid || total <= 4ll * s_live ? a.most_hw : 1;
     const int groups = a.Hkv / hw;
     const long long W = total * groups;
-    // shares of at least two steps a warp: shorter ones cost more to join than they save.  With
-    // few segments a whole number of shares each, at least one: a CTA has one piece then
-    // (of requests of one length)
+    // shares of at least two steps a warp: shorter ones cost more to join than they save; but a share a
+    // segment, as many as there are CTAs for, since a segment's own cost is that of many blocks (25 requests of
+    // up to 4 tokens, 16 heads, no cache: 106 us with 25 CTAs).  With few segments a whole number of shares
+    // each, at least one: a CTA has one piece then (of requests of one length)
     const int least = 4 * kRowWarps / hw;
-    const long long fit = min((W + least - 1) / least, (long long)a.grid), segments = (long long)s_live * groups;
+    const long long segments = (long long)s_live * groups;
+    const long long fit = min(max((W + least - 1) / least, segments), (long long)a.grid);
     used = (int)(2 * segments > a.grid ? fit : segments * max(fit / max(segments, 1ll), 1ll));
     const int c = blockIdx.x;
     const long long lo = c < used ? W * c / used : 0, hi = c < used ? W * (c + 1) / used : 0;
