@@ -148,3 +148,24 @@ def test_zero_queries_and_a_scale_that_makes_one_key_all(rs, n, most):
     check_attention(pool, q, [0, n], [500], 30.0, got)
     at = slots(pool.table, 0, 501, 32)
     assert len(set(at.tolist())) == 501
+
+
+@pytest.mark.parametrize("B,most,ctx_lo,ctx_hi,Hq,Hkv,D,tree,dt", [
+    (25, 4, 0, 0, 64, 16, 128, False, torch.float16), (6, 4, 0, 0, 40, 40, 128, True, torch.bfloat16), (24, 1, 18, 150, 16, 16, 128, True, torch.bfloat16),
+    (700, 1, 0, 50, 8, 4, 64, False, torch.bfloat16), (60, 8, 30, 90, 6, 6, 64, True, torch.float16), (33, 2, 0, 40, 15, 5, 128, False, torch.float16)])
+def test_many_short_requests(rs, B, most, ctx_lo, ctx_hi, Hq, Hkv, D, tree, dt):
+    """Segments of a few blocks, fewer and more than there are CTAs; some requests without tokens."""
+    g = random.Random(B)
+    ns = [g.randrange(0 if b % 7 == 3 else 1, most + 1) for b in range(B)]
+    ctx = [g.randrange(ctx_lo, ctx_hi + 1) for _ in range(B)]
+    off = [0]
+    for x in ns:
+        off.append(off[-1] + x)
+    lens = [c + x for c, x in zip(ctx, ns)]
+    pool = Pool(lens, 16, Hkv, D, 5)
+    fill(rs, pool, lens, dt, 21)
+    q = rows(off[-1] + 1, Hq, D, dt, 23)
+    parents = i32([-1 if i == 0 else g.randrange(i) for x in ns for i in range(x)] + [0]) if tree else None
+    got = attend(rs, pool, q, off, ctx, most, D ** -0.5, parents)
+    check_attention(pool, q, off, ctx, D ** -0.5, got, parents)
+    assert (got[0][-1:] == 7).all() and (got[1][-1:] == 7).all()
