@@ -29,7 +29,10 @@
 // exponentials, a transpose, products), which the twelve warps of an SM do not fill.  Pieces of a cut
 // (request, head) are joined in order by coded_join: the same bits every time.
 //
-// Bound: HBM, of 2 D bytes a key and KV head.
+// Bound: HBM, of 2 D bytes a key and KV head.  Measured: single tokens of 64 requests behind 1024 to 8191
+// keys, 32 / 8 heads of 128, 605 MB, 111-114 us, 5.4 TB/s (107 with the copies alone; 188 from a cache in 16
+// bits); of one request behind 2048 keys 13.5 us, two launches and their chains of reads.  K and V in rings of
+// their own, K refilled as soon as it is in registers, took 119.
 #pragma once
 
 #include "attn_core.cuh"
