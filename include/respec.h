@@ -621,11 +621,10 @@ rs_status rs_coded_append(const uint16_t *k, int64_t k_stride, const uint16_t *v
  *   the rest as for rs_paged_attn.  Size the workspace with the same six sizes.
  * P is rounded to fp16 (2^-12 relative; weights times 2^exponent of V below 2^-32
  * of a row's largest may vanish); bf16 queries are taken as fp16, times a power of
- * two (elements below 2^-39 of a row's largest may vanish).  NaN in V of a key that
- * a row does not see reaches it only where it sees another key of the same 16 slots
- * (max_new x Hq / Hkv <= 32) or where another row of its 128-row tile sees one of
- * the same 128 slots (else).  The result does not depend on what else runs: the same
- * bits every time.
+ * two (elements below 2^-39 of a row's largest may vanish).  NaN in K or V of a key
+ * reaches the rows that see the key (of V, in its column), and no others.  What slots
+ * behind a request's last token hold does not matter.  The result does not depend on
+ * what else runs: the same bits every time.
  */
 size_t rs_coded_attn_workspace_size(int B, int T, int max_new, int Hq, int Hkv, int D);
 rs_status rs_coded_attn(const uint16_t *q, int64_t q_stride, int dtype, const int32_t *new_off,

@@ -33,6 +33,10 @@ __device__ __forceinline__ void decode4(uint32_t four, uint32_t &lo, uint32_t &h
         : "=r"(lo), "=r"(hi)
         : "r"(four));
 }
+// bit 7 of every code that is NaN (0x7f and 0xff)
+__device__ __forceinline__ uint32_t nan_codes(uint32_t four) { return ((four & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// the codes that are not NaN, 0 in the place of those that are
+__device__ __forceinline__ uint32_t without_nan(uint32_t four) { return four & ~((nan_codes(four) >> 7) * 0xffu); }
 // (lo, hi) -> two codes, to nearest even; NaN -> NaN
 __device__ __forceinline__ uint32_t encode2(float lo, float hi) {
     uint32_t c;

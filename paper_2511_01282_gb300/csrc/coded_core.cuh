@@ -21,6 +21,10 @@
 // the chain of one row tile, product, softmax, product, took 2500 cycles a key tile
 // where its bytes take 1500.
 //
+// NaN in V of a key that only some rows see stays out of the products (coded_nan): the converting warps look for it
+// in the tiles with such keys, which costs chunks and trees behind a cache nothing that shows (308 us the trees, 438 the
+// chunks, 436 before) and short prompts without one 6 % (46 of 757 tokens, 224 us and 210).
+//
 // Warps: 0 and 1 MMA issue, 2 Q, 3 copies codes, 4-7 and 8-11 softmax, 12-15 codes to
 // tiles.  Codes come by TMA, two tiles (64 KB at D = 128) ahead; the converting warps load
 // nothing themselves, as their fences, which hand a tile to the tensor core, would wait for
@@ -703,6 +707,11 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
         bool ok = true;
         while (ok && cur.next(pc)) {
             const int n = pc.j1 - pc.j0, tail = pc.keys - (pc.j1 - 1) * kBN;  // keys of the last tile
+            // NaN in V of a key that some row does not see would reach all rows by the product's 0 x NaN.  In V from this
+            // position on, the first with keys that not every row of the piece sees, it is looked for first and becomes
+            // 0 (the rows that see the key get it from coded_nan).
+            const int open = pc.ctx + (a.anc ? 0 : pc.p * 2 * tq + 1);
+            const int look = open < pc.keys && open < pc.j1 * kBN ? v_at(max(open / kBN - pc.j0, 0), n) : 2 * n;
             // (the queries behind two positions, and not between the loop's statements: a jump over so much
             // took 200 cycles a position)
 #pragma unroll 1
@@ -746,52 +755,73 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                     if (!ok) break;
                 }
                 const int end = half ? 2 * n : 2;
+                // A lane's 16 codes are two words of eight: at D = 128 one of each 64 columns (of odd rows the
+                // second first), at D = 64 side by side.  All go to other banks that way, there and here.
+                const int from0 = row0 * D + (D == 128 ? (row0 & 1) * 64 + part * 8 : part * 16);
+                const int step = D == 128 ? (row0 & 1 ? -64 : 64) : 8;
 #pragma unroll 1
-                for (int pos = BF16 && half ? 2 : 0; pos < end; ++pos) {
-                    if (!(ok = quick_wait2(&cfull[cst], cphase, &empty[st], phase ^ 1, s_abort, a.wait_limit))) break;
-                    const unsigned char *codes = smem + S::kCodes + cst * (kBN * D);
-                    unsigned char *tile = smem + S::kRing + st * S::kTile;
-                    // A lane's 16 codes are two words of eight: at D = 128 one of each 64 columns (of odd rows the
-                    // second first), at D = 64 side by side.  All go to other banks that way, there and here.
-                    const unsigned char *const from = codes + row0 * D + (D == 128 ? (row0 & 1) * 64 + part * 8 : part * 16);
-                    const int step = D == 128 ? (row0 & 1 ? -64 : 64) : 8;
-                    // 128-byte swizzle: 16-byte word w of row r at w ^ (r & 7)
-                    unsigned char *const to = tile + row0 * 128;
-                    const int at0 = D == 128 ? (row0 & 1) * 16384 + ((part ^ (row0 & 7)) * 16) : ((2 * part) ^ (row0 & 7)) * 16;
-                    const int at1 = D == 128 ? at0 ^ 16384 : ((2 * part + 1) ^ (row0 & 7)) * 16;
-                    uint2 x[kLoads], y[kLoads];  // (all loads before the first store, which the compiler does not move them over)
-#pragma unroll
-                    for (int i = 0; i < kLoads; ++i) {
-                        x[i] = *reinterpret_cast<const uint2 *>(from + i * 2048);
-                        y[i] = *reinterpret_cast<const uint2 *>(from + i * 2048 + step);
-                    }
-#pragma unroll
-                    for (int i = 0; i < kLoads; ++i) {
-                        uint4 lo, hi;
-                        decode4(x[i].x, lo.x, lo.y);
-                        decode4(x[i].y, lo.z, lo.w);
-                        decode4(y[i].x, hi.x, hi.y);
-                        decode4(y[i].y, hi.z, hi.w);
-                        *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = lo;
-                        *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = hi;
-                    }
-                    if (tail < kBN && tile_at(pos, n) == n - 1)  // behind the last key anything was copied, NaN too
+                for (int pos = BF16 && half ? 2 : 0; ok && pos < end;) {  // (two loops: what is rare stays out of the inner one)
+                    const int stop = min(end, pos < look ? look : pos + 1);
+                    if (pos >= look && (pos == 2 * n - 1 || !(pos & 1))) {  // (V: of even positions, and the last)
+                        if (!(ok = quick_wait(&cfull[cst], cphase, s_abort, a.wait_limit))) break;
+                        // this lane's own words, of keys open .. pc.keys - 1
+                        const int key0 = (pc.j0 + tile_at(pos, n)) * kBN + row0;
+                        const int i1 = min((pc.keys - key0 + kRowsStep - 1) / kRowsStep, kLoads);
+                        unsigned char *codes = smem + S::kCodes + cst * (kBN * D) + from0;
 #pragma unroll 1
-                        for (int i = 0; i < kLoads; ++i)
-                            if (i * kRowsStep + row0 >= tail) {
-                                *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
-                                *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
-                            }
-                    fence_async_smem();
-                    warp_arrive(&full[st]);
-                    warp_arrive(&cempty[cst]);
-                    if (++st == NR) {
-                        st = 0;
-                        phase ^= 1;
+                        for (int i = max((open - key0 + kRowsStep - 1) / kRowsStep, 0); i < i1; ++i) {
+                            uint2 *p = reinterpret_cast<uint2 *>(codes + i * 2048), *q = reinterpret_cast<uint2 *>(codes + i * 2048 + step);
+                            const uint2 x = *p, y = *q;
+                            if (!(nan_codes(x.x) | nan_codes(x.y) | nan_codes(y.x) | nan_codes(y.y))) continue;
+                            *p = make_uint2(without_nan(x.x), without_nan(x.y));
+                            *q = make_uint2(without_nan(y.x), without_nan(y.y));
+                            a.n_pairs[3] = 1;
+                        }
                     }
-                    if (++cst == NC) {
-                        cst = 0;
-                        cphase ^= 1;
+#pragma unroll 1
+                    for (; pos < stop; ++pos) {
+                        if (!(ok = quick_wait2(&cfull[cst], cphase, &empty[st], phase ^ 1, s_abort, a.wait_limit))) break;
+                        const unsigned char *codes = smem + S::kCodes + cst * (kBN * D);
+                        unsigned char *tile = smem + S::kRing + st * S::kTile;
+                        const unsigned char *const from = codes + from0;
+                        // 128-byte swizzle: 16-byte word w of row r at w ^ (r & 7)
+                        unsigned char *const to = tile + row0 * 128;
+                        const int at0 = D == 128 ? (row0 & 1) * 16384 + ((part ^ (row0 & 7)) * 16) : ((2 * part) ^ (row0 & 7)) * 16;
+                        const int at1 = D == 128 ? at0 ^ 16384 : ((2 * part + 1) ^ (row0 & 7)) * 16;
+                        uint2 x[kLoads], y[kLoads];  // (all loads before the first store, which the compiler does not move them over)
+#pragma unroll
+                        for (int i = 0; i < kLoads; ++i) {
+                            x[i] = *reinterpret_cast<const uint2 *>(from + i * 2048);
+                            y[i] = *reinterpret_cast<const uint2 *>(from + i * 2048 + step);
+                        }
+#pragma unroll
+                        for (int i = 0; i < kLoads; ++i) {
+                            uint4 lo, hi;
+                            decode4(x[i].x, lo.x, lo.y);
+                            decode4(x[i].y, lo.z, lo.w);
+                            decode4(y[i].x, hi.x, hi.y);
+                            decode4(y[i].y, hi.z, hi.w);
+                            *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = lo;
+                            *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = hi;
+                        }
+                        if (tail < kBN && tile_at(pos, n) == n - 1)  // behind the last key anything was copied, NaN too
+#pragma unroll 1
+                            for (int i = 0; i < kLoads; ++i)
+                                if (i * kRowsStep + row0 >= tail) {
+                                    *reinterpret_cast<uint4 *>(to + at0 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
+                                    *reinterpret_cast<uint4 *>(to + at1 + i * kRowsStep * 128) = make_uint4(0, 0, 0, 0);
+                                }
+                        fence_async_smem();
+                        warp_arrive(&full[st]);
+                        warp_arrive(&cempty[cst]);
+                        if (++st == NR) {
+                            st = 0;
+                            phase ^= 1;
+                        }
+                        if (++cst == NC) {
+                            cst = 0;
+                            cphase ^= 1;
+                        }
                     }
                 }
             }
@@ -805,6 +835,37 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
     if (tid == 0 && *s_abort) {  // any role gave up: flag every request this CTA touches
         FlCursor again(a, s_bound, M);
         while (again.next(pc)) atomicOr(&a.status[pc.b], RS_ST_TIMEOUT);
+    }
+}
+
+// NaN in V of new tokens, which coded_core kept out of its products, into the rows that see it: a new token and KV head to a
+// warp, four codes to a lane.  Where there was none, the usual case, it returns at once.
+constexpr int kNanThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kNanThreads)
+coded_nan(FlashArgs a) {
+    pdl_enter();
+    if (!a.n_pairs[3]) return;
+    const int lane = threadIdx.x & 31;
+    const long long w0 = blockIdx.x * (kNanThreads / 32) + (threadIdx.x >> 5), warps = gridDim.x * (kNanThreads / 32);
+    for (int b = 0; b < a.B; ++b) {
+        const int4 rq = a.req[b];  // first row, rows, ctx
+        if (a.status[b]) continue;
+        for (long long w = w0; w < (long long)rq.y * a.Hkv; w += warps) {
+            const int i = (int)(w / a.Hkv), h = (int)(w - (long long)i * a.Hkv), key = rq.z + i;
+            const long long id = a.page_table[(long long)b * a.max_pages + (key >> a.page_log2)];
+            const long long slot = (id << a.page_log2) + (key & ((1 << a.page_log2) - 1));
+            const uint32_t at = lane < D / 4 ? nan_codes(reinterpret_cast<const uint32_t *>(a.coded.v + (slot * a.Hkv + h) * D)[lane]) : 0;
+            if (!__any_sync(0xffffffffu, at)) continue;
+            for (int r = i; r < rq.y; ++r) {
+                if (a.anc && !(a.anc[(long long)(rq.x + r) * kAncWords + (i >> 5)] >> (i & 31) & 1u)) continue;
+                uint16_t *o = a.out + ((long long)(rq.x + r) * a.Hq + h * a.G) * D + 4 * lane;
+                for (int k = 0; k < a.G; ++k, o += D)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (at >> (8 * e + 7) & 1u) o[e] = 0x7fff;
+            }
+        }
     }
 }
 

@@ -29,6 +29,9 @@
 // exponentials, a transpose, products), which the twelve warps of an SM do not fill.  Pieces of a cut
 // (request, head) are joined in order by coded_join: the same bits every time.
 //
+// NaN in V of a new token is for the rows that see it, where the products give it to all of a warp's: a piece whose
+// results hold NaN is done again without (a check for each block takes 3 to 7 % of short caches' calls).
+//
 // Bound: HBM, of 2 D bytes a key and KV head.  Measured: single tokens of 64 requests behind 1024 to 8191
 // keys, 32 / 8 heads of 128, 605 MB, 111-114 us, 5.4 TB/s (107 with the copies alone; 188 from a cache in 16
 // bits); of one request behind 2048 keys 13.5 us, two launches and their chains of reads.  K and V in rings of
@@ -248,6 +251,7 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
     unsigned char *smem = smem_raw + (-sm100::smem_u32(smem_raw) & 1023u);
     __shared__ uint64_t s_full[kRowWarps][kS];
     __shared__ int s_gave_up;
+    __shared__ uint32_t s_anc[32];  // a tree's ancestor sets
     volatile int *s_abort = &s_gave_up;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kRowWarps * kS; ++i) sm100::mbar_init(&s_full[0][0] + i, 1);
@@ -270,6 +274,9 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
     const int head = warp % hw, kw = warp / hw, KW = kRowWarps / hw;  // head of the group; the warp's place among the head's
     uint32_t filled = 0, drained = 0;  // stages of this warp's ring, over all pieces
     bool begun = false;
+    // NaN in V of a key that some row does not see reaches all rows by the product's 0 x NaN.  A piece with such keys
+    // whose results hold NaN is done again with 0 in its place, and the rows that see the key get it at the end.
+    bool clean = false;
     while (w.left > 0) {
         const int b = w.b, h = w.h * hw + head, j0 = w.j, nb = w.nb;
         const int j1 = (int)min((long long)nb, j0 + w.left);
@@ -360,6 +367,7 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
                 }
             }
         }
+        if (TREE && warp == 0) s_anc[lane] = anc;
         // the queries, as the product's second operand: row nt 8 + g; this lane's columns are
         // those of the codes that it reads
         uint32_t qf[NT][kSteps][2];
@@ -424,165 +432,186 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
 
         if (!(flag & RS_ST_BAD_TREE)) {  // (else nothing is computed: the request's rows are emptied)
 #pragma unroll 1
-            for (int it = 0; it < mine; ++it) {
-                const int cur = it / kBatch;
-                // the lookups of the next batch, a step at a time
-                if (it % kBatch == 2) id_next = page_of(cur + 1);
-                if (it % kBatch == 5) {
-                    blk_next = block_of(cur + 1, id_next);
-                    exps_next = exps_of(blk_next);
+            for (int it = 0; it < mine && !(flag & RS_ST_TIMEOUT);) {  // (two loops: what is rare stays out of the inner one)
+                const int stop = clean ? it + 1 : mine;
+                const int hidden = j0 + kBl * (kw + KW * it);  // the step's first block
+                if (clean && (hidden + kBl) * kCodeBlock > open) {
+                    unsigned char *v = ring + drained % kS * Sh::kStageBytes + kCodeBlock * D;
+                    if (!quick_wait(&s_full[warp][drained % kS], drained / kS & 1, s_abort, a.wait_limit)) {
+                        flag |= RS_ST_TIMEOUT;
+                        break;
+                    }
+#pragma unroll 1
+                    for (int u = 0; u < kBl; ++u, v += Sh::kBlockBytes)
+                        if ((hidden + u + 1) * kCodeBlock > open)
+                            for (int i = lane; i < D; i += 32) {  // 16-byte words of the block's V
+                                uint4 *p = reinterpret_cast<uint4 *>(v) + i;
+                                *p = make_uint4(without_nan(p->x), without_nan(p->y), without_nan(p->z), without_nan(p->w));
+                            }
+                    sm100::fence_async_smem();  // (the stage is copied to again)
+                    __syncwarp();
                 }
-                if (!quick_wait(&s_full[warp][drained % kS], drained / kS & 1, s_abort, a.wait_limit)) {
-                    flag |= RS_ST_TIMEOUT;
-                    break;
-                }
-                const unsigned char *src = ring + drained % kS * Sh::kStageBytes;
-                ++drained;
-                const int block0 = j0 + kBl * (kw + KW * it), key0 = block0 * kCodeBlock;
-                float s[kBl][NT][4], evf[kBl], two_ek[kBl];
-#pragma unroll
-                for (int u = 0; u < kBl; ++u) {
-                    const int e2 = __shfl_sync(0xffffffffu, exps, it % kBatch * kBl + u);
-                    two_ek[u] = pow2i(code_exp((int)(int8_t)(e2 & 255), bf16));
-                    evf[u] = (float)code_exp((int)(int8_t)(e2 >> 8), bf16);
-                }
-                // S^T: keys g and g + 8 of a block, rows 2 t and 2 t + 1 of every tile; even and odd
-                // steps are summed apart
-                uint4 kc[kBl][Sh::kKLoads];
-#pragma unroll
-                for (int u = 0; u < kBl; ++u)
-#pragma unroll
-                    for (int i = 0; i < Sh::kKLoads; ++i)
-                        kc[u][i] = *reinterpret_cast<const uint4 *>(src + u * Sh::kBlockBytes + word(i / (D / 64) * 8 + g, i % (D / 64) * 4 + t));
-                float s1[kBl][NT][4];
-#pragma unroll
-                for (int u = 0; u < kBl; ++u)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[u][nt][e] = s1[u][nt][e] = 0.f;
-#pragma unroll
-                for (int k = 0; k < kSteps; ++k)
+#pragma unroll 1
+                for (; it < stop; ++it) {
+                    const int cur = it / kBatch;
+                    // the lookups of the next batch, a step at a time
+                    if (it % kBatch == 2) id_next = page_of(cur + 1);
+                    if (it % kBatch == 5) {
+                        blk_next = block_of(cur + 1, id_next);
+                        exps_next = exps_of(blk_next);
+                    }
+                    if (!quick_wait(&s_full[warp][drained % kS], drained / kS & 1, s_abort, a.wait_limit)) {
+                        flag |= RS_ST_TIMEOUT;
+                        break;
+                    }
+                    const unsigned char *src = ring + drained % kS * Sh::kStageBytes;
+                    ++drained;
+                    const int block0 = j0 + kBl * (kw + KW * it), key0 = block0 * kCodeBlock;
+                    float s[kBl][NT][4], evf[kBl], two_ek[kBl];
 #pragma unroll
                     for (int u = 0; u < kBl; ++u) {
-                        const uint4 &x = kc[u][k / 4], &y = kc[u][D / 64 + k / 4];
-                        const uint32_t wx = (k & 3) == 0 ? x.x : (k & 3) == 1 ? x.y : (k & 3) == 2 ? x.z : x.w;
-                        const uint32_t wy = (k & 3) == 0 ? y.x : (k & 3) == 1 ? y.y : (k & 3) == 2 ? y.z : y.w;
-                        uint32_t a0, a1, a2, a3;
-                        decode4(wx, a0, a2);
-                        decode4(wy, a1, a3);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma_f16(NT < 4 && (k & 1) ? s1[u][nt] : s[u][nt], a0, a1, a2, a3, qf[nt][k][0], qf[nt][k][1]);
+                        const int e2 = __shfl_sync(0xffffffffu, exps, it % kBatch * kBl + u);
+                        two_ek[u] = pow2i(code_exp((int)(int8_t)(e2 & 255), bf16));
+                        evf[u] = (float)code_exp((int)(int8_t)(e2 >> 8), bf16);
                     }
-                const bool masked = key0 + kBl * kCodeBlock > open || block0 + kBl > j1;
-                bool grow = false;
+                    // S^T: keys g and g + 8 of a block, rows 2 t and 2 t + 1 of every tile; even and odd
+                    // steps are summed apart
+                    uint4 kc[kBl][Sh::kKLoads];
 #pragma unroll
-                for (int u = 0; u < kBl; ++u)
+                    for (int u = 0; u < kBl; ++u)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
+                        for (int i = 0; i < Sh::kKLoads; ++i)
+                            kc[u][i] = *reinterpret_cast<const uint4 *>(src + u * Sh::kBlockBytes + word(i / (D / 64) * 8 + g, i % (D / 64) * 4 + t));
+                    float s1[kBl][NT][4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[u][nt][e] = (NT < 4 ? s[u][nt][e] + s1[u][nt][e] : s[u][nt][e]) * (factor[nt][e & 1] * two_ek[u]);
-                        if (masked) {
+                    for (int u = 0; u < kBl; ++u)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int key = key0 + u * kCodeBlock + g + (e >> 1) * 8, node = key - ctx;
-                                const bool on = TREE ? node < 0 || (node < 32 && ((see[nt][e & 1] >> node) & 1u)) : key < limit[nt][e & 1];
-                                if (!on || block0 + u >= j1) s[u][nt][e] = -INFINITY;
-                            }
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[u][nt][e] = s1[u][nt][e] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                        for (int u = 0; u < kBl; ++u) {
+                            const uint4 &x = kc[u][k / 4], &y = kc[u][D / 64 + k / 4];
+                            const uint32_t wx = (k & 3) == 0 ? x.x : (k & 3) == 1 ? x.y : (k & 3) == 2 ? x.z : x.w;
+                            const uint32_t wy = (k & 3) == 0 ? y.x : (k & 3) == 1 ? y.y : (k & 3) == 2 ? y.z : y.w;
+                            uint32_t a0, a1, a2, a3;
+                            decode4(wx, a0, a2);
+                            decode4(wy, a1, a3);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma_f16(NT < 4 && (k & 1) ? s1[u][nt] : s[u][nt], a0, a1, a2, a3, qf[nt][k][0], qf[nt][k][1]);
                         }
+                    const bool masked = key0 + kBl * kCodeBlock > open || block0 + kBl > j1;
+                    bool grow = false;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float x = fmaxf(s[u][nt][e], s[u][nt][e + 2]);
-                            grow |= x > m[nt][e] + 8.f || x + evf[u] > ref[nt][e] + 8.f;
-                        }
-                    }
-                if (__any_sync(0xffffffffu, grow)) {
+                    for (int u = 0; u < kBl; ++u)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float x = -INFINITY, y = -INFINITY;  // the largest score, and with its block's ev
+                            for (int e = 0; e < 4; ++e) s[u][nt][e] = (NT < 4 ? s[u][nt][e] + s1[u][nt][e] : s[u][nt][e]) * (factor[nt][e & 1] * two_ek[u]);
+                            if (masked) {
 #pragma unroll
-                            for (int u = 0; u < kBl; ++u) {
-                                const float z = fmaxf(s[u][nt][e], s[u][nt][e + 2]);
-                                x = fmaxf(x, z);
-                                y = fmaxf(y, z + evf[u]);
-                            }
-#pragma unroll
-                            for (int d = 4; d < 32; d *= 2) {
-                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-                                y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, d));
-                            }
-                            if (x > m[nt][e] + 8.f) {
-                                l[nt][e] *= sm100::ex2(m[nt][e] - x);
-                                m[nt][e] = x;
-                            }
-                            if (y > ref[nt][e] + 8.f) {
-                                const float f = sm100::ex2(ref[nt][e] - y);
-                                ref[nt][e] = y;
-#pragma unroll
-                                for (int i = 0; i < kTiles; ++i) {
-                                    o[nt][i][e] *= f;
-                                    o[nt][i][e + 2] *= f;
+                                for (int e = 0; e < 4; ++e) {
+                                    const int key = key0 + u * kCodeBlock + g + (e >> 1) * 8, node = key - ctx;
+                                    const bool on = TREE ? node < 0 || (node < 32 && ((see[nt][e & 1] >> node) & 1u)) : key < limit[nt][e & 1];
+                                    if (!on || block0 + u >= j1) s[u][nt][e] = -INFINITY;
                                 }
                             }
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float x = fmaxf(s[u][nt][e], s[u][nt][e + 2]);
+                                grow |= x > m[nt][e] + 8.f || x + evf[u] > ref[nt][e] + 8.f;
+                            }
                         }
-                }
+                    if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-                for (int u = 0; u < kBl; ++u) {
-                    uint32_t pb[NT][2];  // P'^T as the product's second operand
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        float p[4];
+                            for (int e = 0; e < 2; ++e) {
+                                float x = -INFINITY, y = -INFINITY;  // the largest score, and with its block's ev
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float nm = m[nt][e] == -INFINITY ? 0.f : m[nt][e];
-                            const float nr = ref[nt][e] == -INFINITY ? 0.f : evf[u] + 7.f - ref[nt][e];
-                            l[nt][e] += sm100::ex2(s[u][nt][e] - nm) + sm100::ex2(s[u][nt][e + 2] - nm);
-                            p[e] = sm100::ex2(s[u][nt][e] + nr);
-                            p[e + 2] = sm100::ex2(s[u][nt][e + 2] + nr);
-                        }
-                        pb[nt][0] = transpose8(half2_of(p[0], p[1]));
-                        pb[nt][1] = transpose8(half2_of(p[2], p[3]));
-                    }
-                    uint32_t vc[4][D / 32];
+                                for (int u = 0; u < kBl; ++u) {
+                                    const float z = fmaxf(s[u][nt][e], s[u][nt][e + 2]);
+                                    x = fmaxf(x, z);
+                                    y = fmaxf(y, z + evf[u]);
+                                }
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int key = 2 * t + (y & 1) + 8 * (y >> 1);
-                        const unsigned char *q = src + u * Sh::kBlockBytes + kCodeBlock * D +
-                                                 (D == 128 ? word(key, g) : word(key, g >> 1) + (g & 1) * 8);
-                        if constexpr (D == 128) {
-                            const uint4 x = *reinterpret_cast<const uint4 *>(q);
-                            vc[y][0] = x.x, vc[y][1] = x.y, vc[y][2] = x.z, vc[y][3] = x.w;
-                        } else {
-                            const uint2 x = *reinterpret_cast<const uint2 *>(q);
-                            vc[y][0] = x.x, vc[y][1] = x.y;
-                        }
-                    }
-                    if (key0 + (u + 1) * kCodeBlock > keys || block0 + u >= j1) {  // slots behind the last key hold anything
+                                for (int d = 4; d < 32; d *= 2) {
+                                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+                                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, d));
+                                }
+                                if (x > m[nt][e] + 8.f) {
+                                    l[nt][e] *= sm100::ex2(m[nt][e] - x);
+                                    m[nt][e] = x;
+                                }
+                                if (y > ref[nt][e] + 8.f) {
+                                    const float f = sm100::ex2(ref[nt][e] - y);
+                                    ref[nt][e] = y;
 #pragma unroll
-                        for (int y = 0; y < 4; ++y)
-                            if (block0 + u >= j1 || key0 + u * kCodeBlock + 2 * t + (y & 1) + 8 * (y >> 1) >= keys) {
-#pragma unroll
-                                for (int i = 0; i < D / 32; ++i) vc[y][i] = 0;
+                                    for (int i = 0; i < kTiles; ++i) {
+                                        o[nt][i][e] *= f;
+                                        o[nt][i][e + 2] *= f;
+                                    }
+                                }
                             }
                     }
-                    // O^T: columns D / 8 g + 2 i (+ 1) of tile i
 #pragma unroll
-                    for (int i = 0; i < kTiles; ++i) {
-                        const uint32_t pick = i & 1 ? 0x7362u : 0x5140u;
-                        uint32_t a0, a1, a2, a3;
-                        decode4(__byte_perm(vc[0][i / 2], vc[1][i / 2], pick), a0, a1);
-                        decode4(__byte_perm(vc[2][i / 2], vc[3][i / 2], pick), a2, a3);
+                    for (int u = 0; u < kBl; ++u) {
+                        uint32_t pb[NT][2];  // P'^T as the product's second operand
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][i], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float p[4];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float nm = m[nt][e] == -INFINITY ? 0.f : m[nt][e];
+                                const float nr = ref[nt][e] == -INFINITY ? 0.f : evf[u] + 7.f - ref[nt][e];
+                                l[nt][e] += sm100::ex2(s[u][nt][e] - nm) + sm100::ex2(s[u][nt][e + 2] - nm);
+                                p[e] = sm100::ex2(s[u][nt][e] + nr);
+                                p[e + 2] = sm100::ex2(s[u][nt][e + 2] + nr);
+                            }
+                            pb[nt][0] = transpose8(half2_of(p[0], p[1]));
+                            pb[nt][1] = transpose8(half2_of(p[2], p[3]));
+                        }
+                        uint32_t vc[4][D / 32];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const int key = 2 * t + (y & 1) + 8 * (y >> 1);
+                            const unsigned char *q = src + u * Sh::kBlockBytes + kCodeBlock * D +
+                                                     (D == 128 ? word(key, g) : word(key, g >> 1) + (g & 1) * 8);
+                            if constexpr (D == 128) {
+                                const uint4 x = *reinterpret_cast<const uint4 *>(q);
+                                vc[y][0] = x.x, vc[y][1] = x.y, vc[y][2] = x.z, vc[y][3] = x.w;
+                            } else {
+                                const uint2 x = *reinterpret_cast<const uint2 *>(q);
+                                vc[y][0] = x.x, vc[y][1] = x.y;
+                            }
+                        }
+                        if (key0 + (u + 1) * kCodeBlock > keys || block0 + u >= j1) {  // slots behind the last key hold anything
+#pragma unroll
+                            for (int y = 0; y < 4; ++y)
+                                if (block0 + u >= j1 || key0 + u * kCodeBlock + 2 * t + (y & 1) + 8 * (y >> 1) >= keys) {
+#pragma unroll
+                                    for (int i = 0; i < D / 32; ++i) vc[y][i] = 0;
+                                }
+                        }
+                        // O^T: columns D / 8 g + 2 i (+ 1) of tile i
+#pragma unroll
+                        for (int i = 0; i < kTiles; ++i) {
+                            const uint32_t pick = i & 1 ? 0x7362u : 0x5140u;
+                            uint32_t a0, a1, a2, a3;
+                            decode4(__byte_perm(vc[0][i / 2], vc[1][i / 2], pick), a0, a1);
+                            decode4(__byte_perm(vc[2][i / 2], vc[3][i / 2], pick), a2, a3);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][i], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                        }
                     }
-                }
-                __syncwarp();  // all have read the stage
-                issue(it + kS, cur);
-                if (it % kBatch == kBatch - 1) {
-                    blk = blk_next;
-                    exps = exps_next;
+                    __syncwarp();  // all have read the stage
+                    issue(it + kS, cur);
+                    if (it % kBatch == kBatch - 1) {
+                        blk = blk_next;
+                        exps = exps_next;
+                    }
                 }
             }
         }
@@ -623,6 +652,7 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
         const bool final = j0 == 0 && j1 == nb;
         const int slot = 2 * blockIdx.x + (j0 == 0 ? 1 : 0);
         const float *all = reinterpret_cast<const float *>(smem);
+        bool nan = false;
         for (int i = tid; i < hw * R * (D / 4); i += kRowThreads) {
             const int hr = i / (D / 4), col = i % (D / 4) * 4, hx = hr / R, row = hr - hx * R;  // head of the group, row
             float top = -INFINITY;
@@ -642,6 +672,8 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
             }
             const float f = sum == 0.f ? 0.f : 1.f / sum, z2 = sum == 0.f ? -INFINITY : top + log2f(sum);
             v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+            const float any = (v.x + v.y) + (v.z + v.w);
+            nan |= any != any;
             if (final) {
                 const int tok = row / a.G;
                 const long long orow = (long long)(n0 + tok) * a.Hq + (w.h * hw + hx) * a.G + (row - tok * a.G);
@@ -652,8 +684,35 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
                 if (col == 0) a.part_lse[(slot * hw + hx) * Sh::kRows + row] = z2;
             }
         }
+        if (clean) {  // over what this thread has just stored
+#pragma unroll 1
+            for (int i = tid; i < hw * R * (D / 4); i += kRowThreads) {
+                const int hr = i / (D / 4), col = i % (D / 4) * 4, hx = hr / R, row = hr - hx * R, tok = row / a.G;
+                const int last = min(TREE ? keys : ctx + tok + 1, j1 * kCodeBlock);
+                uint32_t at = 0;
+#pragma unroll 1
+                for (int key = max(open, j0 * kCodeBlock) & -kCodeBlock; key < last; ++key) {  // (from the first block that was changed)
+                    if (TREE && key >= ctx && !(s_anc[tok] >> (key - ctx) & 1u)) continue;
+                    const int id = table[key >> a.c.page_log2];
+                    if (id < 0 || id >= a.c.n_pages) continue;  // (the request is rejected)
+                    const long long slot = ((long long)id << a.c.page_log2) + (key & ((1 << a.c.page_log2) - 1));
+                    at |= nan_codes(*reinterpret_cast<const uint32_t *>(a.c.v + (slot * a.Hkv + w.h * hw + hx) * D + col));
+                }
+                const long long orow = (long long)(n0 + tok) * a.Hq + (w.h * hw + hx) * a.G + (row - tok * a.G);
+#pragma unroll 1
+                for (int e = 0; e < 4; ++e, at >>= 8)
+                    if (at & 0x80u) {
+                        if (final) a.out[orow * D + col + e] = 0x7fff;
+                        else a.part_o[((long long)(slot * hw + hx) * Sh::kRows + row) * D + col + e] = NAN;
+                    }
+            }
+        }
         sm100::fence_async_smem();  // the ring is copied to again
-        __syncthreads();
+        if (__syncthreads_or(nan && !clean && open < keys && j1 * kCodeBlock > open)) {
+            clean = true;
+            continue;
+        }
+        clean = false;
         if (tid == 0) {
             const long long piece = (long long)b * groups + w.h + blockIdx.x;
             a.flag[piece] = (unsigned char)s_flag;

@@ -37,6 +37,8 @@ rs_status coded_launch_d(const FlashArgs &a, const CUtensorMap &tmq, const CUten
     RS_CHECK_LAUNCH(what);
     launch_full(flash_combine<D, BF16>, dim3(std::max(a.grid - 1, 1), a.comb_blocks), dim3(kFlCombThreads), 0, st, a);
     RS_CHECK_LAUNCH(what);
+    launch_pdl(coded_nan<D>, dim3(32), dim3(kNanThreads), 0, st, a);
+    RS_CHECK_LAUNCH(what);
     return RS_OK;
 }
 

@@ -1,7 +1,8 @@
 // flash.cu -- rs_prompt_attn and rs_paged_attn (and rs_coded_attn's long chunks): the
 // plan of the work and the host side of the attention core (flash.cuh).
 // Launches: flash_plan (one CTA, and one per request for draft trees) ->
-// flash_kernel (a CTA per SM) -> flash_combine.
+// flash_kernel (a CTA per SM) -> flash_combine; over a cache in 8 bits coded_core
+// in the place of flash_kernel, and coded_nan at the end.
 #include <cudaTypedefs.h>
 #include <math.h>
 
@@ -175,6 +176,7 @@ flash_plan(FlashArgs a, const int32_t *parents, uint32_t *anc, double kv_bytes, 
         const double used = (double)keys * kv_bytes;
         while (phases < a.max_phases && used > 1.5 * l2 && used > 0.5 * l2 * phases && tiles * a.Hkv / (a.grid * 2 * phases) >= 200) phases *= 2;
         a.n_pairs[2] = phases;
+        a.n_pairs[3] = 0;
     }
 }
 
@@ -209,7 +211,7 @@ Work carve(void *base, int B, int T, int Hq, int Hkv, int D, bool trees) {
     a.cum = cv.take<long long>(pairs + 1);
     a.ent = cv.take<int4>(pairs);
     a.ent_ctx = cv.take<int>(pairs);
-    a.n_pairs = cv.take<int>(3);
+    a.n_pairs = cv.take<int>(4);
     a.bound = cv.take<int4>(F * (grid + 1));
     if (trees) w.anc = cv.take<uint32_t>((size_t)T * kAncWords);
     a.part_m = cv.take<float>(2 * grid * F * kFlRows);

@@ -86,7 +86,7 @@ struct FlashArgs {
     long long *cum;              // [pairs + 1] cost prefix of the pairs of one KV head
     int4 *ent;                   // [pairs] request, pair, first row and rows of the request
     int *ent_ctx;                // [pairs] its ctx
-    int *n_pairs;                // pairs, cost of a segment's start, phases (the plan's choices)
+    int *n_pairs;                // pairs, cost of a segment's start, phases (the plan's choices); 1 where coded_nan has to run
     int4 *bound;                 // [phase][CTA] where the CTA's share starts: (head in phase, pair, tile)
     float *part_o, *part_m, *part_l;
     int max_phases, grid;

@@ -5,7 +5,7 @@ import random
 import pytest
 import torch
 
-from paged_ref import slots
+from paged_ref import causal_mask, slots, tree_mask
 from test_gpu_coded import Pool, attend, check_attention, fill, i32, rows
 
 pytestmark = pytest.mark.gpu
@@ -169,3 +169,62 @@ def test_many_short_requests(rs, B, most, ctx_lo, ctx_hi, Hq, Hkv, D, tree, dt):
     got = attend(rs, pool, q, off, ctx, most, D ** -0.5, parents)
     check_attention(pool, q, off, ctx, D ** -0.5, got, parents)
     assert (got[0][-1:] == 7).all() and (got[1][-1:] == 7).all()
+
+
+def seen_keys(ctx, n, parents=None):
+    see = causal_mask(n, ctx)
+    return see if parents is None else torch.cat([torch.ones(n, ctx, dtype=torch.bool), tree_mask(parents)], 1)
+
+
+# (Hq, Hkv, D, page, ctx, ns): few rows with heads apart (caches of 100 tokens and more) and side by side (shorter ones, and many
+# heads), one, two and four tiles of eight rows; and many rows, of one and two row tiles, of trees over three runs of 128 slots
+@pytest.mark.parametrize("Hq,Hkv,D,page,ctx,ns,dt", [
+    (1, 1, 64, 16, [12], [8], torch.float16), (4, 4, 128, 16, [12, 30], [8, 7], torch.bfloat16), (2, 2, 64, 32, [300, 0, 1000], [5, 8, 2], torch.bfloat16),
+    (8, 2, 128, 64, [140, 5], [4, 3], torch.float16), (4, 2, 64, 16, [15, 47], [16, 9], torch.float16), (8, 2, 128, 16, [250, 3], [8, 8], torch.bfloat16),
+    (1, 1, 128, 32, [7, 100, 2000], [32, 20, 31], torch.float16), (2, 1, 64, 16, [14], [16], torch.bfloat16),
+    (4, 4, 64, 16, [60, 129], [200, 65], torch.float16), (8, 2, 128, 64, [100, 5000], [256, 33], torch.bfloat16), (2, 2, 128, 32, [64], [256], torch.float16),
+    (8, 2, 64, 128, [20000], [250], torch.bfloat16), (3, 1, 64, 32, [0, 500], [256, 90], torch.bfloat16)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_nan_in_new_tokens_reaches_the_rows_that_see_it(rs, Hq, Hkv, D, page, ctx, ns, dt, tree):
+    """NaN in V of some of the new tokens and of the last cached one, in columns of their own: there the rows that see the token,
+    nothing else of any row."""
+    off = [0]
+    for x in ns:
+        off.append(off[-1] + x)
+    lens = [c + x for c, x in zip(ctx, ns)]
+    pool = Pool(lens, page, Hkv, D, 5)
+    fill(rs, pool, lens, dt, 21)
+    q = rows(off[-1], Hq, D, dt, 23)
+    g = random.Random(7)
+    # (node 3 begins a branch that the root's other children do not see)
+    tops = [[-1 if i == 0 else 0 if i < 6 else g.randrange(i) for i in range(x)] for x in ns]
+    parents = i32([p for t in tops for p in t]) if tree else None
+    want = attend(rs, pool, q, off, ctx, max(ns), 0.11, parents)
+    check_attention(pool, q, off, ctx, 0.11, want, parents)
+    nans = torch.zeros(off[-1], Hq, D, dtype=torch.bool)
+    for b, n in enumerate(ns):
+        see = seen_keys(ctx[b], n, tops[b] if tree else None)
+        at = slots(pool.table, b, lens[b], page)
+        for node, h, col, code in ((n - 1, 0, 3, 0x7f), (n // 2, Hkv - 1, D - 1, 0xff), (min(3, n - 1), 0, D // 2 + 1, 0x7f), (n - 1, Hkv - 1, 40, 0xff)):
+            pool.v.view(-1, Hkv, D)[at[ctx[b] + node], h, col] = code
+            nans[off[b]:off[b + 1], h * Hq // Hkv:(h + 1) * Hq // Hkv, col] |= see[:, ctx[b] + node, None]
+        if ctx[b]:  # the last cached token is for all rows
+            pool.v.view(-1, Hkv, D)[at[ctx[b] - 1], 0, 20] = 0x7f
+            nans[off[b]:off[b + 1], :Hq // Hkv, 20] = True
+    got = attend(rs, pool, q, off, ctx, max(ns), 0.11, parents)
+    nans = nans.cuda()
+    assert got[2].tolist() == [0] * len(ns) and torch.equal(got[1], want[1])
+    assert torch.equal(got[0].isnan(), nans), (got[0].isnan() != nans).nonzero()[:5]
+    assert torch.equal(got[0][~nans], want[0][~nans])
+    # NaN in K: whole rows
+    fill(rs, pool, lens, dt, 21)
+    whole = torch.zeros(off[-1], Hq, dtype=torch.bool)
+    for b, n in enumerate(ns):
+        at = slots(pool.table, b, lens[b], page)
+        for node in (n - 1, min(3, n - 1)):
+            pool.k.view(-1, Hkv, D)[at[ctx[b] + node], Hkv - 1, 9] = 0x7f
+            whole[off[b]:off[b + 1], (Hkv - 1) * Hq // Hkv:] |= seen_keys(ctx[b], n, tops[b] if tree else None)[:, ctx[b] + node, None]
+    got = attend(rs, pool, q, off, ctx, max(ns), 0.11, parents)
+    whole = whole.cuda()
+    assert got[2].tolist() == [0] * len(ns) and torch.equal(got[1].isnan(), whole) and got[0][whole].isnan().all()
+    assert torch.equal(got[0][~whole], want[0][~whole]) and torch.equal(got[1][~whole], want[1][~whole])
