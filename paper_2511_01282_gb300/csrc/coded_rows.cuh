@@ -634,15 +634,18 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
                 x += __shfl_xor_sync(0xffffffffu, x, 8);
                 x += __shfl_xor_sync(0xffffffffu, x, 16);
                 const int row = nt * 8 + 2 * t + e;
-                // l >= 1 where there is a weight (the one that set m): the quotient stays finite
-                const float f = x == 0.f ? 0.f : sm100::ex2(ref[nt][e] - 7.f - m[nt][e]) / x;
+                // l >= 1 where there is a weight (the one that set m): the quotient stays finite.  Where V's exponents are
+                // the smallest, the power is below fp32's normal numbers: 2^64 of it then goes to the product
+                const float up = ref[nt][e] - 7.f - m[nt][e];
+                const bool small = up < -60.f;
+                const float f = x == 0.f ? 0.f : sm100::ex2(small ? up + 64.f : up) / x, f2 = small ? 0x1p-64f : 1.f;
                 if (g == 0) s_lse[warp * Sh::kRows + row] = x == 0.f ? -INFINITY : m[nt][e] + log2f(x);
                 float *dst = s_o + row * Sh::kRowStride + D / 8 * g;
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i) {
                     // 0 x NaN of a row without weights
                     *reinterpret_cast<float2 *>(dst + 2 * i) =
-                        x == 0.f ? make_float2(0.f, 0.f) : make_float2(o[nt][i][e] * f, o[nt][i][e + 2] * f);
+                        x == 0.f ? make_float2(0.f, 0.f) : make_float2(o[nt][i][e] * f * f2, o[nt][i][e + 2] * f * f2);
                 }
             }
         __shared__ int s_flag;

@@ -228,3 +228,40 @@ def test_nan_in_new_tokens_reaches_the_rows_that_see_it(rs, Hq, Hkv, D, page, ct
     whole = whole.cuda()
     assert got[2].tolist() == [0] * len(ns) and torch.equal(got[1].isnan(), whole) and got[0][whole].isnan().all()
     assert torch.equal(got[0][~whole], want[0][~whole]) and torch.equal(got[1][~whole], want[1][~whole])
+
+
+@pytest.mark.parametrize("n", [1, 8, 40])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lo,hi", [(-117, -105), (113, 120)])
+def test_the_smallest_and_largest_values(rs, n, D, lo, hi):
+    dt, Hkv = torch.bfloat16, 2
+    pool = Pool([400], 32, Hkv, D, 9)
+    fill(rs, pool, [400], dt, 41, 0.0)
+    g = torch.Generator().manual_seed(1)
+    pool.ve = torch.randint(lo, hi + 1, pool.ve.shape, generator=g).to(torch.int8).cuda()
+    pool.v &= 0xbf  # (codes of 2^8 at exponent 120 are above bf16)
+    q = rows(n, 2 * Hkv, D, dt, 43) * 3
+    got = attend(rs, pool, q, [0, n], [400 - n], n, 0.125)
+    check_attention(pool, q, [0, n], [400 - n], 0.125, got)
+
+
+@pytest.mark.parametrize("n", [1, 8, 40])
+def test_the_smallest_values_behind_larger_ones(rs, n):
+    """Keys of weight 1 and values near 2^-105, 128 slots on some of weight 2^18.75 and values near 2^-117, others of no weight: the first
+    bound the products, the second the weights, and the quotient of the two bounds is below fp32's normal numbers."""
+    dt, D, page, N = torch.bfloat16, 64, 16, 400
+    pool = Pool([N], page, 1, D, 9)
+    fill(rs, pool, [N], dt, 41, 0.0)
+    at = slots(pool.table, 0, N, page)
+    k, ve = pool.k.view(-1, 1, D), pool.ve.view(-1)
+    k[at] = 0
+    k[at[16:], 0, 0] = 0xe0  # -32
+    k[at[128:160], 0, 0] = 0x55  # 13
+    pool.ke.zero_()
+    ve[:] = -117
+    ve[at[0] // 16] = -105
+    q = torch.zeros(n, 2, D, dtype=dt, device="cuda")
+    q[..., 0] = 1.0
+    got = attend(rs, pool, q, [0, n], [N - n], n, 1.0)
+    check_attention(pool, q, [0, n], [N - n], 1.0, got)
+    assert (got[0] != 0).float().mean() > 0.9
