@@ -27,6 +27,10 @@ __device__ __forceinline__ int code_exp(int e, bool bf16) { return min(max(e, co
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+// Factors of scores: towards 0, so that a product above fp32's largest number becomes it and not infinity, of which a
+// score of 0 would be no number (with a minimum behind it the chunks took 450 us and not 438)
+__device__ __forceinline__ float finite_mul(float a, float b) { return __fmul_rz(a, b); }
+
 // four codes -> fp16, exact (NaN stays NaN): the low and the high two
 __device__ __forceinline__ void decode4(uint32_t four, uint32_t &lo, uint32_t &hi) {
     asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"

@@ -452,7 +452,7 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
         const int x = (warp - kFlSoftWarp) >> 2;
         const int r = tid & (kBM - 1);  // row of the tile == tensor memory lane
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-        const float cexp = a.scale * 1.4426950408889634f;  // scores -> log2 domain (scale > 0)
+        const float cexp = fminf(a.scale * 1.4426950408889634f, 3.402823466e38f);  // scores -> log2 domain (scale > 0)
         const int rt = r / G, rg = r - rt * G;
         const uint32_t s_tm = tmem + lane_off + Tm::s(0) + (uint32_t)x * 128;
         const uint32_t p_tm = tmem + lane_off + Tm::p(0) + (uint32_t)x * (kApart ? 64 : 128);
@@ -480,7 +480,7 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                 const int key0 = (pc.j0 + tl) * kBN;
                 if (!(ok = quick_wait(&sfull[x], done & 1, s_abort, a.wait_limit))) return false;
                 tc_fence_after();
-                if (BF16 && tl == first) rowf = cexp * pow2i(s_shift[x * kBM + r]);
+                if (BF16 && tl == first) rowf = finite_mul(cexp, pow2i(s_shift[x * kBM + r]));
                 // the piece's last S has read Q: its buffer is free
                 if (tl + step >= n) warp_arrive(&qfree[x]);
                 // P V of the last tile must be complete before P's columns (where they are
@@ -520,7 +520,7 @@ coded_core(FlashArgs a, const __grid_constant__ CUtensorMap tmq, const __grid_co
                 const uint4 *exps = reinterpret_cast<const uint4 *>(s_exp + (t % S::kExps) * 32);  // of four blocks each
                 auto word = [](const uint4 &e4, int b) { return b == 0 ? e4.x : b == 1 ? e4.y : b == 2 ? e4.z : e4.w; };
                 // (factors are not 0: hidden scores stay -inf)
-                auto factor = [&](const uint4 &e4, int b) { return fmaxf(rowf * __uint_as_float(word(e4, b) & 0xffff0000u), 0x1p-126f); };
+                auto factor = [&](const uint4 &e4, int b) { return fmaxf(finite_mul(rowf, __uint_as_float(word(e4, b) & 0xffff0000u)), 0x1p-126f); };
                 auto offset = [&](const uint4 &e4, int b) { return __uint_as_float(word(e4, b) << 16); };
                 auto load64 = [&](int hh, uint32_t (&va)[32], uint32_t (&vb)[32]) {
                     tmem_ld32(s_tm + hh * 64, va);

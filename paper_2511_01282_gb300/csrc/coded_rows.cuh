@@ -269,7 +269,7 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
     unsigned char *ring = smem + warp * kS * Sh::kStageBytes;
-    const float cexp = a.scale * 1.4426950408889634f;
+    const float cexp = fminf(a.scale * 1.4426950408889634f, 3.402823466e38f);
     const bool bf16 = a.bf16;
     const int head = warp % hw, kw = warp / hw, KW = kRowWarps / hw;  // head of the group; the warp's place among the head's
     uint32_t filled = 0, drained = 0;  // stages of this warp's ring, over all pieces
@@ -422,7 +422,7 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int row = nt * 8 + 2 * t + e, i = row / a.G;
-                factor[nt][e] = cexp * pow2i(__shfl_sync(0xffffffffu, shift, (2 * t + e) * 4));
+                factor[nt][e] = finite_mul(cexp, pow2i(__shfl_sync(0xffffffffu, shift, (2 * t + e) * 4)));
                 limit[nt][e] = row < R ? ctx + i + 1 : 0;
                 see[nt][e] = TREE ? __shfl_sync(0xffffffffu, anc, min(i, 31)) : 0;
                 if (row >= R) see[nt][e] = 0;
@@ -509,7 +509,7 @@ coded_rows(RowsArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_con
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[u][nt][e] = (NT < 4 ? s[u][nt][e] + s1[u][nt][e] : s[u][nt][e]) * (factor[nt][e & 1] * two_ek[u]);
+                            for (int e = 0; e < 4; ++e) s[u][nt][e] = (NT < 4 ? s[u][nt][e] + s1[u][nt][e] : s[u][nt][e]) * finite_mul(factor[nt][e & 1], two_ek[u]);
                             if (masked) {
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {

@@ -1,12 +1,14 @@
 """Attention over the cache in 8 bits where single calls of ordinary sizes do not go: caches so long that KV heads are read side by
 side, waits that run out, two calls at once, sizes that reject one of many requests."""
+import math
 import random
 
 import pytest
 import torch
 
+import coded_ref as cr
 from paged_ref import causal_mask, slots, tree_mask
-from test_gpu_coded import Pool, attend, check_attention, fill, i32, rows
+from test_gpu_coded import Pool, append, attend, check_attention, fill, i32, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -265,3 +267,26 @@ def test_the_smallest_values_behind_larger_ones(rs, n):
     got = attend(rs, pool, q, [0, n], [N - n], n, 1.0)
     check_attention(pool, q, [0, n], [N - n], 1.0, got)
     assert (got[0] != 0).float().mean() > 0.9
+
+
+@pytest.mark.parametrize("n", [1, 8, 40])
+def test_a_score_below_all_numbers_beside_zeros(rs, n):
+    """q.k of -2^240 at one key of a block and 0 at the others, whose factors are above fp32's largest number: equal weights on these."""
+    dt, D, page, N = torch.bfloat16, 64, 16, 200
+    pool = Pool([N], page, 1, D, 9)
+    v = rows(N, 1, D, dt, 42)
+    k = torch.zeros_like(v)
+    k[5, 0, 7] = -2.0 ** 120
+    assert append(rs, pool, k, v, [0, N], [0]) == [0]
+    q = torch.zeros(n, 2, D, dtype=dt, device="cuda")
+    q[..., 7] = 2.0 ** 120
+    out, lse, st = attend(rs, pool, q, [0, n], [N - n], n, 0.125)
+    assert st.tolist() == [0]
+    at = slots(pool.table, 0, N, page)
+    val = cr.values(pool.v, pool.ve).view(-1, D).cuda()[at]
+    for i in range(n):
+        on = torch.arange(N - n + i + 1) != 5
+        mean = val[:N - n + i + 1][on].mean(0)
+        tol = (2.0 ** -9 + 2.0 ** -10) * (mean.abs() + val.abs().mean(0) * 1.1)  # out's rounding, P's
+        assert ((out[i].double() - mean).abs() <= tol).all()
+        assert (lse[i] - math.log(N - n + i)).abs().max() <= 2.0 ** -18
