@@ -55,8 +55,8 @@ class Rotary:
 
     def __call__(self, q, k, pos, out=None, inverse=False):
         """q [T, Hq, D] and k [T, Hkv, D] (rows may be parts of wider ones; either may be None) at the positions pos [T] int32.
-        Returns (q, k) turned: new tensors, or those in `out`, which may be q and k themselves.  inverse: turned back, which is the
-        gradient."""
+        Returns (q, k) turned: new tensors, or those in `out`, which may be q and k themselves.  inverse: by the negative angles,
+        still times `scale`, which is the gradient.  Where q or k requires a gradient the results have theirs, and `out` is refused."""
         x = q if q is not None else k
         if x is None:
             raise ValueError("q or k expected")
@@ -79,9 +79,39 @@ class Rotary:
                     raise ValueError("%s: [%d, heads, %d] of %s expected, not %s of %s" % (name, T, self.D, x.dtype, list(y.shape), y.dtype))
             args += [t, _apart(t), o, _apart(o)]
             outs.append(o)
+        if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, *out)):
+            if any(o is not None for o in out):
+                raise ValueError("out: results with a gradient are new tensors")
+            return _Turned.apply(self, q, k, pos, inverse)
         heads = [0 if t is None else t.shape[1] for t in (q, k)]
         rs.rs_rotary(*args, _CODES[x.dtype], pos, T, *heads, self.D, self.rot, _LAYOUTS[self.layout], self.turns, self.scale, int(inverse))
         return tuple(outs)
+
+
+class _Turned(torch.autograd.Function):
+    """A linear map: its gradient is the same call with the opposite angles."""
+
+    @staticmethod
+    def forward(ctx, rotary, q, k, pos, inverse):
+        ctx.set_materialize_grads(False)
+        ctx.rotary, ctx.inverse = rotary, inverse
+        ctx.save_for_backward(pos)
+        out = rotary(q, k, pos, inverse=inverse)
+        ctx.mark_non_differentiable(*(o for o, needed in zip(out, ctx.needs_input_grad[1:3]) if o is not None and not needed))
+        return out
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        dq, dk = (_rows(g) if g is not None and needed else None for g, needed in zip((dq, dk), ctx.needs_input_grad[1:3]))
+        if dq is None and dk is None:
+            return None, None, None, None, None
+        return (None, *ctx.rotary(dq, dk, ctx.saved_tensors[0], inverse=not ctx.inverse), None, None)
+
+
+def _rows(x):
+    """x as the call takes it: a gradient may be broadcast or transposed."""
+    fits = x.stride(2) == 1 and x.stride(1) == x.shape[2] and _apart(x) >= x.shape[1] * x.shape[2] and _apart(x) % 8 == 0 and x.data_ptr() % 16 == 0
+    return x if fits else x.contiguous()
 
 
 def _apart(x):

@@ -128,3 +128,60 @@ def test_graphs_streams_and_no_rows():
     n = rs.rs_launch_count()
     r(q[:0], k[:0], pos[:0])
     assert rs.rs_launch_count() == n
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_gradients_reach_queries_and_keys(layout, dt, inverse):
+    """Through autograd: the bits of the call with the opposite angles, for parts of wider rows, broadcast and transposed gradients,
+    for one of the two alone, and twice."""
+    from paper_2511_01282_gb300 import rotary
+    D, rot, T = 64, 48, 11
+    r = rotary.Rotary(D, rot, layout, scale=0.75)
+    x = torch.cat(make(T, 3, 2, D, dt)[:2], 1).requires_grad_()
+    pos = make(T, 3, 2, D, dt)[2]
+    wq, wk, _ = make(T, 3, 2, D, dt, 2)
+    a, b = r(x[:, :3], x[:, 3:], pos, inverse=inverse)
+    with torch.no_grad():
+        c, d = r(x[:, :3], x[:, 3:], pos, inverse=inverse)
+        dq, dk = r(wq, wk, pos, inverse=not inverse)
+    assert a.requires_grad and b.requires_grad and not c.requires_grad and torch.equal(a, c) and torch.equal(b, d)
+    g, = torch.autograd.grad((a, b), x, (wq, wk), retain_graph=True)
+    assert torch.equal(g[:, :3], dq) and torch.equal(g[:, 3:], dk)
+    g, = torch.autograd.grad(b, x, wk, retain_graph=True)
+    assert (g[:, :3] == 0).all() and torch.equal(g[:, 3:], dk)
+    # of a sum (one value for all), and with heads and rows the other way round
+    g, = torch.autograd.grad(a.sum(), x, retain_graph=True)
+    with torch.no_grad():
+        assert torch.equal(g[:, :3], r(torch.ones_like(a), None, pos, inverse=not inverse)[0])
+    g, = torch.autograd.grad(a.transpose(0, 1), x, wq.transpose(0, 1).contiguous(), retain_graph=True)
+    assert torch.equal(g[:, :3], dq)
+    # keys alone need one; and the gradient of the gradient, which is linear in what came in
+    k = make(T, 3, 2, D, dt)[1].clone().requires_grad_()
+    q2, k2 = r(wq, k, pos, inverse=inverse)
+    assert k2.requires_grad and not q2.requires_grad
+    w = wk.clone().requires_grad_()
+    g, = torch.autograd.grad(k2, k, w, create_graph=True)
+    gg, = torch.autograd.grad(g, w, wk)
+    with torch.no_grad():
+        assert torch.equal(gg, r(None, wk, pos, inverse=inverse)[1])
+
+
+def test_gradients_of_one_side_stream_and_of_no_rows():
+    from paper_2511_01282_gb300 import rotary
+    q, k, pos = make(50, 4, 2, 128, torch.bfloat16)
+    r = rotary.Rotary(128)
+    want = r(q, None, pos, inverse=True)[0]
+    leaf = torch.zeros_like(q).requires_grad_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a, _ = r(leaf, None, pos)
+        a.backward(q)
+    side.synchronize()
+    assert torch.equal(leaf.grad, want)
+    none = q[:0].clone().requires_grad_()
+    a, _ = r(none, None, pos[:0])
+    a.sum().backward()
+    assert none.grad.shape == (0, 4, 128)

@@ -44,3 +44,12 @@ def test_refusals():
                                (x[..., :32], None, pos, None, "q:"), (x, None, pos, (x[:, :1], None), "q:")]:
         with pytest.raises(ValueError, match=word):
             r(q, k, p, out)
+
+
+def test_results_with_a_gradient_are_new_tensors():
+    r = rotary.Rotary(64, device="cpu")
+    x, pos = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    leaf = x.clone().requires_grad_()
+    for q, k, out in ((leaf, None, (x, None)), (x, leaf, (None, x)), (leaf, x, (leaf, x)), (x, x, (leaf, None))):
+        with pytest.raises(ValueError, match="out"):
+            r(q, k, pos, out)
