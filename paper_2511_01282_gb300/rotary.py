@@ -30,8 +30,8 @@ def frequencies(rot, base=10000.0, factor=1.0, trained=None, low=1.0, high=4.0):
 def turns(freq):
     """The table that the kernel takes: each frequency as a fraction of a turn, in units of 2^-64 (int64 words, on freq's device)."""
     f = freq.double().tolist()
-    if not all(math.isfinite(x) for x in f):
-        raise ValueError("freq: finite values expected")
+    if not all(abs(x) < 2.0 ** 96 for x in f):  # (for larger ones pi would need more digits)
+        raise ValueError("freq: values below 2^96 expected")
     # exact but for the last bit: a quotient in 64-bit floating point would be off by 2^-52, 2^-21 of a turn at position 2^31
     words = [round(Fraction(x) / (2 * _PI) * 2 ** 64) % 2 ** 64 for x in f]
     return torch.tensor([w - 2 ** 64 if w >= 2 ** 63 else w for w in words], dtype=torch.int64, device=freq.device)

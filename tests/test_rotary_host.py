@@ -53,3 +53,14 @@ def test_results_with_a_gradient_are_new_tensors():
     for q, k, out in ((leaf, None, (x, None)), (x, leaf, (None, x)), (leaf, x, (leaf, x)), (x, x, (leaf, None))):
         with pytest.raises(ValueError, match="out"):
             r(q, k, pos, out)
+
+
+def test_frequencies_whose_turns_the_digits_of_pi_do_not_give_are_refused():
+    # 2^95 / (2 pi) x 2^64 takes 157 of the table's 166 bits of pi; 10^40 rather more than it has
+    for f in (1e40, -1e40, 2.0 ** 96):
+        with pytest.raises(ValueError, match="2\\^96"):
+            rotary.turns(torch.tensor([1.0, f], dtype=torch.float64))
+    two_pi = 2 * rotary.Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803")
+    for f in (2.0 ** 95, -2.0 ** 95 * 1.75):
+        want = round(rotary.Fraction(f) / two_pi * 2 ** 64) % 2 ** 64
+        assert rotary.turns(torch.tensor([f], dtype=torch.float64)).item() % 2 ** 64 == want
