@@ -290,3 +290,50 @@ def test_a_score_below_all_numbers_beside_zeros(rs, n):
         tol = (2.0 ** -9 + 2.0 ** -10) * (mean.abs() + val.abs().mean(0) * 1.1)  # out's rounding, P's
         assert ((out[i].double() - mean).abs() <= tol).all()
         assert (lse[i] - math.log(N - n + i)).abs().max() <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("n", [1, 300])
+def test_a_wait_that_has_run_out_is_in_the_status(rs, n, monkeypatch):
+    """With a limit of one cycle some wait does run out (of single tokens most calls have one, of chunks every request), and says so;
+    a request that says nothing has all of its results."""
+    dt, D, Hkv, B = torch.bfloat16, 128, 8, 8
+    lens = [20000 + n] * B
+    pool = Pool(lens, 64, Hkv, D, 6)
+    fill(rs, pool, lens, dt, 71)
+    ctx, off = [20000] * B, [i * n for i in range(B + 1)]
+    q = rows(B * n, 32, D, dt, 73)
+    want = attend(rs, pool, q, off, ctx, n, 0.09)
+    assert want[2].tolist() == [0] * B
+    monkeypatch.setenv("RS_DEBUG_WAIT_LIMIT", "1")
+    told = 0
+    for _ in range(20):
+        out, lse, status = attend(rs, pool, q, off, ctx, n, 0.09)
+        status = status.tolist()
+        assert set(status) <= {0, rs.RS_ST_TIMEOUT}
+        told += sum(s != 0 for s in status)
+        for b, s in enumerate(status):
+            a = slice(off[b], off[b + 1])
+            assert s or (torch.equal(out[a], want[0][a]) and torch.equal(lse[a], want[1][a]))
+        if told:
+            break
+    assert told
+    monkeypatch.delenv("RS_DEBUG_WAIT_LIMIT")
+    again = attend(rs, pool, q, off, ctx, n, 0.09)
+    assert all(torch.equal(a, b) for a, b in zip(want, again))
+
+
+@pytest.mark.parametrize("n", [1, 8, 40])
+def test_rejected_ranges_leave_all_rows_but_the_others(rs, n):
+    dt, D, Hkv = torch.bfloat16, 64, 2
+    lens = [100] * 4
+    pool = Pool(lens, 16, Hkv, D, 6)
+    fill(rs, pool, lens, dt, 71)
+    ctx, q = [100 - n] * 4, rows(4 * n, 4, D, dt, 73)
+    for off, bad in (([0, n, 4 * n + 1, 4 * n + 1, 4 * n + 1], [1, 2, 3]), ([n, 2 * n, n, 2 * n, 3 * n], [1, 2]), ([-1, n, 2 * n, 2 * n, 3 * n], [0])):
+        got = attend(rs, pool, q, off, ctx, n, 0.125)
+        assert [s == rs.RS_ST_BAD_OFFSET for s in got[2].tolist()] == [b in bad for b in range(4)]
+        check_attention(pool, q, off, ctx, 0.125, got, skip=bad)
+        mine = torch.zeros(4 * n, dtype=torch.bool, device="cuda")
+        for b in set(range(4)) - set(bad):
+            mine[off[b]:off[b + 1]] = True
+        assert (got[0][~mine] == 7).all() and (got[1][~mine] == 7).all() and not mine.all()
