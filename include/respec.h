@@ -619,8 +619,9 @@ rs_status rs_coded_append(const uint16_t *k, int64_t k_stride, const uint16_t *v
  *            work is laid out by it.  A request that has more is rejected with
  *            RS_ST_TOO_LARGE.  T where nothing better is known.
  *   the rest as for rs_paged_attn.  Size the workspace with the same six sizes.
- * P is rounded to fp16 (2^-12 relative; weights times 2^exponent of V below 2^-32
- * of a row's largest may vanish); bf16 queries are taken as fp16, times a power of
+ * P is rounded to fp16: weights times 2^exponent of V by up to 2^-11 relative where
+ * they are 2^-21 of a row's largest or more, by up to 2^-32 of the largest below that
+ * (those below 2^-32 may vanish); bf16 queries are taken as fp16, times a power of
  * two (elements below 2^-39 of a row's largest may vanish).  NaN in K or V of a key
  * reaches the rows that see the key (of V, in its column), and no others.  What slots
  * behind a request's last token hold does not matter.  The result does not depend on

@@ -7,8 +7,8 @@
 //     S_rj = q_r.K_j,  s_rj = c 2^(ek) S_rj,  P'_rj = 2^(s_rj + ev - R_r + 7),
 //     O'_r = sum P'_rj V_j,  l_r = sum 2^(s_rj - m_r) = sum_blocks 2^(R_r - 7 - ev - m_r) sum P'_rj
 // with m_r and R_r running bounds of s and of s + ev, moved only when they are exceeded
-// by 2^8 (P' <= 2^15 in fp16, weights times 2^ev down to 2^-32 of the largest stay above
-// its subnormals).  Where ev is so far below R - m that P' would vanish in fp32 while the
+// by 2^8 (the largest P' is 2^7 to 2^15 in fp16: weights times 2^ev are rounded by up to 2^-11 down to
+// 2^-21 of the largest, by up to 2^-32 of the largest below that).  Where ev is so far below R - m that P' would vanish in fp32 while the
 // weight counts, l is summed from its own exponentials.  bf16 queries are scaled by a
 // power of two per row into fp16 (what lies 2^-39 below a row's largest is lost).  The
 // converting warps are the scarcer: with code 2^e in bf16 tiles (five instructions for two
@@ -31,11 +31,11 @@
 // what is on its way (4.2 us a key tile).  K and V tiles share one ring, K a tile ahead:
 // K0 K1 V0 K2 V1 ... V(n-1).
 //
-// Measured: four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 310 us, 4.3 TB/s (the
-// cache in 16 bits takes 403), near what shared memory passes: 224 KB a key tile (products 96, tiles
+// Measured (replayed in a graph): four trees of 65 nodes over 32768 keys (40 heads of 128, bf16) 308 us, 4.4 TB/s
+// (the cache in 16 bits takes 414), near what shared memory passes: 224 KB a key tile (products 96, tiles
 // written 64, codes written and read 64) in 2200 cycles; 200 to 1000 new tokens behind 4000 to
-// 32000 (four requests, 32 / 8 heads of 64, fp16) 440 us, bound by the softmax warps, which share
-// their schedulers with the converting ones (in 16 bits 378 us).
+// 32000 (four requests, 32 / 8 heads of 64, fp16) 438 us, bound by the softmax warps, which share
+// their schedulers with the converting ones (in 16 bits 375 us).
 #pragma once
 
 #include "coded.cuh"
@@ -854,6 +854,7 @@ coded_nan(FlashArgs a) {
         for (long long w = w0; w < (long long)rq.y * a.Hkv; w += warps) {
             const int i = (int)(w / a.Hkv), h = (int)(w - (long long)i * a.Hkv), key = rq.z + i;
             const long long id = a.page_table[(long long)b * a.max_pages + (key >> a.page_log2)];
+            if (id < 0 || id >= a.n_pages) continue;
             const long long slot = (id << a.page_log2) + (key & ((1 << a.page_log2) - 1));
             const uint32_t at = lane < D / 4 ? nan_codes(reinterpret_cast<const uint32_t *>(a.coded.v + (slot * a.Hkv + h) * D)[lane]) : 0;
             if (!__any_sync(0xffffffffu, at)) continue;

@@ -12,8 +12,9 @@
 // of keys are two bytes of two words).  Codes are exact in fp16; the exponents go
 // where they cost nothing: ek into the scores' factor, ev into the exponent of
 //     P'_rj = 2^(s_rj + ev - R_r + 7),   O'_r = sum P'_rj V_j,
-// with R_r a running bound of s + ev (P' <= 2^15 in fp16, 2^-12 relative; weights
-// down to 2^-32 of the largest stay above its subnormals).  l_r = sum 2^(s - m_r) has
+// with R_r a running bound of s + ev (the largest P' is 2^7 to 2^15 in fp16: weights times
+// 2^ev are rounded by up to 2^-11 down to 2^-21 of the largest, by up to 2^-32 of the
+// largest below that).  l_r = sum 2^(s - m_r) has
 // its own bound m_r, so that it does not depend on the values' sizes.  Both move
 // only when they would be exceeded by 2^8.  bf16 queries are scaled by a power of two
 // per row, so that fp16 holds them (what lies 2^-39 below a row's largest is lost).
@@ -33,8 +34,8 @@
 // results hold NaN is done again without (a check for each block takes 3 to 7 % of short caches' calls).
 //
 // Bound: HBM, of 2 D bytes a key and KV head.  Measured: single tokens of 64 requests behind 1024 to 8191
-// keys, 32 / 8 heads of 128, 605 MB, 111-114 us, 5.4 TB/s (107 with the copies alone; 188 from a cache in 16
-// bits); of one request behind 2048 keys 13.5 us, two launches and their chains of reads.  K and V in rings of
+// keys, 32 / 8 heads of 128, 605 MB, 111-114 us, 5.4 TB/s (107 with the copies alone; 183 from a cache in 16
+// bits); of one request behind 2048 keys 13.7 us, two launches and their chains of reads.  K and V in rings of
 // their own, K refilled as soon as it is in registers, took 119.
 #pragma once
 

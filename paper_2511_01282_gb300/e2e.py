@@ -30,7 +30,9 @@ attention weights to the keys they see (``rs_paged_weights``) and a cache
 that has outgrown the budget is cut back to it (``rs_paged_evict``).  With
 ``bits=8`` the pages hold 8 bits a value (``rs_coded_append``,
 ``rs_coded_attn``); the tokens are then those of the rounded cache, not
-exactly the target's.
+exactly the target's, and may depend on the draft model too: a draft token's
+large value raises the exponent of the 16 slots that it shares with accepted
+ones, and they keep it when it is rejected.
 
 With ``rotary=True`` queries and keys are turned by their positions
 (``rs_rotary``) before the cache takes them; a tree's node lies at the prefix's

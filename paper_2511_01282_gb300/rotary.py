@@ -28,7 +28,8 @@ def frequencies(rot, base=10000.0, factor=1.0, trained=None, low=1.0, high=4.0):
 
 
 def turns(freq):
-    """The table that the kernel takes: each frequency as a fraction of a turn, in units of 2^-64 (int64 words, on freq's device)."""
+    """The table that the kernel takes: each frequency as a fraction of a turn, in units of 2^-64 (int64 words, on freq's device).
+    Made on the host, once per model (64 frequencies 0.8 ms, and a wait for those on a device)."""
     f = freq.double().tolist()
     if not all(abs(x) < 2.0 ** 96 for x in f):  # (for larger ones pi would need more digits)
         raise ValueError("freq: values below 2^96 expected")
