@@ -262,5 +262,6 @@ class PagedCache:
         _need(self.weights is not None, "a cache made with track_weights=True expected")
 
     def _set(self, lengths, seen):
-        self.lengths, self.seen = list(lengths), list(seen)
-        self._counts.copy_(torch.tensor([self.lengths, self.seen], dtype=torch.int32))
+        lengths, seen = list(lengths), list(seen)
+        self._counts.copy_(torch.tensor([lengths, seen], dtype=torch.int32))
+        self.lengths, self.seen = lengths, seen

@@ -5,6 +5,8 @@ branches of one answer), ``free`` and ``trim`` give pages back, ``resize`` close
 pages are used is kept on the host; the arrays are moved on the device (``rs_pages_copy``, ``rs_pages_compact``).  None of the five
 may be captured into a CUDA graph, and graphs of the other calls hold on to the arrays that ``resize`` replaces.
 """
+from itertools import islice
+
 import torch
 
 from . import respec as rs
@@ -41,11 +43,15 @@ class SharedCache(PagedCache):
     def _place(self, b):
         _need(0 <= b < self.B, "request %d: there are %d" % (b, self.B))
 
-    def _take(self, n):
-        out = [self._free.pop() for _ in range(n)]
-        for p in out:
+    def _take(self, pages):
+        """pages: the first that _spare has given."""
+        del self._free[len(self._free) - len(pages):]
+        for p in pages:
             self.refs[p] = 1
-        return out
+
+    def _spare(self):
+        """The free pages in the order in which they are given out."""
+        return reversed(self._free)
 
     def _give(self, pages):
         for p in pages:
@@ -53,12 +59,19 @@ class SharedCache(PagedCache):
             if self.refs[p] == 0:
                 self._free.append(p)
 
-    def _enter(self, changes):
-        """changes: (request, first entry, pages) of the table, in one copy."""
+    # A call makes ready on the device all that it needs before it changes anything: one that fails leaves the cache as it was.
+    def _entries(self, changes):
+        """changes: (request, first entry, pages) of the table, as _enter takes them; in one copy."""
         at = [b * self.max_pages + first + i for b, first, pages in changes for i in range(len(pages))]
-        if at:
-            both = torch.tensor([at, [p for _, _, pages in changes for p in pages]], dtype=torch.int64).to(self.device)
-            self.table.view(-1)[both[0]] = both[1].int()
+        if not at:
+            return None
+        both = torch.tensor([at, [p for _, _, pages in changes for p in pages]], dtype=torch.int64).to(self.device)
+        return both[0], both[1].int()
+
+    def _enter(self, entries):
+        if entries:
+            at, pages = entries
+            self.table.view(-1)[at] = pages
 
     def reserve(self, counts):
         """Pages for counts[b] tokens behind request b's cached ones.  Raises, and takes none, where the pool has too few."""
@@ -67,12 +80,12 @@ class SharedCache(PagedCache):
         more = [max(0, -(-(n + c) // self.page_size) - len(h)) if c else 0 for n, c, h in zip(self.lengths, counts, self.held)]
         if sum(more) > len(self._free):
             raise MemoryError("%d pages needed, %d of %d free" % (sum(more), len(self._free), self.n_pages))
-        changes = []
-        for b, n in enumerate(more):
-            if n:
-                changes.append((b, len(self.held[b]), self._take(n)))
-                self.held[b] += changes[-1][2]
-        self._enter(changes)
+        spare = self._spare()
+        changes = [(b, len(self.held[b]), list(islice(spare, n))) for b, n in enumerate(more) if n]
+        self._enter(self._entries(changes))
+        for b, _, own in changes:
+            self._take(own)
+            self.held[b] += own
 
     def fork(self, src, dsts, n=None):
         """Requests dsts, which hold nothing, go on from the first n of request src's cached tokens (None: all of them)."""
@@ -88,32 +101,37 @@ class SharedCache(PagedCache):
         whole = 0 if self.weights is not None else n // self.page_size
         if len(dsts) * (used - whole) > len(self._free):
             raise MemoryError("%d pages needed, %d of %d free" % (len(dsts) * (used - whole), len(self._free), self.n_pages))
-        pairs, changes = [], []
-        for b in dsts:
-            own = self._take(used - whole)
-            pairs += zip(self.held[src][whole:used], own)
-            for p in self.held[src][:whole]:
-                self.refs[p] += 1
-            self.held[b] = self.held[src][:whole] + own
-            changes.append((b, 0, self.held[b]))
+        spare = self._spare()
+        own = [list(islice(spare, used - whole)) for _ in dsts]
+        held = [self.held[src][:whole] + o for o in own]
+        pairs = [pr for o in own for pr in zip(self.held[src][whole:used], o)]
+        entries = self._entries([(b, 0, h) for b, h in zip(dsts, held)])
         if pairs:
             status = torch.empty(1, dtype=torch.int32, device=self.device)
             rs.rs_pages_copy(*self._moved(), torch.tensor(pairs, dtype=torch.int32, device=self.device), len(pairs), status)
             self.report(status)
-        self._enter(changes)
         lengths, seen = list(self.lengths), list(self.seen)
         for b in dsts:
             lengths[b], seen[b] = n, seen[src] - lengths[src] + n
         self._set(lengths, seen)
+        self._enter(entries)
+        for b, h, o in zip(dsts, held, own):
+            self._take(o)
+            for p in h[:whole]:
+                self.refs[p] += 1
+            self.held[b] = h
 
     def _moved(self):
         return (*self._arrays(), self.weights, self.positions, self.bits, self.Hkv, self.D, self.n_pages, self.page_size)
 
-    def _cut(self, b, pages):
+    def _cut(self, b, pages, counts=None):
         gone = self.held[b][pages:]
+        entries = self._entries([(b, pages, [-1] * len(gone))])
+        if counts is not None:
+            self._set(*counts)
+        self._enter(entries)
         self.held[b] = self.held[b][:pages]
         self._give(gone)
-        self._enter([(b, pages, [-1] * len(gone))])
 
     def trim(self, b):
         """Request b's pages behind its cached tokens go back to the pool."""
@@ -123,10 +141,9 @@ class SharedCache(PagedCache):
     def free(self, b):
         """Request b ends: its place holds nothing."""
         self._place(b)
-        self._cut(b, 0)
         lengths, seen = list(self.lengths), list(self.seen)
         lengths[b] = seen[b] = 0
-        self._set(lengths, seen)
+        self._cut(b, 0, (lengths, seen))
 
     def compact(self):
         """The used pages come to lie in front, one behind the other.  Returns their number; waits for the device (a pool of 16384 pages
@@ -164,9 +181,10 @@ class SharedCache(PagedCache):
             out.narrow(dim, 0, used).copy_(x.narrow(dim, 0, used))
             return out
 
-        self.k, self.v, self.k_exps, self.v_exps = (sized(x, 0, pages, used) for x in self._arrays())
         slots = self.page_size
-        self.weights, self.positions = (sized(x, 1, pages * slots, used * slots) for x in (self.weights, self.positions))
+        arrays = [sized(x, 0, pages, used) for x in self._arrays()]
+        arrays += [sized(x, 1, pages * slots, used * slots) for x in (self.weights, self.positions)]
+        self.k, self.v, self.k_exps, self.v_exps, self.weights, self.positions = arrays
         self.n_pages = self._size = pages
         self.refs = self.refs[:used] + [0] * (pages - used)
         self._free = list(range(pages - 1, used - 1, -1))

@@ -293,3 +293,59 @@ def test_a_trees_positions_are_its_depths():
         for i, p in enumerate(parents):
             depth[i] = depth[p] + 1 if p >= 0 else 0
         assert m._positions(1000, torch.tensor(parents, dtype=torch.int32)).tolist() == [1000 + d for d in depth]
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(track_weights=True), dict(bits=8)])
+@pytest.mark.parametrize("call", ["reserve", "fork", "trim", "free", "compact", "shrink", "grow", "advance"])
+def test_a_call_that_fails_on_the_way_changes_nothing(kw, call, monkeypatch):
+    """Whatever it makes of memory in turn, or the library's call, fails: lists, table, lengths and arrays stay as they were.  (A pool that
+    could not be made smaller or larger may be closed up.)"""
+    tokens = {0: list(range(37)), 1: list(range(100, 120))}
+
+    def made():
+        c = _cache(**kw)
+        c.reserve([0, 30, 0, 0])
+        c.reserve([50, 0, 0, 0])
+        for b, t in tokens.items():
+            _write(c, b, 0, t)
+        c.advance([37, 20, 0, 0])
+        return c
+
+    def state(c):
+        return (([list(h) for h in c.held], list(c.refs), list(c._free), list(c.lengths), list(c.seen), c.n_pages, c._size),
+                [x.tolist() for x in (c.table, c.length, c.next)])
+
+    def fails(name, at):
+        """The at-th call of torch.<name> or of the library's call fails.  Whether it came to that."""
+        c = made()
+        before, left, owner = state(c), [at], rs if name.startswith("rs_") else torch
+        whole = getattr(owner, name)
+
+        def f(*a, **k):
+            left[0] -= 1
+            if left[0] == 0:
+                raise RuntimeError("no memory")
+            return whole(*a, **k)
+
+        with monkeypatch.context() as m:
+            m.setattr(owner, name, f)
+            try:
+                dict(reserve=lambda: c.reserve([40, 0, 30, 0]), fork=lambda: c.fork(0, [2, 3]), trim=lambda: c.trim(0), free=lambda: c.free(1),
+                     compact=c.compact, shrink=lambda: c.resize(10), grow=lambda: c.resize(60), advance=lambda: c.advance([3, 1, 0, 0]))[call]()
+            except RuntimeError:
+                pass
+            else:
+                return False
+        if call in ("shrink", "grow"):
+            assert c.n_pages == c._size == 40 and all(x is None or x.shape[0] == 40 for x in c._arrays())
+            assert all(x is None or x.shape[1] == 640 for x in (c.weights, c.positions))
+        else:
+            assert state(c) == before, (name, at)
+        for b, t in tokens.items():
+            rows = c.rows(b, torch.arange(len(t)))
+            assert c.k.view(-1, 2, 64)[rows, 0, 0].long().tolist() == [x % 251 for x in t]
+        assert c.table[0, :4].tolist() + c.table[1, :2].tolist() == c.held[0][:4] + c.held[1]
+        assert all(c.refs[p] == 1 for p in c.held[0] + c.held[1]) and sorted(c._free + c.held[0] + c.held[1]) == list(range(40))
+        return True
+
+    assert sum(fails(name, at) for name in ("tensor", "zeros", "empty", "rs_pages_copy", "rs_pages_compact") for at in range(1, 8))
