@@ -15,6 +15,9 @@ namespace {
 
 // Tiles of eight rows that the calls' requests need at most: 1, 2 or 4; 0: more rows
 // than coded_rows takes.  The core works on 128 rows a KV head, whatever is in them.
+// 64 requests with trees behind 1024 to 8191 keys, 32 / 8 heads of 128, bf16, few rows and core:
+// 8 rows 122 and 180 us, 16 rows 163 and 181, 32 rows 618 and 185 (the third tile's registers do not
+// fit); heads of 64: 82 and 164, 127 and 166, 212 and 169.  So four tiles are too many where caches are long.
 int row_tiles(int max_new, int G) {
     const long long rows = (long long)max_new * G;
     return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= kRowMax ? 4 : 0;
